@@ -1,0 +1,411 @@
+"""The dense half of a graph network, as cases that can be timed and checked: products grouped by node type or expert,
+products in 8-bit integers, and the AdamW step that trains their weights.
+
+    grouped      Y = act(X_g W_g + b_g) for every group g of rows (groot_grouped_product): a typed layer, or the experts of a
+                 routed one, in inference
+    train        the same layer in a training step, without an activation: Y, dX = dY_g W_g^T, dW_g = X_g^T dY_g and db_g
+    int8         Y = act(s_x s_w (Q W^T) + b) from rows that are in 8 bits already (groot_int8_product)
+    int8_linear  the same from rows in floating point, which are cut to 8 bits on the way (groot_int8_linear): serving
+    adamw        one AdamW step over many tensors, its states in 32 bits or in 8 (groot_adamw_step)
+
+Rows of a group are neighbours, `offsets` (int64, on the device) says where each begins.  How the rows fall on the groups
+("rows"): "types" as on a multiplier's graph, 2 n inputs, 2 n outputs and everything else gates; "routed" as a router deals
+them, by a skewed draw that can leave groups empty; "one" a single group without offsets.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+_TYPE = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+_BYTES = {"f32": 4, "bf16": 2, "f16": 2}
+
+LR, BETA1, BETA2, EPS, DECAY = 1e-3, 0.9, 0.95, 1e-8, 0.01
+BLOCK, TOP = 256, 448.0                                    # values that share a scale, largest value of an 8-bit code
+
+
+def _lib():
+    import paper_2511_18297_amd as G                       # only where `own` is true: a tree without the operators runs their plain forms
+    return G
+
+
+def listed():
+    return [
+        # typed layer on one 32-bit multiplier, eight thousand nodes at the classifier's width: latency
+        dict(name="grouped_types_f32_32", op="grouped", type="f32", rows="types", n=7968, groups=3, K=32, N=32),
+        # decoding with routed experts: a batch of tokens, a few for each expert, every weight is read for them
+        dict(name="grouped_decode_bf16", op="grouped", type="bf16", rows="routed", n=128, groups=32, K=2048, N=2048),
+        # prefill with routed experts
+        dict(name="grouped_prefill_bf16", op="grouped", type="bf16", rows="routed", n=16384, groups=8, K=4096, N=4096),
+        # training step of the typed layer on a 512-bit multiplier x 4 at the hidden width, the framework's own type
+        dict(name="train_types_f32_64", op="train", type="f32", rows="types", n=8374272, groups=3, K=64, N=64),
+        # training step of routed experts
+        dict(name="train_routed_bf16", op="train", type="bf16", rows="routed", n=8192, groups=16, K=2048, N=1024),
+        # odd sizes: no row of X or W begins on 16 bytes
+        dict(name="train_odd_f16", op="train", type="f16", rows="routed", n=3001, groups=7, K=1001, N=515),
+        # one token through a served layer
+        dict(name="int8_linear_1_bf16", op="int8_linear", type="bf16", rows="one", n=1, groups=1, K=4096, N=4096),
+        # a decoding batch through a wide served layer whose input was cut to 8 bits before, for all layers that read it
+        dict(name="int8_48_bf16", op="int8", type="bf16", rows="one", n=48, groups=1, K=4096, N=8192),
+        # the typed classifier's layer served on a 256-bit multiplier
+        dict(name="int8_types_f32_64", op="int8", type="f32", rows="types", n=522496, groups=3, K=64, N=64),
+        # prefill through a served layer
+        dict(name="int8_linear_8192_f16", op="int8_linear", type="f16", rows="one", n=8192, groups=1, K=4096, N=8192),
+        # the step of a small classifier: 24 tensors, a launch and little else
+        dict(name="adamw_small_f32", op="adamw", type="f32", grad="f32", bits=32, master=False, tensors=24, total=20000),
+        # a large model trained in bfloat16 with weights of 32 bits beside it, states in 8 bits
+        dict(name="adamw_large_bf16_8bit", op="adamw", type="bf16", grad="bf16", bits=8, master=True, tensors=200, total=400000000),
+    ]
+
+
+def _log(rng, low, high):
+    return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+
+def draw(rng):
+    op = rng.choice(["grouped", "grouped", "train", "train", "int8", "int8_linear", "int8_linear", "adamw", "adamw"])
+    if op == "adamw":
+        kind = rng.choice(["f32", "f32", "bf16", "f16"])
+        return dict(op=op, type=kind, grad=rng.choice(["f32", kind, kind]), bits=rng.choice([8, 32]),
+                    master=kind != "f32" and rng.random() < 0.7, tensors=_log(rng, 1, 200), total=_log(rng, 5000, 200000000))
+    kind = rng.choice(["f32", "bf16", "bf16", "f16"])
+    rows = rng.choice(["types", "routed", "routed", "one"]) if op in ("grouped", "train") else rng.choice(["one", "one", "routed", "types"])
+    groups = {"types": 3, "one": 1}.get(rows) or _log(rng, 2, 64)
+    if rows == "types":
+        K, N, n = rng.choice([16, 32, 48, 64, 100, 128]), rng.choice([5, 16, 32, 64, 64, 128]), _log(rng, 2000, 2000000)
+    else:
+        K, N, n = _log(rng, 64, 4096), _log(rng, 64, 4096), _log(rng, 1, 8192)
+        if rng.random() < 0.7:                             # widths are mostly whole multiples of 64
+            K, N = (w + 64 if w == 3072 else w for w in (-(-K // 64) * 64, -(-N // 64) * 64))
+    limit = (3e10 if kind == "f32" else 1.5e11) / (3 if op == "train" else 1)
+    while n * K * N > limit:
+        n = n // 2 + 1
+    return dict(op=op, type=kind, rows=rows, n=n, groups=groups, K=K, N=N)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------------------------------------------
+def _sizes(case, seed):
+    """rows of every group"""
+    n, E = case["n"], case["groups"]
+    if case["rows"] == "one":
+        return [n]
+    if case["rows"] == "types":                            # 8 n^2 - 7 n nodes: 2 n inputs, 2 n outputs
+        ends = min(n // 3, int(2 * math.sqrt(n / 8)))
+        return [ends, n - 2 * ends, ends]
+    r = np.random.RandomState(seed % (1 << 31))
+    return [int(v) for v in r.multinomial(n, r.dirichlet(np.full(E, 2.0)))]
+
+
+def _tensor_sizes(case):
+    """Half of the tensors are vectors (biases, gains), the others matrices that hold nearly everything."""
+    T, total = case["tensors"], case["total"]
+    small = max(1, min(2048, total // (8 * T)))
+    matrices = (T + 1) // 2
+    each = max(1, (total - (T - matrices) * small) // matrices)
+    return [max(1, each + (each // 2) * (1 - i % 4) - i % 3) if i % 2 == 0 else small for i in range(T)]
+
+
+def _places(case):
+    """Where every tensor begins in the flat buffer: 256 bytes apart at least, as an allocator lays them."""
+    sizes, at, places = _tensor_sizes(case), 0, []
+    for n in sizes:
+        places.append(at)
+        at += -(-n // 256) * 256
+    return sizes, places, at
+
+
+def _inputs(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+
+    def normal(*shape, scale=1.0, type=torch.float32):
+        return torch.empty(shape, device="cuda", dtype=torch.float32).normal_(0, scale, generator=g).to(type)
+    if case["op"] == "adamw":
+        return _adamw_inputs(case, seed, normal)
+    T, n, E, K, N = _TYPE[case["type"]], case["n"], case["groups"], case["K"], case["N"]
+    sizes = _sizes(case, seed)
+    s = dict(op=case["op"], sizes=sizes, offsets=torch.tensor(np.concatenate([[0], np.cumsum(sizes)]), device="cuda"))
+    if case["rows"] == "one":
+        s["offsets"] = None
+    if case["op"] in ("grouped", "train"):
+        s["X"] = torch.relu(normal(n, K)).to(T)             # hidden features behind an activation
+        s["W"], s["b"] = normal(E, K, N, scale=K ** -0.5, type=T), normal(E, N, scale=0.1, type=T)
+        if case["op"] == "train":
+            s["dY"] = normal(n, N, scale=0.1, type=T)       # a loss gradient, scaled
+        return s
+    # served: features whose channels differ in size, weights cut to 8 bits with a scale for each output channel
+    x = normal(n, K) * torch.exp(normal(K, scale=0.5))
+    w = normal(E, N, K, scale=K ** -0.5)
+    s["w_scale"] = w.abs().amax(2) / 127
+    s["W"] = torch.round(w / s["w_scale"][:, :, None]).to(torch.int8)
+    s["b"] = normal(E, N, scale=0.1)
+    if case["op"] == "int8":
+        s["q_scale"] = x.abs().amax(1) / 127
+        s["Q"] = torch.round(x / s["q_scale"][:, None]).to(torch.int8)
+        s["type"] = T
+    else:
+        s["X"] = x.to(T)
+    return s
+
+
+def _adamw_inputs(case, seed, normal):
+    sizes, places, total = _places(case)
+    rms = torch.exp(normal(total // BLOCK, 1, scale=1.0)) * 1e-3     # gradients differ in size from layer to layer
+    grad = (normal(total // BLOCK, BLOCK) * rms).reshape(-1)
+    p = normal(total, scale=0.02)
+    m = (0.3 * (normal(total // BLOCK, BLOCK) * rms)).reshape(-1)
+    root = ((normal(total // BLOCK, BLOCK).abs() + 0.5) * rms).reshape(-1)   # square root of the second moment
+    inside = torch.zeros(total, device="cuda")
+    for n, at in zip(sizes, places):
+        inside[at:at + n] = 1
+    p, grad, m, root = p * inside, grad * inside, m * inside, root * inside
+    s = dict(op="adamw", bits=case["bits"], sizes=sizes, places=places, step=100, seed=seed % 65536,
+             p=p.to(_TYPE[case["type"]]), grad=grad.to(_TYPE[case["grad"]]), master=None)
+    if case["master"]:
+        s["master"] = p
+    if case["bits"] == 32:
+        s["m"], s["v"] = m, root * root
+        return s
+    for name, x in (("m", m), ("v", root)):
+        blocks = x.reshape(-1, BLOCK)
+        scale = blocks.abs().amax(1) / TOP
+        s[name + "_scale"] = scale
+        s[name] = (blocks / scale[:, None].clamp(min=1e-30)).to(torch.float8_e4m3fn).reshape(-1)
+    # which tensor a value belongs to, and its place there: the random number of its rounding goes by both
+    number = torch.zeros(total, dtype=torch.int32, device="cuda")
+    place = torch.zeros(total, dtype=torch.int32, device="cuda")
+    for i, (n, at) in enumerate(zip(sizes, places)):
+        number[at:at + n] = i
+        place[at:at + n] = torch.arange(n, dtype=torch.int32, device="cuda")
+    s["number"], s["place"] = number, place
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    if s["op"] == "adamw":
+        return s
+    n, E, K, N = case["n"], case["groups"], case["K"], case["N"]
+    like = lambda *shape, type=_TYPE[case["type"]]: torch.empty(shape, dtype=type, device="cuda")  # noqa: E731
+    s["Y"] = like(n, N)
+    if s["op"] == "train":
+        s["dX"], s["dW"], s["db"] = like(n, K), like(E, K, N), like(E, N)
+    return s
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# one pass
+# ---------------------------------------------------------------------------------------------------------------
+def _products(x, w, sizes):
+    """x_g w_g for every group, in 32 bits"""
+    return torch.cat([a @ b for a, b in zip(x.split(sizes), w.unbind())])
+
+
+def _plain(s):
+    op, sizes = s["op"], s["sizes"]
+    if op in ("grouped", "train"):
+        x, w, b, T = s["X"].float(), s["W"].float(), s["b"].float(), s["X"].dtype
+        of = torch.cat([t.expand(n, -1) for n, t in zip(sizes, b.unbind())])
+        y = _products(x, w, sizes) + of
+        if op == "grouped":
+            return torch.relu(y).to(T)
+        dy = s["dY"].float()
+        dx = _products(dy, w.transpose(1, 2), sizes)
+        dw = torch.stack([a.t() @ c for a, c in zip(x.split(sizes), dy.split(sizes))])
+        db = torch.stack([c.sum(0) for c in dy.split(sizes)])
+        return {"Y": y.to(T), "dX": dx.to(T), "dW": dw.to(T), "db": db.to(T)}
+    if op == "int8_linear":
+        x, T = s["X"].float(), s["X"].dtype
+        scale = x.abs().amax(1) / 127
+        q = torch.round(x / scale[:, None])
+    else:
+        q, scale, T = s["Q"].float(), s["q_scale"], s["type"]
+    columns = torch.cat([t.expand(n, -1) for n, t in zip(sizes, s["w_scale"].unbind())])
+    of = torch.cat([t.expand(n, -1) for n, t in zip(sizes, s["b"].unbind())])
+    y = _products(q, s["W"].float().transpose(1, 2), sizes) * scale[:, None] * columns + of
+    return (torch.relu(y) if op == "int8" else y).to(T)
+
+
+def _mixed(h):
+    """A 32-bit number from another: shifts and products modulo 2^32 (in 64-bit integers, of which the low 32 bits count)."""
+    h = h ^ (h >> 16)
+    h = (h * 0x85EBCA6B) & 0xFFFFFFFF
+    h = h ^ (h >> 13)
+    h = (h * 0xC2B2AE35) & 0xFFFFFFFF
+    return h ^ (h >> 16)
+
+
+def _key(seed, step, number):
+    """The 32-bit key of one tensor's random numbers in one step."""
+    return _mixed(_mixed(_mixed(number + 0x9E3779B9) ^ (step & 0xFFFFFFFF)) ^ (seed & 0xFFFFFFFF))
+
+
+def _to_codes(x, u):
+    """x on the grid of the 8-bit codes (3 bits behind the leading one, steps of 2^-9 at least), rounded up where the fraction
+    of a step and u in [0, 1) come to a whole one."""
+    _, e = torch.frexp(x)                                  # |x| in [2^(e-1), 2^e)
+    e = torch.clamp(e, min=-5) - 4
+    r = torch.clamp(torch.ldexp(torch.floor(torch.ldexp(x.abs(), -e) + u), e), max=TOP)
+    return torch.where(x < 0, -r, r)
+
+
+def _blocks_to_codes(x, u):
+    """(codes, scales) of blocks of 256 values: the scale takes a block's largest magnitude to the largest code."""
+    blocks = x.reshape(-1, BLOCK)
+    scale = blocks.abs().amax(1) / TOP
+    over = torch.where(scale[:, None] > 0, blocks / scale[:, None], torch.zeros_like(blocks)).reshape(-1)
+    return _to_codes(over, u.float() / 65536), scale
+
+
+def _adamw_plain(s):
+    s["step"] += 1
+    t, bits = s["step"], s["bits"]
+    w = (s["master"] if s["master"] is not None else s["p"]).float()
+    g = s["grad"].float()
+    m, v = s["m"], s["v"]
+    if bits == 8:
+        m = (m.float().reshape(-1, BLOCK) * s["m_scale"][:, None]).reshape(-1)
+        v = (v.float().reshape(-1, BLOCK) * s["v_scale"][:, None]).reshape(-1)
+        v = v * v
+    m = m * BETA1 + g * (1 - BETA1)
+    v = v * BETA2 + (g * g) * (1 - BETA2)
+    root = torch.sqrt(v)
+    w = w * (1 - LR * DECAY) - (LR / (1 - BETA1 ** t)) * (m / (root * (1 / math.sqrt(1 - BETA2 ** t)) + EPS))
+    if s["master"] is not None:
+        s["master"].copy_(w)
+    s["p"].copy_(w)
+    if bits == 32:
+        s["m"].copy_(m)
+        s["v"].copy_(v)
+        return _adamw_state(s)
+    place, number = s["place"].long(), s["number"].long()
+    h = _mixed(place ^ _key(s["seed"], t, number))
+    codes, scale = _blocks_to_codes(m, h & 0xFFFF)
+    s["m"].copy_(codes)
+    s["m_scale"].copy_(scale)
+    codes, scale = _blocks_to_codes(root, h >> 16)         # the root is held, and never as 0 where it is not
+    s["v"].copy_(torch.where((root > 0) & (codes == 0), torch.full_like(codes, 2.0 ** -9), codes))
+    s["v_scale"].copy_(scale)
+    return _adamw_state(s)
+
+
+def _adamw_state(s):
+    return {k: s[k] for k in ("p", "m", "v", "master", "m_scale", "v_scale") if s.get(k) is not None}
+
+
+def _adamw_own(s):
+    G = _lib()
+    if "tensors" not in s:                                 # made once, as a program does beside its optimizer's states
+        def views(flat):
+            return [flat[at:at + n] for n, at in zip(s["sizes"], s["places"])]
+
+        def scales(flat):
+            return [flat[at // BLOCK:at // BLOCK + -(-n // BLOCK)] for n, at in zip(s["sizes"], s["places"])]
+        more = dict(master=views(s["master"])) if s["master"] is not None else {}
+        if s["bits"] == 8:
+            more.update(m_scale=scales(s["m_scale"]), v_scale=scales(s["v_scale"]))
+        s["tensors"] = G.groot_adamw_tensors(views(s["p"]), views(s["grad"]), views(s["m"]), views(s["v"]), **more)
+    s["step"] += 1
+    G.groot_adamw_step(s["tensors"], s["step"], LR, BETA1, BETA2, EPS, DECAY, seed=s["seed"])
+    return _adamw_state(s)
+
+
+def run(s):
+    op = s["op"]
+    if op == "adamw":
+        return _adamw_own(s) if own else _adamw_plain(s)
+    if not own:
+        return _plain(s)
+    G = _lib()
+    if op == "grouped":
+        G.groot_grouped_product(s["X"], s["W"], s["offsets"], s["b"], True, s["Y"])
+        return s["Y"]
+    if op == "train":
+        if "work" not in s:
+            need = G.groot_grouped_product_backward_weights_workspace(s["X"].shape[0], *s["W"].shape, s["X"].dtype)
+            s["work"] = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+        G.groot_grouped_product(s["X"], s["W"], s["offsets"], s["b"], False, s["Y"])
+        G.groot_grouped_product_backward_data(s["dY"], s["W"], s["offsets"], s["dX"])
+        G.groot_grouped_product_backward_weights(s["X"], s["dY"], s["offsets"], s["dW"], s["db"], s["work"])
+        return {k: s[k] for k in ("Y", "dX", "dW", "db")}
+    if op == "int8":
+        G.groot_int8_product(s["Q"], s["q_scale"], s["W"], s["w_scale"], s["offsets"], s["b"], True, s["Y"])
+        return s["Y"]
+    if "work" not in s:
+        s["work"] = torch.empty(max(G.groot_int8_linear_workspace(*s["X"].shape), 16), dtype=torch.uint8, device="cuda")
+    G.groot_int8_linear(s["X"], s["W"], s["w_scale"], s["offsets"], s["b"], False, s["Y"], s["work"])
+    return s["Y"]
+
+
+def work(case):
+    """Every input once, every output once; the products of all groups."""
+    if case["op"] == "adamw":
+        n, p, g = sum(_tensor_sizes(case)), _BYTES[case["type"]], _BYTES[case["grad"]]
+        state = 2 * 2 * (4 if case["bits"] == 32 else 1 + 4 / BLOCK)
+        return {"bytes": n * (g + state + (8 + p if case["master"] else 2 * p)), "flops": 15 * n}
+    n, E, K, N, b = case["n"], min(case["groups"], case["n"]), case["K"], case["N"], _BYTES[case["type"]]
+    product = 2 * n * K * N
+    if case["op"] == "grouped":
+        return {"bytes": b * (n * K + E * K * N + E * N + n * N), "flops": product}
+    if case["op"] == "train":
+        return {"bytes": b * (2 * n * K + 2 * n * N + 2 * E * K * N + 2 * E * N), "flops": 3 * product}
+    x = n * K + 4 * n if case["op"] == "int8" else b * n * K
+    return {"bytes": x + E * K * N + 8 * E * N + b * n * N, "flops": product}
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# the definitions in 64 bits
+# ---------------------------------------------------------------------------------------------------------------
+def exact(case, seed):
+    s = _inputs(case, seed)
+    if case["op"] == "adamw":
+        return _adamw_exact(s)
+    ends = np.cumsum([0] + s["sizes"])
+    rows = [slice(int(a), int(b)) for a, b in zip(ends[:-1], ends[1:])]
+    n, N, K = case["n"], case["N"], case["K"]
+    y = torch.zeros((n, N), dtype=torch.float64, device="cuda")
+    if case["op"] in ("int8", "int8_linear"):
+        for e, r in enumerate(rows):
+            if case["op"] == "int8":
+                q, scale = s["Q"][r].double(), s["q_scale"][r].double()
+            else:
+                x = s["X"][r].double()
+                scale = x.abs().amax(1) / 127
+                q = torch.round(x / scale[:, None])
+            y[r] = torch.mm(q, s["W"][e].double().t()) * (scale[:, None] * s["w_scale"][e].double()) + s["b"][e].double()
+        return y.clamp_(min=0) if case["op"] == "int8" else y
+    dx = torch.zeros((n, K), dtype=torch.float64, device="cuda")
+    dw = torch.zeros((case["groups"], K, N), dtype=torch.float64, device="cuda")
+    db = torch.zeros((case["groups"], N), dtype=torch.float64, device="cuda")
+    for e, r in enumerate(rows):
+        x, w = s["X"][r].double(), s["W"][e].double()
+        y[r] = torch.addmm(s["b"][e].double(), x, w)
+        if case["op"] == "train":
+            d = s["dY"][r].double()
+            dx[r], dw[e], db[e] = torch.mm(d, w.t()), torch.mm(x.t(), d), d.sum(0)
+    return y.clamp_(min=0) if case["op"] == "grouped" else {"Y": y, "dX": dx, "dW": dw, "db": db}
+
+
+def _adamw_exact(s):
+    t = s["step"] + 1
+    held = lambda name: s[name].double() * s[name + "_scale"].double().repeat_interleave(BLOCK) if s["bits"] == 8 else s[name].double()  # noqa: E731
+    m, v = held("m"), held("v")
+    if s["bits"] == 8:
+        v = v ** 2
+    g = s["grad"].double()
+    m += (1 - BETA1) * (g - m)
+    v += (1 - BETA2) * (g ** 2 - v)
+    w = (s["p"] if s["master"] is None else s["master"]).double()
+    w = w - LR * DECAY * w - LR * (m / (1 - BETA1 ** t)) / ((v / (1 - BETA2 ** t)).sqrt() + EPS)
+    out = {"p": w}
+    if s["master"] is not None:
+        out["master"] = w
+    if s["bits"] == 32:
+        return dict(out, m=m, v=v)
+    top = lambda x: x.abs().reshape(-1, BLOCK).amax(1) / TOP  # noqa: E731
+    # the codes depend on which side of a random threshold a value falls: they have no value in 64 bits
+    return dict(out, m=None, v=None, m_scale=top(m), v_scale=top(v.sqrt()))
