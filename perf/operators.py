@@ -4,8 +4,8 @@ products in 8-bit integers, and the AdamW step that trains their weights.
     grouped      Y = act(X_g W_g + b_g) for every group g of rows (groot_grouped_product): a typed layer, or the experts of a
                  routed one, in inference
     train        the same layer in a training step, without an activation: Y, dX = dY_g W_g^T, dW_g = X_g^T dY_g and db_g
-    int8         Y = act(s_x s_w (Q W^T) + b) from rows that are in 8 bits already (groot_int8_product)
-    int8_linear  the same from rows in floating point, which are cut to 8 bits on the way (groot_int8_linear): serving
+    int8         Y = act(s_x s_w (Q W^T) + b) from rows that are in 8 bits already (groot_quantized_product)
+    int8_linear  the same from rows in floating point, which are cut to 8 bits on the way (groot_quantized_linear): serving
     adamw        one AdamW step over many tensors, its states in 32 bits or in 8 (groot_adamw_step)
 
 Rows of a group are neighbours, `offsets` (int64, on the device) says where each begins.  How the rows fall on the groups
@@ -333,11 +333,11 @@ def run(s):
         G.groot_grouped_product_backward_weights(s["X"], s["dY"], s["offsets"], s["dW"], s["db"], s["work"])
         return {k: s[k] for k in ("Y", "dX", "dW", "db")}
     if op == "int8":
-        G.groot_int8_product(s["Q"], s["q_scale"], s["W"], s["w_scale"], s["offsets"], s["b"], True, s["Y"])
+        G.groot_quantized_product(s["Q"], s["q_scale"], s["W"], s["w_scale"], s["offsets"], s["b"], True, s["Y"])
         return s["Y"]
     if "work" not in s:
-        s["work"] = torch.empty(max(G.groot_int8_linear_workspace(*s["X"].shape), 16), dtype=torch.uint8, device="cuda")
-    G.groot_int8_linear(s["X"], s["W"], s["w_scale"], s["offsets"], s["b"], False, s["Y"], s["work"])
+        s["work"] = torch.empty(max(G.groot_quantized_linear_workspace(*s["X"].shape), 16), dtype=torch.uint8, device="cuda")
+    G.groot_quantized_linear(s["X"], s["W"], s["w_scale"], s["offsets"], s["b"], False, s["Y"], s["work"])
     return s["Y"]
 
 
