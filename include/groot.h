@@ -482,6 +482,151 @@ groot_status groot_feature_placement(const groot_plan *plan, void *arena_dev, si
                                      int32_t F, void *hip_stream, size_t *x_offset,
                                      size_t *y_offset, float *best_ms, float *first_ms);
 
+/* ---------------------------------------------------------------------------
+ * Products grouped by node type or expert.  Not in the paper: the dense half
+ * of a layer whose weights differ from one kind of row to the next (primary
+ * inputs, gates and outputs of an AIG; the experts of a routed layer).  Rows
+ * of one group are neighbours: group g has the rows [offsets[g], offsets[g+1])
+ * of X, any number of them, none included.
+ *
+ *   groot_grouped_product                    Y[i,:]  = act(X[i,:] W[g] + bias[g])
+ *   groot_grouped_product_backward_data      dX[i,:] = dY[i,:] W[g]^T
+ *   groot_grouped_product_backward_weights   dW[g]   = sum_i X[i,:]^T dY[i,:],
+ *                                            dbias[g] = sum_i dY[i,:]
+ *
+ * dtype: type of every matrix of the call, GROOT_F32, GROOT_BF16 or GROOT_F16
+ *   (grad_dtype: that of dW and dbias, dtype or GROOT_F32).  Products are
+ *   summed in 32 bits and rounded once to the output's type; GROOT_F32 is
+ *   computed in fp32 throughout.
+ * X, dX [n_rows, K], dY, Y [n_rows, N]: device, `*_stride` elements from row to
+ *   row (at least the width).  W, dW [n_groups, K, N], bias, dbias [n_groups, N]:
+ *   device, contiguous; bias and dbias may be NULL.  Pointers are aligned to
+ *   their type; rows that begin on 16 bytes are read faster.  Outputs must not
+ *   overlap inputs.
+ * relu: 0, or 1 for act(v) = max(v, 0) (NaN stays NaN).
+ * offsets_dev: int64 [n_groups + 1] on the device, ascending, or NULL with
+ *   n_groups = 1 for all rows.  They are read by the kernels only; an offset
+ *   outside [0, n_rows] is taken as the nearer end, a group that ends before it
+ *   begins is empty.  Rows outside every group are not written; dW and dbias of
+ *   an empty group are zeros.
+ * workspace (device, 16-byte aligned, contents overwritten, owned by the
+ *   caller): at least groot_grouped_product_backward_weights_workspace bytes
+ *   (may be 0), for the partial sums of groups that are cut into pieces; they
+ *   meet in a fixed order, so results are the same from run to run.
+ * 1 <= K, N <= 65536, 1 <= n_groups <= 65536, n_rows >= 0.  The calls only
+ * enqueue on hip_stream and allocate nothing.  Errors: EINVAL (NULL, unknown
+ * dtype, alignment, sizes, strides, overlap, workspace too small), ERANGE (more
+ * than 2^31 - 1 output tiles), EHIP.
+ * ------------------------------------------------------------------------- */
+typedef enum { GROOT_F32 = 0, GROOT_BF16 = 1, GROOT_F16 = 2 } groot_dtype;
+
+groot_status groot_grouped_product(int32_t dtype, const void *X_dev, int64_t x_stride, const void *W_dev,
+                                   const int64_t *offsets_dev, const void *bias_dev, int32_t relu,
+                                   void *Y_dev, int64_t y_stride, int64_t n_rows, int32_t n_groups,
+                                   int32_t K, int32_t N, void *hip_stream);
+groot_status groot_grouped_product_backward_data(int32_t dtype, const void *dY_dev, int64_t dy_stride,
+                                                 const void *W_dev, const int64_t *offsets_dev, void *dX_dev,
+                                                 int64_t dx_stride, int64_t n_rows, int32_t n_groups, int32_t K,
+                                                 int32_t N, void *hip_stream);
+groot_status groot_grouped_product_backward_weights_workspace(int32_t dtype, int64_t n_rows, int32_t n_groups,
+                                                              int32_t K, int32_t N, size_t *bytes);
+groot_status groot_grouped_product_backward_weights(int32_t dtype, const void *X_dev, int64_t x_stride,
+                                                    const void *dY_dev, int64_t dy_stride,
+                                                    const int64_t *offsets_dev, int32_t grad_dtype, void *dW_dev,
+                                                    void *dbias_dev, int64_t n_rows, int32_t n_groups, int32_t K,
+                                                    int32_t N, void *workspace_dev, size_t workspace_bytes,
+                                                    void *hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Products in 8-bit integers, for serving trained layers.  Not in the paper.
+ *   groot_quantize_rows   scale[i] = max_k |x[i,k]| times fl(1 / 127),
+ *                         Q[i,k] = x[i,k] / scale[i] rounded to the nearest
+ *                         integer (halves to even), product and division in fp32;
+ *                         a row of zeros has scale 0 and zeros, a row that holds
+ *                         a NaN or an infinity has scale NaN and zeros
+ *   groot_quantized_product  Y[i,j] = act((sum_k Q[i,k] W[g,j,k]) q_scale[i]
+ *                         w_scale[g,j] + bias[g,j]): the sum is exact (int32),
+ *                         the rest fp32 in this order, rounded once to Y's type
+ *   groot_quantized_linear   both after one another from rows in floating point
+ * W int8 [n_groups, N, K] (one row per output channel, contiguous), w_scale
+ * and bias float [n_groups, N] (bias may be NULL), q_scale float [n_rows], Q int8
+ * with q_stride bytes from row to row; groups, offsets, relu, strides, dtype
+ * (of X and Y) and limits as for groot_grouped_product (65536 products of two
+ * 8-bit integers stay below 2^31).  Rows of Q and W that begin on 16 bytes are
+ * read faster.
+ * workspace of groot_quantized_linear: device, 16-byte aligned, at least
+ * groot_quantized_linear_workspace bytes; its contents after the call mean nothing.
+ * The calls only enqueue on hip_stream and allocate nothing.  Errors: as above.
+ * ------------------------------------------------------------------------- */
+groot_status groot_quantize_rows(int32_t dtype, const void *X_dev, int64_t x_stride, int8_t *Q_dev,
+                                 int64_t q_stride, float *scale_dev, int64_t n_rows, int32_t K,
+                                 void *hip_stream);
+groot_status groot_quantized_product(const int8_t *Q_dev, int64_t q_stride, const float *q_scale_dev,
+                                const int8_t *W_dev, const float *w_scale_dev, const int64_t *offsets_dev,
+                                const float *bias_dev, int32_t relu, int32_t dtype, void *Y_dev,
+                                int64_t y_stride, int64_t n_rows, int32_t n_groups, int32_t K, int32_t N,
+                                void *hip_stream);
+groot_status groot_quantized_linear_workspace(int64_t n_rows, int32_t K, size_t *bytes);
+groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_stride, const int8_t *W_dev,
+                               const float *w_scale_dev, const int64_t *offsets_dev, const float *bias_dev,
+                               int32_t relu, void *Y_dev, int64_t y_stride, int64_t n_rows, int32_t n_groups,
+                               int32_t K, int32_t N, void *workspace_dev, size_t workspace_bytes,
+                               void *hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * groot_adamw_step -- one AdamW step over many tensors in few launches.  Not in
+ * the paper: the optimizer behind the layers' gradient calls.  For every value
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   w <- w (1 - lr weight_decay)
+ *        - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in fp32 (the factors of lr, beta and step are computed in fp64 and rounded
+ * once), every operation rounded by itself in the order written.
+ * tensors (host, read during the call): device pointers, n values each.
+ *   w is `param` (param_dtype), or with `master` not NULL the fp32 master, of
+ *   which param becomes the rounded copy; either all tensors of a call have a
+ *   master or none.  grad is of grad_dtype and is multiplied by *grad_scale_dev
+ *   (device float, NULL = 1) first: loss scaling, or clipping by a norm that was
+ *   computed on the device.
+ * state_bits 32: m and v are float [n], m_scale and v_scale are not read.
+ * state_bits 8: m and v are 8-bit floating codes (1 sign, 4 exponent, 3 mantissa
+ *   bits, bias 7, no infinities, 0x7F = NaN) [n] with a float scale for every 256
+ *   neighbouring values (m_scale, v_scale [ceil(n / 256)]): m = code * scale, and
+ *   sqrt(v) = code * scale in `v`, the root because it halves the range that the
+ *   codes have to span.  scale = largest finite magnitude of the block times fl(1 / 448).
+ *   Codes are rounded up or down at random so that the expectation is right:
+ *   |x| / step + u is rounded down, with u = the low (m) or high (v) 16 bits of
+ *   mix(i ^ key) / 65536, i the value's index in its tensor (for i >= 2^32 its low
+ *   32 bits, and key + (i >> 32) * 0x9E3779B9 for key), key = mix(mix(mix(number
+ *   of the tensor in the call + 0x9E3779B9) ^ step) ^ seed), mix the finaliser
+ *   h ^= h >> 16, h *= 0x85EBCA6B, h ^= h >> 13, h *= 0xC2B2AE35, h ^= h >> 16.
+ *   (Rounded to nearest, an average that moves by less than half a code's step
+ *   per call would stand still for good.)  sqrt(v) > 0 is held as the smallest
+ *   code at least, never as 0.  A value that is not finite becomes NaN and
+ *   leaves the others of its block alone.
+ * Pointers are aligned to their type; tensors whose arrays all begin on 16 bytes
+ * are read faster.  Launches one kernel per 48 tensors on hip_stream, allocates
+ * nothing; the descriptors travel as kernel arguments, so the call may be
+ * captured in a HIP graph, with the host values it was given.
+ * Errors: EINVAL (NULL, unknown dtype, n < 0, state_bits, step < 1, lr or
+ * weight_decay not finite or negative, beta outside [0, 1), eps not finite or <= 0), ERANGE (a tensor of
+ * 2^40 values or more), EHIP.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m;
+    void *v;
+    float *m_scale;
+    float *v_scale;
+    float *master;
+    int64_t n;
+} groot_adamw_tensor;
+
+groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int64_t n_tensors, int32_t param_dtype,
+                              int32_t grad_dtype, int32_t state_bits, int64_t step, double lr, double beta1,
+                              double beta2, double eps, double weight_decay, const float *grad_scale_dev,
+                              uint32_t seed, void *hip_stream);
+
 /* What the library decided for an uploaded plan, for diagnostics and benchmarks:
  * "ld_pipelined" (0 the plain LD kernel always, 2 the pipelined one for F = 32,
  * 64, 128 and, on whole graphs, the widths from 20 (5 gather slots per row, and

@@ -28,6 +28,9 @@ EXPORTS = [
     "groot_parts_count", "groot_parts_free", "groot_partition_regrow_device", "groot_dev_part_view",
     "groot_dev_part_plan", "groot_dev_part_download", "groot_dev_part_free", "groot_rows_gather", "groot_rows_scatter",
     "groot_set_tuning", "groot_last_error",
+    "groot_grouped_product", "groot_grouped_product_backward_data", "groot_grouped_product_backward_weights",
+    "groot_grouped_product_backward_weights_workspace", "groot_quantize_rows", "groot_quantized_product", "groot_quantized_linear",
+    "groot_quantized_linear_workspace", "groot_adamw_step",
 ]
 
 # an alternative build of the library (same ABI), for experiments
@@ -91,6 +94,18 @@ _lib.groot_dev_part_free.argtypes = [_vp]
 _lib.groot_dev_part_free.restype = None
 _lib.groot_rows_gather.argtypes = [_vp, _i64, _vp, _vp, _i32, _vp]
 _lib.groot_rows_scatter.argtypes = [_vp, _i64, _vp, _vp, _i32, _vp]
+_psize, _f64 = ctypes.POINTER(ctypes.c_size_t), ctypes.c_double
+_lib.groot_grouped_product.argtypes = [_i32, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _i64, _i64, _i32, _i32, _i32, _vp]
+_lib.groot_grouped_product_backward_data.argtypes = [_i32, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _i32, _i32, _i32, _vp]
+_lib.groot_grouped_product_backward_weights_workspace.argtypes = [_i32, _i64, _i32, _i32, _i32, _psize]
+_lib.groot_grouped_product_backward_weights.argtypes = [_i32, _vp, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _i64, _i32, _i32, _i32,
+                                                        _vp, ctypes.c_size_t, _vp]
+_lib.groot_quantize_rows.argtypes = [_i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp]
+_lib.groot_quantized_product.argtypes = [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i32, _i32, _i32, _vp]
+_lib.groot_quantized_linear_workspace.argtypes = [_i64, _i32, _psize]
+_lib.groot_quantized_linear.argtypes = [_i32, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _vp, _i64, _i64, _i32, _i32, _i32, _vp,
+                                   ctypes.c_size_t, _vp]
+_lib.groot_adamw_step.argtypes = [_vp, _i64, _i32, _i32, _i32, _i64, _f64, _f64, _f64, _f64, _f64, _vp, _u32, _vp]
 _lib.groot_set_tuning.argtypes = [ctypes.c_char_p, _i64]
 _lib.groot_last_error.argtypes = []
 _lib.groot_last_error.restype = ctypes.c_char_p
@@ -551,3 +566,215 @@ def groot_rows_scatter(ids, inp, Y, F: int = None, stream=None) -> None:
 
 def groot_set_tuning(name: str, value: int) -> None:
     _check(_lib.groot_set_tuning(name.encode(), value))
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# the dense half: grouped products, products in 8-bit integers, the AdamW step
+# ---------------------------------------------------------------------------------------------------------------
+GROOT_F32, GROOT_BF16, GROOT_F16 = range(3)
+_DTYPES = {torch.float32: GROOT_F32, torch.bfloat16: GROOT_BF16, torch.float16: GROOT_F16}
+
+
+def _dtype(t, what):
+    try:
+        return _DTYPES[t.dtype]
+    except (KeyError, AttributeError):
+        raise TypeError(f"{what} must be float32, bfloat16 or float16") from None
+
+
+def _rows(t, what, shape, dtype):
+    """Pointer and row stride of a CUDA matrix of this shape and type whose rows are contiguous (any distance apart): the C ABI
+    cannot know buffer sizes, so everything is checked before anything is launched."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if t.dim() != 2 or t.shape != shape:
+        raise ValueError(f"{what} must be {tuple(shape)}, is {tuple(t.shape)}")
+    stride, inner = t.stride()
+    if t.shape[0] <= 1:
+        stride = max(stride, t.shape[1])
+    if (inner != 1 and t.shape[1] > 1) or stride < t.shape[1]:
+        raise ValueError(f"{what} must have contiguous rows that do not overlap")
+    return t.data_ptr(), stride
+
+
+def _array(t, what, shape, dtype):
+    """Pointer of a contiguous CUDA tensor of this shape and type; None stays None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{what} must be a contiguous CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what} must be {tuple(shape)}, is {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def groot_grouped_product(X, W, offsets, bias, relu: bool, Y, stream=None) -> None:
+    """Y[i] = act(X[i] W[g] + bias[g]) for the rows i of every group g.  X [n, K], Y [n, N] (rows may be any distance apart),
+    W [groups, K, N], bias [groups, N] or None, offsets int64 [groups + 1] on the device or None (one group)."""
+    d = _dtype(X, "X")
+    E, K, N = W.shape
+    n = X.shape[0]
+    x, xs = _rows(X, "X", (n, K), X.dtype)
+    y, ys = _rows(Y, "Y", (n, N), X.dtype)
+    _check(_lib.groot_grouped_product(d, x, xs, _array(W, "W", (E, K, N), X.dtype), _array(offsets, "offsets", (E + 1,), torch.int64),
+                                      _array(bias, "bias", (E, N), X.dtype), 1 if relu else 0, y, ys, n, E, K, N,
+                                      _stream_handle(stream)))
+
+
+def groot_grouped_product_backward_data(dY, W, offsets, dX, stream=None) -> None:
+    """dX[i] = dY[i] W[g]^T.  dY [n, N], W [groups, K, N] as in the forward call, dX [n, K]."""
+    d = _dtype(dY, "dY")
+    E, K, N = W.shape
+    n = dY.shape[0]
+    y, ys = _rows(dY, "dY", (n, N), dY.dtype)
+    x, xs = _rows(dX, "dX", (n, K), dY.dtype)
+    _check(_lib.groot_grouped_product_backward_data(d, y, ys, _array(W, "W", (E, K, N), dY.dtype),
+                                                    _array(offsets, "offsets", (E + 1,), torch.int64), x, xs, n, E, K, N,
+                                                    _stream_handle(stream)))
+
+
+def groot_grouped_product_backward_weights_workspace(n_rows: int, groups: int, K: int, N: int, dtype) -> int:
+    """Bytes of device workspace that groot_grouped_product_backward_weights needs (0: none)."""
+    b = ctypes.c_size_t(0)
+    if dtype not in _DTYPES:
+        raise TypeError("dtype must be float32, bfloat16 or float16")
+    _check(_lib.groot_grouped_product_backward_weights_workspace(_DTYPES[dtype], n_rows, groups, K, N, ctypes.byref(b)))
+    return b.value
+
+
+def groot_grouped_product_backward_weights(X, dY, offsets, dW, dbias, workspace, stream=None) -> None:
+    """dW[g] = X_g^T dY_g, dbias[g] = column sums of dY_g (None: not wanted).  dW [groups, K, N] and dbias [groups, N] of X's
+    type or float32; workspace: a contiguous CUDA tensor of at least
+    groot_grouped_product_backward_weights_workspace(n, groups, K, N, X.dtype) bytes, or None where that is 0."""
+    d, gd = _dtype(X, "X"), _dtype(dW, "dW")
+    E, K, N = dW.shape
+    n = X.shape[0]
+    x, xs = _rows(X, "X", (n, K), X.dtype)
+    y, ys = _rows(dY, "dY", (n, N), X.dtype)
+    ws = None if workspace is None else _dev_ptr(workspace, "workspace")
+    _check(_lib.groot_grouped_product_backward_weights(d, x, xs, y, ys, _array(offsets, "offsets", (E + 1,), torch.int64), gd,
+                                                       _array(dW, "dW", (E, K, N), dW.dtype),
+                                                       _array(dbias, "dbias", (E, N), dW.dtype), n, E, K, N, ws,
+                                                       0 if ws is None else workspace.numel() * workspace.element_size(),
+                                                       _stream_handle(stream)))
+
+
+def groot_quantize_rows(X, Q, scale, stream=None) -> None:
+    """scale[i] = max |X[i]| / 127, Q[i] = X[i] / scale[i] rounded.  X [n, K], Q int8 [n, K], scale float32 [n]."""
+    n, K = X.shape
+    x, xs = _rows(X, "X", (n, K), X.dtype)
+    q, qs = _rows(Q, "Q", (n, K), torch.int8)
+    _check(_lib.groot_quantize_rows(_dtype(X, "X"), x, xs, q, qs, _array(scale, "scale", (n,), torch.float32), n, K,
+                                    _stream_handle(stream)))
+
+
+def groot_quantized_product(Q, q_scale, W, w_scale, offsets, bias, relu: bool, Y, stream=None) -> None:
+    """Y[i, j] = act((Q[i] . W[g, j]) q_scale[i] w_scale[g, j] + bias[g, j]).  Q int8 [n, K], q_scale float32 [n], W int8
+    [groups, N, K], w_scale and bias float32 [groups, N] (bias or None), Y [n, N]."""
+    E, N, K = W.shape
+    n = Q.shape[0]
+    q, qs = _rows(Q, "Q", (n, K), torch.int8)
+    y, ys = _rows(Y, "Y", (n, N), Y.dtype)
+    _check(_lib.groot_quantized_product(q, qs, _array(q_scale, "q_scale", (n,), torch.float32), _array(W, "W", (E, N, K), torch.int8),
+                                   _array(w_scale, "w_scale", (E, N), torch.float32),
+                                   _array(offsets, "offsets", (E + 1,), torch.int64), _array(bias, "bias", (E, N), torch.float32),
+                                   1 if relu else 0, _dtype(Y, "Y"), y, ys, n, E, K, N, _stream_handle(stream)))
+
+
+def groot_quantized_linear_workspace(n_rows: int, K: int) -> int:
+    """Bytes of device workspace that groot_quantized_linear needs."""
+    b = ctypes.c_size_t(0)
+    _check(_lib.groot_quantized_linear_workspace(n_rows, K, ctypes.byref(b)))
+    return b.value
+
+
+def groot_quantized_linear(X, W, w_scale, offsets, bias, relu: bool, Y, workspace, stream=None) -> None:
+    """groot_quantize_rows and groot_quantized_product in one call: X [n, K] and Y [n, N] of one floating type; workspace: a
+    contiguous CUDA tensor of at least groot_quantized_linear_workspace(n, K) bytes."""
+    E, N, K = W.shape
+    n = X.shape[0]
+    x, xs = _rows(X, "X", (n, K), X.dtype)
+    y, ys = _rows(Y, "Y", (n, N), X.dtype)
+    _check(_lib.groot_quantized_linear(_dtype(X, "X"), x, xs, _array(W, "W", (E, N, K), torch.int8),
+                                  _array(w_scale, "w_scale", (E, N), torch.float32),
+                                  _array(offsets, "offsets", (E + 1,), torch.int64), _array(bias, "bias", (E, N), torch.float32),
+                                  1 if relu else 0, y, ys, n, E, K, N, _dev_ptr(workspace, "workspace"),
+                                  workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [("param", _vp), ("grad", _vp), ("m", _vp), ("v", _vp), ("m_scale", _vp), ("v_scale", _vp), ("master", _vp),
+                ("n", _i64)]
+
+
+class AdamwTensors:
+    """The descriptors of groot_adamw_step for one list of tensors, checked once; keeps the tensors alive.  Gradients that move
+    from step to step: set_grads."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, master=None):
+        lists = dict(param=params, grad=grads, m=m, v=v, m_scale=m_scale, v_scale=v_scale, master=master)
+        lists = {k: list(x) for k, x in lists.items() if x is not None}
+        self.count = len(lists["param"])
+        if any(len(x) != self.count for x in lists.values()):
+            raise ValueError("the lists must have one tensor for every parameter")
+        if (m_scale is None) != (v_scale is None):
+            raise ValueError("8-bit states need m_scale and v_scale")
+        self.state_bits = 32 if m_scale is None else 8
+        state = torch.float32 if self.state_bits == 32 else torch.float8_e4m3fn
+        self.param_dtype = _dtype(lists["param"][0], "params") if self.count else GROOT_F32
+        param = {v: k for k, v in _DTYPES.items()}[self.param_dtype]
+        self.array = (_AdamwTensor * max(self.count, 1))()
+        self._tensors = {}
+        for name, tensors in lists.items():
+            if name == "grad":
+                continue
+            want = {"param": param, "m": state, "v": state}.get(name, torch.float32)
+            for i, t in enumerate(tensors):
+                n = lists["param"][i].numel()
+                self._set(name, i, t, want, -(-n // 256) if name.endswith("scale") else n)
+            self._tensors[name] = tensors
+        for i, t in enumerate(lists["param"]):
+            self.array[i].n = t.numel()
+        self.set_grads(lists["grad"])
+
+    def _set(self, name, i, t, dtype, n):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+            raise TypeError(f"{name}[{i}] must be a contiguous CUDA tensor")
+        if t.dtype != dtype:
+            raise TypeError(f"{name}[{i}] must be {dtype}")
+        if t.numel() != n:
+            raise ValueError(f"{name}[{i}] holds {t.numel()} elements, {n} are needed")
+        setattr(self.array[i], name, t.data_ptr() or None)
+
+    def set_grads(self, grads):
+        """One gradient for every parameter, of one floating type."""
+        grads = list(grads)
+        if len(grads) != self.count:
+            raise ValueError("the lists must have one tensor for every parameter")
+        self.grad_dtype = _dtype(grads[0], "grads") if self.count else GROOT_F32
+        for i, t in enumerate(grads):
+            self._set("grad", i, t, grads[0].dtype, self.array[i].n)
+        self._tensors["grad"] = grads
+
+
+def groot_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, master=None) -> AdamwTensors:
+    """Lists of contiguous CUDA tensors, one entry per parameter: params and grads float32, bfloat16 or float16 (each list of
+    one type); m, v float32, or with m_scale and v_scale (float32, one value per 256) torch.float8_e4m3fn, v then the root of
+    the second moment; master float32 or None."""
+    return AdamwTensors(params, grads, m, v, m_scale, v_scale, master)
+
+
+def groot_adamw_step(tensors: AdamwTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                     weight_decay: float = 0.01, grad_scale=None, seed: int = 0, stream=None) -> None:
+    """One step, counted from 1.  grad_scale: a CUDA float32 tensor of one element that the gradients are multiplied by."""
+    gs = None
+    if grad_scale is not None:
+        if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:
+            raise TypeError("grad_scale must be one float32")
+        gs = _dev_ptr(grad_scale, "grad_scale")
+    _check(_lib.groot_adamw_step(tensors.array, tensors.count, tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, step, lr,
+                                 beta1, beta2, eps, weight_decay, gs, seed & 0xFFFFFFFF, _stream_handle(stream)))

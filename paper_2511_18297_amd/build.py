@@ -15,8 +15,11 @@ SOURCES = [os.path.join(CSRC, "groot_host.cpp"), os.path.join(CSRC, "groot_kerne
            os.path.join(CSRC, "groot_sage_pipe.hip"), os.path.join(CSRC, "groot_compress.hip"),
            os.path.join(CSRC, "groot_hd_sched_device.hip"), os.path.join(CSRC, "groot_sage_wgrad.hip"),
            os.path.join(CSRC, "groot_pool.hip"),
-           os.path.join(CSRC, "groot_hd_dense.hip")]
-HEADERS = [os.path.join(CSRC, "groot_internal.h"), os.path.join(CSRC, "groot_device.h"),
+           os.path.join(CSRC, "groot_hd_dense.hip"), os.path.join(CSRC, "groot_dense_ops.cpp"),
+           os.path.join(CSRC, "groot_grouped.hip"), os.path.join(CSRC, "groot_int8.hip"),
+           os.path.join(CSRC, "groot_adamw.hip")]
+HEADERS = [os.path.join(CSRC, "groot_dense_ops.h"), os.path.join(CSRC, "groot_dense_device.h"),
+           os.path.join(CSRC, "groot_internal.h"), os.path.join(CSRC, "groot_device.h"),
            os.path.join(ROOT, "include", "groot.h")]
 
 
