@@ -16,6 +16,13 @@ struct RowTile {
     int64_t begin, end;                      // rows of the tile
 };
 
+// a value that is the same in every lane, as a scalar
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
 template <int kRows>
 __device__ __forceinline__ RowTile find_tile(const int64_t *__restrict__ offsets, int32_t groups, int64_t n, int64_t tile)
 {
@@ -45,8 +52,8 @@ __device__ __forceinline__ RowTile find_tile(const int64_t *__restrict__ offsets
         if (tile < before + all) {
             const int at = __popcll(__ballot(before + upto <= tile));
             const int64_t first = before + __shfl(upto, at) - __shfl(mine, at);
-            const int64_t gb = __shfl(b, at), ge = __shfl(e, at), begin = gb + (tile - first) * kRows;
-            return RowTile{g0 + at, begin, begin + kRows < ge ? begin + kRows : ge};
+            const int64_t gb = __shfl(b, at), ge = uniform(__shfl(e, at)), begin = uniform(gb + (tile - first) * kRows);
+            return RowTile{__builtin_amdgcn_readfirstlane(g0 + at), begin, begin + kRows < ge ? begin + kRows : ge};
         }
         before += all;
     }

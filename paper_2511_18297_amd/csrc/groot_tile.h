@@ -1,0 +1,282 @@
+// Matrix-core tiles shared by the grouped products and the products in 8-bit integers.
+//
+// A step of the contraction is 128 bytes of a row whose elements lie along it ("along": 64 values of 16 bits, 32 of fp32, 128 of
+// 8 bits), or as many rows of a matrix whose rows lie across it ("across").  Both operands of a step are staged in LDS by loads
+// that go there directly (16 bytes a lane, no registers), twice: one pair of tiles is computed while the next one arrives.
+//   along   row r at r * 128, its 16-byte piece c at place c ^ (r & 7): the 32 rows that a fragment reads fall on all banks
+//   across  row k of the contraction at k * width, its piece c at c ^ ((k & 3) << 1) (16-bit types): the four rows that a
+//           transposing read of 16 lanes takes fall on different banks
+// A fragment of the 32 x 32 matrix instructions is 16 bytes a lane, from row (lane & 31) and piece 2 s + (lane >> 5) of sub-step
+// s = 0 .. 3; for fp32 that is four instructions of two values of the contraction each, in an order of their own that both
+// operands share.  The operands change places (columns of the result first), so that a lane holds four neighbouring columns.
+#pragma once
+
+#include "groot_dense_device.h"
+
+namespace groot {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v16i __attribute__((ext_vector_type(16)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+typedef bf16_t v8bf __attribute__((ext_vector_type(8)));
+typedef f16_t v8h __attribute__((ext_vector_type(8)));
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+template <typename T>
+struct TileType;
+template <>
+struct TileType<bf16_t> {
+    typedef v16f Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct TileType<f16_t> {
+    typedef v16f Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct TileType<int8_t> {
+    typedef v16i Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+};
+template <>
+struct TileType<float> {
+    typedef v16f Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(a[j]), __int_as_float(b[j]), c, 0, 0, 0);
+        return c;
+    }
+};
+
+constexpr int kStepBytes = 128;
+template <typename T>
+constexpr int kStepValues = kStepBytes / (int)sizeof(T);
+
+__device__ __forceinline__ uint32_t lds_offset(const void *p) { return (uint32_t)(uintptr_t)(lds_char *)p; }
+
+// 16 bytes of every lane from its own address to LDS, lane after lane from `to` on.  The compiler does not see the load: dma_wait
+// before anything reads what arrived.  (A write to m0 needs one wait state before a load that goes by it.)
+__device__ __forceinline__ void dma16(const void *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+
+__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+static __device__ const v4i g_zeros = {0, 0, 0, 0};          // what lies past an end of the contraction
+
+// 16 bytes from any address, of which the first `valid` exist
+template <typename T>
+__device__ __forceinline__ v4i load16(const char *p, int64_t valid)
+{
+    v4i x = {0, 0, 0, 0};
+    if (valid >= 16) {
+        __builtin_memcpy(&x, p, 16);
+    } else {
+        T e[16 / sizeof(T)] = {};
+        for (int k = 0; k < (int)(16 / sizeof(T)); ++k)
+            if ((int64_t)(k * sizeof(T)) < valid) e[k] = ((const T *)p)[k];
+        __builtin_memcpy(&x, e, 16);
+    }
+    return x;
+}
+
+// One operand's tile: kWide rows ("along") or columns ("across").  begin(s) starts the loads of step s, end(s) has them in LDS once
+// the workgroup has passed a barrier.
+template <typename T, int kWide, int kThreads, bool kAcross, bool kAligned>
+struct Stage {
+    static constexpr int kBytes = kWide * kStepBytes, kEach = kBytes / 16 / kThreads;
+    static constexpr int kRowBytes = kAcross ? kWide * (int)sizeof(T) : kStepBytes, kPieces = kRowBytes / 16;
+    static constexpr int kRowsEach = kThreads / kPieces;     // rows of the tile that one load of the workgroup takes
+    static_assert(kBytes % (16 * kThreads) == 0 && kThreads % kPieces == 0, "a whole number of loads of whole rows");
+    static_assert(kAcross ? sizeof(T) == 4 || (kRowsEach % 4 == 0 && kPieces >= 8) : kRowsEach % 8 == 0, "a lane's piece is the same in all its loads");
+
+    const char *src[kAcross ? 1 : kEach];
+    int64_t pitch, limit;                                    // bytes between rows; bytes ("along") or rows ("across") of the contraction
+    int64_t width;                                           // across: bytes of a row from the lane's piece on
+    int32_t piece, row;
+    v4i held[kAligned ? 1 : kEach];
+
+    static __device__ __forceinline__ int swizzle(int r) { return kAcross ? (sizeof(T) == 2 ? (r & 3) << 1 : 0) : r & 7; }
+
+    // along: `base` is the first row's first value, `rows` rows exist, `extent` values of the contraction
+    // across: `base` is the first value of the tile's first column in the contraction's first row, `columns` columns exist
+    __device__ __forceinline__ void init(const T *base, int64_t stride, int64_t exist, int64_t extent)
+    {
+        const int tid = threadIdx.x;
+        row = tid / kPieces;
+        piece = (tid % kPieces) ^ swizzle(row);
+        pitch = stride * (int64_t)sizeof(T);
+        if (kAcross) {
+            limit = extent;
+            width = exist * (int64_t)sizeof(T) - piece * 16;
+            const int64_t last = (exist * (int64_t)sizeof(T) - 1) / 16 * 16;       // a piece past the last column reads the last one
+            src[0] = (const char *)base + row * pitch + (kAligned && width <= 0 ? last : (int64_t)piece * 16);
+        } else {
+            limit = extent * (int64_t)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {                // rows that do not exist read the last one that does
+                const int64_t r = row + i * kRowsEach;
+                src[i] = (const char *)base + (r < exist ? r : exist - 1) * pitch + piece * 16;
+            }
+        }
+    }
+
+    __device__ __forceinline__ void begin(int64_t s, char *tile)
+    {
+        const uint32_t to = lds_offset(tile) + threadIdx.x / kWave * (kWave * 16);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const char *p;
+            int64_t left;
+            if (kAcross) {
+                const int64_t k = s * kStepValues<T> + row + i * kRowsEach;
+                p = src[0] + (s * kStepValues<T> + i * kRowsEach) * pitch;
+                left = k < limit ? width : 0;
+                if (kAligned) p = k < limit ? p : (const char *)&g_zeros;
+            } else {
+                p = src[i] + s * kStepBytes;
+                left = limit - s * kStepBytes - piece * 16;
+                if (kAligned) p = left > 0 ? p : (const char *)&g_zeros;
+            }
+            if constexpr (kAligned) dma16(p, to + i * (kThreads * 16));
+            else held[i] = load16<T>(p, left);
+        }
+    }
+
+    __device__ __forceinline__ void end(char *tile)
+    {
+        if constexpr (!kAligned) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) *(v4i *)(tile + (i * kThreads + threadIdx.x) * 16) = held[i];
+        }
+    }
+
+    // the lane's 16 bytes of the 32 rows (columns) from `first` on, sub-step s
+    static __device__ __forceinline__ v4i fragment(const char *tile, int first, int s)
+    {
+        const int lane = threadIdx.x % kWave, half = lane / 32;
+        if constexpr (!kAcross) {
+            const int r = first + lane % 32;
+            return *(const v4i *)(tile + r * kStepBytes + (((2 * s + half) ^ swizzle(r)) * 16));
+        } else if constexpr (sizeof(T) == 2) {
+            // 16 lanes give the addresses of four rows of 16 columns and get a column's four values each
+            const int i = lane % 16, k = 16 * s + 8 * half + i / 4, c = (first + (lane / 16 % 2) * 16) / 8;
+            const char *p = tile + k * kRowBytes + ((c ^ swizzle(k)) * 16) + (i % 4) * 8;
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p);
+            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(p + 4 * kRowBytes));
+            return __builtin_bit_cast(v4i, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            v4i x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = *(const int *)(tile + (8 * s + 4 * half + j) * kRowBytes + (first + lane % 32) * 4);
+            return x;
+        }
+    }
+};
+
+// The product of two staged operands over `steps` steps: sums[i][j] of the wavefront's 32 x 32 blocks, rows of `A` from row0 on,
+// columns of `B` from col0 on.
+template <typename T, class StageA, class StageB, int kI, int kJ>
+__device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, int64_t steps, int row0, int col0,
+                                             typename TileType<T>::Sum (&sums)[kI][kJ])
+{
+    constexpr int kBoth = StageA::kBytes + StageB::kBytes;
+#pragma unroll
+    for (int i = 0; i < kI; ++i)
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) sums[i][j] = {};
+    if (steps <= 0) return;
+    a.begin(0, lds);
+    b.begin(0, lds + StageA::kBytes);
+    a.end(lds);
+    b.end(lds + StageA::kBytes);
+    dma_wait();
+    __syncthreads();
+    int at = 0;
+#pragma unroll 1
+    for (int64_t s = 0; s < steps; ++s) {
+        char *const now = lds + at, *const next = lds + (kBoth - at);
+        if (s + 1 < steps) {
+            a.begin(s + 1, next);
+            b.begin(s + 1, next + StageA::kBytes);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            v4i fa[kI], fb[kJ];
+#pragma unroll
+            for (int i = 0; i < kI; ++i) fa[i] = StageA::fragment(now, row0 + 32 * i, q);
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) fb[j] = StageB::fragment(now + StageA::kBytes, col0 + 32 * j, q);
+#pragma unroll
+            for (int i = 0; i < kI; ++i)
+#pragma unroll
+                for (int j = 0; j < kJ; ++j) sums[i][j] = TileType<T>::mma(fb[j], fa[i], sums[i][j]);
+        }
+        if (s + 1 < steps) {
+            a.end(next);
+            b.end(next + StageA::kBytes);
+        }
+        dma_wait();
+        __syncthreads();
+        at = kBoth - at;
+    }
+}
+
+// four neighbouring values, `left` of which exist
+template <typename O>
+__device__ __forceinline__ void store_quad(O *p, v4f x, int left, bool whole)
+{
+    typedef O v4o __attribute__((ext_vector_type(4)));
+    if (whole && left >= 4) {
+        v4o r;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = (O)x[k];          // the one rounding to the output's type
+        *(v4o *)p = r;
+    } else {
+        for (int k = 0; k < 4; ++k)
+            if (k < left) p[k] = (O)x[k];
+    }
+}
+
+// Workgroup -> tile: consecutive workgroups go to the eight XCDs in turn, so an XCD takes every eighth one.  Its workgroups are
+// numbered in blocks of `rows` x `cols` neighbouring tiles, which share their operands in its L2.
+struct TileOrder {
+    int32_t rows, cols;                      // of a block, powers of two
+    int32_t col_blocks;
+    uint32_t workgroups;
+    __host__ TileOrder(int64_t row_tiles, int32_t col_tiles)
+    {
+        int32_t block = 32;                  // workgroups that an XCD runs at a time, less where there are not enough for all XCDs
+        while (block > 1 && row_tiles * col_tiles < 8 * block) block /= 2;
+        rows = cols = 1;
+        while (rows < 4 && rows < row_tiles && rows < block) rows *= 2;
+        while (rows * cols < block && cols < col_tiles) cols *= 2;
+        while (rows * cols < block && rows < row_tiles) rows *= 2;
+        block = rows * cols;
+        col_blocks = (col_tiles + cols - 1) / cols;
+        const int64_t blocks = (row_tiles + rows - 1) / rows * col_blocks;
+        workgroups = (uint32_t)((blocks + kXcds - 1) / kXcds * kXcds * block);
+    }
+    __device__ __forceinline__ void find(uint32_t id, int64_t *row_tile, int32_t *col_tile) const
+    {
+        const uint32_t xcd = id % kXcds, seq = id / kXcds, block = rows * cols;
+        const uint32_t b = seq / block * kXcds + xcd, in = seq % block;
+        *row_tile = (int64_t)(b / col_blocks) * rows + in % rows;
+        *col_tile = (int32_t)(b % col_blocks) * cols + in / rows;
+    }
+};
+
+}  // namespace groot
