@@ -516,7 +516,7 @@ groot_status groot_feature_placement(const groot_plan *plan, void *arena_dev, si
  * 1 <= K, N <= 65536, 1 <= n_groups <= 65536, n_rows >= 0.  The calls only
  * enqueue on hip_stream and allocate nothing.  Errors: EINVAL (NULL, unknown
  * dtype, alignment, sizes, strides, overlap, workspace too small), ERANGE (more
- * than 2^31 - 1 output tiles), EHIP.
+ * output tiles than a launch holds: 2^32 lanes), EHIP.
  * ------------------------------------------------------------------------- */
 typedef enum { GROOT_F32 = 0, GROOT_BF16 = 1, GROOT_F16 = 2 } groot_dtype;
 
@@ -609,7 +609,7 @@ groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_
  * captured in a HIP graph, with the host values it was given.
  * Errors: EINVAL (NULL, unknown dtype, n < 0, state_bits, step < 1, lr or
  * weight_decay not finite or negative, beta outside [0, 1), eps not finite or <= 0), ERANGE (a tensor of
- * 2^40 values or more), EHIP.
+ * 2^34 values or more), EHIP.
  * ------------------------------------------------------------------------- */
 typedef struct {
     void *param;

@@ -234,7 +234,7 @@ void adamw_launch(const AdamwBatch &b, int32_t grad_dtype, int bits, uint32_t ch
 int launch_adamw(const groot_adamw_tensor *tensors, int64_t n_tensors, int32_t param_dtype, int32_t grad_dtype, int32_t state_bits,
                  const AdamwFactors &f, const float *grad_scale, uint32_t step, uint32_t seed, void *stream)
 {
-    constexpr uint32_t kMostChunks = 0x7FFFFFFFu;
+    constexpr uint32_t kMostChunks = (1u << 24) - 1;      // a launch holds 2^32 lanes
     AdamwBatch b;
     b.f = f;
     b.grad_scale = grad_scale;
@@ -255,7 +255,7 @@ int launch_adamw(const groot_adamw_tensor *tensors, int64_t n_tensors, int32_t p
         const groot_adamw_tensor &x = tensors[i];
         if (x.n == 0) continue;
         master = x.master != nullptr;
-        const int64_t mine = (x.n + kAdamwChunk - 1) / kAdamwChunk;              // below 2^30 for n below 2^40
+        const int64_t mine = (x.n + kAdamwChunk - 1) / kAdamwChunk;              // at most 2^23 for n below 2^34
         if (b.count == kAdamwTensors || mine > (int64_t)(kMostChunks - chunks))
             if (const int err = flush()) return err;
         chunks += (uint32_t)mine;

@@ -35,6 +35,7 @@ groot_status bad(const char *who, const char *what)
 
 groot_status launched(const char *who, int err)
 {
+    if (err == kErrTooManyTiles) return fail(GROOT_ERANGE, std::string(who) + ": more output tiles than a launch holds");
     return err ? fail(GROOT_EHIP, std::string(who) + ": launch failed: " + hip_error_text(err)) : GROOT_OK;
 }
 
@@ -55,13 +56,6 @@ groot_status check_matrix(const char *who, const char *name, const void *p, int6
     if (stride < width || stride > ((int64_t)1 << 40)) return bad(who, (std::string(name) + ": the row stride is below the width").c_str());
     if (n > 0 && stride > (((int64_t)1 << 60) / n)) return bad(who, (std::string(name) + ": stride x rows is too large").c_str());
     return GROOT_OK;
-}
-
-// the tiles of the smallest tile in use (16 x 16) in any shape fit a launch
-groot_status check_tiles(const char *who, int64_t n, int32_t groups, int64_t columns)
-{
-    const double tiles = ((double)n / 16 + groups) * (double)((columns + 15) / 16);
-    return tiles < 2147483647.0 ? GROOT_OK : fail(GROOT_ERANGE, std::string(who) + ": more than 2^31 - 1 output tiles");
 }
 
 }  // namespace
@@ -90,7 +84,6 @@ groot_status rows_product(const char *who, int32_t dtype, const void *A, int64_t
     const Span in(A, n, a_stride, K, b), to(out, n, out_stride, N, b), w(W, groups, (int64_t)K * N, (int64_t)K * N, b),
         bs(bias, bias ? groups : 0, N, N, b);
     if (to.meets(in) || to.meets(w) || to.meets(bs)) return bad(who, "the output overlaps an input");
-    GROOT_TRY(check_tiles(who, n, groups, N));
     if (n == 0) return GROOT_OK;
     RowsProduct p{A, a_stride, W, transposed, offsets, bias, nullptr, nullptr, relu != 0, out, out_stride, n, groups, K, N};
     return launched(who, launch_grouped_rows(dtype, p, stream));
@@ -167,7 +160,6 @@ extern "C" groot_status groot_grouped_product_backward_weights(int32_t dtype, co
         ws(workspace_dev, need ? 1 : 0, (int64_t)need, (int64_t)need, 1);
     if (w.meets(x) || w.meets(d) || s.meets(x) || s.meets(d) || w.meets(s)) return bad(who, "an output overlaps an input or the other output");
     if (ws.meets(x) || ws.meets(d) || ws.meets(w) || ws.meets(s)) return bad(who, "the workspace overlaps a matrix");
-    GROOT_TRY(check_tiles(who, (int64_t)n_groups * K, 1, N));
     WeightsProduct p{X_dev, dY_dev, x_stride, dy_stride, offsets_dev, dW_dev, dbias_dev, grad_dtype == GROOT_F32, n_rows, n_groups, K, N,
                      workspace_dev};
     return launched(who, launch_grouped_weights(dtype, p, hip_stream));
@@ -185,7 +177,6 @@ extern "C" groot_status groot_quantize_rows(int32_t dtype, const void *X_dev, in
     GROOT_TRY(check_matrix(who, "scale", scale_dev, n_rows, 1, 1, 4));
     const Span x(X_dev, n_rows, x_stride, K, b), q(Q_dev, n_rows, q_stride, K, 1), s(scale_dev, n_rows, 1, 1, 4);
     if (x.meets(q) || x.meets(s) || q.meets(s)) return bad(who, "two of X, Q and scale overlap");
-    GROOT_TRY(check_tiles(who, n_rows, 1, 1));
     if (n_rows == 0) return GROOT_OK;
     return launched(who, launch_quantize_rows(dtype, X_dev, x_stride, Q_dev, q_stride, scale_dev, n_rows, K, hip_stream));
 }
@@ -205,7 +196,6 @@ extern "C" groot_status groot_quantized_product(const int8_t *Q_dev, int64_t q_s
     GROOT_TRY(check_int8(who, W_dev, w_scale_dev, bias_dev, relu, Y_dev, y_stride, n_rows, n_groups, K, N, b));
     const Span to(Y_dev, n_rows, y_stride, N, b), q(Q_dev, n_rows, q_stride, K, 1), s(q_scale_dev, n_rows, 1, 1, 4);
     if (to.meets(q) || to.meets(s)) return bad(who, "Y overlaps an input");
-    GROOT_TRY(check_tiles(who, n_rows, n_groups, N));
     if (n_rows == 0) return GROOT_OK;
     RowsProduct p{Q_dev, q_stride, W_dev, true, offsets_dev, bias_dev, q_scale_dev, w_scale_dev, relu != 0, Y_dev, y_stride, n_rows,
                   n_groups, K, N};
@@ -240,7 +230,6 @@ extern "C" groot_status groot_quantized_linear(int32_t dtype, const void *X_dev,
         w(W_dev, n_groups, (int64_t)K * N, (int64_t)K * N, 1), s(w_scale_dev, n_groups, N, N, 4), bs(bias_dev, bias_dev ? n_groups : 0, N, N, 4);
     if (to.meets(x)) return bad(who, "Y overlaps an input");
     if (ws.meets(to) || ws.meets(x) || ws.meets(w) || ws.meets(s) || ws.meets(bs)) return bad(who, "the workspace overlaps another argument");
-    GROOT_TRY(check_tiles(who, n_rows, n_groups, N));
     if (n_rows == 0) return GROOT_OK;
     int8_t *Q = (int8_t *)workspace_dev;
     float *scale = (float *)(Q + (size_t)n_rows * row);
@@ -269,7 +258,7 @@ extern "C" groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int6
     for (int64_t t = 0; t < n_tensors; ++t) {
         const groot_adamw_tensor &x = tensors[t];
         if (x.n < 0) return bad(who, "a tensor's n is negative");
-        if (x.n >= ((int64_t)1 << 40)) return fail(GROOT_ERANGE, std::string(who) + ": a tensor of 2^40 values or more");
+        if (x.n >= ((int64_t)1 << 34)) return fail(GROOT_ERANGE, std::string(who) + ": a tensor of 2^34 values or more");
         if (x.n == 0) continue;
         if (!x.param || !x.grad || !x.m || !x.v) return bad(who, "a tensor with a NULL array");
         if (state_bits == 8 && (!x.m_scale || !x.v_scale)) return bad(who, "8-bit states need m_scale and v_scale");

@@ -21,7 +21,9 @@ struct RowsProduct {
     int64_t n;
     int32_t groups, K, N;
 };
-// Kernel launchers: hipError_t as int, 0 = success.
+// Kernel launchers: hipError_t as int, 0 = success; kErrTooManyTiles where a launch cannot hold them (2^32 lanes).
+constexpr int kErrTooManyTiles = -4;
+constexpr bool fits_launch(int64_t workgroups, int lanes) { return workgroups < ((int64_t)1 << 32) / lanes; }
 int launch_grouped_rows(int32_t dtype, const RowsProduct &p, void *stream);
 int launch_int8_rows(int32_t out_dtype, const RowsProduct &p, void *stream);
 int launch_quantize_rows(int32_t dtype, const void *X, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int64_t n,

@@ -5,6 +5,13 @@ namespace groot {
 
 namespace {
 
+constexpr int log2_of(int64_t x)
+{
+    int l = 0;
+    while (((int64_t)1 << l) < x) ++l;
+    return l;
+}
+
 // out[i,:] = epilogue(A[i,:] B[g]): a workgroup takes kM rows of a group and kN columns, a wavefront kM / kWavesM x kN / kWavesN
 template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, bool kNMajor, bool kAligned>
 __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const RowsProduct p, const TileOrder order, int32_t col_tiles, bool whole)
@@ -17,7 +24,7 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const Row
     int32_t col_tile;
     order.find(blockIdx.x, &row_tile, &col_tile);
     if (col_tile >= col_tiles) return;
-    const RowTile t = find_tile<kM>(p.offsets, p.groups, p.n, row_tile);
+    const RowTile t = find_tile(p.offsets, p.groups, p.n, row_tile, log2_of(kM));
     if (t.group < 0) return;
     const int32_t j0 = col_tile * kN;
     const int64_t rows = t.end - t.begin;
@@ -76,8 +83,9 @@ int rows_launch(const RowsProduct &p, void *stream)
     const bool aligned = on16(p.A, p.a_stride * b) && on16(p.B, (kNMajor ? p.K : p.N) * b) && p.K * b % 16 == 0;
     const bool whole = (((uintptr_t)p.out | (uintptr_t)(p.out_stride * sizeof(O))) & (4 * sizeof(O) - 1)) == 0;
     constexpr int kThreads = kWavesM * kWavesN * kWave;
-    if (aligned) rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kNMajor, true><<<order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
-    else rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kNMajor, false><<<order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
+    if (!fits_launch(order.workgroups, kThreads)) return kErrTooManyTiles;
+    if (aligned) rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kNMajor, true><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
+    else rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kNMajor, false><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
     return (int)hipGetLastError();
 }
 
@@ -91,26 +99,67 @@ int rows_choose(const RowsProduct &p, void *stream)
     return rows_launch<T, O, 32, 128, 1, 4, kNMajor>(p, stream);
 }
 
-// dW[g] = X_g^T dY_g: a workgroup takes kK x kN of one group's product and walks over the group's rows
+// How the contraction of the weight gradients, a group's rows, is cut: pieces of 2^log_rows rows, so that their number times that of
+// the tiles of dW comes to about 1024 workgroups.  A piece of 512 rows reads eight times what its partial sums are written and read
+// again for.  A group of one piece needs no partial sums.
+struct WeightsSplit {
+    int log_rows;
+    int64_t tiles;                           // pieces of all groups, at most
+    int64_t slots;                           // pieces of groups that are cut, at most
+    WeightsSplit(int64_t n, int32_t groups, bool offsets, int64_t dw_tiles)
+    {
+        log_rows = 9;
+        while (log_rows < 40 && ((int64_t)1024 << log_rows) < n * dw_tiles) ++log_rows;
+        const int64_t rows = (int64_t)1 << log_rows;
+        tiles = (n + rows - 1) / rows + (offsets ? groups : 0);
+        if (tiles < 1) tiles = 1;
+        slots = n <= rows ? 0 : 2 * (n / rows);
+        if (slots > tiles) slots = tiles;
+    }
+};
+
+struct WeightsTile {
+    int32_t k, n;
+};
+// 64 x 64 where dW is no larger (typed layers); 128 x 128
+WeightsTile weights_tile(int32_t K, int32_t N) { return K <= 64 && N <= 64 ? WeightsTile{64, 64} : WeightsTile{128, 128}; }
+
+WeightsSplit weights_split(int64_t n, int32_t groups, bool offsets, int32_t K, int32_t N)
+{
+    const WeightsTile t = weights_tile(K, N);
+    return WeightsSplit(n, groups, offsets, (int64_t)((K + t.k - 1) / t.k) * ((N + t.n - 1) / t.n));
+}
+
+// dW[g] = X_g^T dY_g and the column sums of dY_g: a workgroup takes kK x kN of one group's product and one piece of the group's
+// rows.  The partial sums of a group in several pieces lie in the workspace, piece after piece, K x N and N floats each.
 template <typename T, typename O, int kK, int kN, int kWavesK, int kWavesN, bool kAligned>
-__global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const WeightsProduct p, int32_t k_tiles, int32_t n_tiles)
+__global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const WeightsProduct p, const TileOrder order, int log_rows, int64_t slots,
+                                                                         int32_t k_tiles, int32_t n_tiles)
 {
     constexpr int kThreads = kWavesK * kWavesN * kWave, kI = kK / kWavesK / 32, kJ = kN / kWavesN / 32;
     typedef Stage<T, kK, kThreads, true, kAligned> StageX;
     typedef Stage<T, kN, kThreads, true, kAligned> StageY;
     __shared__ __align__(16) char lds[2 * (StageX::kBytes + StageY::kBytes)];
-    const int32_t n0 = (int32_t)(blockIdx.x % n_tiles) * kN, k0 = (int32_t)(blockIdx.x / n_tiles % k_tiles) * kK;
-    const int32_t g = (int32_t)(blockIdx.x / n_tiles / k_tiles);
-    int64_t begin, end;
-    group_rows(p.offsets, p.n, g, &begin, &end);
+    int64_t row_tile;
+    int32_t n_tile;
+    order.find(blockIdx.x, &row_tile, &n_tile);
+    if (n_tile >= n_tiles) return;
+    const RowTile t = find_tile<true>(p.offsets, p.groups, p.n, row_tile / k_tiles, log_rows);
+    if (t.group < 0) return;
+    const int32_t n0 = n_tile * kN, k0 = (int32_t)(row_tile % k_tiles) * kK;
     StageX x;
     StageY y;
-    x.init((const T *)p.X + begin * p.x_stride + k0, p.x_stride, p.K - k0, end - begin);
-    y.init((const T *)p.dY + begin * p.dy_stride + n0, p.dy_stride, p.N - n0, end - begin);
+    x.init((const T *)p.X + t.begin * p.x_stride + k0, p.x_stride, p.K - k0, t.end - t.begin);
+    y.init((const T *)p.dY + t.begin * p.dy_stride + n0, p.dy_stride, p.N - n0, t.end - t.begin);
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int row0 = wave / kWavesN * (kK / kWavesK), col0 = wave % kWavesN * (kN / kWavesN);
     typename TileType<T>::Sum sums[kI][kJ];
-    tile_product<T>(x, y, lds, (end - begin + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums);
+    float columns[kJ] = {};
+    const bool bias = p.dbias && k0 == 0 && row0 == 0;
+    tile_product<T, true>(x, y, lds, (t.end - t.begin + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums, &columns, bias);
+    const bool alone = t.count == 1;
+    if (!alone && t.shared_before + t.place >= slots) return;   // offsets that do not ascend: more pieces than there are rows for
+    float *const part = (float *)p.workspace + (t.shared_before + t.place) * ((int64_t)p.K * p.N + p.N);
     const bool whole = p.N % 4 == 0 && ((uintptr_t)p.dW & (4 * sizeof(O) - 1)) == 0;
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
@@ -123,44 +172,97 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
                 const int32_t n = n0 + col0 + 32 * j + 8 * q + 4 * (lane / 32);
                 if (n >= p.N) continue;
                 const v4f v = {sums[i][j][4 * q], sums[i][j][4 * q + 1], sums[i][j][4 * q + 2], sums[i][j][4 * q + 3]};
-                store_quad((O *)p.dW + ((int64_t)g * p.K + k) * p.N + n, v, p.N - n, whole);
+                if (alone) store_quad((O *)p.dW + ((int64_t)t.group * p.K + k) * p.N + n, v, p.N - n, whole);
+                else store_quad(part + (int64_t)k * p.N + n, v, p.N - n, p.N % 4 == 0);
             }
+    }
+    if (bias) {
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) {
+            const float s = columns[j] + __shfl_xor(columns[j], 32);
+            const int32_t n = n0 + col0 + 32 * j + lane % 32;
+            if (lane >= 32 || n >= p.N) continue;
+            if (alone) ((O *)p.dbias)[(int64_t)t.group * p.N + n] = (O)s;
+            else part[(int64_t)p.K * p.N + n] = s;
+        }
     }
 }
 
-// dbias[g] = column sums of dY_g: 64 columns to a workgroup, its wavefronts take every fourth row
-template <typename T, typename O>
-__global__ __launch_bounds__(kBlock) void bias_kernel(const WeightsProduct p, int32_t n_tiles)
+// The partial sums of groups in several pieces, added up in fp64 piece after piece (every wavefront of a workgroup a share of them,
+// then the shares), and the zeros of empty groups.  A lane takes four neighbouring values; dbias lies behind dW.
+template <typename O>
+__global__ __launch_bounds__(1024) void weights_sum_kernel(const WeightsProduct p, int log_rows, int64_t slots, uint32_t parts)
 {
-    __shared__ float part[kWavesPerBlock][kWave];
-    const int32_t n = (int32_t)(blockIdx.x % n_tiles) * kWave + threadIdx.x % kWave, g = (int32_t)(blockIdx.x / n_tiles);
-    int64_t begin, end;
+    typedef double v4d __attribute__((ext_vector_type(4)));
+    __shared__ v4d shares[16][kWave];
+    const int32_t g = (int32_t)(blockIdx.x / parts);
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    const int64_t rows = (int64_t)1 << log_rows;
+    int64_t begin, end, before = 0;
     group_rows(p.offsets, p.n, g, &begin, &end);
-    float s = 0.f;
-    if (n < p.N)
-        for (int64_t r = begin + threadIdx.x / kWave; r < end; r += kWavesPerBlock) s += (float)((const T *)p.dY)[r * p.dy_stride + n];
-    part[threadIdx.x / kWave][threadIdx.x % kWave] = s;
-    __syncthreads();
-    if (threadIdx.x < kWave && n < p.N) {
-        for (int w = 1; w < kWavesPerBlock; ++w) s += part[w][threadIdx.x];
-        ((O *)p.dbias)[(int64_t)g * p.N + n] = (O)s;
+    int64_t count = (end - begin + rows - 1) >> log_rows;
+    if (count == 1) return;
+    if (count > 1)
+        for (int32_t g0 = 0; g0 < g; g0 += kWave) {
+            int64_t b = 0, e = 0;
+            if (g0 + lane < g) group_rows(p.offsets, p.n, g0 + lane, &b, &e);
+            const int64_t c = (e - b + rows - 1) >> log_rows;
+            before += __shfl(sum_upto(c > 1 ? c : 0), kWave - 1);
+        }
+    count = before + count <= slots ? count : before < slots ? slots - before : 0;
+    const int64_t dw = (int64_t)p.K * p.N, slot = dw + p.N, at = ((int64_t)(blockIdx.x % parts) * kWave + lane) * 4;
+    const int64_t values = p.dbias ? slot : dw;
+    v4d sum = {0, 0, 0, 0};
+    const float *from = (const float *)p.workspace + before * slot + at;
+    if (slot % 4 == 0 && at + 4 <= values) {
+#pragma unroll 4
+        for (int64_t c = wave; c < count; c += waves) {
+            const v4f x = *(const v4f *)(from + c * slot);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += (double)x[k];
+        }
+    } else {
+        for (int64_t c = wave; c < count; c += waves)
+            for (int k = 0; k < 4; ++k)
+                if (at + k < values) sum[k] += (double)from[c * slot + k];
     }
+    shares[wave][lane] = sum;
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < waves; ++w) sum += shares[w][lane];
+    for (int k = 0; k < 4; ++k) {
+        const int64_t i = at + k;
+        if (i < dw) ((O *)p.dW)[g * dw + i] = (O)(float)sum[k];
+        else if (i < values) ((O *)p.dbias)[(int64_t)g * p.N + (i - dw)] = (O)(float)sum[k];
+    }
+}
+
+template <typename T, typename O, int kK, int kN>
+int weights_launch_tile(const WeightsProduct &p, const WeightsSplit &split, bool aligned, hipStream_t stream)
+{
+    const int32_t k_tiles = (p.K + kK - 1) / kK, n_tiles = (p.N + kN - 1) / kN;
+    const TileOrder order(split.tiles * k_tiles, n_tiles);
+    if (!fits_launch(order.workgroups, kBlock)) return kErrTooManyTiles;
+    if (aligned) weights_kernel<T, O, kK, kN, 2, 2, true><<<(uint32_t)order.workgroups, kBlock, 0, stream>>>(p, order, split.log_rows, split.slots, k_tiles, n_tiles);
+    else weights_kernel<T, O, kK, kN, 2, 2, false><<<(uint32_t)order.workgroups, kBlock, 0, stream>>>(p, order, split.log_rows, split.slots, k_tiles, n_tiles);
+    return (int)hipGetLastError();
 }
 
 template <typename T, typename O>
 int weights_launch(const WeightsProduct &p, void *stream)
 {
-    constexpr int kK = 128, kN = 128;
-    const int32_t k_tiles = (p.K + kK - 1) / kK, n_tiles = (p.N + kN - 1) / kN;
     const int64_t b = sizeof(T);
     const bool aligned = on16(p.X, p.x_stride * b) && on16(p.dY, p.dy_stride * b) && p.K * b % 16 == 0 && p.N * b % 16 == 0;
-    const uint32_t blocks = (uint32_t)((int64_t)p.groups * k_tiles * n_tiles);
-    if (aligned) weights_kernel<T, O, kK, kN, 2, 2, true><<<blocks, kBlock, 0, (hipStream_t)stream>>>(p, k_tiles, n_tiles);
-    else weights_kernel<T, O, kK, kN, 2, 2, false><<<blocks, kBlock, 0, (hipStream_t)stream>>>(p, k_tiles, n_tiles);
-    if (p.dbias) {
-        const int32_t tiles = (p.N + kWave - 1) / kWave;
-        bias_kernel<T, O><<<(uint32_t)((int64_t)p.groups * tiles), kBlock, 0, (hipStream_t)stream>>>(p, tiles);
-    }
+    const WeightsSplit split = weights_split(p.n, p.groups, p.offsets != nullptr, p.K, p.N);
+    const hipStream_t s = (hipStream_t)stream;
+    const int err = weights_tile(p.K, p.N).k == 64 ? weights_launch_tile<T, O, 64, 64>(p, split, aligned, s)
+                                                   : weights_launch_tile<T, O, 128, 128>(p, split, aligned, s);
+    if (err) return err;
+    const uint32_t parts = (uint32_t)(((int64_t)p.K * p.N + p.N + 4 * kWave - 1) / (4 * kWave));
+    int waves = 1;                                           // as many as a group has pieces, on average
+    while (waves < 16 && waves * p.groups < split.tiles) waves *= 2;
+    if (!fits_launch((int64_t)parts * p.groups, waves * kWave)) return kErrTooManyTiles;
+    weights_sum_kernel<O><<<parts * (uint32_t)p.groups, waves * kWave, 0, s>>>(p, split.log_rows, split.slots, parts);
     return (int)hipGetLastError();
 }
 
@@ -180,7 +282,12 @@ int launch_int8_rows(int32_t out_dtype, const RowsProduct &p, void *stream)
     return rows_choose<int8_t, f16_t, true>(p, stream);
 }
 
-size_t grouped_weights_workspace(int32_t, int64_t, int32_t, int32_t, int32_t) { return 0; }
+size_t grouped_weights_workspace(int32_t, int64_t n, int32_t groups, int32_t K, int32_t N)
+{
+    // whether the call will have offsets is not known here: without, there is one group and no more pieces than with
+    const WeightsSplit split = weights_split(n, groups, true, K, N);
+    return (size_t)split.slots * ((size_t)K * N + N) * 4;
+}
 
 int launch_grouped_weights(int32_t dtype, const WeightsProduct &p, void *stream)
 {

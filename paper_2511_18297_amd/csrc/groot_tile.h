@@ -30,6 +30,12 @@ struct TileType;
 template <>
 struct TileType<bf16_t> {
     typedef v16f Sum;
+    // the sum of a fragment's values
+    static __device__ __forceinline__ float total(v4i a)
+    {
+        const v8bf x = __builtin_bit_cast(v8bf, a);
+        return (((float)x[0] + (float)x[1]) + ((float)x[2] + (float)x[3])) + (((float)x[4] + (float)x[5]) + ((float)x[6] + (float)x[7]));
+    }
     static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
@@ -38,6 +44,11 @@ struct TileType<bf16_t> {
 template <>
 struct TileType<f16_t> {
     typedef v16f Sum;
+    static __device__ __forceinline__ float total(v4i a)
+    {
+        const v8h x = __builtin_bit_cast(v8h, a);
+        return (((float)x[0] + (float)x[1]) + ((float)x[2] + (float)x[3])) + (((float)x[4] + (float)x[5]) + ((float)x[6] + (float)x[7]));
+    }
     static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
@@ -51,6 +62,10 @@ struct TileType<int8_t> {
 template <>
 struct TileType<float> {
     typedef v16f Sum;
+    static __device__ __forceinline__ float total(v4i a)
+    {
+        return (__int_as_float(a[0]) + __int_as_float(a[1])) + (__int_as_float(a[2]) + __int_as_float(a[3]));
+    }
     static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
     {
 #pragma unroll
@@ -188,10 +203,11 @@ struct Stage {
 };
 
 // The product of two staged operands over `steps` steps: sums[i][j] of the wavefront's 32 x 32 blocks, rows of `A` from row0 on,
-// columns of `B` from col0 on.
-template <typename T, class StageA, class StageB, int kI, int kJ>
+// columns of `B` from col0 on.  `columns` (where kColumns; wavefronts with `mine`): the sums of B's values, lanes l and l + 32 hold
+// the two halves of column l.
+template <typename T, bool kColumns = false, class StageA, class StageB, int kI, int kJ>
 __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, int64_t steps, int row0, int col0,
-                                             typename TileType<T>::Sum (&sums)[kI][kJ])
+                                             typename TileType<T>::Sum (&sums)[kI][kJ], float (*columns)[kJ] = nullptr, bool mine = false)
 {
     constexpr int kBoth = StageA::kBytes + StageB::kBytes;
 #pragma unroll
@@ -224,6 +240,12 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
             for (int i = 0; i < kI; ++i)
 #pragma unroll
                 for (int j = 0; j < kJ; ++j) sums[i][j] = TileType<T>::mma(fb[j], fa[i], sums[i][j]);
+            if constexpr (kColumns) {
+                if (mine) {
+#pragma unroll
+                    for (int j = 0; j < kJ; ++j) (*columns)[j] += TileType<T>::total(fb[j]);
+                }
+            }
         }
         if (s + 1 < steps) {
             a.end(next);
@@ -256,7 +278,7 @@ __device__ __forceinline__ void store_quad(O *p, v4f x, int left, bool whole)
 struct TileOrder {
     int32_t rows, cols;                      // of a block, powers of two
     int32_t col_blocks;
-    uint32_t workgroups;
+    int64_t workgroups;
     __host__ TileOrder(int64_t row_tiles, int32_t col_tiles)
     {
         int32_t block = 32;                  // workgroups that an XCD runs at a time, less where there are not enough for all XCDs
@@ -268,7 +290,7 @@ struct TileOrder {
         block = rows * cols;
         col_blocks = (col_tiles + cols - 1) / cols;
         const int64_t blocks = (row_tiles + rows - 1) / rows * col_blocks;
-        workgroups = (uint32_t)((blocks + kXcds - 1) / kXcds * kXcds * block);
+        workgroups = (blocks + kXcds - 1) / kXcds * kXcds * block;
     }
     __device__ __forceinline__ void find(uint32_t id, int64_t *row_tile, int32_t *col_tile) const
     {

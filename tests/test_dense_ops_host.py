@@ -115,7 +115,7 @@ def test_workspaces():
     assert L.groot_grouped_product_backward_weights_workspace(0, 10, 1, 8, 8, None) == G.GROOT_EINVAL
     assert L.groot_quantized_linear_workspace(10, 0, ctypes.byref(b)) == G.GROOT_EINVAL and b.value == 77
     assert G.groot_quantized_linear_workspace(10, 64) == 10 * 68
-    need = G.groot_grouped_product_backward_weights_workspace(1 << 20, 3, 64, 64, torch.float32)
+    need = G.groot_grouped_product_backward_weights_workspace(1 << 20, 3, 64, 32, torch.float32)   # the sizes of weights()
     if need:
         assert weights(dtype=0, n=1 << 20, wb=need - 1, X=1 << 40, dY=1 << 42) == G.GROOT_EINVAL
 

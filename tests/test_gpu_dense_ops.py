@@ -74,6 +74,8 @@ SHAPES = [
     ([1100, 20], 520, 264, 8),
     ([16] * 70, 40, 24, 0),
     ([5] * 5 + [0] * 200 + [90], 72, 80, 0),
+    ([40, 0, 5000, 1, 2100], 64, 48, 0),
+    ([9000], 20, 12, 0),
 ]
 
 
@@ -219,6 +221,20 @@ def test_values_that_are_not_finite_stay_in_their_row(kind, n, K):
     dy[:n - 1, 8:72] = 1
     G.groot_grouped_product_backward_weights(inner, dy[:n, 8:72], offsets, dW, None, work)
     assert torch.isfinite(dW).all()
+
+
+def test_offsets_that_do_not_ascend_stay_in_bounds():
+    """groups that overlap ask for more pieces than the rows have room for: nothing beyond the workspace or the outputs is written"""
+    n, K, N = 5000, 64, 64
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    X, dY = matrix(gen, n, K, torch.bfloat16), matrix(gen, n, N, torch.bfloat16)
+    offsets = torch.tensor([0, n] * 20 + [0], device="cuda")
+    need = G.groot_grouped_product_backward_weights_workspace(n, 40, K, N, torch.bfloat16)
+    work = torch.full((need + 4096,), 7, dtype=torch.uint8, device="cuda")
+    dW = torch.empty((40, K, N), device="cuda")
+    G.groot_grouped_product_backward_weights(X, dY, offsets, dW, None, work)
+    assert (work[need:] == 7).all()
 
 
 def test_rows_far_apart():
