@@ -49,20 +49,23 @@ __device__ __forceinline__ void group_rows(const int64_t *__restrict__ offsets, 
     *end = e;
 }
 
-template <bool kShared = false>
+// kAtLeastOne: a group without rows has a tile all the same
+template <bool kShared = false, bool kAtLeastOne = false>
 __device__ __forceinline__ RowTile find_tile(const int64_t *__restrict__ offsets, int32_t groups, int64_t n, int64_t tile, int log_rows)
 {
     const int64_t rows = (int64_t)1 << log_rows;
     if (!offsets) {
         const int64_t begin = tile << log_rows;
-        return RowTile{begin < n ? 0 : -1, begin, begin + rows < n ? begin + rows : n, tile, (n + rows - 1) >> log_rows, 0};
+        const int64_t count = (n + rows - 1) >> log_rows;
+        return RowTile{begin < n || (kAtLeastOne && tile == 0) ? 0 : -1, begin, begin + rows < n ? begin + rows : n, tile, kAtLeastOne && n == 0 ? 1 : count, 0};
     }
     const int lane = threadIdx.x % kWave;
     int64_t before = 0, shared = 0;
     for (int32_t g0 = 0; g0 < groups; g0 += kWave) {
         int64_t b = 0, e = 0;
         if (g0 + lane < groups) group_rows(offsets, n, g0 + lane, &b, &e);
-        const int64_t mine = (e - b + rows - 1) >> log_rows;
+        const int64_t tiles = (e - b + rows - 1) >> log_rows;
+        const int64_t mine = kAtLeastOne && tiles == 0 && g0 + lane < groups ? 1 : tiles;
         const int64_t upto = sum_upto(mine), all = __shfl(upto, kWave - 1);
         const int64_t shared_upto = kShared ? sum_upto(mine > 1 ? mine : 0) : 0;
         if (tile < before + all) {

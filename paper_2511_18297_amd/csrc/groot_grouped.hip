@@ -5,6 +5,8 @@ namespace groot {
 
 namespace {
 
+constexpr int kLdsBytes = 160 * 1024;
+
 constexpr int log2_of(int64_t x)
 {
     int l = 0;
@@ -12,14 +14,70 @@ constexpr int log2_of(int64_t x)
     return l;
 }
 
+// The epilogue of a wavefront's 32 x 32 blocks.  A lane's four neighbouring columns of one row would make stores of 16 bytes in 32
+// rows; the block goes through 4 KB of the wavefront's LDS (16-byte pieces at c ^ (row & 7)), and every store covers eight rows of 32
+// whole columns.  A lane keeps one place in the columns, with its bias and scales, for all rows.
+template <typename T, typename O, int kJ>
+struct Epilogue {
+    v4f bias[kJ], scale[kJ];
+    int32_t col[kJ];
+
+    __device__ __forceinline__ void init(const RowsProduct &p, int32_t group, int32_t first)
+    {
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) {
+            col[j] = first + 32 * j + threadIdx.x % 8 * 4;
+            const int64_t of = (int64_t)group * p.N + col[j];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool in = col[j] + k < p.N;
+                scale[j][k] = std::is_same<T, int8_t>::value && in ? p.b_scale[of + k] : 1.f;
+                bias[j][k] = !p.bias || !in ? 0.f : std::is_same<T, int8_t>::value ? ((const float *)p.bias)[of + k] : (float)((const O *)p.bias)[of + k];
+            }
+        }
+    }
+
+    // rows from `row` of the output on, of which `rows` exist
+    __device__ __forceinline__ void store(const RowsProduct &p, char *scratch, const typename TileType<T>::Sum (&sums)[kJ], int64_t row, int64_t rows, bool whole)
+    {
+        const int lane = threadIdx.x % kWave, m = lane % 32, half = lane / 32;
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const v4f x = {(float)sums[j][4 * q], (float)sums[j][4 * q + 1], (float)sums[j][4 * q + 2], (float)sums[j][4 * q + 3]};
+                *(v4f *)(scratch + m * 128 + (((2 * q + half) ^ (m & 7)) * 16)) = x;
+            }
+            wave_sync();
+            const int32_t left = p.N - col[j];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 8 * i + lane / 8;
+                v4f y = *(const v4f *)(scratch + r * 128 + ((lane % 8 ^ lane / 8) * 16));
+                if (r < rows && left > 0) {
+                    const float s = std::is_same<T, int8_t>::value ? p.a_scale[row + r] : 1.f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (std::is_same<T, int8_t>::value) y[k] = y[k] * s * scale[j][k];
+                        if (p.bias) y[k] += bias[j][k];
+                        if (p.relu && y[k] < 0.f) y[k] = 0.f;
+                    }
+                    store_quad((O *)p.out + (row + r) * p.out_stride + col[j], y, left, whole);
+                }
+            }
+            wave_sync();
+        }
+    }
+};
+
 // out[i,:] = epilogue(A[i,:] B[g]): a workgroup takes kM rows of a group and kN columns, a wavefront kM / kWavesM x kN / kWavesN
-template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, bool kNMajor, bool kAligned>
+template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kNMajor, bool kAligned>
 __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const RowsProduct p, const TileOrder order, int32_t col_tiles, bool whole)
 {
     constexpr int kThreads = kWavesM * kWavesN * kWave, kI = kM / kWavesM / 32, kJ = kN / kWavesN / 32;
     typedef Stage<T, kM, kThreads, false, kAligned> StageA;
     typedef Stage<T, kN, kThreads, !kNMajor, kAligned> StageB;
-    __shared__ __align__(16) char lds[2 * (StageA::kBytes + StageB::kBytes)];
+    __shared__ __align__(16) char lds[(kAligned ? kStages : 2) * (StageA::kBytes + StageB::kBytes)];
     int64_t row_tile;
     int32_t col_tile;
     order.find(blockIdx.x, &row_tile, &col_tile);
@@ -34,47 +92,128 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const Row
     a.init((const T *)p.A + t.begin * p.a_stride, p.a_stride, rows, p.K);
     if (kNMajor) b.init(B + (int64_t)j0 * p.K, p.K, p.N - j0, p.K);
     else b.init(B + j0, p.N, p.N - j0, p.K);
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int wave = threadIdx.x / kWave;
     const int row0 = wave / kWavesN * (kM / kWavesM), col0 = wave % kWavesN * (kN / kWavesN);
     typename TileType<T>::Sum sums[kI][kJ];
-    tile_product<T>(a, b, lds, (p.K + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums);
+    tile_product<T, kStages>(a, b, lds, (p.K + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums);
+    __syncthreads();                                         // LDS is free
+    Epilogue<T, O, kJ> epilogue;
+    epilogue.init(p, t.group, j0 + col0);
 #pragma unroll
-    for (int j = 0; j < kJ; ++j)
+    for (int i = 0; i < kI; ++i) {
+        const int64_t r = row0 + 32 * i;
+        epilogue.store(p, lds + wave * 4096, sums[i], t.begin + r, rows - r, whole);
+    }
+}
+
+// Typed layers: rows of at most 512 bytes, at most 128 columns.  A workgroup takes 2^log_rows rows of one group and keeps the group's
+// weights in LDS; its wavefronts walk over blocks of 32 rows on their own, without a barrier: every one has kStages steps of rows
+// on their way or in LDS, across the blocks' borders.
+// Bound by HBM (64 x 64 in fp32: 512 bytes and 8192 operations a row).
+constexpr int kNarrowBytes = 512, kNarrowRows = 32, kNarrowStage = kNarrowRows * kStepBytes;
+
+template <typename T, typename O, int kN, int kWaves, int kStages, bool kNMajor, bool kAligned>
+__global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct p, int log_rows, int32_t steps, bool whole)
+{
+    constexpr int kThreads = kWaves * kWave, kJ = kN / 32, kEach = kNarrowStage / 16 / kWave;
+    typedef Stage<T, kN, kThreads, !kNMajor, kAligned> StageB;
+    typedef Stage<T, kNarrowRows, kThreads, false, kAligned> Rows;       // its layout in LDS
+    extern __shared__ __align__(16) char lds[];              // weights, then every wavefront's steps
+    const RowTile t = find_tile(p.offsets, p.groups, p.n, blockIdx.x, log_rows);
+    if (t.group < 0) return;
+    const T *B = (const T *)p.B + (int64_t)t.group * p.K * p.N;
+    StageB b;
+    b.init(B, kNMajor ? p.K : p.N, p.N, p.K);
+    for (int s = 0; s < steps; ++s) {
+        b.begin(s, lds + s * StageB::kBytes);
+        b.end(lds + s * StageB::kBytes);
+    }
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    char *const ring = lds + steps * StageB::kBytes + wave * (kStages * kNarrowStage);
+    const int64_t rows = t.end - t.begin, pitch = p.a_stride * (int64_t)sizeof(T);
+    const int32_t blocks = (int32_t)((rows + kNarrowRows - 1) / kNarrowRows), mine = (blocks - wave + kWaves - 1) / kWaves;
+    const int32_t bytes = p.K * (int32_t)sizeof(T), items = mine * steps;
+    const int own = lane / 8, piece = (lane % 8 ^ own) * 16;
+    const char *const from = (const char *)((const T *)p.A + t.begin * p.a_stride) + piece;
+    v4i held[kAligned ? 1 : kEach];
+    // the next step to load: its block of rows and its place in the rows
+    int32_t load_block = wave, load_step = 0;
+    auto begin = [&](int slot) {
+        const int64_t row = (int64_t)load_block * kNarrowRows + own;
+        const int32_t left = load_block < blocks ? bytes - load_step * kStepBytes - piece : 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            int64_t r = row + 8 * i;
+            r = r < rows ? r : rows - 1;
+            const char *q = from + r * pitch + load_step * kStepBytes;
+            if constexpr (kAligned) dma16(left > 0 ? q : (const char *)&g_zeros, lds_offset(ring) + slot * kNarrowStage + i * (kWave * 16));
+            else held[i] = load16<T>(q, left);
+        }
+        if (++load_step == steps) {
+            load_step = 0;
+            load_block += kWaves;
+        }
+    };
+    Epilogue<T, O, kJ> epilogue;
+    epilogue.init(p, t.group, 0);
+    dma_wait();
+    __syncthreads();                                         // the weights are there
+    if (mine <= 0) return;
+    if constexpr (kAligned) {
+#pragma unroll
+        for (int k = 0; k < kStages - 1; ++k) begin(k);
+    } else {
+        begin(0);
+    }
+    typename TileType<T>::Sum sums[1][kJ];
+    int now = 0, next = kStages - 1;
+    int32_t s = 0, block = wave;
+#pragma unroll 1
+    for (int32_t item = 0; item < items; ++item) {
+        if constexpr (kAligned) {
+            // the stores of the last block are among what is waited for where they were issued late enough: less depth, not less safety
+            dma_wait<(kStages - 2) * kEach>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments of the step before have left its place
+            begin(next);
+        } else {
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) *(v4i *)(ring + now * kNarrowStage + (i * kWave + lane) * 16) = held[i];
+            wave_sync();
+            begin(0);
+        }
+        if (s == 0) {
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) sums[0][j] = {};
+        }
+        const char *const a = ring + now * kNarrowStage, *const w = lds + s * StageB::kBytes;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int32_t col = j0 + col0 + 32 * j + 8 * q + 4 * (lane / 32), left = p.N - col;
-            if (left <= 0) continue;
-            const int64_t of = (int64_t)t.group * p.N + col;
-            v4f bias = {0.f, 0.f, 0.f, 0.f}, scale = {1.f, 1.f, 1.f, 1.f};
+            if (s * kStepBytes + q * 32 >= bytes) break;
+            const v4i fa = Rows::fragment(a, 0, q);
+            v4i fb[kJ];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k >= left) break;
-                if (std::is_same<T, int8_t>::value) {
-                    scale[k] = p.b_scale[of + k];
-                    if (p.bias) bias[k] = ((const float *)p.bias)[of + k];
-                } else if (p.bias) bias[k] = (float)((const O *)p.bias)[of + k];
-            }
+            for (int j = 0; j < kJ; ++j) fb[j] = StageB::fragment(w, 32 * j, q);
 #pragma unroll
-            for (int i = 0; i < kI; ++i) {
-                const int64_t r = row0 + 32 * i + lane % 32;
-                if (r >= rows) continue;
-                const int64_t row = t.begin + r;
-                v4f y;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    y[k] = (float)sums[i][j][4 * q + k];
-                    if (std::is_same<T, int8_t>::value) y[k] = y[k] * p.a_scale[row] * scale[k];
-                    if (p.bias) y[k] += bias[k];
-                    if (p.relu && y[k] < 0.f) y[k] = 0.f;
-                }
-                store_quad((O *)p.out + row * p.out_stride + col, y, left, whole);
-            }
+            for (int j = 0; j < kJ; ++j) sums[0][j] = TileType<T>::mma(fb[j], fa, sums[0][j]);
         }
+        if (++s == steps) {
+            const int64_t r = (int64_t)block * kNarrowRows;  // through the place of this step, which is loaded again at the next one
+            epilogue.store(p, ring + now * kNarrowStage, sums[0], t.begin + r, rows - r, whole);
+            s = 0;
+            block += kWaves;
+        }
+        if constexpr (kAligned) {
+            now = now + 1 == kStages ? 0 : now + 1;
+            next = next + 1 == kStages ? 0 : next + 1;
+        }
+    }
+    if constexpr (kAligned) dma_wait();
 }
 
 bool on16(const void *a, int64_t bytes) { return (((uintptr_t)a | (uintptr_t)bytes) & 15) == 0; }
 
-template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, bool kNMajor>
+template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kNMajor>
 int rows_launch(const RowsProduct &p, void *stream)
 {
     const int32_t col_tiles = (p.N + kN - 1) / kN;
@@ -84,24 +223,52 @@ int rows_launch(const RowsProduct &p, void *stream)
     const bool whole = (((uintptr_t)p.out | (uintptr_t)(p.out_stride * sizeof(O))) & (4 * sizeof(O) - 1)) == 0;
     constexpr int kThreads = kWavesM * kWavesN * kWave;
     if (!fits_launch(order.workgroups, kThreads)) return kErrTooManyTiles;
-    if (aligned) rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kNMajor, true><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
-    else rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kNMajor, false><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
+    if (aligned) rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kStages, kNMajor, true><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
+    else rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kStages, kNMajor, false><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
     return (int)hipGetLastError();
+}
+
+template <typename T, typename O, int kN, int kWaves, int kStages, bool kNMajor, bool kAligned>
+int narrow_launch_as(const RowsProduct &p, int log_rows, int32_t steps, bool whole, void *stream)
+{
+    const int64_t workgroups = ((p.n - 1) >> log_rows) + 1 + (p.offsets ? p.groups : 0);
+    const size_t bytes = (size_t)steps * kN * kStepBytes + (size_t)kWaves * kStages * kNarrowStage;
+    if (!fits_launch(workgroups, kWaves * kWave)) return kErrTooManyTiles;
+    auto kernel = narrow_kernel<T, O, kN, kWaves, kStages, kNMajor, kAligned>;
+    static const hipError_t most = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+    if (most != hipSuccess) return (int)most;
+    kernel<<<(uint32_t)workgroups, kWaves * kWave, bytes, (hipStream_t)stream>>>(p, log_rows, steps, whole);
+    return (int)hipGetLastError();
+}
+
+template <typename T, typename O, int kN, bool kNMajor>
+int narrow_launch(const RowsProduct &p, void *stream)
+{
+    const int32_t steps = (int32_t)((p.K * sizeof(T) + kStepBytes - 1) / kStepBytes);
+    const int64_t b = sizeof(T);
+    const bool aligned = on16(p.A, p.a_stride * b) && on16(p.B, (kNMajor ? p.K : p.N) * b) && p.K * b % 16 == 0;
+    const bool whole = (((uintptr_t)p.out | (uintptr_t)(p.out_stride * sizeof(O))) & (4 * sizeof(O) - 1)) == 0;
+    int log_rows = 7;                                        // about 1024 workgroups, of 128 rows at least
+    while (log_rows < 20 && ((int64_t)1024 << log_rows) < p.n) ++log_rows;
+    return aligned ? narrow_launch_as<T, O, kN, 4, 4, kNMajor, true>(p, log_rows, steps, whole, stream)
+                   : narrow_launch_as<T, O, kN, 4, 1, kNMajor, false>(p, log_rows, steps, whole, stream);
 }
 
 template <typename T, typename O, bool kNMajor>
 int rows_choose(const RowsProduct &p, void *stream)
 {
     const int64_t each = p.n / p.groups;                      // rows of a group, on average
-    if (p.N <= 64) return rows_launch<T, O, 128, 64, 4, 1, kNMajor>(p, stream);
-    if (each >= 192 && p.n * p.N >= (int64_t)256 * 256 * 128) return rows_launch<T, O, 256, 256, 2, 4, kNMajor>(p, stream);
-    if (each > 32) return rows_launch<T, O, 128, 128, 2, 2, kNMajor>(p, stream);
-    return rows_launch<T, O, 32, 128, 1, 4, kNMajor>(p, stream);
+    if (p.K * (int)sizeof(T) <= kNarrowBytes && p.N <= 128 && each >= 64)
+        return p.N <= 64 ? narrow_launch<T, O, 64, kNMajor>(p, stream) : narrow_launch<T, O, 128, kNMajor>(p, stream);
+    if (sizeof(T) < 4 && each >= 192 && p.n * p.N >= (int64_t)256 * 256 * 192) return rows_launch<T, O, 256, 256, 2, 4, 2, kNMajor>(p, stream);
+    if (each > 32) return rows_launch<T, O, 128, 128, 2, 2, 2, kNMajor>(p, stream);
+    if ((p.n + 31) / 32 * ((p.N + 127) / 128) + p.groups >= 512) return rows_launch<T, O, 32, 128, 1, 4, 3, kNMajor>(p, stream);
+    return rows_launch<T, O, 32, 64, 1, 2, 6, kNMajor>(p, stream);
 }
 
 // How the contraction of the weight gradients, a group's rows, is cut: pieces of 2^log_rows rows, so that their number times that of
 // the tiles of dW comes to about 1024 workgroups.  A piece of 512 rows reads eight times what its partial sums are written and read
-// again for.  A group of one piece needs no partial sums.
+// again for.  A group of one piece needs no partial sums, and a group without rows is one piece of zeros.
 struct WeightsSplit {
     int log_rows;
     int64_t tiles;                           // pieces of all groups, at most
@@ -144,7 +311,7 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
     int32_t n_tile;
     order.find(blockIdx.x, &row_tile, &n_tile);
     if (n_tile >= n_tiles) return;
-    const RowTile t = find_tile<true>(p.offsets, p.groups, p.n, row_tile / k_tiles, log_rows);
+    const RowTile t = find_tile<true, true>(p.offsets, p.groups, p.n, row_tile / k_tiles, log_rows);
     if (t.group < 0) return;
     const int32_t n0 = n_tile * kN, k0 = (int32_t)(row_tile % k_tiles) * kK;
     StageX x;
@@ -156,7 +323,7 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
     typename TileType<T>::Sum sums[kI][kJ];
     float columns[kJ] = {};
     const bool bias = p.dbias && k0 == 0 && row0 == 0;
-    tile_product<T, true>(x, y, lds, (t.end - t.begin + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums, &columns, bias);
+    tile_product<T, 2, true>(x, y, lds, (t.end - t.begin + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums, &columns, bias);
     const bool alone = t.count == 1;
     if (!alone && t.shared_before + t.place >= slots) return;   // offsets that do not ascend: more pieces than there are rows for
     float *const part = (float *)p.workspace + (t.shared_before + t.place) * ((int64_t)p.K * p.N + p.N);
@@ -188,52 +355,55 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
     }
 }
 
-// The partial sums of groups in several pieces, added up in fp64 piece after piece (every wavefront of a workgroup a share of them,
-// then the shares), and the zeros of empty groups.  A lane takes four neighbouring values; dbias lies behind dW.
+// The partial sums of groups in several pieces, added up in fp64: 16 lanes to 64 neighbouring values, every 16 lanes of a workgroup
+// a share of the pieces, then the shares.  dbias lies behind dW.
 template <typename O>
-__global__ __launch_bounds__(1024) void weights_sum_kernel(const WeightsProduct p, int log_rows, int64_t slots, uint32_t parts)
+__global__ __launch_bounds__(1024) void weights_sum_kernel(const WeightsProduct p, int log_rows, int64_t slots, uint32_t per_group)
 {
     typedef double v4d __attribute__((ext_vector_type(4)));
-    __shared__ v4d shares[16][kWave];
-    const int32_t g = (int32_t)(blockIdx.x / parts);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    __shared__ v4d shares[64][16];
+    const int32_t g = (int32_t)(blockIdx.x / per_group);
+    const int lane = threadIdx.x % kWave, quad = threadIdx.x % 16, share = threadIdx.x / 16, of = blockDim.x / 16;
     const int64_t rows = (int64_t)1 << log_rows;
     int64_t begin, end, before = 0;
     group_rows(p.offsets, p.n, g, &begin, &end);
     int64_t count = (end - begin + rows - 1) >> log_rows;
-    if (count == 1) return;
-    if (count > 1)
-        for (int32_t g0 = 0; g0 < g; g0 += kWave) {
-            int64_t b = 0, e = 0;
-            if (g0 + lane < g) group_rows(p.offsets, p.n, g0 + lane, &b, &e);
-            const int64_t c = (e - b + rows - 1) >> log_rows;
-            before += __shfl(sum_upto(c > 1 ? c : 0), kWave - 1);
-        }
-    count = before + count <= slots ? count : before < slots ? slots - before : 0;
-    const int64_t dw = (int64_t)p.K * p.N, slot = dw + p.N, at = ((int64_t)(blockIdx.x % parts) * kWave + lane) * 4;
-    const int64_t values = p.dbias ? slot : dw;
-    v4d sum = {0, 0, 0, 0};
-    const float *from = (const float *)p.workspace + before * slot + at;
-    if (slot % 4 == 0 && at + 4 <= values) {
-#pragma unroll 4
-        for (int64_t c = wave; c < count; c += waves) {
-            const v4f x = *(const v4f *)(from + c * slot);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] += (double)x[k];
-        }
-    } else {
-        for (int64_t c = wave; c < count; c += waves)
-            for (int k = 0; k < 4; ++k)
-                if (at + k < values) sum[k] += (double)from[c * slot + k];
+    if (count <= 1) return;
+    for (int32_t g0 = 0; g0 < g; g0 += kWave) {
+        int64_t b = 0, e = 0;
+        if (g0 + lane < g) group_rows(p.offsets, p.n, g0 + lane, &b, &e);
+        const int64_t c = (e - b + rows - 1) >> log_rows;
+        before += __shfl(sum_upto(c > 1 ? c : 0), kWave - 1);
     }
-    shares[wave][lane] = sum;
-    __syncthreads();
-    if (wave) return;
-    for (int w = 1; w < waves; ++w) sum += shares[w][lane];
-    for (int k = 0; k < 4; ++k) {
-        const int64_t i = at + k;
-        if (i < dw) ((O *)p.dW)[g * dw + i] = (O)(float)sum[k];
-        else if (i < values) ((O *)p.dbias)[(int64_t)g * p.N + (i - dw)] = (O)(float)sum[k];
+    count = before + count <= slots ? count : before < slots ? slots - before : 0;
+    const int64_t dw = (int64_t)p.K * p.N, slot = dw + p.N, values = p.dbias ? slot : dw;
+    for (int64_t first = (int64_t)(blockIdx.x % per_group) * 64; first < values; first += (int64_t)per_group * 64) {
+        const int64_t at = first + quad * 4;
+        const float *from = (const float *)p.workspace + before * slot + at;
+        v4d sum = {0, 0, 0, 0};
+        if (slot % 4 == 0 && at + 4 <= values) {
+#pragma unroll 4
+            for (int64_t c = share; c < count; c += of) {
+                const v4f x = *(const v4f *)(from + c * slot);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[k] += (double)x[k];
+            }
+        } else {
+            for (int64_t c = share; c < count; c += of)
+                for (int k = 0; k < 4; ++k)
+                    if (at + k < values) sum[k] += (double)from[c * slot + k];
+        }
+        shares[share][quad] = sum;
+        __syncthreads();
+        if (share == 0) {
+            for (int w = 1; w < of; ++w) sum += shares[w][quad];
+            for (int k = 0; k < 4; ++k) {
+                const int64_t i = at + k;
+                if (i < dw) ((O *)p.dW)[g * dw + i] = (O)(float)sum[k];
+                else if (i < values) ((O *)p.dbias)[(int64_t)g * p.N + (i - dw)] = (O)(float)sum[k];
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -258,11 +428,13 @@ int weights_launch(const WeightsProduct &p, void *stream)
     const int err = weights_tile(p.K, p.N).k == 64 ? weights_launch_tile<T, O, 64, 64>(p, split, aligned, s)
                                                    : weights_launch_tile<T, O, 128, 128>(p, split, aligned, s);
     if (err) return err;
-    const uint32_t parts = (uint32_t)(((int64_t)p.K * p.N + p.N + 4 * kWave - 1) / (4 * kWave));
-    int waves = 1;                                           // as many as a group has pieces, on average
-    while (waves < 16 && waves * p.groups < split.tiles) waves *= 2;
-    if (!fits_launch((int64_t)parts * p.groups, waves * kWave)) return kErrTooManyTiles;
-    weights_sum_kernel<O><<<parts * (uint32_t)p.groups, waves * kWave, 0, s>>>(p, split.log_rows, split.slots, parts);
+    if (split.slots == 0) return 0;
+    const int64_t parts = ((int64_t)p.K * p.N + p.N + 63) / 64;
+    int64_t per_group = 8192 / p.groups;
+    per_group = per_group < 1 ? 1 : per_group > parts ? parts : per_group;
+    int lanes = 64;                                          // 16 for every two pieces that a group has on average, 1024 at most
+    while (lanes < 1024 && (int64_t)lanes * p.groups < 8 * split.tiles) lanes *= 2;
+    weights_sum_kernel<O><<<(uint32_t)(per_group * p.groups), lanes, 0, s>>>(p, split.log_rows, split.slots, (uint32_t)per_group);
     return (int)hipGetLastError();
 }
 

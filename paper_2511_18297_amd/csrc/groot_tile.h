@@ -88,7 +88,13 @@ __device__ __forceinline__ void dma16(const void *from, uint32_t to)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
 
-__device__ __forceinline__ void dma_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// until at most kMost of the wavefront's latest loads are on their way
+template <int kMost = 0>
+__device__ __forceinline__ void dma_wait()
+{
+    static_assert(kMost >= 0 && kMost < 64, "vmcnt");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMost) : "memory");
+}
 
 static __device__ const v4i g_zeros = {0, 0, 0, 0};          // what lies past an end of the contraction
 
@@ -112,6 +118,7 @@ __device__ __forceinline__ v4i load16(const char *p, int64_t valid)
 // the workgroup has passed a barrier.
 template <typename T, int kWide, int kThreads, bool kAcross, bool kAligned>
 struct Stage {
+    static constexpr bool kDirect = kAligned;
     static constexpr int kBytes = kWide * kStepBytes, kEach = kBytes / 16 / kThreads;
     static constexpr int kRowBytes = kAcross ? kWide * (int)sizeof(T) : kStepBytes, kPieces = kRowBytes / 16;
     static constexpr int kRowsEach = kThreads / kPieces;     // rows of the tile that one load of the workgroup takes
@@ -202,10 +209,34 @@ struct Stage {
     }
 };
 
+// One step's products of the wavefront's 32 x 32 blocks.
+template <typename T, bool kColumns, class StageA, class StageB, int kI, int kJ>
+__device__ __forceinline__ void tile_step(const char *now, int row0, int col0, typename TileType<T>::Sum (&sums)[kI][kJ], float (*columns)[kJ], bool mine)
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        v4i fa[kI], fb[kJ];
+#pragma unroll
+        for (int i = 0; i < kI; ++i) fa[i] = StageA::fragment(now, row0 + 32 * i, q);
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) fb[j] = StageB::fragment(now + StageA::kBytes, col0 + 32 * j, q);
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) sums[i][j] = TileType<T>::mma(fb[j], fa[i], sums[i][j]);
+        if constexpr (kColumns) {
+            if (mine) {
+#pragma unroll
+                for (int j = 0; j < kJ; ++j) (*columns)[j] += TileType<T>::total(fb[j]);
+            }
+        }
+    }
+}
+
 // The product of two staged operands over `steps` steps: sums[i][j] of the wavefront's 32 x 32 blocks, rows of `A` from row0 on,
-// columns of `B` from col0 on.  `columns` (where kColumns; wavefronts with `mine`): the sums of B's values, lanes l and l + 32 hold
-// the two halves of column l.
-template <typename T, bool kColumns = false, class StageA, class StageB, int kI, int kJ>
+// columns of `B` from col0 on.  kStages pairs of tiles lie in LDS, so that kStages - 1 steps are on their way while one is computed.
+// `columns` (where kColumns; wavefronts with `mine`): the sums of B's values, lanes l and l + 32 hold the two halves of column l.
+template <typename T, int kStages, bool kColumns = false, class StageA, class StageB, int kI, int kJ>
 __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, int64_t steps, int row0, int col0,
                                              typename TileType<T>::Sum (&sums)[kI][kJ], float (*columns)[kJ] = nullptr, bool mine = false)
 {
@@ -215,45 +246,42 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
 #pragma unroll
         for (int j = 0; j < kJ; ++j) sums[i][j] = {};
     if (steps <= 0) return;
-    a.begin(0, lds);
-    b.begin(0, lds + StageA::kBytes);
-    a.end(lds);
-    b.end(lds + StageA::kBytes);
-    dma_wait();
-    __syncthreads();
-    int at = 0;
+    if constexpr (StageA::kDirect) {
+        // a step past the last one loads zeros that nothing reads: every step has the same number of loads to count
+        constexpr int kEach = StageA::kEach + StageB::kEach;
+        auto begin = [&](int64_t s, int at) {
+            a.begin(s, lds + at);
+            b.begin(s, lds + at + StageA::kBytes);
+        };
+#pragma unroll
+        for (int s = 0; s < kStages - 1; ++s) begin(s, s * kBoth);
+        int now = 0, next = (kStages - 1) * kBoth;
 #pragma unroll 1
-    for (int64_t s = 0; s < steps; ++s) {
-        char *const now = lds + at, *const next = lds + (kBoth - at);
-        if (s + 1 < steps) {
-            a.begin(s + 1, next);
-            b.begin(s + 1, next + StageA::kBytes);
+        for (int64_t s = 0; s < steps; ++s) {
+            dma_wait<(kStages - 2) * kEach>();
+            __syncthreads();                                 // step s has arrived, and nobody reads the tile that is loaded next
+            begin(s + kStages - 1, next);
+            tile_step<T, kColumns, StageA, StageB>(lds + now, row0, col0, sums, columns, mine);
+            now = now + kBoth == kStages * kBoth ? 0 : now + kBoth;
+            next = next + kBoth == kStages * kBoth ? 0 : next + kBoth;
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            v4i fa[kI], fb[kJ];
-#pragma unroll
-            for (int i = 0; i < kI; ++i) fa[i] = StageA::fragment(now, row0 + 32 * i, q);
-#pragma unroll
-            for (int j = 0; j < kJ; ++j) fb[j] = StageB::fragment(now + StageA::kBytes, col0 + 32 * j, q);
-#pragma unroll
-            for (int i = 0; i < kI; ++i)
-#pragma unroll
-                for (int j = 0; j < kJ; ++j) sums[i][j] = TileType<T>::mma(fb[j], fa[i], sums[i][j]);
-            if constexpr (kColumns) {
-                if (mine) {
-#pragma unroll
-                    for (int j = 0; j < kJ; ++j) (*columns)[j] += TileType<T>::total(fb[j]);
-                }
-            }
+        dma_wait();                                          // before the workgroup's LDS is anybody else's
+    } else {
+        auto begin = [&](int64_t s) {
+            a.begin(s, lds);
+            b.begin(s, lds);
+        };
+        begin(0);
+        int at = 0;
+#pragma unroll 1
+        for (int64_t s = 0; s < steps; ++s) {
+            a.end(lds + at);
+            b.end(lds + at + StageA::kBytes);
+            __syncthreads();                                 // two tiles: the other one is read no more once all are here
+            if (s + 1 < steps) begin(s + 1);
+            tile_step<T, kColumns, StageA, StageB>(lds + at, row0, col0, sums, columns, mine);
+            at = kBoth - at;
         }
-        if (s + 1 < steps) {
-            a.end(next);
-            b.end(next + StageA::kBytes);
-        }
-        dma_wait();
-        __syncthreads();
-        at = kBoth - at;
     }
 }
 
