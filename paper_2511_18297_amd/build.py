@@ -17,7 +17,7 @@ SOURCES = [os.path.join(CSRC, "groot_host.cpp"), os.path.join(CSRC, "groot_kerne
            os.path.join(CSRC, "groot_pool.hip"),
            os.path.join(CSRC, "groot_hd_dense.hip"), os.path.join(CSRC, "groot_dense_ops.cpp"),
            os.path.join(CSRC, "groot_grouped.hip"), os.path.join(CSRC, "groot_int8.hip"),
-           os.path.join(CSRC, "groot_adamw.hip")]
+           os.path.join(CSRC, "groot_adamw.hip"), os.path.join(CSRC, "groot_few.hip")]
 HEADERS = [os.path.join(CSRC, "groot_dense_ops.h"), os.path.join(CSRC, "groot_dense_device.h"),
            os.path.join(CSRC, "groot_tile.h"),
            os.path.join(CSRC, "groot_internal.h"), os.path.join(CSRC, "groot_device.h"),

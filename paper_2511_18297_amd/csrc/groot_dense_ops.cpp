@@ -231,6 +231,8 @@ extern "C" groot_status groot_quantized_linear(int32_t dtype, const void *X_dev,
     if (to.meets(x)) return bad(who, "Y overlaps an input");
     if (ws.meets(to) || ws.meets(x) || ws.meets(w) || ws.meets(s) || ws.meets(bs)) return bad(who, "the workspace overlaps another argument");
     if (n_rows == 0) return GROOT_OK;
+    RowsProduct x_rows{X_dev, x_stride, W_dev, true, offsets_dev, bias_dev, nullptr, w_scale_dev, relu != 0, Y_dev, y_stride, n_rows, n_groups, K, N};
+    if (few_linear_serves(x_rows)) return launched(who, launch_few_linear(dtype, x_rows, hip_stream));
     int8_t *Q = (int8_t *)workspace_dev;
     float *scale = (float *)(Q + (size_t)n_rows * row);
     int err = launch_quantize_rows(dtype, X_dev, x_stride, Q, (int64_t)row, scale, n_rows, K, hip_stream);

@@ -26,6 +26,13 @@ constexpr int kErrTooManyTiles = -4;
 constexpr bool fits_launch(int64_t workgroups, int lanes) { return workgroups < ((int64_t)1 << 32) / lanes; }
 int launch_grouped_rows(int32_t dtype, const RowsProduct &p, void *stream);
 int launch_int8_rows(int32_t out_dtype, const RowsProduct &p, void *stream);
+// the same for few rows of every group and weights [groups, N, K], where few_rows_serve says so (groot_few.hip)
+bool few_rows_serve(const RowsProduct &p);
+int launch_few_rows(int32_t dtype, const RowsProduct &p, void *stream);
+int launch_few_int8(int32_t out_dtype, const RowsProduct &p, void *stream);
+// ... of rows in floating point that are cut to 8 bits on the way (a_scale is not read)
+bool few_linear_serves(const RowsProduct &p);
+int launch_few_linear(int32_t dtype, const RowsProduct &p, void *stream);
 int launch_quantize_rows(int32_t dtype, const void *X, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int64_t n,
                          int32_t K, void *stream);
 

@@ -1,0 +1,231 @@
+// Few rows against weights whose rows lie along the contraction ([groups, N, K]: the 8-bit products, the input gradients): a
+// workgroup takes up to 16 rows of a group and 16 columns, and its eight wavefronts share the contraction, 128 bytes of every
+// weight row in turn, straight from memory into the fragments of the 16 x 16 matrix instructions.  Nothing is staged: the weights
+// are read once and are nearly everything that is read.  A lane has 32 neighbouring bytes of a step (two instructions), so that
+// four lanes read a row's 128 bytes.  The wavefronts' sums meet in LDS.
+// groot_quantized_linear on up to four rows: every workgroup cuts the rows to 8 bits by itself, into LDS, while its first weights are
+// on their way: one launch in place of two.
+#include "groot_tile.h"
+
+namespace groot {
+
+namespace {
+
+constexpr int kFewRows = 16, kFewCols = 16, kFewWaves = 8, kFewThreads = kFewWaves * kWave, kAhead = 4;
+constexpr int kFusedRows = 4, kFusedBytes = 48 * 1024;       // rows that are cut inside, their bytes in LDS
+
+template <typename T>
+struct FewType;
+template <>
+struct FewType<int8_t> {
+    typedef v4i Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+};
+template <>
+struct FewType<bf16_t> {
+    typedef v4f Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct FewType<f16_t> {
+    typedef v4f Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct FewType<float> {
+    typedef v4f Sum;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(a[j]), __int_as_float(b[j]), c, 0, 0, 0);
+        return c;
+    }
+};
+
+// 16 bytes at offset k of a row of `bytes`, zeros behind its end
+template <typename T, bool kAligned>
+__device__ __forceinline__ v4i piece16(const char *row, int64_t k, int64_t bytes)
+{
+    if constexpr (kAligned) return k < bytes ? *(const v4i *)(row + k) : v4i{0, 0, 0, 0};
+    else return load16<T>(row + k, bytes - k);
+}
+
+// X: the floating type of the rows where they are cut to 8 bits inside, else T
+template <typename T, typename O, typename X, bool kAligned>
+__global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, int32_t col_tiles)
+{
+    constexpr bool kFused = !std::is_same<X, T>::value;
+    typedef typename FewType<T>::Sum Sum;
+    __shared__ Sum part[kFewWaves][kWave];
+    __shared__ float tops[kFusedRows][kFewWaves];
+    extern __shared__ __align__(16) char cut[];              // fused: the rows in 8 bits
+    const RowTile t = find_tile(p.offsets, p.groups, p.n, blockIdx.x / col_tiles, 4);
+    if (t.group < 0) return;
+    const int32_t n0 = (int32_t)(blockIdx.x % col_tiles) * kFewCols;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 16, quarter = lane / 16 * 32;
+    const int rows = (int)(t.end - t.begin);
+    const int64_t bytes = (int64_t)p.K * sizeof(T);
+    const int32_t col = n0 + r < p.N ? n0 + r : p.N - 1;     // columns and rows that do not exist read the last one that does
+    const char *const w = (const char *)((const T *)p.B + ((int64_t)t.group * p.N + col) * p.K) + quarter;
+    const int32_t pieces = (int32_t)((bytes + kStepBytes - 1) / kStepBytes);
+
+    v4i held[kAhead][2];
+    auto load = [&](int32_t s, int i) {
+        const int64_t k = (int64_t)s * kStepBytes;
+        held[i][0] = piece16<T, kAligned>(w, k, bytes - quarter);
+        held[i][1] = piece16<T, kAligned>(w, k + 16, bytes - quarter);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (wave + i * kFewWaves < pieces) load(wave + i * kFewWaves, i);
+
+    const char *x;
+    float x_scale = 1.f;
+    const int32_t cut_row = (p.K + 127) / 128 * 128;
+    if constexpr (kFused) {
+        constexpr int kPer = 16 / sizeof(X), kKeep = 4;      // values of a load, loads of a lane that stay in registers
+        const int32_t loads = (p.K + kPer - 1) / kPer;
+        v4i keep[kFusedRows][kKeep];
+        auto get = [&](int64_t row, int32_t i) {
+            return load16<X>((const char *)((const X *)p.A + row * p.a_stride) + (int64_t)i * 16, ((int64_t)p.K - (int64_t)i * kPer) * (int64_t)sizeof(X));
+        };
+#pragma unroll
+        for (int m = 0; m < kFusedRows; ++m) {
+            if (m >= rows) break;
+            float top = 0.f;
+            bool fine = true;
+            auto look = [&](v4i v) {
+                const RowValues<X> e = row_values<X>(v);
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    const float a = __builtin_fabsf(e.x[k]);
+                    fine = fine && __builtin_isfinite(a);
+                    top = fmaxf(top, a);
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i)
+                if ((int)threadIdx.x + i * kFewThreads < loads) look(keep[m][i] = get(t.begin + m, threadIdx.x + i * kFewThreads));
+            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) look(get(t.begin + m, i));
+            if (!fine) top = __builtin_inff();               // carries the news through the maximum
+#pragma unroll
+            for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+            if (lane == 0) tops[m][wave] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < kFusedRows; ++m) {
+            if (m >= rows) break;
+            float top = tops[m][0];
+#pragma unroll
+            for (int k = 1; k < kFewWaves; ++k) top = fmaxf(top, tops[m][k]);
+            const float scale = row_scale(top);
+            int8_t *const to = (int8_t *)cut + m * cut_row;
+            auto put = [&](v4i v, int32_t i) { row_codes<X>(v, scale, to + (int64_t)i * kPer); };
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i)
+                if ((int)threadIdx.x + i * kFewThreads < loads) put(keep[m][i], threadIdx.x + i * kFewThreads);
+            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) put(get(t.begin + m, i), i);
+            if (m == (int)(threadIdx.x % 256 / 16)) x_scale = scale;
+        }
+        __syncthreads();
+        x = cut + (r < rows ? r : rows - 1) * cut_row + quarter;
+    } else {
+        x = (const char *)((const T *)p.A + (t.begin + (r < rows ? r : rows - 1)) * p.a_stride) + quarter;
+    }
+
+    Sum sum = {};
+    for (int32_t s0 = wave; s0 < pieces; s0 += kAhead * kFewWaves) {
+        v4i fa[kAhead][2], fb[kAhead][2];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int32_t s = s0 + i * kFewWaves;
+            if (s >= pieces) break;
+            const int64_t k = (int64_t)s * kStepBytes;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                fa[i][h] = held[i][h];
+                // what lies behind the row's end in LDS meets zeros of the weights
+                fb[i][h] = kFused ? *(const v4i *)(x + k + 16 * h) : piece16<T, kAligned>(x, k + 16 * h, bytes - quarter);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (s0 + (i + kAhead) * kFewWaves < pieces) load(s0 + (i + kAhead) * kFewWaves, i);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (s0 + i * kFewWaves >= pieces) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sum = FewType<T>::mma(fa[i][h], fb[i][h], sum);
+        }
+    }
+    part[wave][lane] = sum;
+    __syncthreads();
+    // a lane's four values: columns 4 (lane / 16) .. + 3 of row lane % 16
+    if (threadIdx.x >= 256) return;
+    const int m = threadIdx.x / 16, c = threadIdx.x % 16;
+    if (m >= rows || n0 + c >= p.N) return;
+    typename std::remove_reference<decltype(sum[0])>::type v = part[0][c / 4 * 16 + m][c % 4];
+#pragma unroll
+    for (int k = 1; k < kFewWaves; ++k) v += part[k][c / 4 * 16 + m][c % 4];
+    const int64_t row = t.begin + m, of = (int64_t)t.group * p.N + n0 + c;
+    float y = (float)v;
+    if constexpr (std::is_same<T, int8_t>::value) {
+        y = y * (kFused ? x_scale : p.a_scale[row]) * p.b_scale[of];
+        if (p.bias) y += ((const float *)p.bias)[of];
+    } else if (p.bias) y += (float)((const O *)p.bias)[of];
+    if (p.relu && y < 0.f) y = 0.f;
+    ((O *)p.out)[row * p.out_stride + n0 + c] = (O)y;
+}
+
+template <typename T, typename O, typename X>
+int few_launch(const RowsProduct &p, void *stream)
+{
+    constexpr bool kFused = !std::is_same<X, T>::value;
+    const int64_t b = sizeof(T);
+    const bool aligned = (((uintptr_t)p.B | (uintptr_t)(p.K * b)) & 15) == 0 && (kFused || (((uintptr_t)p.A | (uintptr_t)(p.a_stride * b)) & 15) == 0);
+    const int32_t col_tiles = (p.N + kFewCols - 1) / kFewCols;
+    const int64_t workgroups = ((p.n + kFewRows - 1) / kFewRows + (p.offsets ? p.groups : 0)) * col_tiles;
+    if (!fits_launch(workgroups, kFewThreads)) return kErrTooManyTiles;
+    const size_t lds = kFused ? (size_t)p.n * ((p.K + 127) / 128 * 128) : 0;
+    if (aligned) few_kernel<T, O, X, true><<<(uint32_t)workgroups, kFewThreads, lds, (hipStream_t)stream>>>(p, col_tiles);
+    else few_kernel<T, O, X, false><<<(uint32_t)workgroups, kFewThreads, lds, (hipStream_t)stream>>>(p, col_tiles);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+// Groups of at most 16 rows on average.
+bool few_rows_serve(const RowsProduct &p) { return p.b_n_major && p.n <= (int64_t)kFewRows * p.groups; }
+
+int launch_few_rows(int32_t dtype, const RowsProduct &p, void *stream)
+{
+    if (dtype == GROOT_F32) return few_launch<float, float, float>(p, stream);
+    if (dtype == GROOT_BF16) return few_launch<bf16_t, bf16_t, bf16_t>(p, stream);
+    return few_launch<f16_t, f16_t, f16_t>(p, stream);
+}
+
+int launch_few_int8(int32_t out_dtype, const RowsProduct &p, void *stream)
+{
+    if (out_dtype == GROOT_F32) return few_launch<int8_t, float, int8_t>(p, stream);
+    if (out_dtype == GROOT_BF16) return few_launch<int8_t, bf16_t, int8_t>(p, stream);
+    return few_launch<int8_t, f16_t, int8_t>(p, stream);
+}
+
+// Rows in floating point, all of them in every workgroup.
+bool few_linear_serves(const RowsProduct &p) { return p.n <= kFusedRows && p.n * ((p.K + 127) / 128 * 128) <= kFusedBytes; }
+
+int launch_few_linear(int32_t dtype, const RowsProduct &p, void *stream)
+{
+    if (dtype == GROOT_F32) return few_launch<int8_t, float, float>(p, stream);
+    if (dtype == GROOT_BF16) return few_launch<int8_t, bf16_t, bf16_t>(p, stream);
+    return few_launch<int8_t, f16_t, f16_t>(p, stream);
+}
+
+}  // namespace groot

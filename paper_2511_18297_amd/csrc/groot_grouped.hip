@@ -442,6 +442,7 @@ int weights_launch(const WeightsProduct &p, void *stream)
 
 int launch_grouped_rows(int32_t dtype, const RowsProduct &p, void *stream)
 {
+    if (few_rows_serve(p)) return launch_few_rows(dtype, p, stream);
     if (dtype == GROOT_F32) return p.b_n_major ? rows_choose<float, float, true>(p, stream) : rows_choose<float, float, false>(p, stream);
     if (dtype == GROOT_BF16) return p.b_n_major ? rows_choose<bf16_t, bf16_t, true>(p, stream) : rows_choose<bf16_t, bf16_t, false>(p, stream);
     return p.b_n_major ? rows_choose<f16_t, f16_t, true>(p, stream) : rows_choose<f16_t, f16_t, false>(p, stream);
@@ -449,6 +450,7 @@ int launch_grouped_rows(int32_t dtype, const RowsProduct &p, void *stream)
 
 int launch_int8_rows(int32_t out_dtype, const RowsProduct &p, void *stream)
 {
+    if (few_rows_serve(p)) return launch_few_int8(out_dtype, p, stream);
     if (out_dtype == GROOT_F32) return rows_choose<int8_t, float, true>(p, stream);
     if (out_dtype == GROOT_BF16) return rows_choose<int8_t, bf16_t, true>(p, stream);
     return rows_choose<int8_t, f16_t, true>(p, stream);

@@ -1,33 +1,87 @@
 // Rows cut to 8 bits with a scale of their own.
-#include "groot_dense_device.h"
+#include "groot_tile.h"
 
 namespace groot {
 
 namespace {
 
-// one row to a wavefront: its largest magnitude, then its values over scale, halves to even
-template <typename T>
+// kLanes lanes to a row, 16 bytes a load, kKeep loads of a lane in registers: a row that fits them is read once.  Wider rows read
+// the rest a second time, from L2.  Bound by HBM.
+template <typename T, int kLanes, int kKeep>
 __global__ __launch_bounds__(kBlock) void quantize_kernel(const T *__restrict__ X, int64_t x_stride, int8_t *__restrict__ Q, int64_t q_stride,
                                                           float *__restrict__ scale_at, int64_t n, int32_t K)
 {
-    const int lane = threadIdx.x % kWave;
-    for (int64_t row = (int64_t)blockIdx.x * kWavesPerBlock + threadIdx.x / kWave; row < n; row += (int64_t)gridDim.x * kWavesPerBlock) {
-    const T *x = X + row * x_stride;
-    float top = 0.f;
-    bool fine = true;
-    for (int32_t k = lane; k < K; k += kWave) {
-        const float a = __builtin_fabsf((float)x[k]);
-        fine = fine && __builtin_isfinite(a);
-        top = fmaxf(top, a);
-    }
+    constexpr int kPer = 16 / sizeof(T), kRows = kBlock / kLanes;
+    __shared__ float tops[kWavesPerBlock];
+    const int at = threadIdx.x % kLanes;
+    const int32_t loads = (K + kPer - 1) / kPer;
+    const bool whole = (((uintptr_t)Q | (uintptr_t)q_stride) & (kPer - 1)) == 0;
+    for (int64_t first = (int64_t)blockIdx.x * kRows; first < n; first += (int64_t)gridDim.x * kRows) {
+        const int64_t row = first + threadIdx.x / kLanes;
+        const char *const x = (const char *)(X + (row < n ? row : n - 1) * x_stride);
+        auto get = [&](int32_t i) { return load16<T>(x + (int64_t)i * 16, ((int64_t)K - (int64_t)i * kPer) * (int64_t)sizeof(T)); };
+        float top = 0.f;
+        bool fine = true;
+        auto look = [&](v4i v) {
+            const RowValues<T> e = row_values<T>(v);
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    fine = __all(fine);
-    const float scale = top * (1.f / 127.f);
-    for (int32_t k = lane; k < K; k += kWave)
-        Q[row * q_stride + k] = fine && scale > 0.f ? (int8_t)fminf(fmaxf(rintf((float)x[k] / scale), -127.f), 127.f) : (int8_t)0;
-    if (lane == 0) scale_at[row] = fine ? scale : __builtin_nanf("");
+            for (int k = 0; k < kPer; ++k) {
+                const float a = __builtin_fabsf(e.x[k]);
+                fine = fine && __builtin_isfinite(a);
+                top = fmaxf(top, a);
+            }
+        };
+        v4i keep[kKeep];
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i)
+            if (at + i * kLanes < loads) keep[i] = get(at + i * kLanes);
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i)
+            if (at + i * kLanes < loads) look(keep[i]);
+        for (int32_t i = at + kKeep * kLanes; i < loads; i += kLanes) look(get(i));
+        if (!fine) top = __builtin_inff();                   // carries the news through the maximum
+#pragma unroll
+        for (int d = 1; d < (kLanes < kWave ? kLanes : kWave); d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        if constexpr (kLanes > kWave) {
+            __syncthreads();                                 // the row before has read the maxima
+            if (threadIdx.x % kWave == 0) tops[threadIdx.x / kWave] = top;
+            __syncthreads();
+            top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        }
+        if (row >= n) continue;
+        const float scale = row_scale(top);
+        auto put = [&](v4i v, int32_t i) {
+            int8_t *const to = Q + row * q_stride + (int64_t)i * kPer;
+            if (whole && (i + 1) * kPer <= K) {
+                row_codes<T>(v, scale, to);
+            } else {
+                alignas(8) int8_t c[kPer];
+                row_codes<T>(v, scale, c);
+                for (int k = 0; k < kPer; ++k)
+                    if (i * kPer + k < K) to[k] = c[k];
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i)
+            if (at + i * kLanes < loads) put(keep[i], at + i * kLanes);
+        for (int32_t i = at + kKeep * kLanes; i < loads; i += kLanes) put(get(i), i);
+        if (at == 0) scale_at[row] = scale;
     }
+}
+
+template <typename T>
+int quantize_launch(const T *X, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int64_t n, int32_t K, hipStream_t stream)
+{
+    const int64_t loads = ((int64_t)K * sizeof(T) + 15) / 16;
+    auto blocks = [&](int rows) {
+        const int64_t b = (n + rows - 1) / rows;
+        return (uint32_t)(b < (1 << 20) ? b : 1 << 20);
+    };
+    // as many lanes as a row has loads, up to the workgroup's
+    if (loads <= 32) quantize_kernel<T, 16, 2><<<blocks(16), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
+    else if (loads <= 256) quantize_kernel<T, 64, 4><<<blocks(4), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
+    else quantize_kernel<T, 256, 4><<<blocks(1), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
+    return (int)hipGetLastError();
 }
 
 }  // namespace
@@ -35,13 +89,10 @@ __global__ __launch_bounds__(kBlock) void quantize_kernel(const T *__restrict__ 
 int launch_quantize_rows(int32_t dtype, const void *X, int64_t x_stride, int8_t *Q, int64_t q_stride, float *scale, int64_t n,
                          int32_t K, void *stream)
 {
-    const int64_t wanted = (n + kWavesPerBlock - 1) / kWavesPerBlock;
-    const uint32_t blocks = wanted < (1 << 20) ? (uint32_t)wanted : 1 << 20;
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == GROOT_F32) quantize_kernel<float><<<blocks, kBlock, 0, s>>>((const float *)X, x_stride, Q, q_stride, scale, n, K);
-    else if (dtype == GROOT_BF16) quantize_kernel<bf16_t><<<blocks, kBlock, 0, s>>>((const bf16_t *)X, x_stride, Q, q_stride, scale, n, K);
-    else quantize_kernel<f16_t><<<blocks, kBlock, 0, s>>>((const f16_t *)X, x_stride, Q, q_stride, scale, n, K);
-    return (int)hipGetLastError();
+    if (dtype == GROOT_F32) return quantize_launch((const float *)X, x_stride, Q, q_stride, scale, n, K, s);
+    if (dtype == GROOT_BF16) return quantize_launch((const bf16_t *)X, x_stride, Q, q_stride, scale, n, K, s);
+    return quantize_launch((const f16_t *)X, x_stride, Q, q_stride, scale, n, K, s);
 }
 
 }  // namespace groot

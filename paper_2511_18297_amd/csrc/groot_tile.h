@@ -114,6 +114,39 @@ __device__ __forceinline__ v4i load16(const char *p, int64_t valid)
     return x;
 }
 
+// Rows cut to 8 bits.  The 16 bytes of a load as floats; the scale of a row from its largest magnitude (not finite: NaN); the codes of
+// a load, halves to even, zeros where the scale is zero or NaN.
+template <typename X>
+struct RowValues {
+    float x[16 / sizeof(X)];
+};
+template <typename X>
+__device__ __forceinline__ RowValues<X> row_values(v4i v)
+{
+    typedef X vx __attribute__((ext_vector_type(16 / sizeof(X))));
+    const vx e = __builtin_bit_cast(vx, v);
+    RowValues<X> r;
+#pragma unroll
+    for (int k = 0; k < (int)(16 / sizeof(X)); ++k) r.x[k] = (float)e[k];
+    return r;
+}
+
+__device__ __forceinline__ float row_scale(float top) { return __builtin_isfinite(top) ? top * (1.f / 127.f) : __builtin_nanf(""); }
+
+template <typename X>
+__device__ __forceinline__ void row_codes(v4i v, float scale, int8_t *to)
+{
+    constexpr int kPer = 16 / sizeof(X);
+    const RowValues<X> e = row_values<X>(v);
+    union {
+        int8_t c[kPer];
+        uint32_t u[kPer / 4];
+    } q;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) q.c[k] = scale > 0.f ? (int8_t)fminf(fmaxf(rintf(e.x[k] / scale), -127.f), 127.f) : (int8_t)0;
+    __builtin_memcpy(__builtin_assume_aligned(to, kPer), q.u, kPer);
+}
+
 // One operand's tile: kWide rows ("along") or columns ("across").  begin(s) starts the loads of step s, end(s) has them in LDS once
 // the workgroup has passed a barrier.
 template <typename T, int kWide, int kThreads, bool kAcross, bool kAligned>
