@@ -575,27 +575,33 @@ GROOT_F32, GROOT_BF16, GROOT_F16 = range(3)
 _DTYPES = {torch.float32: GROOT_F32, torch.bfloat16: GROOT_BF16, torch.float16: GROOT_F16}
 
 
+_Tensor, _int64, _int8, _float32 = torch.Tensor, torch.int64, torch.int8, torch.float32
+
+
 def _dtype(t, what):
-    try:
-        return _DTYPES[t.dtype]
-    except (KeyError, AttributeError):
-        raise TypeError(f"{what} must be float32, bfloat16 or float16") from None
+    d = _DTYPES.get(t.dtype) if isinstance(t, _Tensor) else None
+    if d is None:
+        raise TypeError(f"{what} must be a float32, bfloat16 or float16 tensor")
+    return d
 
 
-def _rows(t, what, shape, dtype):
+def _rows(t, what, n, width, dtype):
     """Pointer and row stride of a CUDA matrix of this shape and type whose rows are contiguous (any distance apart): the C ABI
-    cannot know buffer sizes, so everything is checked before anything is launched."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    cannot know buffer sizes, so everything is checked before anything is launched.  (A small call is 5 us on the GPU: the checks of
+    its arguments read every property of a tensor once.)"""
+    if not isinstance(t, _Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a CUDA tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}")
-    if t.dim() != 2 or t.shape != shape:
-        raise ValueError(f"{what} must be {tuple(shape)}, is {tuple(t.shape)}")
+    if t.shape != (n, width):
+        raise ValueError(f"{what} must be {(n, width)}, is {tuple(t.shape)}")
     stride, inner = t.stride()
-    if t.shape[0] <= 1:
-        stride = max(stride, t.shape[1])
-    if (inner != 1 and t.shape[1] > 1) or stride < t.shape[1]:
-        raise ValueError(f"{what} must have contiguous rows that do not overlap")
+    if stride < width:
+        if n > 1:
+            raise ValueError(f"{what} must have rows that do not overlap")
+        stride = width
+    if inner != 1 and width > 1:
+        raise ValueError(f"{what} must have contiguous rows")
     return t.data_ptr(), stride
 
 
@@ -603,37 +609,49 @@ def _array(t, what, shape, dtype):
     """Pointer of a contiguous CUDA tensor of this shape and type; None stays None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+    if not isinstance(t, _Tensor) or not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{what} must be a contiguous CUDA tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}")
     if t.shape != shape:
         raise ValueError(f"{what} must be {tuple(shape)}, is {tuple(t.shape)}")
     return t.data_ptr()
 
 
+def _matrix_rows(t, what):
+    if not isinstance(t, _Tensor) or t.dim() != 2:
+        raise TypeError(f"{what} must be a matrix")
+    return t.shape[0]
+
+
+def _weights(t, what):
+    if not isinstance(t, _Tensor) or t.dim() != 3:
+        raise TypeError(f"{what} must have three dimensions, the groups first")
+    return t.shape
+
+
 def groot_grouped_product(X, W, offsets, bias, relu: bool, Y, stream=None) -> None:
     """Y[i] = act(X[i] W[g] + bias[g]) for the rows i of every group g.  X [n, K], Y [n, N] (rows may be any distance apart),
     W [groups, K, N], bias [groups, N] or None, offsets int64 [groups + 1] on the device or None (one group)."""
-    d = _dtype(X, "X")
-    E, K, N = W.shape
-    n = X.shape[0]
-    x, xs = _rows(X, "X", (n, K), X.dtype)
-    y, ys = _rows(Y, "Y", (n, N), X.dtype)
-    _check(_lib.groot_grouped_product(d, x, xs, _array(W, "W", (E, K, N), X.dtype), _array(offsets, "offsets", (E + 1,), torch.int64),
-                                      _array(bias, "bias", (E, N), X.dtype), 1 if relu else 0, y, ys, n, E, K, N,
+    d, T = _dtype(X, "X"), X.dtype
+    E, K, N = _weights(W, "W")
+    n = _matrix_rows(X, "X")
+    x, xs = _rows(X, "X", n, K, T)
+    y, ys = _rows(Y, "Y", n, N, T)
+    _check(_lib.groot_grouped_product(d, x, xs, _array(W, "W", (E, K, N), T), _array(offsets, "offsets", (E + 1,), _int64),
+                                      _array(bias, "bias", (E, N), T), 1 if relu else 0, y, ys, n, E, K, N,
                                       _stream_handle(stream)))
 
 
 def groot_grouped_product_backward_data(dY, W, offsets, dX, stream=None) -> None:
     """dX[i] = dY[i] W[g]^T.  dY [n, N], W [groups, K, N] as in the forward call, dX [n, K]."""
-    d = _dtype(dY, "dY")
-    E, K, N = W.shape
-    n = dY.shape[0]
-    y, ys = _rows(dY, "dY", (n, N), dY.dtype)
-    x, xs = _rows(dX, "dX", (n, K), dY.dtype)
-    _check(_lib.groot_grouped_product_backward_data(d, y, ys, _array(W, "W", (E, K, N), dY.dtype),
-                                                    _array(offsets, "offsets", (E + 1,), torch.int64), x, xs, n, E, K, N,
+    d, T = _dtype(dY, "dY"), dY.dtype
+    E, K, N = _weights(W, "W")
+    n = _matrix_rows(dY, "dY")
+    y, ys = _rows(dY, "dY", n, N, T)
+    x, xs = _rows(dX, "dX", n, K, T)
+    _check(_lib.groot_grouped_product_backward_data(d, y, ys, _array(W, "W", (E, K, N), T),
+                                                    _array(offsets, "offsets", (E + 1,), _int64), x, xs, n, E, K, N,
                                                     _stream_handle(stream)))
 
 
@@ -650,13 +668,13 @@ def groot_grouped_product_backward_weights(X, dY, offsets, dW, dbias, workspace,
     """dW[g] = X_g^T dY_g, dbias[g] = column sums of dY_g (None: not wanted).  dW [groups, K, N] and dbias [groups, N] of X's
     type or float32; workspace: a contiguous CUDA tensor of at least
     groot_grouped_product_backward_weights_workspace(n, groups, K, N, X.dtype) bytes, or None where that is 0."""
-    d, gd = _dtype(X, "X"), _dtype(dW, "dW")
-    E, K, N = dW.shape
-    n = X.shape[0]
-    x, xs = _rows(X, "X", (n, K), X.dtype)
-    y, ys = _rows(dY, "dY", (n, N), X.dtype)
+    d, gd, T = _dtype(X, "X"), _dtype(dW, "dW"), X.dtype
+    E, K, N = _weights(dW, "dW")
+    n = _matrix_rows(X, "X")
+    x, xs = _rows(X, "X", n, K, T)
+    y, ys = _rows(dY, "dY", n, N, T)
     ws = None if workspace is None else _dev_ptr(workspace, "workspace")
-    _check(_lib.groot_grouped_product_backward_weights(d, x, xs, y, ys, _array(offsets, "offsets", (E + 1,), torch.int64), gd,
+    _check(_lib.groot_grouped_product_backward_weights(d, x, xs, y, ys, _array(offsets, "offsets", (E + 1,), _int64), gd,
                                                        _array(dW, "dW", (E, K, N), dW.dtype),
                                                        _array(dbias, "dbias", (E, N), dW.dtype), n, E, K, N, ws,
                                                        0 if ws is None else workspace.numel() * workspace.element_size(),
@@ -665,23 +683,23 @@ def groot_grouped_product_backward_weights(X, dY, offsets, dW, dbias, workspace,
 
 def groot_quantize_rows(X, Q, scale, stream=None) -> None:
     """scale[i] = max |X[i]| / 127, Q[i] = X[i] / scale[i] rounded.  X [n, K], Q int8 [n, K], scale float32 [n]."""
-    n, K = X.shape
-    x, xs = _rows(X, "X", (n, K), X.dtype)
-    q, qs = _rows(Q, "Q", (n, K), torch.int8)
-    _check(_lib.groot_quantize_rows(_dtype(X, "X"), x, xs, q, qs, _array(scale, "scale", (n,), torch.float32), n, K,
+    n, K = _matrix_rows(X, "X"), X.shape[1]
+    x, xs = _rows(X, "X", n, K, X.dtype)
+    q, qs = _rows(Q, "Q", n, K, _int8)
+    _check(_lib.groot_quantize_rows(_dtype(X, "X"), x, xs, q, qs, _array(scale, "scale", (n,), _float32), n, K,
                                     _stream_handle(stream)))
 
 
 def groot_quantized_product(Q, q_scale, W, w_scale, offsets, bias, relu: bool, Y, stream=None) -> None:
     """Y[i, j] = act((Q[i] . W[g, j]) q_scale[i] w_scale[g, j] + bias[g, j]).  Q int8 [n, K], q_scale float32 [n], W int8
     [groups, N, K], w_scale and bias float32 [groups, N] (bias or None), Y [n, N]."""
-    E, N, K = W.shape
-    n = Q.shape[0]
-    q, qs = _rows(Q, "Q", (n, K), torch.int8)
-    y, ys = _rows(Y, "Y", (n, N), Y.dtype)
-    _check(_lib.groot_quantized_product(q, qs, _array(q_scale, "q_scale", (n,), torch.float32), _array(W, "W", (E, N, K), torch.int8),
-                                   _array(w_scale, "w_scale", (E, N), torch.float32),
-                                   _array(offsets, "offsets", (E + 1,), torch.int64), _array(bias, "bias", (E, N), torch.float32),
+    E, N, K = _weights(W, "W")
+    n = _matrix_rows(Q, "Q")
+    q, qs = _rows(Q, "Q", n, K, _int8)
+    y, ys = _rows(Y, "Y", n, N, Y.dtype)
+    _check(_lib.groot_quantized_product(q, qs, _array(q_scale, "q_scale", (n,), _float32), _array(W, "W", (E, N, K), _int8),
+                                   _array(w_scale, "w_scale", (E, N), _float32),
+                                   _array(offsets, "offsets", (E + 1,), _int64), _array(bias, "bias", (E, N), _float32),
                                    1 if relu else 0, _dtype(Y, "Y"), y, ys, n, E, K, N, _stream_handle(stream)))
 
 
@@ -695,13 +713,14 @@ def groot_quantized_linear_workspace(n_rows: int, K: int) -> int:
 def groot_quantized_linear(X, W, w_scale, offsets, bias, relu: bool, Y, workspace, stream=None) -> None:
     """groot_quantize_rows and groot_quantized_product in one call: X [n, K] and Y [n, N] of one floating type; workspace: a
     contiguous CUDA tensor of at least groot_quantized_linear_workspace(n, K) bytes."""
-    E, N, K = W.shape
-    n = X.shape[0]
-    x, xs = _rows(X, "X", (n, K), X.dtype)
-    y, ys = _rows(Y, "Y", (n, N), X.dtype)
-    _check(_lib.groot_quantized_linear(_dtype(X, "X"), x, xs, _array(W, "W", (E, N, K), torch.int8),
-                                  _array(w_scale, "w_scale", (E, N), torch.float32),
-                                  _array(offsets, "offsets", (E + 1,), torch.int64), _array(bias, "bias", (E, N), torch.float32),
+    d, T = _dtype(X, "X"), X.dtype
+    E, N, K = _weights(W, "W")
+    n = _matrix_rows(X, "X")
+    x, xs = _rows(X, "X", n, K, T)
+    y, ys = _rows(Y, "Y", n, N, T)
+    _check(_lib.groot_quantized_linear(d, x, xs, _array(W, "W", (E, N, K), _int8),
+                                  _array(w_scale, "w_scale", (E, N), _float32),
+                                  _array(offsets, "offsets", (E + 1,), _int64), _array(bias, "bias", (E, N), _float32),
                                   1 if relu else 0, y, ys, n, E, K, N, _dev_ptr(workspace, "workspace"),
                                   workspace.numel() * workspace.element_size(), _stream_handle(stream)))
 
@@ -732,7 +751,7 @@ class AdamwTensors:
         for name, tensors in lists.items():
             if name == "grad":
                 continue
-            want = {"param": param, "m": state, "v": state}.get(name, torch.float32)
+            want = {"param": param, "m": state, "v": state}.get(name, _float32)
             for i, t in enumerate(tensors):
                 n = lists["param"][i].numel()
                 self._set(name, i, t, want, -(-n // 256) if name.endswith("scale") else n)

@@ -94,43 +94,46 @@ __device__ __forceinline__ v4f load_codes(const uint8_t *p, float scale, int lef
     return r;
 }
 
-// x on the grid of the codes: |x| / step + u rounded down.  step is a power of two and |x| / step below 16, so both are exact and
-// the sum is rounded once, at 2^-20.
-__device__ __forceinline__ float on_grid(float x, float u)
-{
-    const float a = __builtin_fabsf(x);
-    int e = (int)(__float_as_uint(a) >> 23) - 127;
-    e = e < -6 ? -6 : e;
-    const float inverse = __uint_as_float((uint32_t)(127 + 3 - e) << 23), step = __uint_as_float((uint32_t)(127 - 3 + e) << 23);
-    const float r = fminf(floorf(a * inverse + u) * step, kCodeTop);
-    return __builtin_copysignf(r, x);
-}
-
-// Codes and scale of the wavefront's 256 values: the scale takes the largest finite magnitude to the largest code.  `never0`: a
-// positive value is held as the smallest code at least (a root of 0 beside a first moment above 0 is a step of m / eps).
+// Codes and scale of the wavefront's 256 values: the scale takes the largest finite magnitude to the largest code.  The instruction
+// adds its random number's upper 20 bits behind the three that a code keeps and cuts the rest off (below 2^-6: behind steps of 2^-9).
+// `never0`: a positive value is held as the smallest code at least (a root of 0 beside a first moment above 0 is a step of m / eps).
+// The scale's reciprocal is off by 2^-22 at most, which moves a value's chance to be rounded up by as much.
 template <bool kWhole>
-__device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, const uint32_t (&u16)[4], bool never0, int left)
+__device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, const uint32_t (&random)[4], bool never0, int left)
 {
 #pragma clang fp contract(off)
     float top = 0.f;
+    // one look at four values: their sum is not finite if one of them is not
+    if (__all(__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])))) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const float a = __builtin_fabsf(x[k]);
-        if (__builtin_isfinite(a) && (kWhole || k < left)) top = fmaxf(top, a);
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, __builtin_fabsf(x[k]));   // values that do not exist are zeros
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, __builtin_isfinite(x[k]) ? __builtin_fabsf(x[k]) : 0.f);
     }
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
     const float scale = top * (1.f / kCodeTop);
+    // scales whose reciprocal is not exact enough or infinite: quotients
+    const bool small = scale < 0x1p-100f;
+    const float inverse = small ? 0.f : 1.f / scale;
     v4f r;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const float over = scale > 0.f ? x[k] / scale : 0.f;
-        r[k] = on_grid(over, (float)u16[k] * 0x1p-16f);
-        if (never0 && x[k] > 0.f && r[k] == 0.f) r[k] = kCodeLeast;
-        if (!__builtin_isfinite(x[k])) r[k] = __builtin_nanf("");
+        r[k] = x[k] * inverse;
+        if (small) r[k] = scale > 0.f ? x[k] / scale : 0.f;
+        r[k] = __builtin_amdgcn_fmed3f(r[k], -kCodeTop, kCodeTop);
+        if (never0 && x[k] > 0.f) r[k] = fmaxf(r[k], kCodeLeast);
     }
-    uint32_t c = __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], 0, false);
-    c = __builtin_amdgcn_cvt_pk_fp8_f32(r[2], r[3], c, true);
+    uint32_t c = __builtin_amdgcn_cvt_sr_fp8_f32(r[0], random[0], 0, 0);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(r[1], random[1], c, 1);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(r[2], random[2], c, 2);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(r[3], random[3], c, 3);
+    if (!__all(__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])))) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (!__builtin_isfinite(x[k])) c |= 0x7Fu << (8 * k);
+    }
     if (kWhole) {
         *(uint32_t *)p = c;
     } else {
@@ -139,6 +142,15 @@ __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, 
             if (k < left) p[k] = (uint8_t)(c >> (8 * k));
     }
     if (threadIdx.x % kWave == 0) *scale_at = scale;
+}
+
+// Square root and quotient within an ulp or two, from the instructions: where a value takes 16 bytes (states in 8 bits) the exact ones'
+// 20 instructions more bound the kernel.  The square root of numbers below the normal ones is kept.
+__device__ __forceinline__ float near_root(float v)
+{
+    const bool small = v < 0x1p-96f;
+    const float s = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
+    return small ? s * 0x1p-32f : s;
 }
 
 // the values [at, at + 4) of a tensor, by one lane; all lanes of the wavefront come here
@@ -167,8 +179,9 @@ __device__ __forceinline__ void adamw_values(const AdamwTensor &t, const AdamwFa
         const float gk = scaled ? g[k] * gs : g[k];
         m[k] = m[k] * f.beta1 + gk * f.one_minus_beta1;
         v[k] = v[k] * f.beta2 + (gk * gk) * f.one_minus_beta2;
-        root[k] = sqrtf(v[k]);
-        w[k] = w[k] * f.decay - f.step_size * (m[k] / (root[k] * f.root_factor + f.eps));
+        root[k] = kBits == 8 ? near_root(v[k]) : sqrtf(v[k]);
+        const float denom = root[k] * f.root_factor + f.eps;
+        w[k] = w[k] * f.decay - f.step_size * (kBits == 8 ? m[k] * __builtin_amdgcn_rcpf(denom) : m[k] / denom);
     }
     if (kMaster) store4<float, kWhole>(master, w, left);
     store4<P, kWhole>(param, w, left);
@@ -178,8 +191,8 @@ __device__ __forceinline__ void adamw_values(const AdamwTensor &t, const AdamwFa
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t h = mixed((uint32_t)(at + k) ^ key);
-            low[k] = h & 0xFFFFu;
-            high[k] = h >> 16;
+            low[k] = h << 16;
+            high[k] = h & 0xFFFF0000u;
         }
         store_codes<kWhole>((uint8_t *)t.m + at, t.m_scale + block, m, low, false, left);
         store_codes<kWhole>((uint8_t *)t.v + at, t.v_scale + block, root, high, true, left);

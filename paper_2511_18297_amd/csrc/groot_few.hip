@@ -98,33 +98,19 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, i
 #pragma unroll
         for (int m = 0; m < kFusedRows; ++m) {
             if (m >= rows) break;
-            float top = 0.f;
-            bool fine = true;
-            auto look = [&](v4i v) {
-                const RowValues<X> e = row_values<X>(v);
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    const float a = __builtin_fabsf(e.x[k]);
-                    fine = fine && __builtin_isfinite(a);
-                    top = fmaxf(top, a);
-                }
-            };
+            uint32_t seen = 0;
 #pragma unroll
             for (int i = 0; i < kKeep; ++i)
-                if ((int)threadIdx.x + i * kFewThreads < loads) look(keep[m][i] = get(t.begin + m, threadIdx.x + i * kFewThreads));
-            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) look(get(t.begin + m, i));
-            if (!fine) top = __builtin_inff();               // carries the news through the maximum
-#pragma unroll
-            for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+                if ((int)threadIdx.x + i * kFewThreads < loads) seen = row_look<X>(keep[m][i] = get(t.begin + m, threadIdx.x + i * kFewThreads), seen);
+            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) seen = row_look<X>(get(t.begin + m, i), seen);
+            const float top = row_top_of<kWave>(row_top<X>(seen));
             if (lane == 0) tops[m][wave] = top;
         }
         __syncthreads();
 #pragma unroll
         for (int m = 0; m < kFusedRows; ++m) {
             if (m >= rows) break;
-            float top = tops[m][0];
-#pragma unroll
-            for (int k = 1; k < kFewWaves; ++k) top = fmaxf(top, tops[m][k]);
+            const float top = row_top_of<kFewWaves>(tops[m][lane % kFewWaves]);
             const float scale = row_scale(top);
             int8_t *const to = (int8_t *)cut + m * cut_row;
             auto put = [&](v4i v, int32_t i) { row_codes<X>(v, scale, to + (int64_t)i * kPer); };

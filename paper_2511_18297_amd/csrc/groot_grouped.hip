@@ -15,7 +15,7 @@ constexpr int log2_of(int64_t x)
 }
 
 // The epilogue of a wavefront's 32 x 32 blocks.  A lane's four neighbouring columns of one row would make stores of 16 bytes in 32
-// rows; the block goes through 4 KB of the wavefront's LDS (16-byte pieces at c ^ (row & 7)), and every store covers eight rows of 32
+// rows; the block goes through 4 KB of the wavefront's LDS (its pieces where swizzle_along has them), and every store covers eight rows of 32
 // whole columns.  A lane keeps one place in the columns, with its bias and scales, for all rows.
 template <typename T, typename O, int kJ>
 struct Epilogue {
@@ -46,14 +46,14 @@ struct Epilogue {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const v4f x = {(float)sums[j][4 * q], (float)sums[j][4 * q + 1], (float)sums[j][4 * q + 2], (float)sums[j][4 * q + 3]};
-                *(v4f *)(scratch + m * 128 + (((2 * q + half) ^ (m & 7)) * 16)) = x;
+                *(v4f *)(scratch + m * 128 + (((2 * q + half) ^ swizzle_along<128>(m)) * 16)) = x;
             }
             wave_sync();
             const int32_t left = p.N - col[j];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 8 * i + lane / 8;
-                v4f y = *(const v4f *)(scratch + r * 128 + ((lane % 8 ^ lane / 8) * 16));
+                v4f y = *(const v4f *)(scratch + r * 128 + ((lane % 8 ^ swizzle_along<128>(r)) * 16));
                 if (r < rows && left > 0) {
                     const float s = std::is_same<T, int8_t>::value ? p.a_scale[row + r] : 1.f;
 #pragma unroll
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const Row
     const int wave = threadIdx.x / kWave;
     const int row0 = wave / kWavesN * (kM / kWavesM), col0 = wave % kWavesN * (kN / kWavesN);
     typename TileType<T>::Sum sums[kI][kJ];
-    tile_product<T, kStages>(a, b, lds, (p.K + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums);
+    tile_product<T, kStages>(a, b, lds, (p.K + StageA::kValues - 1) / StageA::kValues, row0, col0, sums);
     __syncthreads();                                         // LDS is free
     Epilogue<T, O, kJ> epilogue;
     epilogue.init(p, t.group, j0 + col0);
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
 {
     constexpr int kThreads = kWaves * kWave, kJ = kN / 32, kEach = kNarrowStage / 16 / kWave;
     typedef Stage<T, kN, kThreads, !kNMajor, kAligned> StageB;
-    typedef Stage<T, kNarrowRows, kThreads, false, kAligned> Rows;       // its layout in LDS
+    typedef Stage<T, kNarrowRows, kBlock, false, kAligned> Rows;       // its layout in LDS
     extern __shared__ __align__(16) char lds[];              // weights, then every wavefront's steps
     const RowTile t = find_tile(p.offsets, p.groups, p.n, blockIdx.x, log_rows);
     if (t.group < 0) return;
@@ -133,19 +133,20 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
     const int64_t rows = t.end - t.begin, pitch = p.a_stride * (int64_t)sizeof(T);
     const int32_t blocks = (int32_t)((rows + kNarrowRows - 1) / kNarrowRows), mine = (blocks - wave + kWaves - 1) / kWaves;
     const int32_t bytes = p.K * (int32_t)sizeof(T), items = mine * steps;
-    const int own = lane / 8, piece = (lane % 8 ^ own) * 16;
-    const char *const from = (const char *)((const T *)p.A + t.begin * p.a_stride) + piece;
+    const int own = lane / 8;
+    const char *const from = (const char *)((const T *)p.A + t.begin * p.a_stride);
     v4i held[kAligned ? 1 : kEach];
     // the next step to load: its block of rows and its place in the rows
     int32_t load_block = wave, load_step = 0;
     auto begin = [&](int slot) {
         const int64_t row = (int64_t)load_block * kNarrowRows + own;
-        const int32_t left = load_block < blocks ? bytes - load_step * kStepBytes - piece : 0;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
+            const int32_t at = load_step * kStepBytes + (lane % 8 ^ swizzle_along<kStepBytes>(8 * i + own)) * 16;
+            const int32_t left = load_block < blocks ? bytes - at : 0;
             int64_t r = row + 8 * i;
             r = r < rows ? r : rows - 1;
-            const char *q = from + r * pitch + load_step * kStepBytes;
+            const char *q = from + r * pitch + at;
             if constexpr (kAligned) dma16(left > 0 ? q : (const char *)&g_zeros, lds_offset(ring) + slot * kNarrowStage + i * (kWave * 16));
             else held[i] = load16<T>(q, left);
         }
@@ -213,18 +214,25 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
 
 bool on16(const void *a, int64_t bytes) { return (((uintptr_t)a | (uintptr_t)bytes) & 15) == 0; }
 
-template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kNMajor>
+template <typename T, bool kNMajor>
+bool rows_aligned(const RowsProduct &p)
+{
+    const int64_t b = sizeof(T);
+    return on16(p.A, p.a_stride * b) && on16(p.B, (kNMajor ? p.K : p.N) * b) && p.K * b % 16 == 0;
+}
+
+template <typename O>
+bool out_whole(const RowsProduct &p) { return (((uintptr_t)p.out | (uintptr_t)(p.out_stride * sizeof(O))) & (4 * sizeof(O) - 1)) == 0; }
+
+template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kNMajor, bool kAligned>
 int rows_launch(const RowsProduct &p, void *stream)
 {
     const int32_t col_tiles = (p.N + kN - 1) / kN;
     const TileOrder order((p.n + kM - 1) / kM + (p.offsets ? p.groups : 0), col_tiles);
-    const int64_t b = sizeof(T);
-    const bool aligned = on16(p.A, p.a_stride * b) && on16(p.B, (kNMajor ? p.K : p.N) * b) && p.K * b % 16 == 0;
-    const bool whole = (((uintptr_t)p.out | (uintptr_t)(p.out_stride * sizeof(O))) & (4 * sizeof(O) - 1)) == 0;
     constexpr int kThreads = kWavesM * kWavesN * kWave;
     if (!fits_launch(order.workgroups, kThreads)) return kErrTooManyTiles;
-    if (aligned) rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kStages, kNMajor, true><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
-    else rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kStages, kNMajor, false><<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, whole);
+    rows_kernel<T, O, kM, kN, kWavesM, kWavesN, kStages, kNMajor, kAligned>
+        <<<(uint32_t)order.workgroups, kThreads, 0, (hipStream_t)stream>>>(p, order, col_tiles, out_whole<O>(p));
     return (int)hipGetLastError();
 }
 
@@ -245,13 +253,50 @@ template <typename T, typename O, int kN, bool kNMajor>
 int narrow_launch(const RowsProduct &p, void *stream)
 {
     const int32_t steps = (int32_t)((p.K * sizeof(T) + kStepBytes - 1) / kStepBytes);
-    const int64_t b = sizeof(T);
-    const bool aligned = on16(p.A, p.a_stride * b) && on16(p.B, (kNMajor ? p.K : p.N) * b) && p.K * b % 16 == 0;
-    const bool whole = (((uintptr_t)p.out | (uintptr_t)(p.out_stride * sizeof(O))) & (4 * sizeof(O) - 1)) == 0;
-    int log_rows = 7;                                        // about 1024 workgroups, of 128 rows at least
+    const bool aligned = rows_aligned<T, kNMajor>(p), whole = out_whole<O>(p);
+    int log_rows = 8;                                        // about 1024 workgroups, of 256 rows at least
     while (log_rows < 20 && ((int64_t)1024 << log_rows) < p.n) ++log_rows;
-    return aligned ? narrow_launch_as<T, O, kN, 4, 4, kNMajor, true>(p, log_rows, steps, whole, stream)
-                   : narrow_launch_as<T, O, kN, 4, 1, kNMajor, false>(p, log_rows, steps, whole, stream);
+    // 16 wavefronts to a CU with a step of their own on the way each; 8 with two or three were 8 % slower at 64 x 64, 14 % at 128 x 128
+    return aligned ? narrow_launch_as<T, O, kN, 8, 2, kNMajor, true>(p, log_rows, steps, whole, stream)
+                   : narrow_launch_as<T, O, kN, 8, 1, kNMajor, false>(p, log_rows, steps, whole, stream);
+}
+
+// What a step of the contraction (128 bytes) takes, in ns, where the GPU's 256 CUs hold up to 256 or up to 512 tiles at a time
+// (K = 4096 bytes, fp32: MFMA-bound; the others: products of 2, 1, 1/2 .. steps' latency).  A tile's rows and columns and how many
+// stages of it lie in LDS:
+//                        256 x 256, 2   128 x 128, 2   128 x 128, 4   64 x 128, 3   64 x 64, 5   32 x 128, 4   32 x 64, 6
+struct TileCost {
+    int32_t rows, cols, to256, to512;        // to512 0: one tile to a CU
+};
+constexpr int kTileKinds = 7;
+constexpr TileCost kTile16[kTileKinds] = {{256, 256, 2060, 0}, {128, 128, 1000, 1270}, {128, 128, 790, 0}, {64, 128, 550, 840},
+                                          {64, 64, 380, 570}, {32, 128, 410, 630}, {32, 64, 400, 420}};
+constexpr TileCost kTile32[kTileKinds] = {{256, 256, 9260, 0}, {128, 128, 2360, 4540}, {128, 128, 2370, 0}, {64, 128, 1330, 2370},
+                                          {64, 64, 830, 1370}, {32, 128, 870, 1430}, {32, 64, 820, 880}};
+
+// The kind of tile that takes the least time by that table; rows that do not begin on 16 bytes go through registers, for which three
+// of the kinds are built.
+template <typename T>
+int choose_tile(int64_t n, int32_t groups, bool offsets, int32_t N, bool aligned)
+{
+    int best = -1;
+    double least = 0;
+    for (int k = 0; k < kTileKinds; ++k) {
+        if (!aligned && k != 1 && k != 4 && k != 6) continue;
+        if (sizeof(T) == 4 && k == 0) continue;
+        const TileCost &c = sizeof(T) == 4 ? kTile32[k] : kTile16[k];
+        // a group's last tile is half full, on average
+        double rows = offsets ? (double)n / c.rows + 0.5 * groups : (double)((n + c.rows - 1) / c.rows);
+        const double least_rows = (double)(n < groups ? n : groups);
+        rows = rows < least_rows ? least_rows : rows;
+        const double tiles = rows * ((N + c.cols - 1) / c.cols), at_once = c.to512 ? 512 : 256;
+        const double full = (double)(int64_t)(tiles / at_once), rest = tiles - full * at_once, all = c.to512 ? c.to512 : c.to256;
+        double time = full * all + (rest <= 0 ? 0 : rest > 256 ? c.to512 : c.to256);
+        // ragged groups: the number is a guess, and near or above a full GPU half a round more is
+        if (offsets && tiles > 0.8 * at_once) time = (tiles / at_once + 0.5) * all;
+        if (best < 0 || time < least) best = k, least = time;
+    }
+    return best;
 }
 
 template <typename T, typename O, bool kNMajor>
@@ -260,23 +305,48 @@ int rows_choose(const RowsProduct &p, void *stream)
     const int64_t each = p.n / p.groups;                      // rows of a group, on average
     if (p.K * (int)sizeof(T) <= kNarrowBytes && p.N <= 128 && each >= 64)
         return p.N <= 64 ? narrow_launch<T, O, 64, kNMajor>(p, stream) : narrow_launch<T, O, 128, kNMajor>(p, stream);
-    if (sizeof(T) < 4 && each >= 192 && p.n * p.N >= (int64_t)256 * 256 * 192) return rows_launch<T, O, 256, 256, 2, 4, 2, kNMajor>(p, stream);
-    if (each > 32) return rows_launch<T, O, 128, 128, 2, 2, 2, kNMajor>(p, stream);
-    if ((p.n + 31) / 32 * ((p.N + 127) / 128) + p.groups >= 512) return rows_launch<T, O, 32, 128, 1, 4, 3, kNMajor>(p, stream);
-    return rows_launch<T, O, 32, 64, 1, 2, 6, kNMajor>(p, stream);
+    const bool aligned = rows_aligned<T, kNMajor>(p);
+    const int kind = choose_tile<T>(p.n, p.groups, p.offsets != nullptr, p.N, aligned);
+    if (!aligned) {
+        if (kind == 1) return rows_launch<T, O, 128, 128, 2, 2, 2, kNMajor, false>(p, stream);
+        if (kind == 4) return rows_launch<T, O, 64, 64, 2, 2, 2, kNMajor, false>(p, stream);
+        return rows_launch<T, O, 32, 64, 1, 2, 2, kNMajor, false>(p, stream);
+    }
+    switch (kind) {
+    case 0:
+        if constexpr (sizeof(T) < 4) return rows_launch<T, O, 256, 256, 2, 4, 2, kNMajor, true>(p, stream);
+    case 1: return rows_launch<T, O, 128, 128, 2, 2, 2, kNMajor, true>(p, stream);
+    case 2: return rows_launch<T, O, 128, 128, 2, 2, 4, kNMajor, true>(p, stream);
+    case 3: return rows_launch<T, O, 64, 128, 2, 2, 3, kNMajor, true>(p, stream);
+    case 4: return rows_launch<T, O, 64, 64, 2, 2, 5, kNMajor, true>(p, stream);
+    case 5: return rows_launch<T, O, 32, 128, 1, 4, 4, kNMajor, true>(p, stream);
+    default: return rows_launch<T, O, 32, 64, 1, 2, 6, kNMajor, true>(p, stream);
+    }
 }
 
-// How the contraction of the weight gradients, a group's rows, is cut: pieces of 2^log_rows rows, so that their number times that of
-// the tiles of dW comes to about 1024 workgroups.  A piece of 512 rows reads eight times what its partial sums are written and read
-// again for.  A group of one piece needs no partial sums, and a group without rows is one piece of zeros.
+// How the weight gradients are cut.  Tiles of dW of 64 x 64 where it is no larger (typed layers), of 256 x 256 where all groups' fill
+// the GPU, else of 128 x 128.  The contraction, a group's rows, is cut into pieces of 2^log_rows rows where there are fewer tiles than
+// workgroups that the GPU holds; a piece of 512 rows reads eight times what its partial sums are written and read again for.  A
+// group of one piece needs no partial sums, and a group without rows is one piece of zeros.
 struct WeightsSplit {
+    int32_t tile;                            // 64, 128 or 256
+    int32_t k_tiles, n_tiles;
     int log_rows;
     int64_t tiles;                           // pieces of all groups, at most
     int64_t slots;                           // pieces of groups that are cut, at most
-    WeightsSplit(int64_t n, int32_t groups, bool offsets, int64_t dw_tiles)
+    WeightsSplit(int32_t dtype, int64_t n, int32_t groups, bool offsets, int32_t K, int32_t N)
     {
+        const auto tiles_of = [](int32_t width, int32_t by) { return (width + by - 1) / by; };
+        tile = K <= 64 && N <= 64 ? 64 : 128;
+        if (dtype != GROOT_F32 && (int64_t)tiles_of(K, 256) * tiles_of(N, 256) * groups >= 192 && n >= (int64_t)256 * groups) tile = 256;
+        k_tiles = tiles_of(K, tile);
+        n_tiles = tiles_of(N, tile);
+        const int64_t wanted = tile == 64 ? 1024 : 256;
         log_rows = 9;
-        while (log_rows < 40 && ((int64_t)1024 << log_rows) < n * dw_tiles) ++log_rows;
+        while (log_rows < 40 && (wanted << log_rows) < n * k_tiles * n_tiles) ++log_rows;
+        // enough tiles without cutting: only groups of four times the average are cut
+        if ((int64_t)groups * k_tiles * n_tiles >= wanted)
+            while (log_rows < 40 && ((int64_t)groups << log_rows) < 4 * n) ++log_rows;
         const int64_t rows = (int64_t)1 << log_rows;
         tiles = (n + rows - 1) / rows + (offsets ? groups : 0);
         if (tiles < 1) tiles = 1;
@@ -285,28 +355,16 @@ struct WeightsSplit {
     }
 };
 
-struct WeightsTile {
-    int32_t k, n;
-};
-// 64 x 64 where dW is no larger (typed layers); 128 x 128
-WeightsTile weights_tile(int32_t K, int32_t N) { return K <= 64 && N <= 64 ? WeightsTile{64, 64} : WeightsTile{128, 128}; }
-
-WeightsSplit weights_split(int64_t n, int32_t groups, bool offsets, int32_t K, int32_t N)
-{
-    const WeightsTile t = weights_tile(K, N);
-    return WeightsSplit(n, groups, offsets, (int64_t)((K + t.k - 1) / t.k) * ((N + t.n - 1) / t.n));
-}
-
 // dW[g] = X_g^T dY_g and the column sums of dY_g: a workgroup takes kK x kN of one group's product and one piece of the group's
 // rows.  The partial sums of a group in several pieces lie in the workspace, piece after piece, K x N and N floats each.
-template <typename T, typename O, int kK, int kN, int kWavesK, int kWavesN, bool kAligned>
+template <typename T, typename O, int kK, int kN, int kWavesK, int kWavesN, int kStages, bool kAligned>
 __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const WeightsProduct p, const TileOrder order, int log_rows, int64_t slots,
                                                                          int32_t k_tiles, int32_t n_tiles)
 {
     constexpr int kThreads = kWavesK * kWavesN * kWave, kI = kK / kWavesK / 32, kJ = kN / kWavesN / 32;
     typedef Stage<T, kK, kThreads, true, kAligned> StageX;
     typedef Stage<T, kN, kThreads, true, kAligned> StageY;
-    __shared__ __align__(16) char lds[2 * (StageX::kBytes + StageY::kBytes)];
+    __shared__ __align__(16) char lds[(kAligned ? kStages : 2) * (StageX::kBytes + StageY::kBytes)];
     int64_t row_tile;
     int32_t n_tile;
     order.find(blockIdx.x, &row_tile, &n_tile);
@@ -323,7 +381,7 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
     typename TileType<T>::Sum sums[kI][kJ];
     float columns[kJ] = {};
     const bool bias = p.dbias && k0 == 0 && row0 == 0;
-    tile_product<T, 2, true>(x, y, lds, (t.end - t.begin + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums, &columns, bias);
+    tile_product<T, kStages, true>(x, y, lds, (t.end - t.begin + kStepValues<T> - 1) / kStepValues<T>, row0, col0, sums, &columns, bias);
     const bool alone = t.count == 1;
     if (!alone && t.shared_before + t.place >= slots) return;   // offsets that do not ascend: more pieces than there are rows for
     float *const part = (float *)p.workspace + (t.shared_before + t.place) * ((int64_t)p.K * p.N + p.N);
@@ -355,15 +413,17 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
     }
 }
 
-// The partial sums of groups in several pieces, added up in fp64: 16 lanes to 64 neighbouring values, every 16 lanes of a workgroup
-// a share of the pieces, then the shares.  dbias lies behind dW.
+// The partial sums of groups in several pieces, added up in fp64.  A lane takes four neighbouring values; `shares` (a power of two)
+// lanes of a workgroup take the same four, each a share of the pieces, and their sums meet in LDS.  dbias lies behind dW.
+constexpr int kSumLanes = 512;
+
 template <typename O>
-__global__ __launch_bounds__(1024) void weights_sum_kernel(const WeightsProduct p, int log_rows, int64_t slots, uint32_t per_group)
+__global__ __launch_bounds__(kSumLanes) void weights_sum_kernel(const WeightsProduct p, int log_rows, int64_t slots, uint32_t per_group, int shares)
 {
     typedef double v4d __attribute__((ext_vector_type(4)));
-    __shared__ v4d shares[64][16];
+    __shared__ v4d sums[kSumLanes];
     const int32_t g = (int32_t)(blockIdx.x / per_group);
-    const int lane = threadIdx.x % kWave, quad = threadIdx.x % 16, share = threadIdx.x / 16, of = blockDim.x / 16;
+    const int lane = threadIdx.x % kWave, quads = kSumLanes / shares, quad = threadIdx.x % quads, share = threadIdx.x / quads;
     const int64_t rows = (int64_t)1 << log_rows;
     int64_t begin, end, before = 0;
     group_rows(p.offsets, p.n, g, &begin, &end);
@@ -377,64 +437,84 @@ __global__ __launch_bounds__(1024) void weights_sum_kernel(const WeightsProduct 
     }
     count = before + count <= slots ? count : before < slots ? slots - before : 0;
     const int64_t dw = (int64_t)p.K * p.N, slot = dw + p.N, values = p.dbias ? slot : dw;
-    for (int64_t first = (int64_t)(blockIdx.x % per_group) * 64; first < values; first += (int64_t)per_group * 64) {
+    for (int64_t first = (int64_t)(blockIdx.x % per_group) * quads * 4; first < values; first += (int64_t)per_group * quads * 4) {
         const int64_t at = first + quad * 4;
         const float *from = (const float *)p.workspace + before * slot + at;
         v4d sum = {0, 0, 0, 0};
         if (slot % 4 == 0 && at + 4 <= values) {
 #pragma unroll 4
-            for (int64_t c = share; c < count; c += of) {
+            for (int64_t c = share; c < count; c += shares) {
                 const v4f x = *(const v4f *)(from + c * slot);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) sum[k] += (double)x[k];
             }
         } else {
-            for (int64_t c = share; c < count; c += of)
+            for (int64_t c = share; c < count; c += shares)
                 for (int k = 0; k < 4; ++k)
                     if (at + k < values) sum[k] += (double)from[c * slot + k];
         }
-        shares[share][quad] = sum;
-        __syncthreads();
-        if (share == 0) {
-            for (int w = 1; w < of; ++w) sum += shares[w][quad];
+        if (shares > 1) {
+            sums[threadIdx.x] = sum;
+            __syncthreads();
+            if (share == 0)
+                for (int w = 1; w < shares; ++w) sum += sums[w * quads + quad];
+            __syncthreads();
+            if (share) continue;
+        }
+        const v4f total = {(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]};
+        if (at + 4 <= dw) {
+            store_quad((O *)p.dW + g * dw + at, total, 4, ((uintptr_t)p.dW | (uintptr_t)(dw * sizeof(O))) % (4 * sizeof(O)) == 0);
+        } else {
             for (int k = 0; k < 4; ++k) {
                 const int64_t i = at + k;
-                if (i < dw) ((O *)p.dW)[g * dw + i] = (O)(float)sum[k];
-                else if (i < values) ((O *)p.dbias)[(int64_t)g * p.N + (i - dw)] = (O)(float)sum[k];
+                if (i < dw) ((O *)p.dW)[g * dw + i] = (O)total[k];
+                else if (i < values) ((O *)p.dbias)[(int64_t)g * p.N + (i - dw)] = (O)total[k];
             }
         }
-        __syncthreads();
     }
 }
 
-template <typename T, typename O, int kK, int kN>
-int weights_launch_tile(const WeightsProduct &p, const WeightsSplit &split, bool aligned, hipStream_t stream)
+template <typename T, typename O, int kTile, int kWavesK, int kWavesN, int kStages, bool kAligned>
+int weights_launch_tile(const WeightsProduct &p, const WeightsSplit &split, hipStream_t stream)
 {
-    const int32_t k_tiles = (p.K + kK - 1) / kK, n_tiles = (p.N + kN - 1) / kN;
-    const TileOrder order(split.tiles * k_tiles, n_tiles);
-    if (!fits_launch(order.workgroups, kBlock)) return kErrTooManyTiles;
-    if (aligned) weights_kernel<T, O, kK, kN, 2, 2, true><<<(uint32_t)order.workgroups, kBlock, 0, stream>>>(p, order, split.log_rows, split.slots, k_tiles, n_tiles);
-    else weights_kernel<T, O, kK, kN, 2, 2, false><<<(uint32_t)order.workgroups, kBlock, 0, stream>>>(p, order, split.log_rows, split.slots, k_tiles, n_tiles);
+    constexpr int kThreads = kWavesK * kWavesN * kWave;
+    const TileOrder order(split.tiles * split.k_tiles, split.n_tiles);
+    if (!fits_launch(order.workgroups, kThreads)) return kErrTooManyTiles;
+    weights_kernel<T, O, kTile, kTile, kWavesK, kWavesN, kStages, kAligned>
+        <<<(uint32_t)order.workgroups, kThreads, 0, stream>>>(p, order, split.log_rows, split.slots, split.k_tiles, split.n_tiles);
     return (int)hipGetLastError();
 }
 
 template <typename T, typename O>
-int weights_launch(const WeightsProduct &p, void *stream)
+int weights_launch(int32_t dtype, const WeightsProduct &p, void *stream)
 {
     const int64_t b = sizeof(T);
     const bool aligned = on16(p.X, p.x_stride * b) && on16(p.dY, p.dy_stride * b) && p.K * b % 16 == 0 && p.N * b % 16 == 0;
-    const WeightsSplit split = weights_split(p.n, p.groups, p.offsets != nullptr, p.K, p.N);
+    WeightsSplit split(dtype, p.n, p.groups, p.offsets != nullptr, p.K, p.N);
     const hipStream_t s = (hipStream_t)stream;
-    const int err = weights_tile(p.K, p.N).k == 64 ? weights_launch_tile<T, O, 64, 64>(p, split, aligned, s)
-                                                   : weights_launch_tile<T, O, 128, 128>(p, split, aligned, s);
+    int err = 0;
+    if (split.tile == 64) {
+        err = aligned ? weights_launch_tile<T, O, 64, 2, 2, 2, true>(p, split, s) : weights_launch_tile<T, O, 64, 2, 2, 2, false>(p, split, s);
+    } else if (split.tile == 128 || !aligned) {
+        // the same pieces of rows in smaller tiles: the 256 x 256 one is not built for rows that go through registers
+        split.k_tiles = (p.K + 127) / 128;
+        split.n_tiles = (p.N + 127) / 128;
+        // four stages where a CU has one tile at most
+        const bool few = (int64_t)p.groups * split.k_tiles * split.n_tiles <= 256 && split.slots == 0;
+        err = !aligned ? weights_launch_tile<T, O, 128, 2, 2, 2, false>(p, split, s)
+              : few    ? weights_launch_tile<T, O, 128, 2, 2, 4, true>(p, split, s)
+                       : weights_launch_tile<T, O, 128, 2, 2, 2, true>(p, split, s);
+    } else if constexpr (sizeof(T) == 2) {
+        err = weights_launch_tile<T, O, 256, 2, 4, 2, true>(p, split, s);
+    }
     if (err) return err;
     if (split.slots == 0) return 0;
-    const int64_t parts = ((int64_t)p.K * p.N + p.N + 63) / 64;
-    int64_t per_group = 8192 / p.groups;
+    int shares = 1;                                          // a share for every four pieces that a group has on average, 64 at most
+    while (shares < 64 && (int64_t)shares * 4 * p.groups < split.tiles) shares *= 2;
+    const int64_t parts = ((int64_t)p.K * p.N + p.N + kSumLanes / shares * 4 - 1) / (kSumLanes / shares * 4);
+    int64_t per_group = 4096 / p.groups;
     per_group = per_group < 1 ? 1 : per_group > parts ? parts : per_group;
-    int lanes = 64;                                          // 16 for every two pieces that a group has on average, 1024 at most
-    while (lanes < 1024 && (int64_t)lanes * p.groups < 8 * split.tiles) lanes *= 2;
-    weights_sum_kernel<O><<<(uint32_t)(per_group * p.groups), lanes, 0, s>>>(p, split.log_rows, split.slots, (uint32_t)per_group);
+    weights_sum_kernel<O><<<(uint32_t)(per_group * p.groups), kSumLanes, 0, s>>>(p, split.log_rows, split.slots, (uint32_t)per_group, shares);
     return (int)hipGetLastError();
 }
 
@@ -456,18 +536,18 @@ int launch_int8_rows(int32_t out_dtype, const RowsProduct &p, void *stream)
     return rows_choose<int8_t, f16_t, true>(p, stream);
 }
 
-size_t grouped_weights_workspace(int32_t, int64_t n, int32_t groups, int32_t K, int32_t N)
+size_t grouped_weights_workspace(int32_t dtype, int64_t n, int32_t groups, int32_t K, int32_t N)
 {
     // whether the call will have offsets is not known here: without, there is one group and no more pieces than with
-    const WeightsSplit split = weights_split(n, groups, true, K, N);
+    const WeightsSplit split(dtype, n, groups, true, K, N);
     return (size_t)split.slots * ((size_t)K * N + N) * 4;
 }
 
 int launch_grouped_weights(int32_t dtype, const WeightsProduct &p, void *stream)
 {
-    if (dtype == GROOT_F32) return weights_launch<float, float>(p, stream);
-    if (dtype == GROOT_BF16) return p.grad_f32 ? weights_launch<bf16_t, float>(p, stream) : weights_launch<bf16_t, bf16_t>(p, stream);
-    return p.grad_f32 ? weights_launch<f16_t, float>(p, stream) : weights_launch<f16_t, f16_t>(p, stream);
+    if (dtype == GROOT_F32) return weights_launch<float, float>(dtype, p, stream);
+    if (dtype == GROOT_BF16) return p.grad_f32 ? weights_launch<bf16_t, float>(dtype, p, stream) : weights_launch<bf16_t, bf16_t>(dtype, p, stream);
+    return p.grad_f32 ? weights_launch<f16_t, float>(dtype, p, stream) : weights_launch<f16_t, f16_t>(dtype, p, stream);
 }
 
 }  // namespace groot

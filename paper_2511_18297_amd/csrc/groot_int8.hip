@@ -20,33 +20,22 @@ __global__ __launch_bounds__(kBlock) void quantize_kernel(const T *__restrict__ 
         const int64_t row = first + threadIdx.x / kLanes;
         const char *const x = (const char *)(X + (row < n ? row : n - 1) * x_stride);
         auto get = [&](int32_t i) { return load16<T>(x + (int64_t)i * 16, ((int64_t)K - (int64_t)i * kPer) * (int64_t)sizeof(T)); };
-        float top = 0.f;
-        bool fine = true;
-        auto look = [&](v4i v) {
-            const RowValues<T> e = row_values<T>(v);
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                const float a = __builtin_fabsf(e.x[k]);
-                fine = fine && __builtin_isfinite(a);
-                top = fmaxf(top, a);
-            }
-        };
         v4i keep[kKeep];
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
             if (at + i * kLanes < loads) keep[i] = get(at + i * kLanes);
+        uint32_t seen = 0;
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
-            if (at + i * kLanes < loads) look(keep[i]);
-        for (int32_t i = at + kKeep * kLanes; i < loads; i += kLanes) look(get(i));
-        if (!fine) top = __builtin_inff();                   // carries the news through the maximum
-#pragma unroll
-        for (int d = 1; d < (kLanes < kWave ? kLanes : kWave); d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+            if (at + i * kLanes < loads) seen = row_look<T>(keep[i], seen);
+        for (int32_t i = at + kKeep * kLanes; i < loads; i += kLanes) seen = row_look<T>(get(i), seen);
+        float top = row_top_of<(kLanes < kWave ? kLanes : kWave)>(row_top<T>(seen));
         if constexpr (kLanes > kWave) {
             __syncthreads();                                 // the row before has read the maxima
             if (threadIdx.x % kWave == 0) tops[threadIdx.x / kWave] = top;
             __syncthreads();
-            top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+            static_assert(kWavesPerBlock == 4, "the maxima of four wavefronts");
+            top = row_top_of<4>(tops[threadIdx.x % 4]);
         }
         if (row >= n) continue;
         const float scale = row_scale(top);

@@ -1,13 +1,14 @@
 // Matrix-core tiles shared by the grouped products and the products in 8-bit integers.
 //
-// A step of the contraction is 128 bytes of a row whose elements lie along it ("along": 64 values of 16 bits, 32 of fp32, 128 of
-// 8 bits), or as many rows of a matrix whose rows lie across it ("across").  Both operands of a step are staged in LDS by loads
+// A step of the contraction is 128 (or 64) bytes of a row whose elements lie along it ("along": 64 values of 16 bits, 32 of fp32,
+// 128 of 8 bits), or as many rows of a matrix whose rows lie across it ("across").  Both operands of a step are staged in LDS by loads
 // that go there directly (16 bytes a lane, no registers), twice: one pair of tiles is computed while the next one arrives.
-//   along   row r at r * 128, its 16-byte piece c at place c ^ (r & 7): the 32 rows that a fragment reads fall on all banks
-//   across  row k of the contraction at k * width, its piece c at c ^ ((k & 3) << 1) (16-bit types): the four rows that a
-//           transposing read of 16 lanes takes fall on different banks
+// LDS has 64 banks: 16 lanes of a 16-byte read, 32 of an 8-byte and 64 of a 4-byte one are served at a time, if they fall on different
+// ones.  So pieces of 16 bytes are kept at other places than their own, by the row that they belong to (swizzle_along / _across):
+//   along   the 16 rows that 16 lanes read at one piece cover all places of 256 bytes
+//   across  16-bit types: the four rows that a transposing read takes 64 bytes of cover 256 bytes; fp32: the two rows of 128 bytes
 // A fragment of the 32 x 32 matrix instructions is 16 bytes a lane, from row (lane & 31) and piece 2 s + (lane >> 5) of sub-step
-// s = 0 .. 3; for fp32 that is four instructions of two values of the contraction each, in an order of their own that both
+// s = 0 .. 3 (0, 1); for fp32 that is four instructions of two values of the contraction each, in an order of their own that both
 // operands share.  The operands change places (columns of the result first), so that a lane holds four neighbouring columns.
 #pragma once
 
@@ -114,8 +115,9 @@ __device__ __forceinline__ v4i load16(const char *p, int64_t valid)
     return x;
 }
 
-// Rows cut to 8 bits.  The 16 bytes of a load as floats; the scale of a row from its largest magnitude (not finite: NaN); the codes of
-// a load, halves to even, zeros where the scale is zero or NaN.
+// Rows cut to 8 bits: the 16 bytes of a load as floats, their largest magnitude, the scale of a row, its codes.  (A wavefront's
+// instruction takes four cycles: at 25 instructions a value, with a division each, cutting 8192 x 4096 values was bound by them, 38 us
+// in place of the 16 that the bytes take.)
 template <typename X>
 struct RowValues {
     float x[16 / sizeof(X)];
@@ -131,32 +133,101 @@ __device__ __forceinline__ RowValues<X> row_values(v4i v)
     return r;
 }
 
+// Magnitudes compare like their bits without the sign, infinities and NaN above all numbers.  `top`: the largest so far, one value of
+// fp32 or two of 16 bits.
+template <typename X>
+__device__ __forceinline__ uint32_t row_look(v4i v, uint32_t top)
+{
+    typedef unsigned short u2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(X) == 4) {
+            const uint32_t a = (uint32_t)v[k] & 0x7FFFFFFFu;
+            top = a > top ? a : top;
+        } else {
+            top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u2, (uint32_t)v[k] & 0x7FFF7FFFu), __builtin_bit_cast(u2, top)));
+        }
+    }
+    return top;
+}
+// the larger magnitude of two looks, or of one's two halves, as a float
+template <typename X>
+__device__ __forceinline__ float row_top(uint32_t top)
+{
+    if constexpr (sizeof(X) == 4) {
+        return __uint_as_float(top);
+    } else {
+        const uint16_t a = (uint16_t)top, b = (uint16_t)(top >> 16), c = a > b ? a : b;
+        return (float)__builtin_bit_cast(X, c);
+    }
+}
+// ... over kLanes neighbouring lanes; NaN where a value is not finite
+template <int kLanes>
+__device__ __forceinline__ float row_top_of(float top)
+{
+    uint32_t t = __float_as_uint(top);
+#pragma unroll
+    for (int d = 1; d < kLanes; d *= 2) {
+        const uint32_t o = __shfl_xor(t, d);
+        t = o > t ? o : t;
+    }
+    return __uint_as_float(t);
+}
+
 __device__ __forceinline__ float row_scale(float top) { return __builtin_isfinite(top) ? top * (1.f / 127.f) : __builtin_nanf(""); }
 
+// The codes of a load: x / scale, halves to even; zeros where the scale is zero or NaN.  x times the reciprocal is within 2^-15 of the
+// quotient, so it rounds to the same integer unless it lies that near to a half; then, and for scales whose reciprocal is
+// inexact or infinite, the quotient itself is computed.
 template <typename X>
 __device__ __forceinline__ void row_codes(v4i v, float scale, int8_t *to)
 {
     constexpr int kPer = 16 / sizeof(X);
+    constexpr float kRound = 12582912.f;                     // 1.5 * 2^23: what is added to it is rounded to an integer
     const RowValues<X> e = row_values<X>(v);
-    union {
-        int8_t c[kPer];
-        uint32_t u[kPer / 4];
-    } q;
+    uint32_t q[kPer];
+    bool near = !(scale > 0x1p-100f);
+    const float r = 1.f / scale;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) q.c[k] = scale > 0.f ? (int8_t)fminf(fmaxf(rintf(e.x[k] / scale), -127.f), 127.f) : (int8_t)0;
-    __builtin_memcpy(__builtin_assume_aligned(to, kPer), q.u, kPer);
+    for (int k = 0; k < kPer; ++k) {
+        const float t = e.x[k] * r, whole = t + kRound, off = t - (whole - kRound);
+        q[k] = __float_as_uint(whole);
+        near = near || __builtin_fabsf(off) > 0.5f - 0x1p-14f;
+    }
+    if (near) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) q[k] = scale > 0.f ? (uint32_t)(int)fminf(fmaxf(rintf(e.x[k] / scale), -127.f), 127.f) : 0u;
+    }
+    uint32_t u[kPer / 4];
+#pragma unroll
+    for (int k = 0; k < kPer / 4; ++k)
+        u[k] = (q[4 * k] & 0xFFu) | (q[4 * k + 1] & 0xFFu) << 8 | (q[4 * k + 2] & 0xFFu) << 16 | q[4 * k + 3] << 24;
+    __builtin_memcpy(__builtin_assume_aligned(to, kPer), u, kPer);
+}
+
+// row r of kStep bytes
+template <int kStep>
+__device__ __forceinline__ int swizzle_along(int r)
+{
+    return kStep == 128 ? r / 2 & 7 : r / 4 & 3;
+}
+// row k of kRowBytes
+template <typename T, int kRowBytes>
+__device__ __forceinline__ int swizzle_across(int k)
+{
+    return sizeof(T) == 4 ? (k / 4 & 1) << 3 : kRowBytes == 128 ? (k / 2 & 1) << 2 : (k & 3) << 2;
 }
 
 // One operand's tile: kWide rows ("along") or columns ("across").  begin(s) starts the loads of step s, end(s) has them in LDS once
 // the workgroup has passed a barrier.
-template <typename T, int kWide, int kThreads, bool kAcross, bool kAligned>
+template <typename T, int kWide, int kThreads, bool kAcross, bool kAligned, int kStep = kStepBytes>
 struct Stage {
     static constexpr bool kDirect = kAligned;
-    static constexpr int kBytes = kWide * kStepBytes, kEach = kBytes / 16 / kThreads;
-    static constexpr int kRowBytes = kAcross ? kWide * (int)sizeof(T) : kStepBytes, kPieces = kRowBytes / 16;
+    static constexpr int kBytes = kWide * kStep, kValues = kStep / (int)sizeof(T), kSubSteps = kStep / 32, kEach = kBytes / 16 / kThreads;
+    static constexpr int kRowBytes = kAcross ? kWide * (int)sizeof(T) : kStep, kPieces = kRowBytes / 16;
     static constexpr int kRowsEach = kThreads / kPieces;     // rows of the tile that one load of the workgroup takes
     static_assert(kBytes % (16 * kThreads) == 0 && kThreads % kPieces == 0, "a whole number of loads of whole rows");
-    static_assert(kAcross ? sizeof(T) == 4 || (kRowsEach % 4 == 0 && kPieces >= 8) : kRowsEach % 8 == 0, "a lane's piece is the same in all its loads");
+    static_assert(kAcross ? kRowsEach % (sizeof(T) == 4 ? 8 : 4) == 0 && kRowBytes >= (sizeof(T) == 4 ? 256 : 128) : kRowsEach % 16 == 0, "a lane's piece is the same in all its loads");
 
     const char *src[kAcross ? 1 : kEach];
     int64_t pitch, limit;                                    // bytes between rows; bytes ("along") or rows ("across") of the contraction
@@ -164,7 +235,10 @@ struct Stage {
     int32_t piece, row;
     v4i held[kAligned ? 1 : kEach];
 
-    static __device__ __forceinline__ int swizzle(int r) { return kAcross ? (sizeof(T) == 2 ? (r & 3) << 1 : 0) : r & 7; }
+    static __device__ __forceinline__ int swizzle(int r) 
+    {
+        return kAcross ? swizzle_across<T, kRowBytes>(r) : swizzle_along<kStep>(r);
+    }
 
     // along: `base` is the first row's first value, `rows` rows exist, `extent` values of the contraction
     // across: `base` is the first value of the tile's first column in the contraction's first row, `columns` columns exist
@@ -189,21 +263,23 @@ struct Stage {
         }
     }
 
-    __device__ __forceinline__ void begin(int64_t s, char *tile)
+    // the loads [first, last) of a lane's kEach
+    __device__ __forceinline__ void begin(int64_t s, char *tile, int first = 0, int last = kEach)
     {
         const uint32_t to = lds_offset(tile) + threadIdx.x / kWave * (kWave * 16);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
+            if (i < first || i >= last) continue;
             const char *p;
             int64_t left;
             if (kAcross) {
-                const int64_t k = s * kStepValues<T> + row + i * kRowsEach;
-                p = src[0] + (s * kStepValues<T> + i * kRowsEach) * pitch;
+                const int64_t k = s * kValues + row + i * kRowsEach;
+                p = src[0] + (s * kValues + i * kRowsEach) * pitch;
                 left = k < limit ? width : 0;
                 if (kAligned) p = k < limit ? p : (const char *)&g_zeros;
             } else {
-                p = src[i] + s * kStepBytes;
-                left = limit - s * kStepBytes - piece * 16;
+                p = src[i] + s * kStep;
+                left = limit - s * kStep - piece * 16;
                 if (kAligned) p = left > 0 ? p : (const char *)&g_zeros;
             }
             if constexpr (kAligned) dma16(p, to + i * (kThreads * 16));
@@ -225,7 +301,7 @@ struct Stage {
         const int lane = threadIdx.x % kWave, half = lane / 32;
         if constexpr (!kAcross) {
             const int r = first + lane % 32;
-            return *(const v4i *)(tile + r * kStepBytes + (((2 * s + half) ^ swizzle(r)) * 16));
+            return *(const v4i *)(tile + r * kStep + (((2 * s + half) ^ swizzle(r)) * 16));
         } else if constexpr (sizeof(T) == 2) {
             // 16 lanes give the addresses of four rows of 16 columns and get a column's four values each
             const int i = lane % 16, k = 16 * s + 8 * half + i / 4, c = (first + (lane / 16 % 2) * 16) / 8;
@@ -236,44 +312,53 @@ struct Stage {
         } else {
             v4i x;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = *(const int *)(tile + (8 * s + 4 * half + j) * kRowBytes + (first + lane % 32) * 4);
+            for (int j = 0; j < 4; ++j) {
+                const int k = 8 * s + 4 * half + j, c = (first + lane % 32) / 4;
+                x[j] = *(const int *)(tile + k * kRowBytes + ((c ^ swizzle(k)) * 16) + lane % 4 * 4);
+            }
             return x;
         }
     }
 };
 
-// One step's products of the wavefront's 32 x 32 blocks.
-template <typename T, bool kColumns, class StageA, class StageB, int kI, int kJ>
-__device__ __forceinline__ void tile_step(const char *now, int row0, int col0, typename TileType<T>::Sum (&sums)[kI][kJ], float (*columns)[kJ], bool mine)
-{
+// The fragments of one sub-step of the wavefront's blocks, and their products.
+template <typename T, class StageA, class StageB, int kI, int kJ>
+struct Fragments {
+    v4i a[kI], b[kJ];
+
+    __device__ __forceinline__ void read(const char *tile, int row0, int col0, int q)
+    {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        v4i fa[kI], fb[kJ];
+        for (int j = 0; j < kJ; ++j) b[j] = StageB::fragment(tile + StageA::kBytes, col0 + 32 * j, q);
 #pragma unroll
-        for (int i = 0; i < kI; ++i) fa[i] = StageA::fragment(now, row0 + 32 * i, q);
-#pragma unroll
-        for (int j = 0; j < kJ; ++j) fb[j] = StageB::fragment(now + StageA::kBytes, col0 + 32 * j, q);
-#pragma unroll
-        for (int i = 0; i < kI; ++i)
-#pragma unroll
-            for (int j = 0; j < kJ; ++j) sums[i][j] = TileType<T>::mma(fb[j], fa[i], sums[i][j]);
-        if constexpr (kColumns) {
-            if (mine) {
-#pragma unroll
-                for (int j = 0; j < kJ; ++j) (*columns)[j] += TileType<T>::total(fb[j]);
-            }
-        }
+        for (int i = 0; i < kI; ++i) a[i] = StageA::fragment(tile, row0 + 32 * i, q);
     }
-}
+    // the blocks [first, last) of kI * kJ
+    __device__ __forceinline__ void multiply(typename TileType<T>::Sum (&sums)[kI][kJ], int first = 0, int last = kI * kJ) const
+    {
+#pragma unroll
+        for (int k = 0; k < kI * kJ; ++k)
+            if (k >= first && k < last) sums[k / kJ][k % kJ] = TileType<T>::mma(b[k % kJ], a[k / kJ], sums[k / kJ][k % kJ]);
+    }
+    __device__ __forceinline__ void add_columns(float (&columns)[kJ]) const
+    {
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) columns[j] += TileType<T>::total(b[j]);
+    }
+};
 
 // The product of two staged operands over `steps` steps: sums[i][j] of the wavefront's 32 x 32 blocks, rows of `A` from row0 on,
 // columns of `B` from col0 on.  kStages pairs of tiles lie in LDS, so that kStages - 1 steps are on their way while one is computed.
+// The fragments of a sub-step are read while the one before is multiplied, across the steps' borders too: the barrier lies before the
+// last sub-step's products, whose fragments are in registers by then.
 // `columns` (where kColumns; wavefronts with `mine`): the sums of B's values, lanes l and l + 32 hold the two halves of column l.
 template <typename T, int kStages, bool kColumns = false, class StageA, class StageB, int kI, int kJ>
 __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, int64_t steps, int row0, int col0,
                                              typename TileType<T>::Sum (&sums)[kI][kJ], float (*columns)[kJ] = nullptr, bool mine = false)
 {
-    constexpr int kBoth = StageA::kBytes + StageB::kBytes;
+    constexpr int kBoth = StageA::kBytes + StageB::kBytes, kQ = StageA::kSubSteps;
+    static_assert(kQ % 2 == 0, "the two sets of fragments take turns");
+    Fragments<T, StageA, StageB, kI, kJ> f[2];
 #pragma unroll
     for (int i = 0; i < kI; ++i)
 #pragma unroll
@@ -281,22 +366,41 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
     if (steps <= 0) return;
     if constexpr (StageA::kDirect) {
         // a step past the last one loads zeros that nothing reads: every step has the same number of loads to count
-        constexpr int kEach = StageA::kEach + StageB::kEach;
-        auto begin = [&](int64_t s, int at) {
-            a.begin(s, lds + at);
-            b.begin(s, lds + at + StageA::kBytes);
+        constexpr int kEach = StageA::kEach + StageB::kEach, kHalf = kI * kJ / 2;
+        auto begin = [&](int64_t s, int at, int first, int last) {
+            a.begin(s, lds + at, first, last);
+            b.begin(s, lds + at + StageA::kBytes, first - StageA::kEach, last - StageA::kEach);
         };
 #pragma unroll
-        for (int s = 0; s < kStages - 1; ++s) begin(s, s * kBoth);
-        int now = 0, next = (kStages - 1) * kBoth;
+        for (int s = 0; s < kStages - 1; ++s) begin(s, s * kBoth, 0, kEach);
+        int now = 0, free = (kStages - 1) * kBoth;           // the tiles that are read, and those that are loaded next
+        dma_wait<(kStages - 2) * kEach>();
+        __syncthreads();
+        f[0].read(lds, row0, col0, 0);
 #pragma unroll 1
         for (int64_t s = 0; s < steps; ++s) {
-            dma_wait<(kStages - 2) * kEach>();
-            __syncthreads();                                 // step s has arrived, and nobody reads the tile that is loaded next
-            begin(s + kStages - 1, next);
-            tile_step<T, kColumns, StageA, StageB>(lds + now, row0, col0, sums, columns, mine);
-            now = now + kBoth == kStages * kBoth ? 0 : now + kBoth;
-            next = next + kBoth == kStages * kBoth ? 0 : next + kBoth;
+#pragma unroll
+            for (int q = 0; q < kQ; ++q) {
+                // the loads are issued between the products, a few at a time: all at once they would hold the wavefront up
+                if (q + 1 < kQ) f[(q + 1) % 2].read(lds + now, row0, col0, q + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                f[q % 2].multiply(sums, 0, kHalf);
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int kSpread = kStages == 2 ? 1 : kQ;
+                if (q < kSpread) begin(s + kStages - 1, free, q * kEach / kSpread, (q + 1) * kEach / kSpread);
+                if (q + 1 == kQ && s + 1 < steps) {
+                    free = now;
+                    now = now + kBoth == kStages * kBoth ? 0 : now + kBoth;
+                    dma_wait<(kStages - 2) * kEach>();
+                    __syncthreads();                         // the next step has arrived, and nobody reads the tiles of this one
+                    f[0].read(lds + now, row0, col0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                f[q % 2].multiply(sums, kHalf);
+                if constexpr (kColumns)
+                    if (mine) f[q % 2].add_columns(*columns);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         dma_wait();                                          // before the workgroup's LDS is anybody else's
     } else {
@@ -312,7 +416,13 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
             b.end(lds + at + StageA::kBytes);
             __syncthreads();                                 // two tiles: the other one is read no more once all are here
             if (s + 1 < steps) begin(s + 1);
-            tile_step<T, kColumns, StageA, StageB>(lds + at, row0, col0, sums, columns, mine);
+#pragma unroll
+            for (int q = 0; q < kQ; ++q) {
+                f[0].read(lds + at, row0, col0, q);
+                f[0].multiply(sums);
+                if constexpr (kColumns)
+                    if (mine) f[0].add_columns(*columns);
+            }
             at = kBoth - at;
         }
     }
