@@ -609,7 +609,7 @@ groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_
  * captured in a HIP graph, with the host values it was given.
  * Errors: EINVAL (NULL, unknown dtype, n < 0, state_bits, step < 1, lr or
  * weight_decay not finite or negative, beta outside [0, 1), eps not finite or <= 0), ERANGE (a tensor of
- * 2^34 values or more), EHIP.
+ * 2^33 values or more), EHIP.
  * ------------------------------------------------------------------------- */
 typedef struct {
     void *param;

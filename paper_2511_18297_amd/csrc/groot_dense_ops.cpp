@@ -260,7 +260,7 @@ extern "C" groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int6
     for (int64_t t = 0; t < n_tensors; ++t) {
         const groot_adamw_tensor &x = tensors[t];
         if (x.n < 0) return bad(who, "a tensor's n is negative");
-        if (x.n >= ((int64_t)1 << 34)) return fail(GROOT_ERANGE, std::string(who) + ": a tensor of 2^34 values or more");
+        if (x.n >= ((int64_t)1 << 33)) return fail(GROOT_ERANGE, std::string(who) + ": a tensor of 2^33 values or more");
         if (x.n == 0) continue;
         if (!x.param || !x.grad || !x.m || !x.v) return bad(who, "a tensor with a NULL array");
         if (state_bits == 8 && (!x.m_scale || !x.v_scale)) return bad(who, "8-bit states need m_scale and v_scale");
