@@ -50,10 +50,10 @@ struct FewType<float> {
 
 // 16 bytes at offset k of a row of `bytes`, zeros behind its end
 template <typename T, bool kAligned>
-__device__ __forceinline__ v4i piece16(const char *row, int64_t k, int64_t bytes)
+__device__ __forceinline__ v4i piece16(const char *row, int64_t k, int64_t bytes, bool short_row)
 {
     if constexpr (kAligned) return k < bytes ? *(const v4i *)(row + k) : v4i{0, 0, 0, 0};
-    else return load16<T>(row + k, bytes - k);
+    else return load16<T>(row + k, bytes - k, short_row);
 }
 
 // X: the floating type of the rows where they are cut to 8 bits inside, else T
@@ -73,13 +73,14 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, i
     const int64_t bytes = (int64_t)p.K * sizeof(T);
     const int32_t col = n0 + r < p.N ? n0 + r : p.N - 1;     // columns and rows that do not exist read the last one that does
     const char *const w = (const char *)((const T *)p.B + ((int64_t)t.group * p.N + col) * p.K) + quarter;
+    const bool short_row = bytes < 16;
     const int32_t pieces = (int32_t)((bytes + kStepBytes - 1) / kStepBytes);
 
     v4i held[kAhead][2];
     auto load = [&](int32_t s, int i) {
         const int64_t k = (int64_t)s * kStepBytes;
-        held[i][0] = piece16<T, kAligned>(w, k, bytes - quarter);
-        held[i][1] = piece16<T, kAligned>(w, k + 16, bytes - quarter);
+        held[i][0] = piece16<T, kAligned>(w, k, bytes - quarter, short_row);
+        held[i][1] = piece16<T, kAligned>(w, k + 16, bytes - quarter, short_row);
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, i
         const int32_t loads = (p.K + kPer - 1) / kPer;
         v4i keep[kFusedRows][kKeep];
         auto get = [&](int64_t row, int32_t i) {
-            return load16<X>((const char *)((const X *)p.A + row * p.a_stride) + (int64_t)i * 16, ((int64_t)p.K - (int64_t)i * kPer) * (int64_t)sizeof(X));
+            return load16<X>((const char *)((const X *)p.A + row * p.a_stride) + (int64_t)i * 16, ((int64_t)p.K - (int64_t)i * kPer) * (int64_t)sizeof(X), (int64_t)p.K * sizeof(X) < 16);
         };
 #pragma unroll
         for (int m = 0; m < kFusedRows; ++m) {
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, i
             for (int h = 0; h < 2; ++h) {
                 fa[i][h] = held[i][h];
                 // what lies behind the row's end in LDS meets zeros of the weights
-                fb[i][h] = kFused ? *(const v4i *)(x + k + 16 * h) : piece16<T, kAligned>(x, k + 16 * h, bytes - quarter);
+                fb[i][h] = kFused ? *(const v4i *)(x + k + 16 * h) : piece16<T, kAligned>(x, k + 16 * h, bytes - quarter, short_row);
             }
         }
 #pragma unroll

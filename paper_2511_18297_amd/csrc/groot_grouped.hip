@@ -89,9 +89,9 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const Row
     const T *B = (const T *)p.B + (int64_t)t.group * p.K * p.N;
     StageA a;
     StageB b;
-    a.init((const T *)p.A + t.begin * p.a_stride, p.a_stride, rows, p.K);
-    if (kNMajor) b.init(B + (int64_t)j0 * p.K, p.K, p.N - j0, p.K);
-    else b.init(B + j0, p.N, p.N - j0, p.K);
+    a.init((const T *)p.A + t.begin * p.a_stride, p.a_stride, rows, p.K, p.K);
+    if (kNMajor) b.init(B + (int64_t)j0 * p.K, p.K, p.N - j0, p.K, p.K);
+    else b.init(B + j0, p.N, p.N - j0, p.K, p.N);
     const int wave = threadIdx.x / kWave;
     const int row0 = wave / kWavesN * (kM / kWavesM), col0 = wave % kWavesN * (kN / kWavesN);
     typename TileType<T>::Sum sums[kI][kJ];
@@ -116,14 +116,14 @@ template <typename T, typename O, int kN, int kWaves, int kStages, bool kNMajor,
 __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct p, int log_rows, int32_t steps, bool whole)
 {
     constexpr int kThreads = kWaves * kWave, kJ = kN / 32, kEach = kNarrowStage / 16 / kWave;
-    typedef Stage<T, kN, kThreads, !kNMajor, kAligned> StageB;
+    typedef Stage<T, kN, kThreads, !kNMajor, false> StageB;  // once, through registers: from any address
     typedef Stage<T, kNarrowRows, kBlock, false, kAligned> Rows;       // its layout in LDS
     extern __shared__ __align__(16) char lds[];              // weights, then every wavefront's steps
     const RowTile t = find_tile(p.offsets, p.groups, p.n, blockIdx.x, log_rows);
     if (t.group < 0) return;
     const T *B = (const T *)p.B + (int64_t)t.group * p.K * p.N;
     StageB b;
-    b.init(B, kNMajor ? p.K : p.N, p.N, p.K);
+    b.init(B, kNMajor ? p.K : p.N, p.N, p.K, kNMajor ? p.K : p.N);
     for (int s = 0; s < steps; ++s) {
         b.begin(s, lds + s * StageB::kBytes);
         b.end(lds + s * StageB::kBytes);
@@ -136,6 +136,8 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
     const int own = lane / 8;
     const char *const from = (const char *)((const T *)p.A + t.begin * p.a_stride);
     v4i held[kAligned ? 1 : kEach];
+    int32_t valid[kAligned ? 1 : kEach];
+    const bool short_row = bytes < 16;
     // the next step to load: its block of rows and its place in the rows
     int32_t load_block = wave, load_step = 0;
     auto begin = [&](int slot) {
@@ -148,7 +150,10 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
             r = r < rows ? r : rows - 1;
             const char *q = from + r * pitch + at;
             if constexpr (kAligned) dma16(left > 0 ? q : (const char *)&g_zeros, lds_offset(ring) + slot * kNarrowStage + i * (kWave * 16));
-            else held[i] = load16<T>(q, left);
+            else {
+                valid[i] = left;
+                held[i] = short_row ? short16<T>(q, left) : raw16(load_block < blocks ? q : from + r * pitch + bytes, left);
+            }
         }
         if (++load_step == steps) {
             load_step = 0;
@@ -179,7 +184,7 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
         } else {
             wave_sync();
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) *(v4i *)(ring + now * kNarrowStage + (i * kWave + lane) * 16) = held[i];
+            for (int i = 0; i < kEach; ++i) *(v4i *)(ring + now * kNarrowStage + (i * kWave + lane) * 16) = short_row ? held[i] : cut16(held[i], valid[i]);
             wave_sync();
             begin(0);
         }
@@ -253,7 +258,7 @@ template <typename T, typename O, int kN, bool kNMajor>
 int narrow_launch(const RowsProduct &p, void *stream)
 {
     const int32_t steps = (int32_t)((p.K * sizeof(T) + kStepBytes - 1) / kStepBytes);
-    const bool aligned = rows_aligned<T, kNMajor>(p), whole = out_whole<O>(p);
+    const bool aligned = on16(p.A, p.a_stride * (int64_t)sizeof(T)) && p.K * (int64_t)sizeof(T) % 16 == 0, whole = out_whole<O>(p);
     int log_rows = 8;                                        // about 1024 workgroups, of 256 rows at least
     while (log_rows < 20 && ((int64_t)1024 << log_rows) < p.n) ++log_rows;
     // 16 wavefronts to a CU with a step of their own on the way each; 8 with two or three were 8 % slower at 64 x 64, 14 % at 128 x 128
@@ -374,8 +379,8 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
     const int32_t n0 = n_tile * kN, k0 = (int32_t)(row_tile % k_tiles) * kK;
     StageX x;
     StageY y;
-    x.init((const T *)p.X + t.begin * p.x_stride + k0, p.x_stride, p.K - k0, t.end - t.begin);
-    y.init((const T *)p.dY + t.begin * p.dy_stride + n0, p.dy_stride, p.N - n0, t.end - t.begin);
+    x.init((const T *)p.X + t.begin * p.x_stride + k0, p.x_stride, p.K - k0, t.end - t.begin, p.K);
+    y.init((const T *)p.dY + t.begin * p.dy_stride + n0, p.dy_stride, p.N - n0, t.end - t.begin, p.N);
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int row0 = wave / kWavesN * (kK / kWavesK), col0 = wave % kWavesN * (kN / kWavesN);
     typename TileType<T>::Sum sums[kI][kJ];

@@ -19,11 +19,18 @@ __global__ __launch_bounds__(kBlock) void quantize_kernel(const T *__restrict__ 
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < n; first += (int64_t)gridDim.x * kRows) {
         const int64_t row = first + threadIdx.x / kLanes;
         const char *const x = (const char *)(X + (row < n ? row : n - 1) * x_stride);
-        auto get = [&](int32_t i) { return load16<T>(x + (int64_t)i * 16, ((int64_t)K - (int64_t)i * kPer) * (int64_t)sizeof(T)); };
+        const bool short_row = (int64_t)K * sizeof(T) < 16;
+        auto left = [&](int32_t i) { return ((int64_t)K - (int64_t)i * kPer) * (int64_t)sizeof(T); };
+        auto get = [&](int32_t i) { return load16<T>(x + (int64_t)i * 16, left(i), short_row); };
         v4i keep[kKeep];
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
-            if (at + i * kLanes < loads) keep[i] = get(at + i * kLanes);
+            if (at + i * kLanes < loads) keep[i] = short_row ? get(at + i * kLanes) : raw16(x + (int64_t)(at + i * kLanes) * 16, left(at + i * kLanes));
+        if (!short_row) {
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i)
+                if (at + i * kLanes < loads) keep[i] = cut16(keep[i], left(at + i * kLanes));
+        }
         uint32_t seen = 0;
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)

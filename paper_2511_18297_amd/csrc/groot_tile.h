@@ -99,20 +99,36 @@ __device__ __forceinline__ void dma_wait()
 
 static __device__ const v4i g_zeros = {0, 0, 0, 0};          // what lies past an end of the contraction
 
-// 16 bytes from any address, of which the first `valid` exist
-template <typename T>
-__device__ __forceinline__ v4i load16(const char *p, int64_t valid)
+// 16 bytes of a row from any address p, of which the first `valid` exist (none: 0 or less): where some do not, the row's last 16 bytes
+// are loaded in their place, so that no load waits for a branch, and cut16 moves them to their places with zeros behind.  Rows of
+// less than 16 bytes (short_row) go value by value.
+__device__ __forceinline__ v4i raw16(const char *p, int64_t valid)
 {
-    v4i x = {0, 0, 0, 0};
-    if (valid >= 16) {
-        __builtin_memcpy(&x, p, 16);
-    } else {
-        T e[16 / sizeof(T)] = {};
-        for (int k = 0; k < (int)(16 / sizeof(T)); ++k)
-            if ((int64_t)(k * sizeof(T)) < valid) e[k] = ((const T *)p)[k];
-        __builtin_memcpy(&x, e, 16);
-    }
+    v4i x;
+    __builtin_memcpy(&x, valid >= 16 ? p : p + (valid - 16), 16);
     return x;
+}
+__device__ __forceinline__ v4i cut16(v4i x, int64_t valid)
+{
+    if (valid >= 16) return x;
+    if (valid <= 0) return v4i{0, 0, 0, 0};
+    return __builtin_bit_cast(v4i, __builtin_bit_cast(unsigned __int128, x) >> (8 * (16 - (int)valid)));
+}
+template <typename T>
+__device__ __forceinline__ v4i short16(const char *p, int64_t valid)
+{
+    v4i x;
+    T e[16 / sizeof(T)] = {};
+#pragma unroll
+    for (int k = 0; k < (int)(16 / sizeof(T)); ++k)
+        if ((int64_t)(k * sizeof(T)) < valid) e[k] = ((const T *)p)[k];
+    __builtin_memcpy(&x, e, 16);
+    return x;
+}
+template <typename T>
+__device__ __forceinline__ v4i load16(const char *p, int64_t valid, bool short_row)
+{
+    return short_row ? short16<T>(p, valid) : cut16(raw16(p, valid), valid);
 }
 
 // Rows cut to 8 bits: the 16 bytes of a load as floats, their largest magnitude, the scale of a row, its codes.  (A wavefront's
@@ -234,16 +250,20 @@ struct Stage {
     int64_t width;                                           // across: bytes of a row from the lane's piece on
     int32_t piece, row;
     v4i held[kAligned ? 1 : kEach];
+    int32_t valid[kAligned ? 1 : kEach];
+    bool short_row;
 
     static __device__ __forceinline__ int swizzle(int r) 
     {
         return kAcross ? swizzle_across<T, kRowBytes>(r) : swizzle_along<kStep>(r);
     }
 
-    // along: `base` is the first row's first value, `rows` rows exist, `extent` values of the contraction
-    // across: `base` is the first value of the tile's first column in the contraction's first row, `columns` columns exist
-    __device__ __forceinline__ void init(const T *base, int64_t stride, int64_t exist, int64_t extent)
+    // along: `base` is the first row's first value, `exist` rows exist, `extent` values of the contraction
+    // across: `base` is the first value of the tile's first column in the contraction's first row, `exist` columns exist from there on
+    // row_values: of a whole row
+    __device__ __forceinline__ void init(const T *base, int64_t stride, int64_t exist, int64_t extent, int64_t row_values)
     {
+        short_row = row_values * (int64_t)sizeof(T) < 16;
         const int tid = threadIdx.x;
         row = tid / kPieces;
         piece = (tid % kPieces) ^ swizzle(row);
@@ -277,13 +297,18 @@ struct Stage {
                 p = src[0] + (s * kValues + i * kRowsEach) * pitch;
                 left = k < limit ? width : 0;
                 if (kAligned) p = k < limit ? p : (const char *)&g_zeros;
+                else if (k >= limit) p += (limit - 1 - k) * pitch + width;   // behind the end of the last row
             } else {
                 p = src[i] + s * kStep;
                 left = limit - s * kStep - piece * 16;
                 if (kAligned) p = left > 0 ? p : (const char *)&g_zeros;
             }
-            if constexpr (kAligned) dma16(p, to + i * (kThreads * 16));
-            else held[i] = load16<T>(p, left);
+            if constexpr (kAligned) {
+                dma16(p, to + i * (kThreads * 16));
+            } else {
+                valid[i] = left >= 16 ? 16 : left <= 0 ? 0 : (int32_t)left;
+                held[i] = short_row ? short16<T>(p, left) : raw16(p, left);
+            }
         }
     }
 
@@ -291,7 +316,7 @@ struct Stage {
     {
         if constexpr (!kAligned) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) *(v4i *)(tile + (i * kThreads + threadIdx.x) * 16) = held[i];
+            for (int i = 0; i < kEach; ++i) *(v4i *)(tile + (i * kThreads + threadIdx.x) * 16) = short_row ? held[i] : cut16(held[i], valid[i]);
         }
     }
 
