@@ -14,6 +14,24 @@ constexpr int log2_of(int64_t x)
     return l;
 }
 
+// A wavefront's 32 x 32 block of sums through 4 KB of its LDS: a lane writes its four quads of neighbouring columns of one row, and
+// reads places lane % 8 of rows lane / 8 + 8 e.
+template <typename S>
+__device__ __forceinline__ void block_to_lds(char *scratch, const S &sums)
+{
+    const int lane = threadIdx.x % kWave, m = lane % 32, half = lane / 32;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const v4f x = {(float)sums[4 * q], (float)sums[4 * q + 1], (float)sums[4 * q + 2], (float)sums[4 * q + 3]};
+        *(v4f *)(scratch + m * 128 + (((2 * q + half) ^ swizzle_along<128>(m)) * 16)) = x;
+    }
+    wave_sync();
+}
+__device__ __forceinline__ v4f row_of_block(const char *scratch, int r)
+{
+    return *(const v4f *)(scratch + r * 128 + ((threadIdx.x % 8 ^ swizzle_along<128>(r)) * 16));
+}
+
 // The epilogue of a wavefront's 32 x 32 blocks.  A lane's four neighbouring columns of one row would make stores of 16 bytes in 32
 // rows; the block goes through 4 KB of the wavefront's LDS (its pieces where swizzle_along has them), and every store covers eight rows of 32
 // whole columns.  A lane keeps one place in the columns, with its bias and scales, for all rows.
@@ -40,20 +58,15 @@ struct Epilogue {
     // rows from `row` of the output on, of which `rows` exist
     __device__ __forceinline__ void store(const RowsProduct &p, char *scratch, const typename TileType<T>::Sum (&sums)[kJ], int64_t row, int64_t rows, bool whole)
     {
-        const int lane = threadIdx.x % kWave, m = lane % 32, half = lane / 32;
+        const int lane = threadIdx.x % kWave;
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const v4f x = {(float)sums[j][4 * q], (float)sums[j][4 * q + 1], (float)sums[j][4 * q + 2], (float)sums[j][4 * q + 3]};
-                *(v4f *)(scratch + m * 128 + (((2 * q + half) ^ swizzle_along<128>(m)) * 16)) = x;
-            }
-            wave_sync();
+            block_to_lds(scratch, sums[j]);
             const int32_t left = p.N - col[j];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 8 * i + lane / 8;
-                v4f y = *(const v4f *)(scratch + r * 128 + ((lane % 8 ^ swizzle_along<128>(r)) * 16));
+                v4f y = row_of_block(scratch, r);
                 if (r < rows && left > 0) {
                     const float s = std::is_same<T, int8_t>::value ? p.a_scale[row + r] : 1.f;
 #pragma unroll
@@ -329,12 +342,12 @@ int rows_choose(const RowsProduct &p, void *stream)
     }
 }
 
-// How the weight gradients are cut.  Tiles of dW of 64 x 64 where it is no larger (typed layers), of 256 x 256 where all groups' fill
-// the GPU, else of 128 x 128.  The contraction, a group's rows, is cut into pieces of 2^log_rows rows where there are fewer tiles than
+// How the weight gradients are cut.  Tiles of dW of 256 x 256 where all groups' fill the GPU, else of 128, or 64 along a side that is
+// no longer (typed layers).  The contraction, a group's rows, is cut into pieces of 2^log_rows rows where there are fewer tiles than
 // workgroups that the GPU holds; a piece of 512 rows reads eight times what its partial sums are written and read again for.  A
 // group of one piece needs no partial sums, and a group without rows is one piece of zeros.
 struct WeightsSplit {
-    int32_t tile;                            // 64, 128 or 256
+    int32_t k_tile, n_tile;                  // 64 or 128 each, or both 256
     int32_t k_tiles, n_tiles;
     int log_rows;
     int64_t tiles;                           // pieces of all groups, at most
@@ -342,11 +355,12 @@ struct WeightsSplit {
     WeightsSplit(int32_t dtype, int64_t n, int32_t groups, bool offsets, int32_t K, int32_t N)
     {
         const auto tiles_of = [](int32_t width, int32_t by) { return (width + by - 1) / by; };
-        tile = K <= 64 && N <= 64 ? 64 : 128;
-        if (dtype != GROOT_F32 && (int64_t)tiles_of(K, 256) * tiles_of(N, 256) * groups >= 192 && n >= (int64_t)256 * groups) tile = 256;
-        k_tiles = tiles_of(K, tile);
-        n_tiles = tiles_of(N, tile);
-        const int64_t wanted = tile == 64 ? 1024 : 256;
+        k_tile = K <= 64 ? 64 : 128;
+        n_tile = N <= 64 ? 64 : 128;
+        if (dtype != GROOT_F32 && (int64_t)tiles_of(K, 256) * tiles_of(N, 256) * groups >= 192 && n >= (int64_t)256 * groups) k_tile = n_tile = 256;
+        k_tiles = tiles_of(K, k_tile);
+        n_tiles = tiles_of(N, n_tile);
+        const int64_t wanted = k_tile == 64 || n_tile == 64 ? 1024 : 256;
         log_rows = 9;
         while (log_rows < 40 && (wanted << log_rows) < n * k_tiles * n_tiles) ++log_rows;
         // enough tiles without cutting: only groups of four times the average are cut
@@ -390,22 +404,25 @@ __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const 
     const bool alone = t.count == 1;
     if (!alone && t.shared_before + t.place >= slots) return;   // offsets that do not ascend: more pieces than there are rows for
     float *const part = (float *)p.workspace + (t.shared_before + t.place) * ((int64_t)p.K * p.N + p.N);
-    const bool whole = p.N % 4 == 0 && ((uintptr_t)p.dW & (4 * sizeof(O) - 1)) == 0;
+    const bool whole = p.N % 4 == 0 && (!alone || ((uintptr_t)p.dW & (4 * sizeof(O) - 1)) == 0);
+    __syncthreads();                                         // LDS is free
+    char *const scratch = lds + wave * 4096;
 #pragma unroll
-    for (int i = 0; i < kI; ++i) {
-        const int32_t k = k0 + row0 + 32 * i + lane % 32;
-        if (k >= p.K) continue;
+    for (int i = 0; i < kI; ++i)
 #pragma unroll
-        for (int j = 0; j < kJ; ++j)
+        for (int j = 0; j < kJ; ++j) {
+            block_to_lds(scratch, sums[i][j]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int32_t n = n0 + col0 + 32 * j + 8 * q + 4 * (lane / 32);
-                if (n >= p.N) continue;
-                const v4f v = {sums[i][j][4 * q], sums[i][j][4 * q + 1], sums[i][j][4 * q + 2], sums[i][j][4 * q + 3]};
+            for (int e = 0; e < 4; ++e) {
+                const int r = 8 * e + lane / 8;
+                const int32_t k = k0 + row0 + 32 * i + r, n = n0 + col0 + 32 * j + lane % 8 * 4;
+                const v4f v = row_of_block(scratch, r);
+                if (k >= p.K || n >= p.N) continue;
                 if (alone) store_quad((O *)p.dW + ((int64_t)t.group * p.K + k) * p.N + n, v, p.N - n, whole);
-                else store_quad(part + (int64_t)k * p.N + n, v, p.N - n, p.N % 4 == 0);
+                else store_quad(part + (int64_t)k * p.N + n, v, p.N - n, whole);
             }
-    }
+            wave_sync();
+        }
     if (bias) {
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
@@ -479,15 +496,31 @@ __global__ __launch_bounds__(kSumLanes) void weights_sum_kernel(const WeightsPro
     }
 }
 
-template <typename T, typename O, int kTile, int kWavesK, int kWavesN, int kStages, bool kAligned>
+template <typename T, typename O, int kK, int kN, int kWavesK, int kWavesN, int kStages, bool kAligned>
 int weights_launch_tile(const WeightsProduct &p, const WeightsSplit &split, hipStream_t stream)
 {
     constexpr int kThreads = kWavesK * kWavesN * kWave;
-    const TileOrder order(split.tiles * split.k_tiles, split.n_tiles);
+    const int32_t k_tiles = (p.K + kK - 1) / kK, n_tiles = (p.N + kN - 1) / kN;
+    const TileOrder order(split.tiles * k_tiles, n_tiles);
     if (!fits_launch(order.workgroups, kThreads)) return kErrTooManyTiles;
-    weights_kernel<T, O, kTile, kTile, kWavesK, kWavesN, kStages, kAligned>
-        <<<(uint32_t)order.workgroups, kThreads, 0, stream>>>(p, order, split.log_rows, split.slots, split.k_tiles, split.n_tiles);
+    weights_kernel<T, O, kK, kN, kWavesK, kWavesN, kStages, kAligned>
+        <<<(uint32_t)order.workgroups, kThreads, 0, stream>>>(p, order, split.log_rows, split.slots, k_tiles, n_tiles);
     return (int)hipGetLastError();
+}
+
+template <typename T, typename O, bool kAligned>
+int weights_launch_as(const WeightsProduct &p, const WeightsSplit &split, hipStream_t s)
+{
+    if (split.k_tile == 64 && split.n_tile == 64) return weights_launch_tile<T, O, 64, 64, 2, 2, 2, kAligned>(p, split, s);
+    if (split.k_tile == 64) return weights_launch_tile<T, O, 64, 128, 2, 2, 2, kAligned>(p, split, s);
+    if (split.n_tile == 64) return weights_launch_tile<T, O, 128, 64, 2, 2, 2, kAligned>(p, split, s);
+    if constexpr (kAligned) {
+        if constexpr (sizeof(T) == 2)
+            if (split.k_tile == 256) return weights_launch_tile<T, O, 256, 256, 2, 4, 2, true>(p, split, s);
+        // four stages where a CU has one tile at most
+        if ((int64_t)p.groups * split.k_tiles * split.n_tiles <= 256 && split.slots == 0) return weights_launch_tile<T, O, 128, 128, 2, 2, 4, true>(p, split, s);
+    }
+    return weights_launch_tile<T, O, 128, 128, 2, 2, 2, kAligned>(p, split, s);   // also for 256 x 256, not built for rows through registers
 }
 
 template <typename T, typename O>
@@ -495,23 +528,9 @@ int weights_launch(int32_t dtype, const WeightsProduct &p, void *stream)
 {
     const int64_t b = sizeof(T);
     const bool aligned = on16(p.X, p.x_stride * b) && on16(p.dY, p.dy_stride * b) && p.K * b % 16 == 0 && p.N * b % 16 == 0;
-    WeightsSplit split(dtype, p.n, p.groups, p.offsets != nullptr, p.K, p.N);
+    const WeightsSplit split(dtype, p.n, p.groups, p.offsets != nullptr, p.K, p.N);
     const hipStream_t s = (hipStream_t)stream;
-    int err = 0;
-    if (split.tile == 64) {
-        err = aligned ? weights_launch_tile<T, O, 64, 2, 2, 2, true>(p, split, s) : weights_launch_tile<T, O, 64, 2, 2, 2, false>(p, split, s);
-    } else if (split.tile == 128 || !aligned) {
-        // the same pieces of rows in smaller tiles: the 256 x 256 one is not built for rows that go through registers
-        split.k_tiles = (p.K + 127) / 128;
-        split.n_tiles = (p.N + 127) / 128;
-        // four stages where a CU has one tile at most
-        const bool few = (int64_t)p.groups * split.k_tiles * split.n_tiles <= 256 && split.slots == 0;
-        err = !aligned ? weights_launch_tile<T, O, 128, 2, 2, 2, false>(p, split, s)
-              : few    ? weights_launch_tile<T, O, 128, 2, 2, 4, true>(p, split, s)
-                       : weights_launch_tile<T, O, 128, 2, 2, 2, true>(p, split, s);
-    } else if constexpr (sizeof(T) == 2) {
-        err = weights_launch_tile<T, O, 256, 2, 4, 2, true>(p, split, s);
-    }
+    const int err = aligned ? weights_launch_as<T, O, true>(p, split, s) : weights_launch_as<T, O, false>(p, split, s);
     if (err) return err;
     if (split.slots == 0) return 0;
     int shares = 1;                                          // a share for every four pieces that a group has on average, 64 at most
