@@ -186,13 +186,130 @@ int few_launch(const RowsProduct &p, void *stream)
     return (int)hipGetLastError();
 }
 
+// Few rows against weights whose rows lie across the contraction ([groups, K, N]: the forward products): 64 columns to a workgroup, its
+// eight wavefronts take 32 (fp32: 16) rows of the weights in turn.  A lane has four neighbouring columns of 8 (4) rows, so that 16
+// lanes read 128 (256) bytes of a row, and puts the values of a column next to one another in registers; column 4 c + j goes through
+// the j-th of four instructions.  Three of a wavefront's blocks of rows are on their way while one is multiplied.
+constexpr int kAcrossCols = 64, kAcrossAhead = 3;
+
+template <typename T>
+struct AcrossBlock {
+    static constexpr int kRows = sizeof(T) == 2 ? 32 : 16, kLoads = kRows / 4, kWords = sizeof(T);   // 2 or 4 words of four columns
+    typedef int W __attribute__((ext_vector_type(sizeof(T))));
+    W w[kLoads];
+    v4i x;
+
+    // rows k0 + kLoads * (lane / 16) .. of the weights from `w0`, the lane's row of X from `x0`
+    __device__ __forceinline__ void load(const char *w0, int64_t pitch, const char *x0, int32_t k0, int32_t K, bool short_row)
+    {
+        const int32_t k = k0 + kLoads * (int32_t)(threadIdx.x % kWave / 16);
+        if (k0 + kRows <= K) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) __builtin_memcpy(&w[i], w0 + (int64_t)(k + i) * pitch, sizeof(W));
+            __builtin_memcpy(&x, x0 + (int64_t)k * sizeof(T), 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                w[i] = W{};
+                if (k + i < K) __builtin_memcpy(&w[i], w0 + (int64_t)(k + i) * pitch, sizeof(W));
+            }
+            x = load16<T>(x0 + (int64_t)k * sizeof(T), (int64_t)(K - k) * (int64_t)sizeof(T), short_row);
+        }
+    }
+    __device__ __forceinline__ void multiply(v4f (&sums)[4]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 2) {
+                v4i a;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(w[2 * i + 1][j / 2], w[2 * i][j / 2], j % 2 ? 0x07060302 : 0x05040100);
+                sums[j] = FewType<T>::mma(a, x, sums[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sums[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(w[i][j]), __int_as_float(x[i]), sums[j], 0, 0, 0);
+            }
+        }
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void few_across_kernel(const RowsProduct p, int32_t col_tiles)
+{
+    typedef AcrossBlock<T> Block;
+    __shared__ v4f part[kFewWaves][4][kWave];
+    const RowTile t = find_tile(p.offsets, p.groups, p.n, blockIdx.x / col_tiles, 4);
+    if (t.group < 0) return;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 16;
+    const int rows = (int)(t.end - t.begin);
+    const auto column = [&](int c) {                         // the last lanes repeat columns rather than read past a row's end
+        const int32_t col = (int32_t)(blockIdx.x % col_tiles) * kAcrossCols + 4 * c;
+        return col < p.N - 4 ? col : p.N - 4;
+    };
+    const char *const w0 = (const char *)((const T *)p.B + (int64_t)t.group * p.K * p.N + column(r));
+    const char *const x0 = (const char *)((const T *)p.A + (t.begin + (r < rows ? r : rows - 1)) * p.a_stride);
+    const int64_t pitch = (int64_t)p.N * sizeof(T);
+    const bool short_row = (int64_t)p.K * sizeof(T) < 16;
+    const int32_t blocks = (p.K + Block::kRows - 1) / Block::kRows;
+    Block held[kAcrossAhead];
+    v4f sums[4] = {};
+#pragma unroll
+    for (int i = 0; i < kAcrossAhead; ++i)
+        if (wave + i * kFewWaves < blocks) held[i].load(w0, pitch, x0, (wave + i * kFewWaves) * Block::kRows, p.K, short_row);
+    for (int32_t b0 = wave; b0 < blocks; b0 += kAcrossAhead * kFewWaves) {
+#pragma unroll
+        for (int i = 0; i < kAcrossAhead; ++i) {
+            const int32_t b = b0 + i * kFewWaves;
+            if (b >= blocks) break;
+            held[i].multiply(sums);
+            if (b + kAcrossAhead * kFewWaves < blocks) held[i].load(w0, pitch, x0, (b + kAcrossAhead * kFewWaves) * Block::kRows, p.K, short_row);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[wave][j][lane] = sums[j];
+    __syncthreads();
+    // lane l holds row l % 16 and, in its four values, c = 4 (l / 16) .. + 3
+    if (threadIdx.x >= 256) return;
+    const int m = threadIdx.x / 16, c = threadIdx.x % 16;
+    if (m >= rows) return;
+    const int32_t col = column(c);
+    const int64_t row = t.begin + m, of = (int64_t)t.group * p.N + col;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float y = 0.f;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k) y += part[k][j][c / 4 * 16 + m][c % 4];
+        if (p.bias) y += (float)((const T *)p.bias)[of + j];
+        if (p.relu && y < 0.f) y = 0.f;
+        ((T *)p.out)[row * p.out_stride + col + j] = (T)y;
+    }
+}
+
+template <typename T>
+int few_across_launch(const RowsProduct &p, void *stream)
+{
+    const int32_t col_tiles = (p.N + kAcrossCols - 1) / kAcrossCols;
+    const int64_t workgroups = ((p.n + kFewRows - 1) / kFewRows + (p.offsets ? p.groups : 0)) * col_tiles;
+    if (!fits_launch(workgroups, kFewThreads)) return kErrTooManyTiles;
+    few_across_kernel<T><<<(uint32_t)workgroups, kFewThreads, 0, (hipStream_t)stream>>>(p, col_tiles);
+    return (int)hipGetLastError();
+}
+
 }  // namespace
 
-// Groups of at most 16 rows on average.
-bool few_rows_serve(const RowsProduct &p) { return p.b_n_major && p.n <= (int64_t)kFewRows * p.groups; }
+// Groups of at most 16 rows on average.  Forward products of up to 512 workgroups: above, the tiles' longer pieces of the weights' rows
+// bring more than the wavefronts' shares (one row, 4096 x 4096: 12.1 us here, 19.3 in tiles; 15 groups of 2560 x 2176: 35 and 40; 32 of
+// 2048 x 2048: 53 and 48.5).
+bool few_rows_serve(const RowsProduct &p)
+{
+    if (p.n > (int64_t)kFewRows * p.groups) return false;
+    return p.b_n_major || (p.N >= 4 && (int64_t)p.groups * ((p.N + kAcrossCols - 1) / kAcrossCols) <= 512);
+}
 
 int launch_few_rows(int32_t dtype, const RowsProduct &p, void *stream)
 {
+    if (!p.b_n_major)
+        return dtype == GROOT_F32 ? few_across_launch<float>(p, stream) : dtype == GROOT_BF16 ? few_across_launch<bf16_t>(p, stream) : few_across_launch<f16_t>(p, stream);
     if (dtype == GROOT_F32) return few_launch<float, float, float>(p, stream);
     if (dtype == GROOT_BF16) return few_launch<bf16_t, bf16_t, bf16_t>(p, stream);
     return few_launch<f16_t, f16_t, f16_t>(p, stream);

@@ -135,12 +135,6 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
     const RowTile t = find_tile(p.offsets, p.groups, p.n, blockIdx.x, log_rows);
     if (t.group < 0) return;
     const T *B = (const T *)p.B + (int64_t)t.group * p.K * p.N;
-    StageB b;
-    b.init(B, kNMajor ? p.K : p.N, p.N, p.K, kNMajor ? p.K : p.N);
-    for (int s = 0; s < steps; ++s) {
-        b.begin(s, lds + s * StageB::kBytes);
-        b.end(lds + s * StageB::kBytes);
-    }
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     char *const ring = lds + steps * StageB::kBytes + wave * (kStages * kNarrowStage);
     const int64_t rows = t.end - t.begin, pitch = p.a_stride * (int64_t)sizeof(T);
@@ -173,16 +167,24 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
             load_block += kWaves;
         }
     };
-    Epilogue<T, O, kJ> epilogue;
-    epilogue.init(p, t.group, 0);
-    dma_wait();
-    __syncthreads();                                         // the weights are there
-    if (mine <= 0) return;
     if constexpr (kAligned) {
 #pragma unroll
         for (int k = 0; k < kStages - 1; ++k) begin(k);
     } else {
         begin(0);
+    }
+    StageB b;
+    b.init(B, kNMajor ? p.K : p.N, p.N, p.K, kNMajor ? p.K : p.N);
+    for (int s = 0; s < steps; ++s) {
+        b.begin(s, lds + s * StageB::kBytes);
+        b.end(lds + s * StageB::kBytes);
+    }
+    Epilogue<T, O, kJ> epilogue;
+    epilogue.init(p, t.group, 0);
+    __syncthreads();                                         // the weights are there
+    if (mine <= 0) {
+        if constexpr (kAligned) dma_wait();                  // its first loads, of zeros
+        return;
     }
     typename TileType<T>::Sum sums[1][kJ];
     int now = 0, next = kStages - 1;
