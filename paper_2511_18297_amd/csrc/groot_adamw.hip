@@ -97,34 +97,58 @@ __device__ __forceinline__ v4f load_codes(const uint8_t *p, float scale, int lef
     return r;
 }
 
+// The quotient x / s, rounded as a division rounds it, from the reciprocal r of s rounded to nearest (Markstein): r's product is a last
+// place off at most, and its remainder, exact in one fused operation, decides.  For s and x / s well inside fp32's range.
+__device__ __forceinline__ float quotient(float x, float s, float r)
+{
+    const float q = x * r;
+    return __builtin_fmaf(__builtin_fmaf(-q, s, x), r, q);
+}
+
+// Four square roots, rounded to nearest (but for one in some millions, a last place off), in the same way.  (Where a value takes 16
+// bytes, the ones of the mathematical library bound the kernel: 115 instructions a value in all.)
+__device__ __forceinline__ v4f roots(v4f v)
+{
+    const float low = fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), high = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+    v4f r;
+    if (__all(low > 0x1p-96f && high < 0x1p96f && __builtin_isfinite((v[0] + v[1]) + (v[2] + v[3])))) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float y = __builtin_amdgcn_rsqf(v[k]), g = v[k] * y;
+            r[k] = __builtin_fmaf(__builtin_fmaf(-g, g, v[k]), 0.5f * y, g);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = sqrtf(v[k]);
+    }
+    return r;
+}
+
 // Codes and scale of the wavefront's 256 values: the scale takes the largest finite magnitude to the largest code.  The instruction
 // adds its random number's upper 20 bits behind the three that a code keeps and cuts the rest off (below 2^-6: behind steps of 2^-9).
 // `never0`: a positive value is held as the smallest code at least (a root of 0 beside a first moment above 0 is a step of m / eps).
-// The scale's reciprocal is off by 2^-22 at most, which moves a value's chance to be rounded up by as much.
 template <bool kWhole>
 __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, const uint32_t (&random)[4], bool never0, int left)
 {
-#pragma clang fp contract(off)
     float top = 0.f;
     // one look at four values: their sum is not finite if one of them is not
-    if (__all(__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])))) {
+    const bool finite = __all(__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) top = fmaxf(top, __builtin_fabsf(x[k]));   // values that do not exist are zeros
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) top = fmaxf(top, __builtin_isfinite(x[k]) ? __builtin_fabsf(x[k]) : 0.f);
-    }
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, finite || __builtin_isfinite(x[k]) ? __builtin_fabsf(x[k]) : 0.f);   // values that do not exist are zeros
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
     const float scale = top * (1.f / kCodeTop);
-    // scales whose reciprocal is not exact enough or infinite: quotients
-    const bool small = scale < 0x1p-100f;
-    const float inverse = small ? 0.f : 1.f / scale;
     v4f r;
+    if (scale > 0x1p-96f) {                                  // the same for the whole wavefront
+        const float inverse = 1.f / scale;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = quotient(x[k], scale, inverse);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = scale > 0.f ? x[k] / scale : 0.f;
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        r[k] = x[k] * inverse;
-        if (small) r[k] = scale > 0.f ? x[k] / scale : 0.f;
         r[k] = __builtin_amdgcn_fmed3f(r[k], -kCodeTop, kCodeTop);
         if (never0 && x[k] > 0.f) r[k] = fmaxf(r[k], kCodeLeast);
     }
@@ -132,7 +156,7 @@ __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, 
     c = __builtin_amdgcn_cvt_sr_fp8_f32(r[1], random[1], c, 1);
     c = __builtin_amdgcn_cvt_sr_fp8_f32(r[2], random[2], c, 2);
     c = __builtin_amdgcn_cvt_sr_fp8_f32(r[3], random[3], c, 3);
-    if (!__all(__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])))) {
+    if (!finite) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (!__builtin_isfinite(x[k])) c |= 0x7Fu << (8 * k);
@@ -145,15 +169,6 @@ __device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, 
             if (k < left) p[k] = (uint8_t)(c >> (8 * k));
     }
     if (threadIdx.x % kWave == 0) *scale_at = scale;
-}
-
-// Square root and quotient within an ulp or two, from the instructions: where a value takes 16 bytes (states in 8 bits) the exact ones'
-// 20 instructions more bound the kernel.  The square root of numbers below the normal ones is kept.
-__device__ __forceinline__ float near_root(float v)
-{
-    const bool small = v < 0x1p-96f;
-    const float s = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
-    return small ? s * 0x1p-32f : s;
 }
 
 // the values [at, at + 4) of a tensor, by one lane; all lanes of the wavefront come here
@@ -176,13 +191,22 @@ __device__ __forceinline__ void adamw_values(const AdamwTensor &t, const AdamwFa
         m = load4<float, kWhole>((const float *)t.m + at, left);
         v = load4<float, kWhole>((const float *)t.v + at, left);
     }
-    v4f root;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float gk = scaled ? g[k] * gs : g[k];
         m[k] = m[k] * f.beta1 + gk * f.one_minus_beta1;
         v[k] = v[k] * f.beta2 + (gk * gk) * f.one_minus_beta2;
-        root[k] = kBits == 8 ? near_root(v[k]) : sqrtf(v[k]);
+    }
+    v4f root;
+    if (kBits == 8) {
+        root = roots(v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) root[k] = sqrtf(v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        // 8 bits: the step's quotient within two last places, far below what the codes leave of m
         const float denom = root[k] * f.root_factor + f.eps;
         w[k] = w[k] * f.decay - f.step_size * (kBits == 8 ? m[k] * __builtin_amdgcn_rcpf(denom) : m[k] / denom);
     }

@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
 #pragma unroll
             for (int j = 0; j < kJ; ++j) fb[j] = StageB::fragment(w, 32 * j, q);
 #pragma unroll
-            for (int j = 0; j < kJ; ++j) sums[0][j] = TileType<T>::mma(fb[j], fa, sums[0][j]);
+            for (int n = 0; n < kJ * TileType<T>::kParts; ++n) sums[0][n % kJ] = TileType<T>::mma(fb[n % kJ], fa, sums[0][n % kJ], n / kJ);
         }
         if (++s == steps) {
             const int64_t r = (int64_t)block * kNarrowRows;  // through the place of this step, which is loaded again at the next one

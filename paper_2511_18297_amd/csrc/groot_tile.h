@@ -31,13 +31,14 @@ struct TileType;
 template <>
 struct TileType<bf16_t> {
     typedef v16f Sum;
+    static constexpr int kParts = 1;         // instructions that a fragment takes
     // the sum of a fragment's values
     static __device__ __forceinline__ float total(v4i a)
     {
         const v8bf x = __builtin_bit_cast(v8bf, a);
         return (((float)x[0] + (float)x[1]) + ((float)x[2] + (float)x[3])) + (((float)x[4] + (float)x[5]) + ((float)x[6] + (float)x[7]));
     }
-    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c, int part)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
     }
@@ -45,12 +46,13 @@ struct TileType<bf16_t> {
 template <>
 struct TileType<f16_t> {
     typedef v16f Sum;
+    static constexpr int kParts = 1;
     static __device__ __forceinline__ float total(v4i a)
     {
         const v8h x = __builtin_bit_cast(v8h, a);
         return (((float)x[0] + (float)x[1]) + ((float)x[2] + (float)x[3])) + (((float)x[4] + (float)x[5]) + ((float)x[6] + (float)x[7]));
     }
-    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c, int part)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
     }
@@ -58,21 +60,20 @@ struct TileType<f16_t> {
 template <>
 struct TileType<int8_t> {
     typedef v16i Sum;
-    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+    static constexpr int kParts = 1;
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c, int part) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
 template <>
 struct TileType<float> {
     typedef v16f Sum;
+    static constexpr int kParts = 4;
     static __device__ __forceinline__ float total(v4i a)
     {
         return (__int_as_float(a[0]) + __int_as_float(a[1])) + (__int_as_float(a[2]) + __int_as_float(a[3]));
     }
-    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c)
+    static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c, int part)
     {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            c = __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(a[j]), __int_as_float(b[j]), c, 0, 0, 0);
-        return c;
+return __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(a[part]), __int_as_float(b[part]), c, 0, 0, 0);
     }
 };
 
@@ -358,12 +359,16 @@ struct Fragments {
 #pragma unroll
         for (int i = 0; i < kI; ++i) a[i] = StageA::fragment(tile, row0 + 32 * i, q);
     }
-    // the blocks [first, last) of kI * kJ
-    __device__ __forceinline__ void multiply(typename TileType<T>::Sum (&sums)[kI][kJ], int first = 0, int last = kI * kJ) const
+    // the first or second half of the products (0, 1): instructions that follow one another add to different blocks
+    __device__ __forceinline__ void multiply(typename TileType<T>::Sum (&sums)[kI][kJ], int half) const
     {
+        constexpr int kBlocks = kI * kJ, kAll = kBlocks * TileType<T>::kParts;
 #pragma unroll
-        for (int k = 0; k < kI * kJ; ++k)
-            if (k >= first && k < last) sums[k / kJ][k % kJ] = TileType<T>::mma(b[k % kJ], a[k / kJ], sums[k / kJ][k % kJ]);
+        for (int n = 0; n < kAll; ++n) {
+            if (n < half * kAll / 2 || n >= (half + 1) * kAll / 2) continue;
+            const int i = n % kBlocks / kJ, j = n % kJ;
+            sums[i][j] = TileType<T>::mma(b[j], a[i], sums[i][j], n / kBlocks);
+        }
     }
     __device__ __forceinline__ void add_columns(float (&columns)[kJ]) const
     {
@@ -391,7 +396,7 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
     if (steps <= 0) return;
     if constexpr (StageA::kDirect) {
         // a step past the last one loads zeros that nothing reads: every step has the same number of loads to count
-        constexpr int kEach = StageA::kEach + StageB::kEach, kHalf = kI * kJ / 2;
+        constexpr int kEach = StageA::kEach + StageB::kEach;
         auto begin = [&](int64_t s, int at, int first, int last) {
             a.begin(s, lds + at, first, last);
             b.begin(s, lds + at + StageA::kBytes, first - StageA::kEach, last - StageA::kEach);
@@ -409,7 +414,7 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
                 // the loads are issued between the products, a few at a time: all at once they would hold the wavefront up
                 if (q + 1 < kQ) f[(q + 1) % 2].read(lds + now, row0, col0, q + 1);
                 __builtin_amdgcn_sched_barrier(0);
-                f[q % 2].multiply(sums, 0, kHalf);
+                f[q % 2].multiply(sums, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 constexpr int kSpread = kStages == 2 ? 1 : kQ;
                 if (q < kSpread) begin(s + kStages - 1, free, q * kEach / kSpread, (q + 1) * kEach / kSpread);
@@ -421,7 +426,7 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
                     f[0].read(lds + now, row0, col0, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                f[q % 2].multiply(sums, kHalf);
+                f[q % 2].multiply(sums, 1);
                 if constexpr (kColumns)
                     if (mine) f[q % 2].add_columns(*columns);
                 __builtin_amdgcn_sched_barrier(0);
@@ -444,7 +449,8 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
 #pragma unroll
             for (int q = 0; q < kQ; ++q) {
                 f[0].read(lds + at, row0, col0, q);
-                f[0].multiply(sums);
+                f[0].multiply(sums, 0);
+                f[0].multiply(sums, 1);
                 if constexpr (kColumns)
                     if (mine) f[0].add_columns(*columns);
             }
