@@ -237,6 +237,74 @@ def test_offsets_that_do_not_ascend_stay_in_bounds():
     assert (work[need:] == 7).all()
 
 
+# sizes at which the larger tiles and the kernels for many columns and few rows are taken: (sizes of the groups, K, N)
+LARGE = [([8192], 72, 4096), ([4000, 100, 60], 136, 2100), ([2048], 264, 2048), ([900], 200, 1100), ([256], 640, 4096), ([33] * 8, 1024, 640),
+         ([300], 3600, 3600), ([700] * 16, 520, 1032), ([1] * 20, 640, 2048), ([9, 16, 2], 1000, 2052), ([7], 300, 5000), ([20000], 64, 96)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("case", range(len(LARGE)))
+def test_large_sizes(kind, case):
+    dtype, (sizes, K, N) = TYPES[kind], LARGE[case]
+    n, E, X, dY, W, b = case_tensors(dtype, sizes, K, N, 0, 300 + case)
+    offsets = offsets_of(sizes) if E > 1 else None
+    parts = lambda t: t.double().split(sizes)  # noqa: E731
+    Y, dX = out_matrix(n, N, dtype), out_matrix(n, K, dtype)
+    G.groot_grouped_product(X, W, offsets, b, False, Y)
+    want = torch.cat([x @ w + c for x, w, c in zip(parts(X), W.double(), b.double())])
+    terms = torch.cat([x.abs() @ w.abs() + c.abs() for x, w, c in zip(parts(X), W.double(), b.double())])
+    close(Y, want, sum_bound(terms, K + 1) + rounding(want, dtype) * 1.01, "Y")
+    G.groot_grouped_product_backward_data(dY, W, offsets, dX)
+    want = torch.cat([d @ w.t() for d, w in zip(parts(dY), W.double())])
+    terms = torch.cat([d.abs() @ w.abs().t() for d, w in zip(parts(dY), W.double())])
+    close(dX, want, sum_bound(terms, N) + rounding(want, dtype) * 1.01, "dX")
+    work = torch.full((max(16, G.groot_grouped_product_backward_weights_workspace(n, E, K, N, dtype)),), 255, dtype=torch.uint8, device="cuda")
+    dW, db = torch.full((E, K, N), float("nan"), device="cuda").to(dtype), torch.full((E, N), float("nan"), device="cuda").to(dtype)
+    G.groot_grouped_product_backward_weights(X, dY, offsets, dW, db, work)
+    rows = torch.tensor(sizes, device="cuda", dtype=torch.float64)
+    want = torch.stack([x.t() @ d for x, d in zip(parts(X), parts(dY))])
+    terms = torch.stack([x.abs().t() @ d.abs() for x, d in zip(parts(X), parts(dY))])
+    close(dW, want, sum_bound(terms, rows[:, None, None]) + rounding(want, dtype) * 1.01, "dW")
+    want = torch.stack([d.sum(0) for d in parts(dY)])
+    terms = torch.stack([d.abs().sum(0) for d in parts(dY)])
+    close(db, want, sum_bound(terms, rows[:, None]) + rounding(want, dtype) * 1.01, "db")
+
+
+@pytest.mark.parametrize("case", range(len(LARGE)))
+def test_quantized_product_large_sizes(case):
+    sizes, K, N = LARGE[case]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(400 + case)
+    n, E = sum(sizes), len(sizes)
+    Q = torch.randint(-127, 128, (n, K), generator=gen, device="cuda", dtype=torch.int8)
+    W = torch.randint(-127, 128, (E, N, K), generator=gen, device="cuda", dtype=torch.int8)
+    qs, ws = torch.rand(n, generator=gen, device="cuda") * 0.01, torch.rand((E, N), generator=gen, device="cuda") * 0.01
+    Y = out_matrix(n, N, torch.float32)
+    G.groot_quantized_product(Q, qs, W, ws, offsets_of(sizes) if E > 1 else None, None, False, Y)
+    dots = torch.cat([q @ w.t() for q, w in zip(Q.double().split(sizes), W.double())])
+    want = dots * qs.double()[:, None] * ws.double()[group_of(sizes)]
+    close(Y, want, 4 * 2.0 ** -24 * want.abs(), "Y")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_no_rows_at_all(kind):
+    dtype = TYPES[kind]
+    X, dY, W = torch.empty((0, 40), dtype=dtype, device="cuda"), torch.empty((0, 24), dtype=dtype, device="cuda"), torch.ones((3, 40, 24), dtype=dtype, device="cuda")
+    offsets = torch.zeros(4, dtype=torch.int64, device="cuda")
+    G.groot_grouped_product(X, W, offsets, None, False, dY)
+    G.groot_grouped_product_backward_data(dY, W, offsets, X)
+    for many in (offsets, None):
+        E = 3 if many is not None else 1
+        dW, db = torch.full((E, 40, 24), 7.0, device="cuda").to(dtype), torch.full((E, 24), 7.0, device="cuda").to(dtype)
+        G.groot_grouped_product_backward_weights(X, dY, many, dW, db, None)
+        assert not dW.any() and not db.any()
+    Q, W8 = torch.empty((0, 40), dtype=torch.int8, device="cuda"), torch.ones((3, 24, 40), dtype=torch.int8, device="cuda")
+    s, ws = torch.empty(0, device="cuda"), torch.ones((3, 24), device="cuda")
+    G.groot_quantize_rows(X, Q, s)
+    G.groot_quantized_product(Q, s, W8, ws, offsets, None, False, dY)
+    G.groot_quantized_linear(X, W8, ws, offsets, None, False, dY, torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
 def test_rows_far_apart():
     """element offsets beyond 2^32"""
     stride, n, K, N = (1 << 27) + 8, 40, 64, 32
