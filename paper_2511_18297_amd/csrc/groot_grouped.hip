@@ -183,8 +183,9 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
     StageB b;
     b.init(B, kNMajor ? p.K : p.N, p.N, p.K, kNMajor ? p.K : p.N);
     for (int s = 0; s < steps; ++s) {
-        b.begin(s, lds + s * StageB::kBytes);
-        b.end(lds + s * StageB::kBytes);
+        typename StageB::Held h;
+        b.template load<true>(s, h);
+        b.template put<true>(h, lds + s * StageB::kBytes);
     }
     Epilogue<T, O, kJ> epilogue;
     epilogue.init(p, t.group, 0);
@@ -310,7 +311,7 @@ int choose_tile(int64_t n, int32_t groups, bool offsets, int32_t N, bool aligned
     double least = 0;
     for (int k = 0; k < kTileKinds; ++k) {
         if (!aligned && k != 1 && k != 4 && k != 6) continue;
-        if (sizeof(T) == 4 && k == 0) continue;
+        if (sizeof(T) == 4 && (k == 0 || k == 2)) continue;  // never the least
         const TileCost &c = sizeof(T) == 4 ? kTile32[k] : kTile16[k];
         // a group's last tile is half full, on average
         double rows = offsets ? (double)n / c.rows + 0.5 * groups : (double)((n + c.rows - 1) / c.rows);
@@ -343,7 +344,8 @@ int rows_choose(const RowsProduct &p, void *stream)
     case 0:
         if constexpr (sizeof(T) < 4) return rows_launch<T, O, 256, 256, 2, 4, 2, kNMajor, true>(p, stream);
     case 1: return rows_launch<T, O, 128, 128, 2, 2, 2, kNMajor, true>(p, stream);
-    case 2: return rows_launch<T, O, 128, 128, 2, 2, 4, kNMajor, true>(p, stream);
+    case 2:
+        if constexpr (sizeof(T) < 4) return rows_launch<T, O, 128, 128, 2, 2, 4, kNMajor, true>(p, stream);
     case 3: return rows_launch<T, O, 64, 128, 2, 2, 3, kNMajor, true>(p, stream);
     case 4: return rows_launch<T, O, 64, 64, 2, 2, 5, kNMajor, true>(p, stream);
     case 5: return rows_launch<T, O, 32, 128, 1, 4, 4, kNMajor, true>(p, stream);

@@ -251,12 +251,16 @@ struct Stage {
     static_assert(kBytes % (16 * kThreads) == 0 && kThreads % kPieces == 0, "a whole number of loads of whole rows");
     static_assert(kAcross ? kRowsEach % (sizeof(T) == 4 ? 8 : 4) == 0 && kRowBytes >= (sizeof(T) == 4 ? 256 : 128) : kRowsEach % 16 == 0, "a lane's piece is the same in all its loads");
 
+    // what is on its way through registers where rows begin anywhere, and how much of it exists
+    struct Held {
+        v4i x[kEach];
+        int32_t valid[kEach];
+    };
+
     const char *src[kAcross ? 1 : kEach];
     int64_t pitch, limit;                                    // bytes between rows; bytes ("along") or rows ("across") of the contraction
     int64_t width;                                           // across: bytes of a row from the lane's piece on
     int32_t piece, row;
-    v4i held[kAligned ? 1 : kEach];
-    int32_t valid[kAligned ? 1 : kEach];
     bool short_row;
 
     static __device__ __forceinline__ int swizzle(int r) 
@@ -289,41 +293,52 @@ struct Stage {
         }
     }
 
-    // the loads [first, last) of a lane's kEach
-    __device__ __forceinline__ void begin(int64_t s, char *tile, int first = 0, int last = kEach)
+    // where a lane's load i of step s begins, and how many bytes of its row are left there (none: 0 or less)
+    __device__ __forceinline__ const char *place(int64_t s, int i, int64_t *left) const
+    {
+        if constexpr (kAcross) {
+            const int64_t k = s * kValues + row + i * kRowsEach;
+            const char *p = src[0] + (s * kValues + i * kRowsEach) * pitch;
+            *left = k < limit ? width : 0;
+            if (!kAligned && k >= limit) p += (limit - 1 - k) * pitch + width;   // behind the end of the last row
+            return p;
+        } else {
+            *left = limit - s * kStep - piece * 16;
+            return src[i] + s * kStep;
+        }
+    }
+    // direct: the loads [first, last) of a lane's kEach, zeros for what does not exist
+    __device__ __forceinline__ void begin(int64_t s, char *tile, int first = 0, int last = kEach) const
     {
         const uint32_t to = lds_offset(tile) + threadIdx.x / kWave * (kWave * 16);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             if (i < first || i >= last) continue;
-            const char *p;
             int64_t left;
-            if (kAcross) {
-                const int64_t k = s * kValues + row + i * kRowsEach;
-                p = src[0] + (s * kValues + i * kRowsEach) * pitch;
-                left = k < limit ? width : 0;
-                if (kAligned) p = k < limit ? p : (const char *)&g_zeros;
-                else if (k >= limit) p += (limit - 1 - k) * pitch + width;   // behind the end of the last row
-            } else {
-                p = src[i] + s * kStep;
-                left = limit - s * kStep - piece * 16;
-                if (kAligned) p = left > 0 ? p : (const char *)&g_zeros;
-            }
-            if constexpr (kAligned) {
-                dma16(p, to + i * (kThreads * 16));
-            } else {
-                valid[i] = left >= 16 ? 16 : left <= 0 ? 0 : (int32_t)left;
-                held[i] = short_row ? short16<T>(p, left) : raw16(p, left);
-            }
+            const char *p = place(s, i, &left);
+            // across, a piece past the last column has the last column's place: only the row decides
+            const bool in = kAcross ? s * kValues + row + i * kRowsEach < limit : left > 0;
+            dma16(in ? p : (const char *)&g_zeros, to + i * (kThreads * 16));
         }
     }
-
-    __device__ __forceinline__ void end(char *tile)
+    // through registers
+    template <bool kShort>
+    __device__ __forceinline__ void load(int64_t s, Held &h) const
     {
-        if constexpr (!kAligned) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) *(v4i *)(tile + (i * kThreads + threadIdx.x) * 16) = short_row ? held[i] : cut16(held[i], valid[i]);
+        for (int i = 0; i < kEach; ++i) {
+            int64_t left;
+            const char *p = place(s, i, &left);
+            h.valid[i] = left >= 16 ? 16 : left <= 0 ? 0 : (int32_t)left;
+            h.x[i] = kShort && short_row ? short16<T>(p, left) : raw16(p, left);
         }
+    }
+    template <bool kShort>
+    __device__ __forceinline__ void put(const Held &h, char *tile) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            *(v4i *)(tile + (i * kThreads + threadIdx.x) * 16) = kShort && short_row ? h.x[i] : cut16(h.x[i], h.valid[i]);
     }
 
     // the lane's 16 bytes of the 32 rows (columns) from `first` on, sub-step s
@@ -382,6 +397,45 @@ struct Fragments {
     }
 };
 
+// ... of operands that go through registers: kSets steps are on their way in them, two tiles lie in LDS.  More of them pay where a CU
+// has few small tiles (2000 rows, K = 3001, N = 301: 51 us with one, 34 with more); elsewhere the registers cost wavefronts.
+template <typename T, bool kColumns, bool kShort, class StageA, class StageB, int kI, int kJ>
+__device__ __forceinline__ void tile_product_held(const StageA &a, const StageB &b, char *lds, int64_t steps, int row0, int col0,
+                                                  typename TileType<T>::Sum (&sums)[kI][kJ], float (*columns)[kJ], bool mine)
+{
+    constexpr int kBoth = StageA::kBytes + StageB::kBytes, kSets = kShort || kColumns || kI * kJ > 1 ? 1 : 2;
+    typename StageA::Held ha[kSets];
+    typename StageB::Held hb[kSets];
+    Fragments<T, StageA, StageB, kI, kJ> f;
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {                        // a step past the last one loads the ends of rows, which nothing reads
+        a.template load<kShort>(u, ha[u]);
+        b.template load<kShort>(u, hb[u]);
+    }
+    int at = 0;
+#pragma unroll 1
+    for (int64_t s0 = 0; s0 < steps; s0 += kSets) {
+#pragma unroll
+        for (int u = 0; u < kSets; ++u) {
+            if (s0 + u >= steps) break;
+            a.template put<kShort>(ha[u], lds + at);
+            b.template put<kShort>(hb[u], lds + at + StageA::kBytes);
+            __syncthreads();                                 // two tiles: the other one is read no more once all are here
+            a.template load<kShort>(s0 + u + kSets, ha[u]);
+            b.template load<kShort>(s0 + u + kSets, hb[u]);
+#pragma unroll
+            for (int q = 0; q < StageA::kSubSteps; ++q) {
+                f.read(lds + at, row0, col0, q);
+                f.multiply(sums, 0);
+                f.multiply(sums, 1);
+                if constexpr (kColumns)
+                    if (mine) f.add_columns(*columns);
+            }
+            at = kBoth - at;
+        }
+    }
+}
+
 // The product of two staged operands over `steps` steps: sums[i][j] of the wavefront's 32 x 32 blocks, rows of `A` from row0 on,
 // columns of `B` from col0 on.  kStages pairs of tiles lie in LDS, so that kStages - 1 steps are on their way while one is computed.
 // The fragments of a sub-step are read while the one before is multiplied, across the steps' borders too: the barrier lies before the
@@ -393,13 +447,13 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
 {
     constexpr int kBoth = StageA::kBytes + StageB::kBytes, kQ = StageA::kSubSteps;
     static_assert(kQ % 2 == 0, "the two sets of fragments take turns");
-    Fragments<T, StageA, StageB, kI, kJ> f[2];
 #pragma unroll
     for (int i = 0; i < kI; ++i)
 #pragma unroll
         for (int j = 0; j < kJ; ++j) sums[i][j] = {};
     if (steps <= 0) return;
     if constexpr (StageA::kDirect) {
+        Fragments<T, StageA, StageB, kI, kJ> f[2];
         // a step past the last one loads zeros that nothing reads: every step has the same number of loads to count
         constexpr int kEach = StageA::kEach + StageB::kEach;
         auto begin = [&](int64_t s, int at, int first, int last) {
@@ -440,28 +494,8 @@ __device__ __forceinline__ void tile_product(StageA &a, StageB &b, char *lds, in
         }
         dma_wait();                                          // before the workgroup's LDS is anybody else's
     } else {
-        auto begin = [&](int64_t s) {
-            a.begin(s, lds);
-            b.begin(s, lds);
-        };
-        begin(0);
-        int at = 0;
-#pragma unroll 1
-        for (int64_t s = 0; s < steps; ++s) {
-            a.end(lds + at);
-            b.end(lds + at + StageA::kBytes);
-            __syncthreads();                                 // two tiles: the other one is read no more once all are here
-            if (s + 1 < steps) begin(s + 1);
-#pragma unroll
-            for (int q = 0; q < kQ; ++q) {
-                f[0].read(lds + at, row0, col0, q);
-                f[0].multiply(sums, 0);
-                f[0].multiply(sums, 1);
-                if constexpr (kColumns)
-                    if (mine) f[0].add_columns(*columns);
-            }
-            at = kBoth - at;
-        }
+        if (a.short_row || b.short_row) tile_product_held<T, kColumns, true>(a, b, lds, steps, row0, col0, sums, columns, mine);
+        else tile_product_held<T, kColumns, false>(a, b, lds, steps, row0, col0, sums, columns, mine);
     }
 }
 
