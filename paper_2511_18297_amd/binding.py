@@ -619,15 +619,24 @@ def _array(t, what, shape, dtype):
 
 
 def _matrix_rows(t, what):
-    if not isinstance(t, _Tensor) or t.dim() != 2:
-        raise TypeError(f"{what} must be a matrix")
-    return t.shape[0]
+    try:
+        n, _ = t.shape
+    except (AttributeError, ValueError):
+        raise TypeError(f"{what} must be a matrix") from None
+    return n
 
 
 def _weights(t, what):
-    if not isinstance(t, _Tensor) or t.dim() != 3:
-        raise TypeError(f"{what} must have three dimensions, the groups first")
-    return t.shape
+    try:
+        E, K, N = t.shape
+    except (AttributeError, ValueError):
+        raise TypeError(f"{what} must have three dimensions, the groups first") from None
+    return E, K, N
+
+
+def _stream(stream):
+    """The handle of a stream, by default of the current one; called after a CUDA tensor was seen, so there is a context."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
 
 
 def groot_grouped_product(X, W, offsets, bias, relu: bool, Y, stream=None) -> None:
@@ -640,7 +649,7 @@ def groot_grouped_product(X, W, offsets, bias, relu: bool, Y, stream=None) -> No
     y, ys = _rows(Y, "Y", n, N, T)
     _check(_lib.groot_grouped_product(d, x, xs, _array(W, "W", (E, K, N), T), _array(offsets, "offsets", (E + 1,), _int64),
                                       _array(bias, "bias", (E, N), T), 1 if relu else 0, y, ys, n, E, K, N,
-                                      _stream_handle(stream)))
+                                      _stream(stream)))
 
 
 def groot_grouped_product_backward_data(dY, W, offsets, dX, stream=None) -> None:
@@ -652,7 +661,7 @@ def groot_grouped_product_backward_data(dY, W, offsets, dX, stream=None) -> None
     x, xs = _rows(dX, "dX", n, K, T)
     _check(_lib.groot_grouped_product_backward_data(d, y, ys, _array(W, "W", (E, K, N), T),
                                                     _array(offsets, "offsets", (E + 1,), _int64), x, xs, n, E, K, N,
-                                                    _stream_handle(stream)))
+                                                    _stream(stream)))
 
 
 def groot_grouped_product_backward_weights_workspace(n_rows: int, groups: int, K: int, N: int, dtype) -> int:
@@ -678,7 +687,7 @@ def groot_grouped_product_backward_weights(X, dY, offsets, dW, dbias, workspace,
                                                        _array(dW, "dW", (E, K, N), dW.dtype),
                                                        _array(dbias, "dbias", (E, N), dW.dtype), n, E, K, N, ws,
                                                        0 if ws is None else workspace.numel() * workspace.element_size(),
-                                                       _stream_handle(stream)))
+                                                       _stream(stream)))
 
 
 def groot_quantize_rows(X, Q, scale, stream=None) -> None:
@@ -687,7 +696,7 @@ def groot_quantize_rows(X, Q, scale, stream=None) -> None:
     x, xs = _rows(X, "X", n, K, X.dtype)
     q, qs = _rows(Q, "Q", n, K, _int8)
     _check(_lib.groot_quantize_rows(_dtype(X, "X"), x, xs, q, qs, _array(scale, "scale", (n,), _float32), n, K,
-                                    _stream_handle(stream)))
+                                    _stream(stream)))
 
 
 def groot_quantized_product(Q, q_scale, W, w_scale, offsets, bias, relu: bool, Y, stream=None) -> None:
@@ -700,7 +709,7 @@ def groot_quantized_product(Q, q_scale, W, w_scale, offsets, bias, relu: bool, Y
     _check(_lib.groot_quantized_product(q, qs, _array(q_scale, "q_scale", (n,), _float32), _array(W, "W", (E, N, K), _int8),
                                    _array(w_scale, "w_scale", (E, N), _float32),
                                    _array(offsets, "offsets", (E + 1,), _int64), _array(bias, "bias", (E, N), _float32),
-                                   1 if relu else 0, _dtype(Y, "Y"), y, ys, n, E, K, N, _stream_handle(stream)))
+                                   1 if relu else 0, _dtype(Y, "Y"), y, ys, n, E, K, N, _stream(stream)))
 
 
 def groot_quantized_linear_workspace(n_rows: int, K: int) -> int:
@@ -722,7 +731,7 @@ def groot_quantized_linear(X, W, w_scale, offsets, bias, relu: bool, Y, workspac
                                   _array(w_scale, "w_scale", (E, N), _float32),
                                   _array(offsets, "offsets", (E + 1,), _int64), _array(bias, "bias", (E, N), _float32),
                                   1 if relu else 0, y, ys, n, E, K, N, _dev_ptr(workspace, "workspace"),
-                                  workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+                                  workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 class _AdamwTensor(ctypes.Structure):
@@ -796,4 +805,4 @@ def groot_adamw_step(tensors: AdamwTensors, step: int, lr: float, beta1: float =
             raise TypeError("grad_scale must be one float32")
         gs = _dev_ptr(grad_scale, "grad_scale")
     _check(_lib.groot_adamw_step(tensors.address, tensors.count, tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, step, lr,
-                                 beta1, beta2, eps, weight_decay, gs, seed & 0xFFFFFFFF, _stream_handle(stream)))
+                                 beta1, beta2, eps, weight_decay, gs, seed & 0xFFFFFFFF, _stream(stream)))

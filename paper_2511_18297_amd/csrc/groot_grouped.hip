@@ -289,10 +289,10 @@ int narrow_launch(const RowsProduct &p, void *stream)
                    : narrow_launch_as<T, O, kN, 8, 1, kNMajor, false>(p, log_rows, steps, whole, stream);
 }
 
-// What a step of the contraction (128 bytes) takes, in ns, where the GPU's 256 CUs hold up to 256 or up to 512 tiles at a time
-// (K = 4096 bytes, fp32: MFMA-bound; the others: products of 2, 1, 1/2 .. steps' latency).  A tile's rows and columns and how many
-// stages of it lie in LDS:
-//                        256 x 256, 2   128 x 128, 2   128 x 128, 4   64 x 128, 3   64 x 64, 5   32 x 128, 4   32 x 64, 6
+// What a step of the contraction (128 bytes of every row) takes, in ns, with up to 256 and with up to 512 tiles of a kind on the GPU's
+// 256 CUs, measured over K of 4096 bytes on one group whose tiles come out even.  fp32 is bound by its matrix instructions at every
+// size; the others by theirs in large tiles, by the latency of a step's loads in small ones.  The kinds, rows x columns and stages:
+//   256 x 256, 2; 128 x 128, 2; 128 x 128, 4; 64 x 128, 3; 64 x 64, 5; 32 x 128, 4; 32 x 64, 6
 struct TileCost {
     int32_t rows, cols, to256, to512;        // to512 0: one tile to a CU
 };
