@@ -97,15 +97,7 @@ __device__ __forceinline__ v4f load_codes(const uint8_t *p, float scale, int lef
     return r;
 }
 
-// The quotient x / s, rounded as a division rounds it, from the reciprocal r of s rounded to nearest (Markstein): r's product is a last
-// place off at most, and its remainder, exact in one fused operation, decides.  For s and x / s well inside fp32's range.
-__device__ __forceinline__ float quotient(float x, float s, float r)
-{
-    const float q = x * r;
-    return __builtin_fmaf(__builtin_fmaf(-q, s, x), r, q);
-}
-
-// Four square roots, rounded to nearest (but for one in some millions, a last place off), in the same way.  (Where a value takes 16
+// Four square roots, rounded to nearest (but for one in some millions, a last place off), as quotient() has quotients.  (Where a value takes 16
 // bytes, the ones of the mathematical library bound the kernel: 115 instructions a value in all.)
 __device__ __forceinline__ v4f roots(v4f v)
 {

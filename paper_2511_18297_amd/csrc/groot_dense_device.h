@@ -9,6 +9,14 @@ namespace groot {
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
+// The quotient x / s, rounded as a division rounds it, from the reciprocal r of s rounded to nearest (Markstein): r's product is a last
+// place off at most, and its remainder, exact in one fused operation, decides.  For s and x / s well inside fp32's range.
+__device__ __forceinline__ float quotient(float x, float s, float r)
+{
+    const float q = x * r;
+    return __builtin_fmaf(__builtin_fmaf(-q, s, x), r, q);
+}
+
 // a value that is the same in every lane, as a scalar
 __device__ __forceinline__ int64_t uniform(int64_t x)
 {

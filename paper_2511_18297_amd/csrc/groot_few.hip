@@ -90,20 +90,29 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, i
     float x_scale = 1.f;
     const int32_t cut_row = (p.K + 127) / 128 * 128;
     if constexpr (kFused) {
-        constexpr int kPer = 16 / sizeof(X), kKeep = 4;      // values of a load, loads of a lane that stay in registers
+        constexpr int kPer = 16 / sizeof(X), kKeep = 2;      // values of a load, loads of a lane that stay in registers
         const int32_t loads = (p.K + kPer - 1) / kPer;
         v4i keep[kFusedRows][kKeep];
-        auto get = [&](int64_t row, int32_t i) {
-            return load16<X>((const char *)((const X *)p.A + row * p.a_stride) + (int64_t)i * 16, ((int64_t)p.K - (int64_t)i * kPer) * (int64_t)sizeof(X), (int64_t)p.K * sizeof(X) < 16);
-        };
+        const auto from = [&](int m, int32_t i) { return (const char *)((const X *)p.A + (t.begin + m) * p.a_stride) + (int64_t)i * 16; };
+        const auto left = [&](int32_t i) { return ((int64_t)p.K - (int64_t)i * kPer) * (int64_t)sizeof(X); };
+        const auto get = [&](int m, int32_t i) { return cut16(raw16(from(m, i), left(i)), left(i)); };
+        // no branch around the loads: past a row's end its last 16 bytes come, of which nothing stays
+#pragma unroll
+        for (int m = 0; m < kFusedRows; ++m) {
+            if (m >= rows) break;
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i) keep[m][i] = raw16(from(m, threadIdx.x + i * kFewThreads), left(threadIdx.x + i * kFewThreads));
+        }
 #pragma unroll
         for (int m = 0; m < kFusedRows; ++m) {
             if (m >= rows) break;
             uint32_t seen = 0;
 #pragma unroll
-            for (int i = 0; i < kKeep; ++i)
-                if ((int)threadIdx.x + i * kFewThreads < loads) seen = row_look<X>(keep[m][i] = get(t.begin + m, threadIdx.x + i * kFewThreads), seen);
-            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) seen = row_look<X>(get(t.begin + m, i), seen);
+            for (int i = 0; i < kKeep; ++i) {
+                keep[m][i] = cut16(keep[m][i], left(threadIdx.x + i * kFewThreads));
+                seen = row_look<X>(keep[m][i], seen);
+            }
+            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) seen = row_look<X>(get(m, i), seen);
             const float top = row_top_of<kWave>(row_top<X>(seen));
             if (lane == 0) tops[m][wave] = top;
         }
@@ -118,7 +127,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, i
 #pragma unroll
             for (int i = 0; i < kKeep; ++i)
                 if ((int)threadIdx.x + i * kFewThreads < loads) put(keep[m][i], threadIdx.x + i * kFewThreads);
-            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) put(get(t.begin + m, i), i);
+            for (int32_t i = threadIdx.x + kKeep * kFewThreads; i < loads; i += kFewThreads) put(get(m, i), i);
             if (m == (int)(threadIdx.x % 256 / 16)) x_scale = scale;
         }
         __syncthreads();
@@ -322,8 +331,8 @@ int launch_few_int8(int32_t out_dtype, const RowsProduct &p, void *stream)
     return few_launch<int8_t, f16_t, int8_t>(p, stream);
 }
 
-// Rows in floating point, all of them in every workgroup.
-bool few_linear_serves(const RowsProduct &p) { return p.n <= kFusedRows && p.n * ((p.K + 127) / 128 * 128) <= kFusedBytes; }
+// Rows in floating point, all of them in every workgroup; of 16 bytes at least.
+bool few_linear_serves(const RowsProduct &p) { return p.n <= kFusedRows && p.K >= 8 && p.n * ((p.K + 127) / 128 * 128) <= kFusedBytes; }
 
 int launch_few_linear(int32_t dtype, const RowsProduct &p, void *stream)
 {

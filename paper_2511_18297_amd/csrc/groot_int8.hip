@@ -8,7 +8,7 @@ namespace {
 // kLanes lanes to a row, 16 bytes a load, kKeep loads of a lane in registers: a row that fits them is read once.  Wider rows read
 // the rest a second time, from L2.  8192 rows of 4096 values, float16: 25 us for 101 MB, 4 TB/s: a workgroup's way from its loads over
 // the maximum to its stores is what the 8 of them on a CU cannot hide.
-template <typename T, int kLanes, int kKeep>
+template <typename T, int kLanes, int kKeep, bool kShort>
 __global__ __launch_bounds__(kBlock) void quantize_kernel(const T *__restrict__ X, int64_t x_stride, int8_t *__restrict__ Q, int64_t q_stride,
                                                           float *__restrict__ scale_at, int64_t n, int32_t K)
 {
@@ -20,22 +20,19 @@ __global__ __launch_bounds__(kBlock) void quantize_kernel(const T *__restrict__ 
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < n; first += (int64_t)gridDim.x * kRows) {
         const int64_t row = first + threadIdx.x / kLanes;
         const char *const x = (const char *)(X + (row < n ? row : n - 1) * x_stride);
-        const bool short_row = (int64_t)K * sizeof(T) < 16;
         auto left = [&](int32_t i) { return ((int64_t)K - (int64_t)i * kPer) * (int64_t)sizeof(T); };
-        auto get = [&](int32_t i) { return load16<T>(x + (int64_t)i * 16, left(i), short_row); };
+        auto get = [&](int32_t i) { return load16<T>(x + (int64_t)i * 16, left(i), kShort); };
+        // no branch around the loads: past the row's end its last 16 bytes come, of which nothing stays
         v4i keep[kKeep];
 #pragma unroll
         for (int i = 0; i < kKeep; ++i)
-            if (at + i * kLanes < loads) keep[i] = short_row ? get(at + i * kLanes) : raw16(x + (int64_t)(at + i * kLanes) * 16, left(at + i * kLanes));
-        if (!short_row) {
-#pragma unroll
-            for (int i = 0; i < kKeep; ++i)
-                if (at + i * kLanes < loads) keep[i] = cut16(keep[i], left(at + i * kLanes));
-        }
+            keep[i] = kShort ? short16<T>(x + (int64_t)(at + i * kLanes) * 16, left(at + i * kLanes)) : raw16(x + (int64_t)(at + i * kLanes) * 16, left(at + i * kLanes));
         uint32_t seen = 0;
 #pragma unroll
-        for (int i = 0; i < kKeep; ++i)
-            if (at + i * kLanes < loads) seen = row_look<T>(keep[i], seen);
+        for (int i = 0; i < kKeep; ++i) {
+            if constexpr (!kShort) keep[i] = cut16(keep[i], left(at + i * kLanes));
+            seen = row_look<T>(keep[i], seen);
+        }
         for (int32_t i = at + kKeep * kLanes; i < loads; i += kLanes) seen = row_look<T>(get(i), seen);
         float top = row_top_of<(kLanes < kWave ? kLanes : kWave)>(row_top<T>(seen));
         if constexpr (kLanes > kWave) {
@@ -75,9 +72,10 @@ int quantize_launch(const T *X, int64_t x_stride, int8_t *Q, int64_t q_stride, f
         return (uint32_t)(b < (1 << 20) ? b : 1 << 20);
     };
     // as many lanes as a row has loads, up to the workgroup's
-    if (loads <= 32) quantize_kernel<T, 16, 2><<<blocks(16), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
-    else if (loads <= 256) quantize_kernel<T, 64, 4><<<blocks(4), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
-    else quantize_kernel<T, 256, 4><<<blocks(1), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
+    if (K * sizeof(T) < 16) quantize_kernel<T, 16, 1, true><<<blocks(16), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
+    else if (loads <= 32) quantize_kernel<T, 16, 2, false><<<blocks(16), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
+    else if (loads <= 256) quantize_kernel<T, 64, 4, false><<<blocks(4), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
+    else quantize_kernel<T, 256, 4, false><<<blocks(1), kBlock, 0, stream>>>(X, x_stride, Q, q_stride, scale, n, K);
     return (int)hipGetLastError();
 }
 

@@ -198,9 +198,7 @@ __device__ __forceinline__ float row_top_of(float top)
 
 __device__ __forceinline__ float row_scale(float top) { return __builtin_isfinite(top) ? top * (1.f / 127.f) : __builtin_nanf(""); }
 
-// The codes of a load: x / scale, halves to even; zeros where the scale is zero or NaN.  x times the reciprocal is within 2^-15 of the
-// quotient, so it rounds to the same integer unless it lies that near to a half; then, and for scales whose reciprocal is
-// inexact or infinite, the quotient itself is computed.
+// The codes of a load: x / scale, halves to even; zeros where the scale is zero or NaN.
 template <typename X>
 __device__ __forceinline__ void row_codes(v4i v, float scale, int8_t *to)
 {
@@ -208,15 +206,11 @@ __device__ __forceinline__ void row_codes(v4i v, float scale, int8_t *to)
     constexpr float kRound = 12582912.f;                     // 1.5 * 2^23: what is added to it is rounded to an integer
     const RowValues<X> e = row_values<X>(v);
     uint32_t q[kPer];
-    bool near = !(scale > 0x1p-100f);
-    const float r = 1.f / scale;
+    if (scale > 0x1p-96f) {                                  // the same for a row
+        const float r = 1.f / scale;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        const float t = e.x[k] * r, whole = t + kRound, off = t - (whole - kRound);
-        q[k] = __float_as_uint(whole);
-        near = near || __builtin_fabsf(off) > 0.5f - 0x1p-14f;
-    }
-    if (near) {
+        for (int k = 0; k < kPer; ++k) q[k] = __float_as_uint(quotient(e.x[k], scale, r) + kRound);
+    } else {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) q[k] = scale > 0.f ? (uint32_t)(int)fminf(fmaxf(rintf(e.x[k] / scale), -127.f), 127.f) : 0u;
     }
