@@ -138,8 +138,7 @@ __device__ __forceinline__ v4i load16(const char *p, int64_t valid, bool short_r
 }
 
 // Rows cut to 8 bits: the 16 bytes of a load as floats, their largest magnitude, the scale of a row, its codes.  (A wavefront's
-// instruction takes four cycles: at 25 instructions a value, with a division each, cutting 8192 x 4096 values was bound by them, 38 us
-// in place of the 16 that the bytes take.)
+// instruction takes four cycles: 25 a value, with a division each, bound cutting 8192 x 4096 values at 38 us where the bytes take 16.)
 template <typename X>
 struct RowValues {
     float x[16 / sizeof(X)];
