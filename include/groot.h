@@ -6,7 +6,9 @@
  * the EDA-graph adjacency built from an And-Inverter Graph, the split of its
  * rows into a high-degree and a low-degree class, the two kernels that
  * multiply the adjacency with the node-feature matrix, and the partition of a
- * large graph into sub-graphs whose boundary edges are re-grown.
+ * large graph into sub-graphs whose boundary edges are re-grown.  Beside it
+ * stands the dense half of a network on such graphs: products grouped by node
+ * type with their gradients, products in 8-bit integers, the AdamW step.
  *
  * Conventions
  *   - Every call returns a groot_status and never throws or aborts; on failure

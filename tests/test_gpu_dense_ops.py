@@ -239,7 +239,8 @@ def test_offsets_that_do_not_ascend_stay_in_bounds():
 
 # sizes at which the larger tiles and the kernels for many columns and few rows are taken: (sizes of the groups, K, N)
 LARGE = [([8192], 72, 4096), ([4000, 100, 60], 136, 2100), ([2048], 264, 2048), ([900], 200, 1100), ([256], 640, 4096), ([33] * 8, 1024, 640),
-         ([300], 3600, 3600), ([700] * 16, 520, 1032), ([1] * 20, 640, 2048), ([9, 16, 2], 1000, 2052), ([7], 300, 5000), ([20000], 64, 96)]
+         ([300], 3600, 3600), ([700] * 16, 520, 1032), ([1] * 20, 640, 2048), ([9, 16, 2], 1000, 2052), ([7], 300, 5000), ([20000], 64, 96),
+         ([5, 11], 77, 131), ([2], 1001, 515), ([16], 33, 6), ([1, 0, 3], 5, 9), ([70, 300], 3, 70), ([600], 1003, 258)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
