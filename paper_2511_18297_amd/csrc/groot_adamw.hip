@@ -233,13 +233,10 @@ __global__ __launch_bounds__(kBlock) void adamw_kernel(const AdamwBatch b)
     const uint32_t before = which ? b.t[which - 1].chunks_to & ~kUnaligned : 0;
     const bool scaled = b.grad_scale != nullptr;
     const float gs = scaled ? *b.grad_scale : 1.f;
-    const int64_t from = (int64_t)(chunk - before) * kAdamwChunk;
-    if (!(t.chunks_to & kUnaligned) && from + kAdamwChunk <= t.n) {
-        adamw_values<P, G, kMaster, kBits, true>(t, b.f, gs, scaled, from + threadIdx.x * kAdamwPerLane);
-        return;
-    }
-    const int64_t wave = from + threadIdx.x / kWave * kAdamwBlock;              // the same for the whole wavefront
-    if (wave < t.n) adamw_values<P, G, kMaster, kBits, false>(t, b.f, gs, scaled, wave + lane * kAdamwPerLane);
+    const int64_t wave = (int64_t)(chunk - before) * kAdamwChunk + threadIdx.x / kWave * kAdamwBlock;   // the same for the whole wavefront
+    if (wave >= t.n) return;
+    if (!(t.chunks_to & kUnaligned) && wave + kAdamwBlock <= t.n) adamw_values<P, G, kMaster, kBits, true>(t, b.f, gs, scaled, wave + lane * kAdamwPerLane);
+    else adamw_values<P, G, kMaster, kBits, false>(t, b.f, gs, scaled, wave + lane * kAdamwPerLane);
 }
 
 template <typename P, typename G, bool kMaster>
