@@ -14,6 +14,12 @@ namespace {
 constexpr int kFewRows = 16, kFewCols = 16, kFewWaves = 8, kFewThreads = kFewWaves * kWave, kAhead = 4;
 constexpr int kFusedRows = 4, kFusedBytes = 48 * 1024;       // rows that are cut inside, their bytes in LDS
 
+constexpr int32_t few_tiles(int32_t N, int cols) { return (N + cols - 1) / cols; }
+int64_t few_workgroups(const RowsProduct &p, int cols)
+{
+    return ((p.n + kFewRows - 1) / kFewRows + (p.offsets ? p.groups : 0)) * few_tiles(p.N, cols);
+}
+
 template <typename T>
 struct FewType;
 template <>
@@ -186,8 +192,8 @@ int few_launch(const RowsProduct &p, void *stream)
     constexpr bool kFused = !std::is_same<X, T>::value;
     const int64_t b = sizeof(T);
     const bool aligned = (((uintptr_t)p.B | (uintptr_t)(p.K * b)) & 15) == 0 && (kFused || (((uintptr_t)p.A | (uintptr_t)(p.a_stride * b)) & 15) == 0);
-    const int32_t col_tiles = (p.N + kFewCols - 1) / kFewCols;
-    const int64_t workgroups = ((p.n + kFewRows - 1) / kFewRows + (p.offsets ? p.groups : 0)) * col_tiles;
+    const int32_t col_tiles = few_tiles(p.N, kFewCols);
+    const int64_t workgroups = few_workgroups(p, kFewCols);
     if (!fits_launch(workgroups, kFewThreads)) return kErrTooManyTiles;
     const size_t lds = kFused ? (size_t)p.n * ((p.K + 127) / 128 * 128) : 0;
     if (aligned) few_kernel<T, O, X, true><<<(uint32_t)workgroups, kFewThreads, lds, (hipStream_t)stream>>>(p, col_tiles);
@@ -297,8 +303,8 @@ __global__ __launch_bounds__(kFewThreads) void few_across_kernel(const RowsProdu
 template <typename T>
 int few_across_launch(const RowsProduct &p, void *stream)
 {
-    const int32_t col_tiles = (p.N + kAcrossCols - 1) / kAcrossCols;
-    const int64_t workgroups = ((p.n + kFewRows - 1) / kFewRows + (p.offsets ? p.groups : 0)) * col_tiles;
+    const int32_t col_tiles = few_tiles(p.N, kAcrossCols);
+    const int64_t workgroups = few_workgroups(p, kAcrossCols);
     if (!fits_launch(workgroups, kFewThreads)) return kErrTooManyTiles;
     few_across_kernel<T><<<(uint32_t)workgroups, kFewThreads, 0, (hipStream_t)stream>>>(p, col_tiles);
     return (int)hipGetLastError();
@@ -308,11 +314,11 @@ int few_across_launch(const RowsProduct &p, void *stream)
 
 // Groups of at most 16 rows on average.  Forward products of up to 512 workgroups: above, the tiles' longer pieces of the weights' rows
 // bring more than the wavefronts' shares (one row, 4096 x 4096: 12.1 us here, 19.3 in tiles; 15 groups of 2560 x 2176: 35 and 40; 32 of
-// 2048 x 2048: 53 and 48.5).
+// 2048 x 2048: 53 and 48.5).  Weights along the contraction: up to what a launch holds, 2^23 workgroups; tiles take fewer.
 bool few_rows_serve(const RowsProduct &p)
 {
     if (p.n > (int64_t)kFewRows * p.groups) return false;
-    return p.b_n_major || (p.N >= 4 && (int64_t)p.groups * ((p.N + kAcrossCols - 1) / kAcrossCols) <= 512);
+    return p.b_n_major ? fits_launch(few_workgroups(p, kFewCols), kFewThreads) : p.N >= 4 && (int64_t)p.groups * few_tiles(p.N, kAcrossCols) <= 512;
 }
 
 int launch_few_rows(int32_t dtype, const RowsProduct &p, void *stream)
@@ -332,7 +338,10 @@ int launch_few_int8(int32_t out_dtype, const RowsProduct &p, void *stream)
 }
 
 // Rows in floating point, all of them in every workgroup; of 16 bytes at least.
-bool few_linear_serves(const RowsProduct &p) { return p.n <= kFusedRows && p.K >= 8 && p.n * ((p.K + 127) / 128 * 128) <= kFusedBytes; }
+bool few_linear_serves(const RowsProduct &p)
+{
+    return p.n <= kFusedRows && p.K >= 8 && p.n * ((p.K + 127) / 128 * 128) <= kFusedBytes && fits_launch(few_workgroups(p, kFewCols), kFewThreads);
+}
 
 int launch_few_linear(int32_t dtype, const RowsProduct &p, void *stream)
 {

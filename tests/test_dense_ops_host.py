@@ -104,6 +104,14 @@ def test_too_many_tiles():
     assert weights(E=65536, K=65536, N=65536, xs=65536, dys=65536, n=0, dW=1 << 52, db=1 << 56, ws=1 << 58, wb=1 << 40) == G.GROOT_ERANGE
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls pass the checks, and their addresses are not memory")
+def test_few_rows_of_many_groups_are_not_refused():
+    """more workgroups than a launch holds where few rows would go by themselves; the tiles hold them"""
+    assert data(n=16384, E=1024, K=65536, N=16, dys=16, dxs=65536, dX=1 << 44, W=1 << 45) != G.GROOT_ERANGE
+    assert product(n=32768, E=2048, K=16, N=32768, qs=16, ys=32768, Y=1 << 44, W=1 << 45) != G.GROOT_ERANGE
+    assert linear(n=1, E=2048, K=8, N=65536, xs=8, ys=65536, Y=1 << 44, W=1 << 45, w=1 << 46, bias=None) != G.GROOT_ERANGE
+
+
 def test_nothing_to_do():
     assert grouped(n=0) == data(n=0) == product(n=0) == linear(n=0) == quantize(n=0) == G.GROOT_OK
 

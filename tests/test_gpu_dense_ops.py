@@ -287,6 +287,39 @@ def test_quantized_product_large_sizes(case):
     close(Y, want, 4 * 2.0 ** -24 * want.abs(), "Y")
 
 
+def test_few_rows_of_many_groups_and_columns():
+    """more workgroups than a launch holds, were few rows taken by themselves; small integers, whose sums are exact"""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(12)
+
+    def small(*shape, dtype):
+        return torch.randint(-2, 3, shape, generator=gen, device="cuda", dtype=torch.int8).to(dtype)
+    n, E, K, N = 16384, 1024, 65536, 16
+    dY, W, offsets = small(n, N, dtype=torch.bfloat16), small(E, K, N, dtype=torch.bfloat16), offsets_of([16] * E)
+    dX = out_matrix(n, K, torch.bfloat16)
+    G.groot_grouped_product_backward_data(dY, W, offsets, dX)
+    for g in range(0, E, 93):
+        assert torch.equal(dX[16 * g:16 * g + 16].float(), dY[16 * g:16 * g + 16].float() @ W[g].float().t().contiguous()), g
+    assert torch.isfinite(dX).all()
+    del dY, W, dX
+    n, E, K, N = 32768, 2048, 16, 32768
+    Q, W, ones, scales = small(n, K, dtype=torch.int8), small(E, N, K, dtype=torch.int8), torch.ones(n, device="cuda"), torch.ones((E, N), device="cuda")
+    Y = out_matrix(n, N, torch.bfloat16)
+    G.groot_quantized_product(Q, ones, W, scales, offsets_of([16] * E), None, False, Y)
+    for g in range(0, E, 178):
+        assert torch.equal(Y[16 * g:16 * g + 16].float(), Q[16 * g:16 * g + 16].float() @ W[g].float().t().contiguous()), g
+    assert torch.isfinite(Y).all()
+    del Q, W, Y, scales
+    E, K, N = 2048, 8, 65536
+    X, W, scales = small(1, K, dtype=torch.float32), small(E, N, K, dtype=torch.int8), torch.ones((E, N), device="cuda")
+    X[0, 0] = 2.0
+    Y, work = out_matrix(1, N, torch.float32), torch.empty(G.groot_quantized_linear_workspace(1, K), dtype=torch.uint8, device="cuda")
+    G.groot_quantized_linear(X, W, scales, offsets_of([0] * 1500 + [1] + [0] * (E - 1501)), None, False, Y, work)
+    q, top = quantized(X)
+    want = (q.double() @ W[1500].double().t()) * top.double()[:, None]
+    close(Y, want, 4 * 2.0 ** -24 * want.abs(), "Y")
+
+
 @pytest.mark.parametrize("kind", TYPES)
 def test_no_rows_at_all(kind):
     dtype = TYPES[kind]
