@@ -781,12 +781,13 @@ class AdamwTensors:
         self._kept[name] = tensors
 
     def set_grads(self, grads):
-        """One gradient for every parameter, of one floating type."""
+        """One gradient for every parameter, of one floating type.  Where it raises, the gradients stay those of before."""
         grads = list(grads)
         if len(grads) != self.count:
             raise ValueError("the lists must have one tensor for every parameter")
-        self.grad_dtype = _dtype(grads[0], "grads") if grads else GROOT_F32
+        dtype = _dtype(grads[0], "grads") if grads else GROOT_F32
         self._column(1, "grads", grads, grads[0].dtype if grads else None, self._counts)
+        self.grad_dtype = dtype
 
 
 def groot_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, master=None) -> AdamwTensors:

@@ -171,3 +171,28 @@ def test_binding_refuses_what_the_library_cannot_see():
         G.groot_adamw_tensors([x], [x], [x], [x], m_scale=[x])
     with pytest.raises(TypeError):
         G.groot_adamw_tensors([x], [x], [x], [x])
+
+
+class OnDevice(torch.Tensor):
+    """a tensor in host memory that calls itself one on the device: for checks that end before anything reads it"""
+    is_cuda = True
+
+
+def on_device(*shape, dtype=torch.float32):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnDevice)
+
+
+def test_refused_gradients_leave_the_descriptors_as_they_were():
+    params, grads, m, v = ([on_device(300), on_device(20)] for _ in range(4))
+    t = G.groot_adamw_tensors(params, grads, m, v)
+    before = t.array.copy()
+    bf16 = torch.bfloat16
+    for bad, error in (([on_device(300, dtype=bf16), on_device(21, dtype=bf16)], ValueError), ([on_device(300, dtype=bf16), on_device(20)], TypeError),
+                       ([on_device(300, dtype=bf16), torch.zeros(20, dtype=bf16)], TypeError), ([on_device(300, dtype=bf16)], ValueError)):
+        with pytest.raises(error):
+            t.set_grads(bad)
+        assert t.grad_dtype == G.GROOT_F32 and (t.array == before).all()
+    good = [on_device(300, dtype=bf16), on_device(20, dtype=bf16)]
+    t.set_grads(good)
+    assert t.grad_dtype == G.GROOT_BF16 and t.array[:, 1].tolist() == [g.data_ptr() for g in good]
+    assert (t.array[:, [0, 2, 3, 4, 5, 6, 7]] == before[:, [0, 2, 3, 4, 5, 6, 7]]).all()
