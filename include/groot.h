@@ -610,8 +610,9 @@ groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_
  * nothing; the descriptors travel as kernel arguments, so the call may be
  * captured in a HIP graph, with the host values it was given.
  * Errors: EINVAL (NULL, unknown dtype, n < 0, state_bits, step < 1, lr or
- * weight_decay not finite or negative, beta outside [0, 1), eps not finite or <= 0), ERANGE (a tensor of
- * 2^33 values or more), EHIP.
+ * weight_decay not finite or negative, beta outside [0, 1), eps not finite or <= 0; the same of what is left of
+ * eps, lr / (1 - beta1^step) and 1 - lr weight_decay in fp32: not finite, or an eps of 0), ERANGE (a tensor of 2^33
+ * values or more), EHIP.
  * ------------------------------------------------------------------------- */
 typedef struct {
     void *param;

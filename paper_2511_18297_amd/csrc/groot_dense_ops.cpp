@@ -253,8 +253,19 @@ extern "C" groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int6
     if (step < 1) return bad(who, "step counts from 1");
     if (!(std::isfinite(lr) && lr >= 0) || !(std::isfinite(weight_decay) && weight_decay >= 0)) return bad(who, "lr and weight_decay must be finite and not negative");
     if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1)) return bad(who, "beta1 and beta2 must be in [0, 1)");
-    if (!(std::isfinite(eps) && eps > 0)) return bad(who, "eps must be finite and positive");
     if (!aligned(grad_scale_dev, 4)) return bad(who, "grad_scale is not aligned to its type");
+    AdamwFactors f;
+    f.decay = (float)(1.0 - lr * weight_decay);
+    f.step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+    f.beta1 = (float)beta1;
+    f.one_minus_beta1 = (float)(1.0 - beta1);
+    f.beta2 = (float)beta2;
+    f.one_minus_beta2 = (float)(1.0 - beta2);
+    f.root_factor = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    f.eps = (float)eps;
+    // the factors that the kernel goes by: a denominator of 0 + 0, or 0 x infinity, would be NaN for values that nothing moves
+    if (!(std::isfinite(f.eps) && f.eps > 0)) return bad(who, "eps must be finite and positive in fp32");
+    if (!std::isfinite(f.step_size) || !std::isfinite(f.decay)) return bad(who, "lr / (1 - beta1^step) and 1 - lr weight_decay must be finite in fp32");
     const int sb = state_bits == 8 ? 1 : 4;
     bool master = false, first = true;
     for (int64_t t = 0; t < n_tensors; ++t) {
@@ -272,15 +283,6 @@ extern "C" groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int6
         first = false;
     }
     if (first) return GROOT_OK;
-    AdamwFactors f;
-    f.decay = (float)(1.0 - lr * weight_decay);
-    f.step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-    f.beta1 = (float)beta1;
-    f.one_minus_beta1 = (float)(1.0 - beta1);
-    f.beta2 = (float)beta2;
-    f.one_minus_beta2 = (float)(1.0 - beta2);
-    f.root_factor = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
-    f.eps = (float)eps;
     return launched(who, launch_adamw(tensors, n_tensors, param_dtype, grad_dtype, state_bits, f, grad_scale_dev, (uint32_t)step, seed,
                                       hip_stream));
 }

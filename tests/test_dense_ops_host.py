@@ -155,6 +155,16 @@ def test_adamw_refused():
     assert L.groot_adamw_step(None, 2, 0, 0, 32, 1, 1e-3, 0.9, 0.99, 1e-8, 0.0, None, 0, None) == G.GROOT_EINVAL
 
 
+def test_adamw_refuses_factors_that_fp32_cannot_hold():
+    """the kernel computes in fp32: an eps that is 0 there divides 0 by 0, a step of infinity multiplies 0 by it"""
+    for change in (dict(eps=1e-60), dict(eps=1e-320), dict(eps=7e-46), dict(eps=1e39), dict(lr=1e300), dict(lr=4e38), dict(lr=1e37, b1=0.99),
+                   dict(lr=1e20, wd=1e300), dict(lr=1e200, wd=1e200)):
+        assert adamw(n=0, **change) == G.GROOT_EINVAL, change
+        assert adamw(n=0, bits=8, **change) == G.GROOT_EINVAL, change
+    for change in (dict(eps=1e-39), dict(eps=1.5e-45), dict(eps=3e38), dict(lr=1e37), dict(lr=0.0, wd=0.0), dict(lr=1e37, wd=10.0)):
+        assert adamw(n=0, **change) == G.GROOT_OK, change
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     x, w, y = torch.zeros(4, 8), torch.zeros(1, 8, 8), torch.zeros(4, 8)
     with pytest.raises(TypeError):
