@@ -580,9 +580,10 @@ groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_
  * the paper: the optimizer behind the layers' gradient calls.  For every value
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
  *   w <- w (1 - lr weight_decay)
- *        - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in fp32 (the factors of lr, beta and step are computed in fp64 and rounded
- * once), every operation rounded by itself in the order written.
+ *        - lr / (1 - beta1^step) * (m / (sqrt(v) * (1 / sqrt(1 - beta2^step)) + eps))
+ * in fp32, with states of 32 bits as with those of 8: every operation on a value
+ * is rounded by itself in the order written, the factors of lr, beta, step and
+ * weight_decay are computed in fp64 and rounded once.
  * tensors (host, read during the call): device pointers, n values each.
  *   w is `param` (param_dtype), or with `master` not NULL the fp32 master, of
  *   which param becomes the rounded copy; either all tensors of a call have a

@@ -97,13 +97,29 @@ __device__ __forceinline__ v4f load_codes(const uint8_t *p, float scale, int lef
     return r;
 }
 
-// Four square roots, rounded to nearest (but for one in some millions, a last place off), as quotient() has quotients.  (Where a value takes 16
-// bytes, the ones of the mathematical library bound the kernel: 115 instructions a value in all.)
-__device__ __forceinline__ v4f roots(v4f v)
+// Square roots and quotients of 8-bit states, rounded as the mathematical library's and the division's, from three and six instructions
+// each where all values of the wavefront are of an ordinary size.  (Where a value takes 16 bytes, the library's bound the kernel: 115
+// instructions a value in all.)  The instructions behind them were compared with fp64, rounded, for every value of their ranges: a
+// reciprocal is off in a ninth of the cases by itself and in none with one step of Newton's, a root with its remainder in none.
+// ordinary: |m| in (2^-80, 2^60), v in (2^-96, 2^32), none of them NaN, in the whole wavefront
+__device__ __forceinline__ bool ordinary(v4f m, v4f v)
 {
-    const float low = fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), high = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+    float least = __builtin_fabsf(m[0]), most = least, low = v[0], high = low;
+#pragma unroll
+    for (int k = 1; k < 4; ++k) {
+        const float a = __builtin_fabsf(m[k]);
+        least = fminf(least, a);
+        most = __builtin_elementwise_maximum(most, a);       // NaN if one of them is
+        low = fminf(low, v[k]);
+        high = __builtin_elementwise_maximum(high, v[k]);
+    }
+    return __all(low > 0x1p-96f && high < 0x1p32f && least > 0x1p-80f && most < 0x1p60f);
+}
+
+__device__ __forceinline__ v4f roots(v4f v, bool usual)
+{
     v4f r;
-    if (__all(low > 0x1p-96f && high < 0x1p96f && __builtin_isfinite((v[0] + v[1]) + (v[2] + v[3])))) {
+    if (usual) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float y = __builtin_amdgcn_rsqf(v[k]), g = v[k] * y;
@@ -116,17 +132,40 @@ __device__ __forceinline__ v4f roots(v4f v)
     return r;
 }
 
+// m / d for d of 2^-64 to 2^80 where `usual`
+__device__ __forceinline__ v4f quotients(v4f m, v4f d, bool usual)
+{
+    v4f q;
+    if (usual) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float r = __builtin_amdgcn_rcpf(d[k]);
+            q[k] = quotient(m[k], d[k], __builtin_fmaf(__builtin_fmaf(-d[k], r, 1.f), r, r));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = m[k] / d[k];
+    }
+    return q;
+}
+
 // Codes and scale of the wavefront's 256 values: the scale takes the largest finite magnitude to the largest code.  The instruction
 // adds its random number's upper 20 bits behind the three that a code keeps and cuts the rest off (below 2^-6: behind steps of 2^-9).
 // `never0`: a positive value is held as the smallest code at least (a root of 0 beside a first moment above 0 is a step of m / eps).
+// `usual`: the values are known to be finite.
 template <bool kWhole>
-__device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, const uint32_t (&random)[4], bool never0, int left)
+__device__ __forceinline__ void store_codes(uint8_t *p, float *scale_at, v4f x, const uint32_t (&random)[4], bool never0, int left, bool usual)
 {
-    float top = 0.f;
     // one look at four values: their sum is not finite if one of them is not
-    const bool finite = __all(__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])));
+    const bool finite = usual || __all(__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])));
+    float top = 0.f;                                         // values that do not exist are zeros
+    if (finite) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, finite || __builtin_isfinite(x[k]) ? __builtin_fabsf(x[k]) : 0.f);   // values that do not exist are zeros
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, __builtin_fabsf(x[k]));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, __builtin_isfinite(x[k]) ? __builtin_fabsf(x[k]) : 0.f);
+    }
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
     const float scale = top * (1.f / kCodeTop);
@@ -189,19 +228,25 @@ __device__ __forceinline__ void adamw_values(const AdamwTensor &t, const AdamwFa
         m[k] = m[k] * f.beta1 + gk * f.one_minus_beta1;
         v[k] = v[k] * f.beta2 + (gk * gk) * f.one_minus_beta2;
     }
-    v4f root;
+    v4f root, denom, step;
+    bool usual = false;
     if (kBits == 8) {
-        root = roots(v);
+        usual = ordinary(m, v);
+        root = roots(v, usual);
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) root[k] = sqrtf(v[k]);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        // 8 bits: the step's quotient within two last places, far below what the codes leave of m
-        const float denom = root[k] * f.root_factor + f.eps;
-        w[k] = w[k] * f.decay - f.step_size * (kBits == 8 ? m[k] * __builtin_amdgcn_rcpf(denom) : m[k] / denom);
+    for (int k = 0; k < 4; ++k) denom[k] = root[k] * f.root_factor + f.eps;
+    if (kBits == 8) {
+        step = quotients(m, denom, usual && f.eps > 0x1p-60f && f.eps < 0x1p36f && f.root_factor < 0x1p30f);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) step[k] = m[k] / denom[k];
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = w[k] * f.decay - f.step_size * step[k];
     if (kMaster) store4<float, kWhole>(master, w, left);
     store4<P, kWhole>(param, w, left);
     if (kBits == 8) {
@@ -213,8 +258,8 @@ __device__ __forceinline__ void adamw_values(const AdamwTensor &t, const AdamwFa
             low[k] = h << 16;
             high[k] = h & 0xFFFF0000u;
         }
-        store_codes<kWhole>((uint8_t *)t.m + at, t.m_scale + block, m, low, false, left);
-        store_codes<kWhole>((uint8_t *)t.v + at, t.v_scale + block, root, high, true, left);
+        store_codes<kWhole>((uint8_t *)t.m + at, t.m_scale + block, m, low, false, left, usual);
+        store_codes<kWhole>((uint8_t *)t.v + at, t.v_scale + block, root, high, true, left, usual);
     } else {
         store4<float, kWhole>((float *)t.m + at, m, left);
         store4<float, kWhole>((float *)t.v + at, v, left);

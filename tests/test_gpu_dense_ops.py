@@ -574,6 +574,56 @@ def test_adamw(bits, param, grad, master, shift):
         adamw_check(s, old, step, seed=77)
 
 
+def adamw_fp32(s, step, lr, b1, b2, eps, wd):
+    """the new weights, every operation in fp32 by itself, on the CPU, in the order that the call states"""
+    cut = lambda x: torch.tensor(np.float32(x))  # noqa: E731
+    out = []
+    for i, g in enumerate(s["g"]):
+        g, n = g.cpu().float(), g.numel()
+        m, v = (s[k][i].cpu().float() for k in ("m", "v"))
+        if "m_scale" in s:
+            m, v = (x * s[k][i].cpu().repeat_interleave(256)[:n] for x, k in ((m, "m_scale"), (v, "v_scale")))
+            v = v * v
+        m = m * cut(b1) + g * cut(1 - b1)
+        v = v * cut(b2) + (g * g) * cut(1 - b2)
+        root = v.double().sqrt().float()                     # rounded once (the CPU's own root of fp32 tensors is off by a place here and there)
+        denom = root * cut(1 / math.sqrt(1 - b2 ** step)) + cut(eps)
+        w = (s["p"] if s["master"] is None else s["master"])[i].cpu().float()
+        out.append(w * cut(1 - lr * wd) - cut(lr / (1 - b1 ** step)) * (m / denom))
+    return out
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param, grad, master", [("f32", "f32", False), ("bf16", "bf16", True)])
+@pytest.mark.parametrize("weights", [0.0, 1.0])
+def test_adamw_rounds_every_operation_by_itself(bits, param, grad, master, weights):
+    """bit for bit: in 8 bits as in 32, and where values lie outside the range of the short divisions"""
+    for eps, spread in ((1e-8, 1.0), (1e-39, 1.0), (1e-8, 1e-18), (1e-3, 1e12)):
+        s = adamw_case([400000, 1001], TYPES[param], TYPES[grad], bits, master, 21)
+        for k in ("p", "master"):
+            for t in s[k] or []:
+                t.mul_(weights)
+        for t in s["g"]:
+            t.mul_(spread)
+        if bits == 8:
+            for t in s["m_scale"] + s["v_scale"]:
+                t.mul_(spread)
+        for k, power in (("m", 1), ("v", 2)):
+            if bits == 32:
+                for t in s[k]:
+                    t.mul_(spread ** power)
+        s["g"][1][:600] = 0                                  # two blocks that hold nothing, and one in part
+        s["m"][1][:600] = torch.zeros(600, device="cuda").to(s["m"][1].dtype)
+        s["v"][1][:600] = torch.zeros(600, device="cuda").to(s["v"][1].dtype)
+        want = adamw_fp32(s, 3, LR, B1, B2, eps, WD)
+        more = {k: s[k] for k in ("m_scale", "v_scale") if k in s}
+        G.groot_adamw_step(G.groot_adamw_tensors(s["p"], s["g"], s["m"], s["v"], master=s["master"], **more), 3, LR, B1, B2, eps, WD, seed=4)
+        for i, w in enumerate(want):
+            got = (s["p"] if s["master"] is None else s["master"])[i].cpu()
+            assert torch.isfinite(got).all()
+            assert torch.equal(got, w), (eps, spread, i, int((got != w).sum()), w.numel())
+
+
 def test_adamw_gradient_scale_and_repeats():
     for bits in (32, 8):
         s = adamw_case([1000, 300], torch.float32, torch.float32, bits, False, 3)
