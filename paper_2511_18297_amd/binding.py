@@ -740,8 +740,10 @@ class _AdamwTensor(ctypes.Structure):
 
 
 class AdamwTensors:
-    """The descriptors of groot_adamw_step for one list of tensors, checked once; keeps the tensors alive.  Gradients that move
-    from step to step: set_grads."""
+    """The descriptors of groot_adamw_step for one list of tensors, checked once.  They hold addresses, and keep the memory behind them: a tensor that is given other memory afterwards
+    (`p.data = ...`, `module.to(...)`, a gradient that autograd makes anew) is not followed.  Gradients that move from step to
+    step: set_grads.  Parameters or states that move: new descriptors.  A step looks at one tensor, each in its turn, and raises
+    RuntimeError where it has moved; storages must not be resized."""
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, master=None):
         params, grads, m, v, m_scale, v_scale, master = (None if x is None else list(x) for x in (params, grads, m, v, m_scale, v_scale, master))
@@ -757,19 +759,24 @@ class AdamwTensors:
         # one row of eight 64-bit words for every tensor: the layout of _AdamwTensor
         self.array = np.zeros((max(self.count, 1), 8), dtype=np.int64)
         self.address = self.array.ctypes.data
-        self._counts, self._kept = counts, {}
-        self._column(0, "params", params, params[0].dtype if params else None, counts)
-        self.set_grads(grads)
-        self._column(2, "m", m, state, counts)
-        self._column(3, "v", v, state, counts)
+        self._counts, self._memory = counts, {}
+        # what is written: name, place in a row, tensors, type, sizes
+        written = [("params", 0, params, params[0].dtype if params else None, counts), ("m", 2, m, state, counts), ("v", 3, v, state, counts)]
         if m_scale is not None:
-            self._column(4, "m_scale", m_scale, torch.float32, blocks)
-            self._column(5, "v_scale", v_scale, torch.float32, blocks)
+            written += [("m_scale", 4, m_scale, torch.float32, blocks), ("v_scale", 5, v_scale, torch.float32, blocks)]
         if master is not None:
-            self._column(6, "master", master, torch.float32, counts)
+            written.append(("master", 6, master, torch.float32, counts))
+        for name, at, tensors, dtype, sizes in written:
+            self._addresses(name, tensors, dtype, sizes)
+        self._turn, self._looks = 0, [None] * self.count
+        self.set_grads(grads)
+        for name, at, tensors, dtype, sizes in written:
+            self._take(at, name, tensors)
+            self._looks += zip(tensors, self.array[:, at].tolist())
         self.array[:self.count, 7] = counts
 
-    def _column(self, at, name, tensors, dtype, counts):
+    @staticmethod
+    def _addresses(name, tensors, dtype, counts):
         for i, (t, n) in enumerate(zip(tensors, counts)):
             if not isinstance(t, _Tensor) or not t.is_cuda or not t.is_contiguous():
                 raise TypeError(f"{name}[{i}] must be a contiguous CUDA tensor")
@@ -777,8 +784,11 @@ class AdamwTensors:
                 raise TypeError(f"{name}[{i}] must be {dtype}")
             if t.numel() != n:
                 raise ValueError(f"{name}[{i}] holds {t.numel()} elements, {n} are needed")
+        return [t.data_ptr() for t in tensors]
+
+    def _take(self, at, name, tensors):
         self.array[:self.count, at] = [t.data_ptr() for t in tensors]
-        self._kept[name] = tensors
+        self._memory[name] = [t.detach() for t in tensors]   # the memory stays, whatever becomes of the tensor
 
     def set_grads(self, grads):
         """One gradient for every parameter, of one floating type.  Where it raises, the gradients stay those of before."""
@@ -786,8 +796,16 @@ class AdamwTensors:
         if len(grads) != self.count:
             raise ValueError("the lists must have one tensor for every parameter")
         dtype = _dtype(grads[0], "grads") if grads else GROOT_F32
-        self._column(1, "grads", grads, grads[0].dtype if grads else None, self._counts)
+        addresses = self._addresses("grads", grads, grads[0].dtype if grads else None, self._counts)
+        self._take(1, "grads", grads)
+        self._looks[:self.count] = zip(grads, addresses)
         self.grad_dtype = dtype
+
+    def _look(self):
+        self._turn = turn = self._turn + 1 if self._turn + 1 < len(self._looks) else 0
+        tensor, address = self._looks[turn]
+        if tensor.data_ptr() != address:
+            raise RuntimeError("a tensor has moved since its descriptor was made (new descriptors, or set_grads, follow it)")
 
 
 def groot_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, master=None) -> AdamwTensors:
@@ -800,6 +818,8 @@ def groot_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, master=
 def groot_adamw_step(tensors: AdamwTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                      weight_decay: float = 0.01, grad_scale=None, seed: int = 0, stream=None) -> None:
     """One step, counted from 1.  grad_scale: a CUDA float32 tensor of one element that the gradients are multiplied by."""
+    if tensors.count:
+        tensors._look()
     gs = None
     if grad_scale is not None:
         if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:

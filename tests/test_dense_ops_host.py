@@ -3,6 +3,7 @@ import ctypes
 
 import pytest
 import torch
+from torch.multiprocessing.reductions import StorageWeakRef
 
 from util import ensure_built
 
@@ -206,3 +207,16 @@ def test_refused_gradients_leave_the_descriptors_as_they_were():
     t.set_grads(good)
     assert t.grad_dtype == G.GROOT_BF16 and t.array[:, 1].tolist() == [g.data_ptr() for g in good]
     assert (t.array[:, [0, 2, 3, 4, 5, 6, 7]] == before[:, [0, 2, 3, 4, 5, 6, 7]]).all()
+
+
+def test_descriptors_keep_the_memory_that_they_point_to():
+    lists = {k: [on_device(300), on_device(300)] for k in ("params", "grads", "m", "v", "master")}
+    t = G.groot_adamw_tensors(**lists)
+    storages = [StorageWeakRef(x.untyped_storage()) for tensors in lists.values() for x in tensors]
+    addresses = t.array.copy()
+    for tensors in lists.values():
+        for x in tensors:
+            x.data = torch.zeros(7)                          # as Module.to does with its parameters
+    assert not any(s.expired() for s in storages) and (t.array == addresses).all()
+    del t
+    assert all(s.expired() for s in storages)

@@ -624,6 +624,34 @@ def test_adamw_rounds_every_operation_by_itself(bits, param, grad, master, weigh
             assert torch.equal(got, w), (eps, spread, i, int((got != w).sum()), w.numel())
 
 
+def test_adamw_tensors_that_move():
+    def make():
+        return adamw_case([300, 20, 5000], torch.float32, torch.float32, 32, False, 5)
+
+    def tensors_of(s):
+        return G.groot_adamw_tensors(s["p"], s["g"], s["m"], s["v"])
+    for k in ("p", "g", "m", "v"):
+        s = make()
+        tensors = tensors_of(s)
+        for step in range(1, 30):
+            G.groot_adamw_step(tensors, step, LR)
+        s[k][1].data = s[k][1].clone()
+        with pytest.raises(RuntimeError, match="moved"):
+            for step in range(30, 60):
+                G.groot_adamw_step(tensors, step, LR)
+        old = clone(s)
+        G.groot_adamw_step(tensors_of(s), 7, LR, B1, B2, EPS, WD)
+        adamw_check(s, old, 7)
+    s, t = make(), make()
+    tensors = tensors_of(s)
+    s["g"] = t["g"] = [g * 0.5 for g in s["g"]]              # as autograd makes them anew
+    tensors.set_grads(s["g"])
+    for step in range(1, 30):
+        G.groot_adamw_step(tensors, step, LR)
+        G.groot_adamw_step(tensors_of(t), step, LR)
+    assert all(torch.equal(a, b) for k in ("p", "m", "v") for a, b in zip(s[k], t[k]))
+
+
 def test_adamw_gradient_scale_and_repeats():
     for bits in (32, 8):
         s = adamw_case([1000, 300], torch.float32, torch.float32, bits, False, 3)
