@@ -190,7 +190,7 @@ class OnDevice(torch.Tensor):
 
 
 def on_device(*shape, dtype=torch.float32):
-    return torch.zeros(shape, dtype=dtype).as_subclass(OnDevice)
+    return torch.Tensor._make_subclass(OnDevice, torch.zeros(shape, dtype=dtype))
 
 
 def test_refused_gradients_leave_the_descriptors_as_they_were():
