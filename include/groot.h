@@ -607,7 +607,9 @@ groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_
  *   code at least, never as 0.  A value that is not finite becomes NaN and
  *   leaves the others of its block alone.
  * Pointers are aligned to their type; tensors whose arrays all begin on 16 bytes
- * are read faster.  Launches one kernel per 48 tensors on hip_stream, allocates
+ * are read faster.  An array that is written (all but grad) must not overlap any
+ * other array of the call; that is the caller's to see to, since looking for it
+ * among all arrays takes longer than a small step does.  Launches one kernel per 48 tensors on hip_stream, allocates
  * nothing; the descriptors travel as kernel arguments, so the call may be
  * captured in a HIP graph, with the host values it was given.
  * Errors: EINVAL (NULL, unknown dtype, n < 0, state_bits, step < 1, lr or

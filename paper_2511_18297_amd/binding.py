@@ -740,7 +740,8 @@ class _AdamwTensor(ctypes.Structure):
 
 
 class AdamwTensors:
-    """The descriptors of groot_adamw_step for one list of tensors, checked once.  They hold addresses, and keep the memory behind them: a tensor that is given other memory afterwards
+    """The descriptors of groot_adamw_step for one list of tensors, checked once: types, sizes, and that no array that a step writes
+    overlaps another.  They hold addresses, and keep the memory behind them: a tensor that is given other memory afterwards
     (`p.data = ...`, `module.to(...)`, a gradient that autograd makes anew) is not followed.  Gradients that move from step to
     step: set_grads.  Parameters or states that move: new descriptors.  A step looks at one tensor, each in its turn, and raises
     RuntimeError where it has moved; storages must not be resized."""
@@ -766,13 +767,19 @@ class AdamwTensors:
             written += [("m_scale", 4, m_scale, torch.float32, blocks), ("v_scale", 5, v_scale, torch.float32, blocks)]
         if master is not None:
             written.append(("master", 6, master, torch.float32, counts))
-        for name, at, tensors, dtype, sizes in written:
-            self._addresses(name, tensors, dtype, sizes)
-        self._turn, self._looks = 0, [None] * self.count
+        addresses = [self._addresses(name, tensors, dtype, sizes) for name, _, tensors, dtype, sizes in written]
+        spans = [self._spans(a, w[2], w[4]) for a, w in zip(addresses, written)]
+        begin, end = (np.concatenate([s[k] for s in spans]) for k in (0, 1))
+        order = np.argsort(begin, kind="stable")
+        self._begin, self._end = begin[order], end[order]
+        if (self._end[:-1] > self._begin[1:]).any():
+            raise ValueError("two of the arrays that a step writes overlap")
+        self._turn, self._tensors, self._at = 0, [None] * self.count, [0] * self.count      # what a step looks at
         self.set_grads(grads)
-        for name, at, tensors, dtype, sizes in written:
-            self._take(at, name, tensors)
-            self._looks += zip(tensors, self.array[:, at].tolist())
+        for (_, at, tensors, _, _), a in zip(written, addresses):
+            self._take(at, tensors, a)
+            self._tensors += tensors
+            self._at += a
         self.array[:self.count, 7] = counts
 
     @staticmethod
@@ -786,9 +793,16 @@ class AdamwTensors:
                 raise ValueError(f"{name}[{i}] holds {t.numel()} elements, {n} are needed")
         return [t.data_ptr() for t in tensors]
 
-    def _take(self, at, name, tensors):
-        self.array[:self.count, at] = [t.data_ptr() for t in tensors]
-        self._memory[name] = [t.detach() for t in tensors]   # the memory stays, whatever becomes of the tensor
+    @staticmethod
+    def _spans(addresses, tensors, counts):
+        """First address and the one behind the last, of the tensors (of one type) that hold something."""
+        begin = np.array(addresses, dtype=np.int64)
+        end = begin + np.array(counts, dtype=np.int64) * (tensors[0].element_size() if tensors else 1)
+        return begin[end > begin], end[end > begin]
+
+    def _take(self, at, tensors, addresses):
+        self.array[:self.count, at] = addresses
+        self._memory[at] = [t.untyped_storage() for t in tensors]   # the memory stays, whatever becomes of the tensor
 
     def set_grads(self, grads):
         """One gradient for every parameter, of one floating type.  Where it raises, the gradients stay those of before."""
@@ -797,14 +811,18 @@ class AdamwTensors:
             raise ValueError("the lists must have one tensor for every parameter")
         dtype = _dtype(grads[0], "grads") if grads else GROOT_F32
         addresses = self._addresses("grads", grads, grads[0].dtype if grads else None, self._counts)
-        self._take(1, "grads", grads)
-        self._looks[:self.count] = zip(grads, addresses)
+        if self._begin.size:
+            begin, end = self._spans(addresses, grads, self._counts)
+            before = np.searchsorted(self._begin, end) - 1   # the last written array that begins before a gradient ends
+            if ((before >= 0) & (self._end[before] > begin)).any():
+                raise ValueError("a gradient overlaps an array that a step writes")
+        self._take(1, grads, addresses)
+        self._tensors[:self.count], self._at[:self.count] = grads, addresses
         self.grad_dtype = dtype
 
     def _look(self):
-        self._turn = turn = self._turn + 1 if self._turn + 1 < len(self._looks) else 0
-        tensor, address = self._looks[turn]
-        if tensor.data_ptr() != address:
+        self._turn = turn = self._turn + 1 if self._turn + 1 < len(self._at) else 0
+        if self._tensors[turn].data_ptr() != self._at[turn]:
             raise RuntimeError("a tensor has moved since its descriptor was made (new descriptors, or set_grads, follow it)")
 
 

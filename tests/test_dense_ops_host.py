@@ -220,3 +220,29 @@ def test_descriptors_keep_the_memory_that_they_point_to():
     assert not any(s.expired() for s in storages) and (t.array == addresses).all()
     del t
     assert all(s.expired() for s in storages)
+
+
+def test_arrays_that_overlap():
+    def make(**change):
+        lists = dict(params=[on_device(300), on_device(20)], grads=[on_device(300), on_device(20)], m=[on_device(300), on_device(20)],
+                     v=[on_device(300), on_device(20)])
+        lists.update(change)
+        return G.groot_adamw_tensors(**lists)
+    whole, once = on_device(1000), on_device(300)
+    bf16, codes = torch.bfloat16, torch.float8_e4m3fn
+    for change in (dict(params=[whole[:300], whole[280:300]]), dict(params=[whole[10:310], whole[:20]]), dict(params=[once, once[100:120]]),
+                   dict(m=[once, on_device(20)], v=[once, on_device(20)]), dict(params=[once, on_device(20)], master=[once, on_device(20)]),
+                   dict(params=[once, on_device(20)], grads=[once, on_device(20)]), dict(params=[on_device(300), once[:20]], grads=[once, on_device(20)]),
+                   dict(params=[on_device(300), once[299:300]], grads=[once, on_device(1)], m=[on_device(300), on_device(1)], v=[on_device(300), on_device(1)]),
+                   dict(m=[on_device(300, dtype=codes), on_device(20, dtype=codes)], v=[on_device(300, dtype=codes), on_device(20, dtype=codes)],
+                        m_scale=[once[:2], once[4:5]], v_scale=[once[2:4], once[4:5]])):
+        with pytest.raises(ValueError, match="overlap"):
+            make(**change)
+    # neighbours, a gradient of two parameters, arrays of nothing
+    t = make(params=[whole[:300], whole[300:320]], m=[whole[320:620], whole[980:]], v=[whole[640:940], whole[620:640]])
+    make(grads=[once, once[:20]])
+    make(params=[on_device(300), whole[5:5]], grads=[on_device(300), once[3:3]], m=[on_device(300), whole[5:5]], v=[on_device(300), whole[5:5]])
+    before = t.array.copy()
+    with pytest.raises(ValueError, match="overlap"):
+        t.set_grads([whole.view(bf16)[:300], on_device(20, dtype=bf16)])
+    assert t.grad_dtype == G.GROOT_F32 and (t.array == before).all()
