@@ -9,8 +9,6 @@ namespace groot {
 
 namespace {
 
-constexpr int kLdsBytes = 160 * 1024;
-
 constexpr int log2_of(int64_t x)
 {
     int l = 0;
@@ -130,20 +128,22 @@ __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const Row
 // on their way or in LDS, across the blocks' borders.
 // Bound by HBM: 64 x 64 in fp32 is 512 bytes and 8192 operations a row; 8.4 M rows take 0.87 ms, 4.9 TB/s, where the bytes alone take
 // 0.69 and the fp32 matrix instructions 0.44.  Through tiles, the weights staged for 128 rows at a time, they took 1.3 ms.
+// kSteps: how many steps of weights LDS holds.
 constexpr int kNarrowBytes = 512, kNarrowRows = 32, kNarrowStage = kNarrowRows * kStepBytes;
 
-template <typename T, typename O, int kN, int kWaves, int kStages, bool kNMajor, bool kAligned>
+template <typename T, typename O, int kN, int kWaves, int kStages, int kSteps, bool kNMajor, bool kAligned>
 __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct p, int log_rows, int32_t steps, bool whole)
 {
     constexpr int kThreads = kWaves * kWave, kJ = kN / 32, kEach = kNarrowStage / 16 / kWave;
     typedef Stage<T, kN, kThreads, !kNMajor, false> StageB;  // once, through registers: from any address
     typedef Stage<T, kNarrowRows, kBlock, false, kAligned> Rows;       // its layout in LDS
-    extern __shared__ __align__(16) char lds[];              // weights, then every wavefront's steps
+    constexpr int kRing = kStages * kNarrowStage;
+    __shared__ __align__(16) char lds[kWaves * kRing + kSteps * StageB::kBytes];       // every wavefront's steps, then the weights
     const RowTile t = find_tile(p.offsets, p.groups, p.n, blockIdx.x, log_rows);
     if (t.group < 0) return;
     const T *B = (const T *)p.B + (int64_t)t.group * p.K * p.N;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    char *const ring = lds + steps * StageB::kBytes + wave * (kStages * kNarrowStage);
+    char *const ring = lds + wave * kRing, *const weights = lds + kWaves * kRing;
     const int64_t rows = t.end - t.begin, pitch = p.a_stride * (int64_t)sizeof(T);
     const int32_t blocks = (int32_t)((rows + kNarrowRows - 1) / kNarrowRows), mine = (blocks - wave + kWaves - 1) / kWaves;
     const int32_t bytes = p.K * (int32_t)sizeof(T), items = mine * steps;
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
     for (int s = 0; s < steps; ++s) {
         typename StageB::Held h;
         b.template load<true>(s, h);
-        b.template put<true>(h, lds + s * StageB::kBytes);
+        b.template put<true>(h, weights + s * StageB::kBytes);
     }
     Epilogue<T, O, kJ> epilogue;
     epilogue.init(p, t.group, 0);
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
 #pragma unroll
             for (int j = 0; j < kJ; ++j) sums[0][j] = {};
         }
-        const char *const a = ring + now * kNarrowStage, *const w = lds + s * StageB::kBytes;
+        const char *const a = ring + now * kNarrowStage, *const w = weights + s * StageB::kBytes;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             if (s * kStepBytes + q * 32 >= bytes) break;
@@ -264,29 +264,37 @@ int rows_launch(const RowsProduct &p, void *stream)
     return (int)hipGetLastError();
 }
 
-template <typename T, typename O, int kN, int kWaves, int kStages, bool kNMajor, bool kAligned>
-int narrow_launch_as(const RowsProduct &p, int log_rows, int32_t steps, bool whole, void *stream)
+template <typename T, typename O, int kN, int kStages, int kSteps, bool kNMajor, bool kAligned>
+int narrow_launch_as(const RowsProduct &p, int log_rows, int32_t steps, void *stream)
 {
+    constexpr int kWaves = 8;
     const int64_t workgroups = ((p.n - 1) >> log_rows) + 1 + (p.offsets ? p.groups : 0);
-    const size_t bytes = (size_t)steps * kN * kStepBytes + (size_t)kWaves * kStages * kNarrowStage;
     if (!fits_launch(workgroups, kWaves * kWave)) return kErrTooManyTiles;
-    auto kernel = narrow_kernel<T, O, kN, kWaves, kStages, kNMajor, kAligned>;
-    static const hipError_t most = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
-    if (most != hipSuccess) return (int)most;
-    kernel<<<(uint32_t)workgroups, kWaves * kWave, bytes, (hipStream_t)stream>>>(p, log_rows, steps, whole);
+    narrow_kernel<T, O, kN, kWaves, kStages, kSteps, kNMajor, kAligned>
+        <<<(uint32_t)workgroups, kWaves * kWave, 0, (hipStream_t)stream>>>(p, log_rows, steps, out_whole<O>(p));
     return (int)hipGetLastError();
 }
 
+// LDS of as many steps as leave a CU the workgroups that the row's own number would: 160 KB hold two of 80, three of 48 or 53, four of 40.
+// (A size at the launch would have to be asked of the runtime first, above 64 KB, for every device.)
 template <typename T, typename O, int kN, bool kNMajor>
 int narrow_launch(const RowsProduct &p, void *stream)
 {
     const int32_t steps = (int32_t)((p.K * sizeof(T) + kStepBytes - 1) / kStepBytes);
-    const bool aligned = on16(p.A, p.a_stride * (int64_t)sizeof(T)) && p.K * (int64_t)sizeof(T) % 16 == 0, whole = out_whole<O>(p);
+    static_assert(kNarrowBytes == 4 * kStepBytes, "at most four steps");
+    const bool aligned = on16(p.A, p.a_stride * (int64_t)sizeof(T)) && p.K * (int64_t)sizeof(T) % 16 == 0;
     int log_rows = 8;                                        // about 1024 workgroups, of 256 rows at least
     while (log_rows < 20 && ((int64_t)1024 << log_rows) < p.n) ++log_rows;
     // 16 wavefronts to a CU with a step of their own on the way each; 8 with two or three were 8 % slower at 64 x 64, 14 % at 128 x 128
-    return aligned ? narrow_launch_as<T, O, kN, 8, 2, kNMajor, true>(p, log_rows, steps, whole, stream)
-                   : narrow_launch_as<T, O, kN, 8, 1, kNMajor, false>(p, log_rows, steps, whole, stream);
+    if (aligned) {
+        constexpr int kSome = kN == 64 ? 2 : 1;              // 80 KB, else 96 or 128
+        return steps <= kSome ? narrow_launch_as<T, O, kN, 2, kSome, kNMajor, true>(p, log_rows, steps, stream)
+                              : narrow_launch_as<T, O, kN, 2, 4, kNMajor, true>(p, log_rows, steps, stream);
+    }
+    constexpr int kSome = kN == 64 ? 2 : 3;                  // 40, 48 or 64 KB; 48, 80 or 96
+    return steps == 1       ? narrow_launch_as<T, O, kN, 1, 1, kNMajor, false>(p, log_rows, steps, stream)
+           : steps <= kSome ? narrow_launch_as<T, O, kN, 1, kSome, kNMajor, false>(p, log_rows, steps, stream)
+                            : narrow_launch_as<T, O, kN, 1, 4, kNMajor, false>(p, log_rows, steps, stream);
 }
 
 // What a step of the contraction (128 bytes of every row) takes, in ns, with up to 256 and with up to 512 tiles of a kind on the GPU's

@@ -7,6 +7,9 @@ Tolerances, all derived from the arithmetic that the calls state:
   * 8-bit products: the integer sum is exact; its conversion, two products and a sum round once each.
 """
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -764,3 +767,38 @@ def test_on_a_stream_of_its_own_and_replayed_from_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(outs, wanted[k])), k
         torch.randn(1000, device="cuda").sum().item()
+
+
+FIRST_CALL_CAPTURED = """
+import torch
+import paper_2511_18297_amd as G
+gen = torch.Generator(device="cuda")
+gen.manual_seed(1)
+cases = []
+for dtype, n, K, N, pad in ((torch.float32, 4096, 64, 64, 0), (torch.float32, 4096, 128, 128, 0), (torch.bfloat16, 4096, 200, 100, 0), (torch.float16, 4096, 250, 120, 1)):
+    X = torch.randint(-2, 3, (n, K + pad), generator=gen, device="cuda").to(dtype)[:, :K]
+    W = torch.randint(-1, 2, (1, K, N), generator=gen, device="cuda").to(dtype)
+    cases.append((X, W, torch.empty((n, N), dtype=dtype, device="cuda")))
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    for X, W, Y in cases:
+        G.groot_grouped_product(X, W, None, None, False, Y)
+for replay in range(3):
+    for X, W, Y in cases:
+        X.mul_(-1)
+        Y.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    for X, W, Y in cases:
+        want = X.double() @ W[0].double()
+        assert (Y.double() - want).abs().max() <= 2.0 ** -8 * want.abs().max(), (replay, Y.dtype)
+print("captured")
+"""
+
+
+def test_narrow_rows_whose_first_call_is_captured():
+    """in a process that has not called them: nothing has to be asked of the runtime before"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALL_CAPTURED], cwd=root, capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0 and "captured" in done.stdout, done.stderr[-2000:]
