@@ -274,6 +274,39 @@ def test_large_sizes(kind, case):
     close(db, want, sum_bound(terms, rows[:, None]) + rounding(want, dtype) * 1.01, "db")
 
 
+# around the borders of the pieces of 512 rows or more that a group's rows are cut into, in tiles of 64, 128 and 256, rows that begin
+# on 16 bytes and that do not: (sizes of the groups, K, N, pad of the rows)
+PIECES = [([n], 64, 64, 0) for n in (1, 511, 512, 513, 1023, 1024, 1025)] + [
+    ([512 * 5 - 1, 512 * 3, 512 * 2 + 1, 0, 1, 512], 64, 48, 0), ([1537, 511, 2048], 60, 33, 1), ([20000], 64, 96, 0), ([9000], 20, 12, 0),
+    ([9001], 20, 12, 1), ([8192, 8193], 72, 136, 0), ([2049, 0, 4095, 1], 200, 300, 0), ([2047, 0, 4097, 1], 200, 300, 1), ([33000, 511], 200, 200, 0),
+    ([5000] + [60] * 15, 1024, 1024, 0), ([60] * 15 + [6145], 1024, 1024, 0), ([8192], 4096, 4096, 0), ([70000, 3, 66001], 32, 32, 0),
+    ([600000], 16, 32, 0), ([524289, 524288], 48, 5, 0)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("case", range(len(PIECES)))
+def test_weight_gradients_lose_no_row(kind, case):
+    """Small integers: every partial sum is a whole number below 2^24, so that dW and dbias are exact, whatever the order, and a row
+    that is left out or taken twice shows."""
+    dtype, (sizes, K, N, pad) = TYPES[kind], PIECES[case]
+    n, E = sum(sizes), len(sizes)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(500 + case)
+    X = torch.randint(1, 3, (n, K + pad), generator=gen, device="cuda").to(dtype)[:, pad // 2:pad // 2 + K]
+    dY = torch.randint(-2, 3, (n, N + pad), generator=gen, device="cuda").to(dtype)[:, pad // 2:pad // 2 + N]
+    dY[:, 0] = 1                                             # a column of ones: the sums of X's columns, and the number of rows
+    work = torch.empty(max(16, G.groot_grouped_product_backward_weights_workspace(n, E, K, N, dtype)), dtype=torch.uint8, device="cuda")
+    want = torch.stack([x.double().t() @ d.double() for x, d in zip(X.split(sizes), dY.split(sizes))])
+    want_db = torch.stack([d.double().sum(0) for d in dY.split(sizes)])
+    for offsets in [offsets_of(sizes)] + [None] * (E == 1):
+        for junk in (0, 255):
+            dW, db = torch.full((E, K, N), float("nan"), device="cuda"), torch.full((E, N), float("nan"), device="cuda")
+            work.fill_(junk)
+            G.groot_grouped_product_backward_weights(X, dY, offsets, dW, db, work)
+            assert torch.equal(dW.double(), want), int((dW.double() != want).sum())
+            assert torch.equal(db.double(), want_db), int((db.double() != want_db).sum())
+
+
 @pytest.mark.parametrize("case", range(len(LARGE)))
 def test_quantized_product_large_sizes(case):
     sizes, K, N = LARGE[case]
