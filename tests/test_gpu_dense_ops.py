@@ -698,6 +698,35 @@ def test_adamw_gradient_scale_and_repeats():
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for k in ("p", "m", "v") for a, b in zip(s[k], t[k]))
 
 
+def test_adamw_of_a_tensor_beyond_32_bits(monkeypatch):
+    """the values, codes, scales and random numbers about the place 2^32 of one tensor, and at its ends"""
+    n, step, seed = (1 << 32) + 1300, 6, 9
+    zeros = lambda k, dtype: torch.zeros(k, dtype=dtype, device="cuda")  # noqa: E731
+    bf16, codes = torch.bfloat16, torch.float8_e4m3fn
+    s = dict(p=[zeros(n, bf16)], g=[zeros(n, bf16)], m=[zeros(n, torch.uint8).view(codes)], v=[zeros(n, torch.uint8).view(codes)],
+             m_scale=[zeros(-(-n // 256), torch.float32)], v_scale=[zeros(-(-n // 256), torch.float32)], master=None)
+    places = [(0, 1024), ((1 << 31) - 512, (1 << 31) + 512), ((1 << 32) - 1024, n)]        # whole blocks, but the last
+    part = lambda x, k, a, b: x[k][0][a // 256:-(-b // 256)] if "scale" in k else x[k][0][a:b]  # noqa: E731
+    olds = []
+    for seed_of, (a, b) in enumerate(places):
+        here = adamw_case([b - a], bf16, bf16, 8, False, 40 + seed_of)
+        for k in s:
+            if s[k] is not None:
+                part(s, k, a, b).view(torch.uint8).copy_(here[k][0].view(torch.uint8))
+        olds.append(here)
+    G.groot_adamw_step(G.groot_adamw_tensors(s["p"], s["g"], s["m"], s["v"], m_scale=s["m_scale"], v_scale=s["v_scale"]), step, LR, B1, B2, EPS, WD, seed=seed)
+    for (a, b), old in zip(places, olds):
+        def randoms_here(i, count, step, seed):
+            at = torch.arange(a, b, device="cuda")
+            key = mixed(mixed(mixed(i + 0x9E3779B9) ^ step) ^ seed)
+            h = mixed((at & 0xFFFFFFFF) ^ ((key + (at >> 32) * 0x9E3779B9) & 0xFFFFFFFF))
+            return (h & 0xFFFF).double() / 65536, (h >> 16).double() / 65536
+        monkeypatch.setattr(sys.modules[__name__], "randoms", randoms_here)
+        adamw_check({k: None if s[k] is None else [part(s, k, a, b)] for k in s}, old, step, seed)
+    for a, b in ((1024, 1 << 20), ((1 << 31) + 512, (1 << 31) + (1 << 20)), ((1 << 32) - (1 << 20), (1 << 32) - 1024)):
+        assert not any(s[k][0][a:b].view(torch.uint8).any() for k in ("p", "m", "v"))       # what lies between stayed
+
+
 def test_adamw_values_that_are_not_finite():
     for bits in (32, 8):
         s, t = (adamw_case([600], torch.float32, torch.float32, bits, False, 3) for _ in range(2))
