@@ -13,6 +13,7 @@ import sys
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 if ROOT not in sys.path:
@@ -55,6 +56,7 @@ class Aggregate(torch.autograd.Function):
         return Y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         dY = dY.contiguous()
         dX = torch.empty_like(dY)
@@ -75,15 +77,20 @@ class Typed(torch.autograd.Function):
         return Y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         X, W, offsets = ctx.saved_tensors
         dY = dY.contiguous()
-        dX, dW = torch.empty_like(X), torch.empty_like(W)
-        db = torch.empty((W.shape[0], W.shape[2]), dtype=W.dtype, device="cuda") if ctx.bias else None
-        need = G.groot_grouped_product_backward_weights_workspace(X.shape[0], *W.shape, X.dtype)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
-        G.groot_grouped_product_backward_data(dY, W, offsets, dX)
-        G.groot_grouped_product_backward_weights(X, dY, offsets, dW, db, workspace)
+        dX = dW = db = None
+        if ctx.needs_input_grad[0]:
+            dX = torch.empty_like(X)
+            G.groot_grouped_product_backward_data(dY, W, offsets, dX)
+        if ctx.needs_input_grad[1] or ctx.needs_input_grad[2]:
+            dW = torch.empty_like(W)
+            db = torch.empty((W.shape[0], W.shape[2]), dtype=W.dtype, device="cuda") if ctx.bias else None
+            need = G.groot_grouped_product_backward_weights_workspace(X.shape[0], *W.shape, X.dtype)
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+            G.groot_grouped_product_backward_weights(X, dY, offsets, dW, db, workspace)
         return dX, dW, db, None
 
 

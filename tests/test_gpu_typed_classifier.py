@@ -43,3 +43,25 @@ def test_typed_layer_gradients_against_autograd():
     terms = [R.cpu().double().abs() @ W64.detach().abs().sum(0).t(), X64.detach().abs().t() @ R.cpu().double().abs(), R.cpu().double().abs().sum(0)]
     for g, w, t, adds in zip(got, want, terms, (N, n, n)):
         assert ((g.cpu().double() - w).abs() <= (adds + 3) * 2.0 ** -23 * t).all()
+
+
+def test_second_derivatives_are_refused():
+    """the gradient calls have no gradients of their own: a second derivative would leave out what goes through them"""
+    m = T.Multiplier(8)
+    X = torch.randn((m.X.shape[0], 12), device="cuda").requires_grad_(True)
+    W, b = torch.randn((3, 12, 20), device="cuda").requires_grad_(True), torch.zeros((3, 20), device="cuda")
+    for out in (T.Typed.apply(X, W, b, m.offsets), T.Aggregate.apply(X, m)):
+        g, = torch.autograd.grad(out.square().sum(), X, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            (g * X).sum().backward()
+
+
+def test_only_the_gradients_that_are_asked_for():
+    m = T.Multiplier(8)
+    wants = torch.randn((m.X.shape[0], 12), device="cuda"), torch.randn((3, 12, 20), device="cuda"), torch.randn((3, 20), device="cuda")
+    R = torch.randn((m.X.shape[0], 20), device="cuda")
+    full = torch.autograd.grad((T.Typed.apply(*(t.requires_grad_(True) for t in wants), m.offsets) * R).sum(), wants)
+    for ask in ((0,), (1,), (2,), (0, 2), (1, 2)):
+        some = [t.detach().requires_grad_(i in ask) for i, t in enumerate(wants)]
+        got = torch.autograd.grad((T.Typed.apply(*some, m.offsets) * R).sum(), [some[i] for i in ask])
+        assert all(torch.equal(g, full[i]) for g, i in zip(got, ask))
