@@ -209,8 +209,8 @@ constexpr int kAcrossCols = 64, kAcrossAhead = 3;
 
 template <typename T>
 struct AcrossBlock {
-    static constexpr int kRows = sizeof(T) == 2 ? 32 : 16, kLoads = kRows / 4, kWords = sizeof(T);   // 2 or 4 words of four columns
-    typedef int W __attribute__((ext_vector_type(sizeof(T))));
+    static constexpr int kRows = sizeof(T) == 2 ? 32 : 16, kLoads = kRows / 4;
+    typedef int W __attribute__((ext_vector_type(sizeof(T))));       // four columns: 2 or 4 words
     W w[kLoads];
     v4i x;
 

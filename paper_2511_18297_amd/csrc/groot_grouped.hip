@@ -25,13 +25,13 @@ __device__ __forceinline__ void block_to_lds(char *scratch, const S &sums)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const v4f x = {(float)sums[4 * q], (float)sums[4 * q + 1], (float)sums[4 * q + 2], (float)sums[4 * q + 3]};
-        *(v4f *)(scratch + m * 128 + (((2 * q + half) ^ swizzle_along<128>(m)) * 16)) = x;
+        *(v4f *)(scratch + m * 128 + (((2 * q + half) ^ swizzle_along(m)) * 16)) = x;
     }
     wave_sync();
 }
 __device__ __forceinline__ v4f row_of_block(const char *scratch, int r)
 {
-    return *(const v4f *)(scratch + r * 128 + ((threadIdx.x % 8 ^ swizzle_along<128>(r)) * 16));
+    return *(const v4f *)(scratch + r * 128 + ((threadIdx.x % 8 ^ swizzle_along(r)) * 16));
 }
 
 // The epilogue of a wavefront's 32 x 32 blocks.  A lane's four neighbouring columns of one row would make stores of 16 bytes in 32
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kWaves *kWave) void narrow_kernel(const RowsProduct
         const int64_t row = (int64_t)load_block * kNarrowRows + own;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int32_t at = load_step * kStepBytes + (lane % 8 ^ swizzle_along<kStepBytes>(8 * i + own)) * 16;
+            const int32_t at = load_step * kStepBytes + (lane % 8 ^ swizzle_along(8 * i + own)) * 16;
             const int32_t left = load_block < blocks ? bytes - at : 0;
             int64_t r = row + 8 * i;
             r = r < rows ? r : rows - 1;
@@ -302,12 +302,12 @@ int narrow_launch(const RowsProduct &p, void *stream)
 // size; the others by theirs in large tiles, by the latency of a step's loads in small ones.  The kinds, rows x columns and stages:
 //   256 x 256, 2; 128 x 128, 2; 128 x 128, 4; 64 x 128, 3; 64 x 64, 5; 32 x 128, 4; 32 x 64, 6
 struct TileCost {
-    int32_t rows, cols, to256, to512;        // to512 0: one tile to a CU
+    int32_t rows, cols, to256, to512;        // to512 0: one tile to a CU; to256 0: not built, as it would never be the least
 };
 constexpr int kTileKinds = 7;
 constexpr TileCost kTile16[kTileKinds] = {{256, 256, 2060, 0}, {128, 128, 1000, 1270}, {128, 128, 790, 0}, {64, 128, 550, 840},
                                           {64, 64, 380, 570}, {32, 128, 410, 630}, {32, 64, 400, 420}};
-constexpr TileCost kTile32[kTileKinds] = {{256, 256, 9260, 0}, {128, 128, 2360, 4540}, {128, 128, 2370, 0}, {64, 128, 1330, 2370},
+constexpr TileCost kTile32[kTileKinds] = {{256, 256, 0, 0}, {128, 128, 2360, 4540}, {128, 128, 0, 0}, {64, 128, 1330, 2370},
                                           {64, 64, 830, 1370}, {32, 128, 870, 1430}, {32, 64, 820, 880}};
 
 // The kind of tile that takes the least time by that table; rows that do not begin on 16 bytes go through registers, for which three
@@ -319,8 +319,8 @@ int choose_tile(int64_t n, int32_t groups, bool offsets, int32_t N, bool aligned
     double least = 0;
     for (int k = 0; k < kTileKinds; ++k) {
         if (!aligned && k != 1 && k != 4 && k != 6) continue;
-        if (sizeof(T) == 4 && (k == 0 || k == 2)) continue;  // never the least
         const TileCost &c = sizeof(T) == 4 ? kTile32[k] : kTile16[k];
+        if (!c.to256) continue;
         // a group's last tile is half full, on average
         double rows = offsets ? (double)n / c.rows + 0.5 * groups : (double)((n + c.rows - 1) / c.rows);
         const double least_rows = (double)(n < groups ? n : groups);

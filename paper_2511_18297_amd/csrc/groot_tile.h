@@ -5,7 +5,7 @@
 // without bank conflicts, and 8.9 TB/s come in from L2.  More stages of smaller steps, 4 or 16 wavefronts, 128-wide tiles and
 // fragments read earlier were all measured and are within 5 % or slower.
 //
-// A step of the contraction is 128 (or 64) bytes of a row whose elements lie along it ("along": 64 values of 16 bits, 32 of fp32,
+// A step of the contraction is 128 bytes of a row whose elements lie along it ("along": 64 values of 16 bits, 32 of fp32,
 // 128 of 8 bits), or as many rows of a matrix whose rows lie across it ("across").  Both operands of a step are staged in LDS by loads
 // that go there directly (16 bytes a lane, no registers), twice: one pair of tiles is computed while the next one arrives.
 // LDS has 64 banks: 16 lanes of a 16-byte read, 32 of an 8-byte and 64 of a 4-byte one are served at a time, if they fall on different
@@ -13,7 +13,7 @@
 //   along   the 16 rows that 16 lanes read at one piece cover all places of 256 bytes
 //   across  16-bit types: the four rows that a transposing read takes 64 bytes of cover 256 bytes; fp32: the two rows of 128 bytes
 // A fragment of the 32 x 32 matrix instructions is 16 bytes a lane, from row (lane & 31) and piece 2 s + (lane >> 5) of sub-step
-// s = 0 .. 3 (0, 1); for fp32 that is four instructions of two values of the contraction each, in an order of their own that both
+// s = 0 .. 3; for fp32 that is four instructions of two values of the contraction each, in an order of their own that both
 // operands share.  The operands change places (columns of the result first), so that a lane holds four neighbouring columns.
 #pragma once
 
@@ -78,7 +78,7 @@ struct TileType<float> {
     }
     static __device__ __forceinline__ Sum mma(v4i a, v4i b, Sum c, int part)
     {
-return __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(a[part]), __int_as_float(b[part]), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(__int_as_float(a[part]), __int_as_float(b[part]), c, 0, 0, 0);
     }
 };
 
@@ -220,12 +220,8 @@ __device__ __forceinline__ void row_codes(v4i v, float scale, int8_t *to)
     __builtin_memcpy(__builtin_assume_aligned(to, kPer), u, kPer);
 }
 
-// row r of kStep bytes
-template <int kStep>
-__device__ __forceinline__ int swizzle_along(int r)
-{
-    return kStep == 128 ? r / 2 & 7 : r / 4 & 3;
-}
+// row r of kStepBytes
+__device__ __forceinline__ int swizzle_along(int r) { return r / 2 & 7; }
 // row k of kRowBytes
 template <typename T, int kRowBytes>
 __device__ __forceinline__ int swizzle_across(int k)
@@ -235,11 +231,11 @@ __device__ __forceinline__ int swizzle_across(int k)
 
 // One operand's tile: kWide rows ("along") or columns ("across").  begin(s) starts the loads of step s, end(s) has them in LDS once
 // the workgroup has passed a barrier.
-template <typename T, int kWide, int kThreads, bool kAcross, bool kAligned, int kStep = kStepBytes>
+template <typename T, int kWide, int kThreads, bool kAcross, bool kAligned>
 struct Stage {
     static constexpr bool kDirect = kAligned;
-    static constexpr int kBytes = kWide * kStep, kValues = kStep / (int)sizeof(T), kSubSteps = kStep / 32, kEach = kBytes / 16 / kThreads;
-    static constexpr int kRowBytes = kAcross ? kWide * (int)sizeof(T) : kStep, kPieces = kRowBytes / 16;
+    static constexpr int kBytes = kWide * kStepBytes, kValues = kStepBytes / (int)sizeof(T), kSubSteps = kStepBytes / 32, kEach = kBytes / 16 / kThreads;
+    static constexpr int kRowBytes = kAcross ? kWide * (int)sizeof(T) : kStepBytes, kPieces = kRowBytes / 16;
     static constexpr int kRowsEach = kThreads / kPieces;     // rows of the tile that one load of the workgroup takes
     static_assert(kBytes % (16 * kThreads) == 0 && kThreads % kPieces == 0, "a whole number of loads of whole rows");
     static_assert(kAcross ? kRowsEach % (sizeof(T) == 4 ? 8 : 4) == 0 && kRowBytes >= (sizeof(T) == 4 ? 256 : 128) : kRowsEach % 16 == 0, "a lane's piece is the same in all its loads");
@@ -256,9 +252,9 @@ struct Stage {
     int32_t piece, row;
     bool short_row;
 
-    static __device__ __forceinline__ int swizzle(int r) 
+    static __device__ __forceinline__ int swizzle(int r)
     {
-        return kAcross ? swizzle_across<T, kRowBytes>(r) : swizzle_along<kStep>(r);
+        return kAcross ? swizzle_across<T, kRowBytes>(r) : swizzle_along(r);
     }
 
     // along: `base` is the first row's first value, `exist` rows exist, `extent` values of the contraction
@@ -296,8 +292,8 @@ struct Stage {
             if (!kAligned && k >= limit) p += (limit - 1 - k) * pitch + width;   // behind the end of the last row
             return p;
         } else {
-            *left = limit - s * kStep - piece * 16;
-            return src[i] + s * kStep;
+            *left = limit - s * kStepBytes - piece * 16;
+            return src[i] + s * kStepBytes;
         }
     }
     // direct: the loads [first, last) of a lane's kEach, zeros for what does not exist
@@ -340,7 +336,7 @@ struct Stage {
         const int lane = threadIdx.x % kWave, half = lane / 32;
         if constexpr (!kAcross) {
             const int r = first + lane % 32;
-            return *(const v4i *)(tile + r * kStep + (((2 * s + half) ^ swizzle(r)) * 16));
+            return *(const v4i *)(tile + r * kStepBytes + (((2 * s + half) ^ swizzle(r)) * 16));
         } else if constexpr (sizeof(T) == 2) {
             // 16 lanes give the addresses of four rows of 16 columns and get a column's four values each
             const int i = lane % 16, k = 16 * s + 8 * half + i / 4, c = (first + (lane / 16 % 2) * 16) / 8;
