@@ -92,7 +92,7 @@ __device__ __forceinline__ uint32_t lds_offset(const void *p) { return (uint32_t
 // before anything reads what arrived.  (A write to m0 needs one wait state before a load that goes by it.)
 __device__ __forceinline__ void dma16(const void *from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
 
 // until at most kMost of the wavefront's latest loads are on their way
