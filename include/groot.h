@@ -548,7 +548,9 @@ groot_status groot_grouped_product_backward_weights(int32_t dtype, const void *X
  *                         a NaN or an infinity has scale NaN and zeros
  *   groot_quantized_product  Y[i,j] = act((sum_k Q[i,k] W[g,j,k]) q_scale[i]
  *                         w_scale[g,j] + bias[g,j]): the sum is exact (int32),
- *                         the rest fp32 in this order, rounded once to Y's type
+ *                         the rest fp32 in this order, every operation rounded by
+ *                         itself, and once to Y's type: a row's result does not
+ *                         depend on the rows that it is served with
  *   groot_quantized_linear   both after one another from rows in floating point
  * W int8 [n_groups, N, K] (one row per output channel, contiguous), w_scale
  * and bias float [n_groups, N] (bias may be NULL), q_scale float [n_rows], Q int8

@@ -66,6 +66,7 @@ __device__ __forceinline__ v4i piece16(const char *row, int64_t k, int64_t bytes
 template <typename T, typename O, typename X, bool kAligned>
 __global__ __launch_bounds__(kFewThreads) void few_kernel(const RowsProduct p, int32_t col_tiles)
 {
+#pragma clang fp contract(off)
     constexpr bool kFused = !std::is_same<X, T>::value;
     typedef typename FewType<T>::Sum Sum;
     __shared__ Sum part[kFewWaves][kWave];

@@ -60,6 +60,7 @@ struct Epilogue {
     // rows from `row` of the output on, of which `rows` exist
     __device__ __forceinline__ void store(const RowsProduct &p, char *scratch, const typename TileType<T>::Sum (&sums)[kJ], int64_t row, int64_t rows, bool whole)
     {
+#pragma clang fp contract(off)                               // scales and bias round one by one, here as for few rows: a row's result is the same in any batch
         const int lane = threadIdx.x % kWave;
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {

@@ -464,6 +464,25 @@ def test_quantized_product(kind, case):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("K, N", [(64, 64), (200, 256), (77, 31), (1024, 640)])
+def test_quantized_rows_are_the_same_in_every_batch(kind, K, N):
+    """bit for bit what the call states: the sum in fp32, times the row's scale, times the column's, plus the bias, one rounding each
+    and one to the output's type; so it does not matter how many rows are served together"""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(K + N)
+    Q = torch.randint(-127, 128, (5000, K), generator=gen, device="cuda", dtype=torch.int8)
+    W = torch.randint(-127, 128, (1, N, K), generator=gen, device="cuda", dtype=torch.int8)
+    qs, ws = torch.rand(5000, generator=gen, device="cuda"), torch.rand((1, N), generator=gen, device="cuda")
+    b = torch.randn((1, N), generator=gen, device="cuda") * 1e4
+    dots = (Q.double() @ W[0].double().t()).cpu().float()
+    want = (dots * qs.cpu()[:, None] * ws.cpu() + b.cpu()).to(TYPES[kind])
+    for n in (1, 4, 16, 17, 48, 300, 5000):
+        Y = out_matrix(n, N, TYPES[kind])
+        G.groot_quantized_product(Q[:n], qs[:n], W, ws, None, b, False, Y)
+        assert torch.equal(Y.cpu(), want[:n]), (n, int((Y.cpu() != want[:n]).sum()))
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("sizes, K, N", [([1], 4096, 1024), ([1], 100, 37), ([4], 513, 200), ([16], 1024, 512), ([17], 768, 260), ([48], 2048, 520),
                                          ([1, 0, 2, 1], 640, 96), ([130, 200], 256, 192), ([600], 1030, 390)])
 def test_quantized_linear(kind, sizes, K, N):
