@@ -602,7 +602,8 @@ groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_
  *   |x| / step + u is rounded down, with u = the low (m) or high (v) 16 bits of
  *   mix(i ^ key) / 65536, i the value's index in its tensor (for i >= 2^32 its low
  *   32 bits, and key + (i >> 32) * 0x9E3779B9 for key), key = mix(mix(mix(number
- *   of the tensor in the call + 0x9E3779B9) ^ step) ^ seed), mix the finaliser
+ *   of the tensor in the call + 0x9E3779B9) ^ step) ^ seed), step's low 32 bits,
+ *   mix a published 32-bit finaliser (Austin Appleby's, in the public domain):
  *   h ^= h >> 16, h *= 0x85EBCA6B, h ^= h >> 13, h *= 0xC2B2AE35, h ^= h >> 16.
  *   (Rounded to nearest, an average that moves by less than half a code's step
  *   per call would stand still for good.)  sqrt(v) > 0 is held as the smallest
@@ -611,9 +612,10 @@ groot_status groot_quantized_linear(int32_t dtype, const void *X_dev, int64_t x_
  * Pointers are aligned to their type; tensors whose arrays all begin on 16 bytes
  * are read faster.  An array that is written (all but grad) must not overlap any
  * other array of the call; that is the caller's to see to, since looking for it
- * among all arrays takes longer than a small step does.  Launches one kernel per 48 tensors on hip_stream, allocates
- * nothing; the descriptors travel as kernel arguments, so the call may be
- * captured in a HIP graph, with the host values it was given.
+ * among all arrays takes longer than a small step does.  Launches one kernel per
+ * 48 tensors on hip_stream, allocates nothing; the descriptors travel as kernel
+ * arguments, so the call may be captured in a HIP graph, with the host values it
+ * was given.
  * Errors: EINVAL (NULL, unknown dtype, n < 0, state_bits, step < 1, lr or
  * weight_decay not finite or negative, beta outside [0, 1), eps not finite or <= 0; the same of what is left of
  * eps, lr / (1 - beta1^step) and 1 - lr weight_decay in fp32: not finite, or an eps of 0), ERANGE (a tensor of 2^33

@@ -1,8 +1,9 @@
 // One AdamW step over many tensors: the descriptors of up to 48 tensors travel as kernel arguments, a workgroup finds its tensor
 // from its number and takes kAdamwChunk values of it, four to a lane.
-// Bound by HBM: 16.06 bytes a value with states in 8 bits, bfloat16 parameters and a master (400 M values: 1.06 ms, 6.06 TB/s), 28 with
-// fp32 all through (100 M: 0.44 ms, 6.3 TB/s); a large copy reaches 6.2.  Nothing is read or written twice, so loads and stores are
-// told not to keep their lines (without: 1.12 and 0.51 ms), and every workgroup has one set of loads (with two: 1.25 and 0.52 ms).
+// Bound by HBM: 16.06 bytes a value with states in 8 bits, bfloat16 parameters and a master (400 M values: 1.08 to 1.11 ms from card to
+// card, 5.8 to 5.95 TB/s), 28 with fp32 all through (100 M: 0.44 ms, 6.3 TB/s); a large copy reaches 6.2.  Nothing is read or written
+// twice, so loads and stores are told not to keep their lines (without: 1.12 where it took 1.06, and 0.51), and every workgroup has one
+// set of loads (with two: 1.25 and 0.52 ms).
 #include "groot_dense_device.h"
 
 namespace groot {

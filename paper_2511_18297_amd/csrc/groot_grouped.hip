@@ -87,7 +87,7 @@ struct Epilogue {
 };
 
 // Decoding 128 rows over 32 groups of 2048 x 2048 in bfloat16: 48 us, 5.5 TB/s of weights; 16384 rows over 8 groups of 4096 x 4096:
-// 580 us, 0.95 PFLOP/s (1088 tiles of 256 x 256 on 256 CUs: five rounds where 4.25 would do).
+// 570 to 590 us, 0.93 to 0.97 PFLOP/s (1088 tiles of 256 x 256 on 256 CUs: five rounds where 4.25 would do).
 // out[i,:] = epilogue(A[i,:] B[g]): a workgroup takes kM rows of a group and kN columns, a wavefront kM / kWavesM x kN / kWavesN
 template <typename T, typename O, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kNMajor, bool kAligned>
 __global__ __launch_bounds__(kWavesM *kWavesN *kWave) void rows_kernel(const RowsProduct p, const TileOrder order, int32_t col_tiles, bool whole)
