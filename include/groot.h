@@ -8,7 +8,8 @@
  * multiply the adjacency with the node-feature matrix, and the partition of a
  * large graph into sub-graphs whose boundary edges are re-grown.  Beside it
  * stands the dense half of a network on such graphs: products grouped by node
- * type with their gradients, products in 8-bit integers, the AdamW step.
+ * type with their gradients, products in 8-bit integers, the AdamW step, the
+ * routing of rows to experts, the root-mean-square norm.
  *
  * Conventions
  *   - Every call returns a groot_status and never throws or aborts; on failure
@@ -636,6 +637,121 @@ groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int64_t n_tenso
                               int32_t grad_dtype, int32_t state_bits, int64_t step, double lr, double beta1,
                               double beta2, double eps, double weight_decay, const float *grad_scale_dev,
                               uint32_t seed, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Routing rows to experts.  Not in the paper: what stands around the grouped
+ * products of a routed layer.
+ *   groot_route            scores -> experts, weights, places, offsets
+ *   groot_routed_rows      R[places[i,s],:] = X[i,:]
+ *   (the experts' products, with `offsets`: groot_grouped_product)
+ *   groot_routed_sum       out[i,:] = addend[i,:] + sum_s weights[i,s] R[places[i,s],:]
+ * and their gradients: groot_routed_sum_backward, groot_routed_sum of the
+ * gradient of R without weights (that of X), groot_route_backward.
+ *
+ * scores [n_rows, n_experts] of dtype, `score_stride` elements from row to row.
+ * gate: p = GROOT_SOFTMAX or GROOT_SIGMOID of a row's scores.
+ * The choice goes by c = p + bias[e] (bias: float [n_experts], counts for the
+ *   choice only), computed and compared in 64 bits; without a bias, and with set_best = 1,
+ *   by the scores themselves.  An expert is closed to a row where its score is
+ *   -inf or its bias -inf or NaN.
+ * Sets: the experts make n_sets sets of neighbours (n_sets divides n_experts);
+ *   a set counts what its set_best (1 or 2) best open experts' c come to, and the
+ *   open_sets that count most stay open (a set without an open expert counts
+ *   -inf).  n_sets = open_sets = 1: no sets.
+ * experts int32 [n_rows, top_k]: the top_k experts of largest c, descending;
+ *   ties, here and between sets, go to the lowest number.  -1 where none is left.
+ * weights float [n_rows, top_k]: factor p, or with `renormalise` factor p
+ *   over the sum of p of the row's chosen experts; 0 where there is none.  A row
+ *   with a NaN among its scores, or with +inf under softmax, has no
+ *   experts and weights of NaN, which show in groot_routed_sum.
+ * places int32 [n_rows, top_k]: where (row, slot) comes when all are put in the
+ *   order of their experts, the rows of each in their own order; -1 without an expert.
+ * offsets int64 [n_experts + 1]: where each expert's places begin; the last is
+ *   their number.  Rows of R behind it are not written.
+ * groot_route_backward: dscores (of dtype, fully overwritten) from the gradient
+ *   of the weights; the choice has none.  NaN in rows whose weights are NaN, 0 at -inf.
+ * workspace of groot_route: device, 16-byte aligned, groot_route_workspace bytes (may be 0).
+ * 1 <= n_experts <= 1024, 1 <= top_k <= 32, n_sets <= 64, top_k at most what
+ * the open sets hold, n_rows * top_k < 2^31.
+ *
+ * X, R, out, addend, dout, dR: matrices of dtype and `width` columns (1 to 65536),
+ *   R and dR of n_places rows.  A place outside [0, n_places) is as -1: nothing
+ *   is written, and for a sum R reads as a row of zeros there (a weight of NaN still
+ *   makes the sum NaN).  Places that are written must be distinct.  weights NULL:
+ *   ones; addend NULL: zeros.  Sums in fp32 in the order of the slots, from the
+ *   addend on, rounded once.
+ * groot_routed_rows also takes GROOT_I8, and copies a scale for each row where
+ *   x_scale and r_scale (float, or both NULL) are given.
+ * groot_routed_sum_backward: dR[places[i,s],:] = weights[i,s] dout[i,:],
+ *   dweights[i,s] = dout[i,:] . R[places[i,s],:] (0 without a place); dR or
+ *   dweights may be NULL, and R where dweights is.
+ * Results are the same from run to run.  The calls only enqueue on hip_stream and
+ * allocate nothing.  Outputs must not overlap each other or inputs.  Errors: EINVAL
+ * (NULL, unknown dtype or gate, alignment, sizes, strides, overlap, workspace too small),
+ * ERANGE (2^31 slots or places), EHIP.
+ * ------------------------------------------------------------------------- */
+#define GROOT_I8 3                           /* groot_routed_rows only */
+typedef enum { GROOT_SOFTMAX = 0, GROOT_SIGMOID = 1 } groot_gate;
+
+groot_status groot_route_workspace(int64_t n_rows, int32_t n_experts, int32_t top_k, size_t *bytes);
+groot_status groot_route(int32_t dtype, const void *scores_dev, int64_t score_stride, const float *bias_dev, int32_t gate,
+                         int32_t n_sets, int32_t open_sets, int32_t set_best, int32_t renormalise, double factor,
+                         int32_t *experts_dev, float *weights_dev, int32_t *places_dev, int64_t *offsets_dev,
+                         int64_t n_rows, int32_t n_experts, int32_t top_k, void *workspace_dev,
+                         size_t workspace_bytes, void *hip_stream);
+groot_status groot_route_backward(int32_t dtype, const void *scores_dev, int64_t score_stride, int32_t gate,
+                                  int32_t renormalise, double factor, const int32_t *experts_dev,
+                                  const float *dweights_dev, void *dscores_dev, int64_t ds_stride, int64_t n_rows,
+                                  int32_t n_experts, int32_t top_k, void *hip_stream);
+groot_status groot_routed_rows(int32_t dtype, const void *X_dev, int64_t x_stride, const float *x_scale_dev,
+                               const int32_t *places_dev, int32_t top_k, void *R_dev, int64_t r_stride,
+                               float *r_scale_dev, int64_t n_rows, int64_t n_places, int32_t width, void *hip_stream);
+groot_status groot_routed_sum(int32_t dtype, const void *R_dev, int64_t r_stride, const int32_t *places_dev,
+                              const float *weights_dev, const void *addend_dev, int64_t addend_stride, int32_t top_k,
+                              void *out_dev, int64_t out_stride, int64_t n_rows, int64_t n_places, int32_t width,
+                              void *hip_stream);
+groot_status groot_routed_sum_backward(int32_t dtype, const void *dout_dev, int64_t dout_stride, const void *R_dev,
+                                       int64_t r_stride, const int32_t *places_dev, const float *weights_dev,
+                                       int32_t top_k, void *dR_dev, int64_t dr_stride, float *dweights_dev,
+                                       int64_t n_rows, int64_t n_places, int32_t width, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Root-mean-square norm of rows.  Not in the paper: the norm in front of a
+ * layer, with the residual stream's addition, and with rows in 8 bits for
+ * groot_quantized_product.
+ *   h = x + residual, in fp32, rounded to dtype (without a residual h = x)
+ *   rstd = 1 / sqrt(mean of h^2 + eps), sum, mean and root in 64 bits, rounded once to fp32
+ *   y = (h rstd) gain, in fp32, every operation rounded by itself
+ *   Y = y rounded to dtype;  Q, q_scale = y cut to 8 bits as groot_quantize_rows
+ *   does: q_scale = max |y| times fl(1 / 127), Q = y / q_scale to the nearest integer,
+ *   halves to even; a row that holds a NaN or an infinity has scale NaN and zeros
+ * X, residual, H, Y [n_rows, width] of dtype, Q int8, gain [width] of dtype, q_scale
+ *   and rstd float [n_rows].  residual and gain may be NULL (none; ones), and
+ *   every output that is not wanted (Q and q_scale together).  H and Y may each
+ *   be one of X and residual, the same address and stride (a stream that is
+ *   updated in place); otherwise outputs overlap nothing.
+ * groot_rms_norm_backward: with a = dY gain and c = mean of a h over the row,
+ *   dX = rstd (a - h rstd^2 c) + dH, the gradient of x and of the residual alike
+ *   (dH [n_rows, width]: the gradient that comes to h by another way, or NULL);
+ *   dgain [width] (dtype or float by grad_dtype, or NULL) = sum over the rows of
+ *   dY (h rstd).  H: the rows h as groot_rms_norm gave them (X without a
+ *   residual), rstd from the same call.  The rows' parts of dgain meet in a fixed
+ *   order.  Outputs overlap nothing.
+ * workspace (device, 16-byte aligned, contents overwritten): at least
+ *   groot_rms_norm_backward_workspace bytes; not needed where dgain is NULL.
+ * 1 <= width <= 65536, eps > 0.  The calls only enqueue on hip_stream and
+ * allocate nothing.  Errors: EINVAL, EHIP.
+ * ------------------------------------------------------------------------- */
+groot_status groot_rms_norm(int32_t dtype, const void *X_dev, int64_t x_stride, const void *residual_dev,
+                            int64_t residual_stride, const void *gain_dev, double eps, void *H_dev, int64_t h_stride,
+                            void *Y_dev, int64_t y_stride, int8_t *Q_dev, int64_t q_stride, float *q_scale_dev,
+                            float *rstd_dev, int64_t n_rows, int32_t width, void *hip_stream);
+groot_status groot_rms_norm_backward_workspace(int32_t dtype, int64_t n_rows, int32_t width, size_t *bytes);
+groot_status groot_rms_norm_backward(int32_t dtype, const void *H_dev, int64_t h_stride, const float *rstd_dev,
+                                     const void *gain_dev, const void *dY_dev, int64_t dy_stride, const void *dH_dev,
+                                     int64_t dh_stride, void *dX_dev, int64_t dx_stride, int32_t grad_dtype,
+                                     void *dgain_dev, int64_t n_rows, int32_t width, void *workspace_dev,
+                                     size_t workspace_bytes, void *hip_stream);
 
 /* What the library decided for an uploaded plan, for diagnostics and benchmarks:
  * "ld_pipelined" (0 the plain LD kernel always, 2 the pipelined one for F = 32,

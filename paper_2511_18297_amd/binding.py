@@ -31,6 +31,8 @@ EXPORTS = [
     "groot_grouped_product", "groot_grouped_product_backward_data", "groot_grouped_product_backward_weights",
     "groot_grouped_product_backward_weights_workspace", "groot_quantize_rows", "groot_quantized_product", "groot_quantized_linear",
     "groot_quantized_linear_workspace", "groot_adamw_step",
+    "groot_route_workspace", "groot_route", "groot_route_backward", "groot_routed_rows", "groot_routed_sum", "groot_routed_sum_backward",
+    "groot_rms_norm", "groot_rms_norm_backward_workspace", "groot_rms_norm_backward",
 ]
 
 # an alternative build of the library (same ABI), for experiments
@@ -106,6 +108,15 @@ _lib.groot_quantized_linear_workspace.argtypes = [_i64, _i32, _psize]
 _lib.groot_quantized_linear.argtypes = [_i32, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _vp, _i64, _i64, _i32, _i32, _i32, _vp,
                                    ctypes.c_size_t, _vp]
 _lib.groot_adamw_step.argtypes = [_vp, _i64, _i32, _i32, _i32, _i64, _f64, _f64, _f64, _f64, _f64, _vp, _u32, _vp]
+_lib.groot_route_workspace.argtypes = [_i64, _i32, _i32, _psize]
+_lib.groot_route.argtypes = [_i32, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _f64, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp, ctypes.c_size_t, _vp]
+_lib.groot_route_backward.argtypes = [_i32, _vp, _i64, _i32, _i32, _f64, _vp, _vp, _vp, _i64, _i64, _i32, _i32, _vp]
+_lib.groot_routed_rows.argtypes = [_i32, _vp, _i64, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _i64, _i32, _vp]
+_lib.groot_routed_sum.argtypes = [_i32, _vp, _i64, _vp, _vp, _vp, _i64, _i32, _vp, _i64, _i64, _i64, _i32, _vp]
+_lib.groot_routed_sum_backward.argtypes = [_i32, _vp, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _i64, _i32, _vp]
+_lib.groot_rms_norm.argtypes = [_i32, _vp, _i64, _vp, _i64, _vp, _f64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i32, _vp]
+_lib.groot_rms_norm_backward_workspace.argtypes = [_i32, _i64, _i32, _psize]
+_lib.groot_rms_norm_backward.argtypes = [_i32, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _i32, _vp, ctypes.c_size_t, _vp]
 _lib.groot_set_tuning.argtypes = [ctypes.c_char_p, _i64]
 _lib.groot_last_error.argtypes = []
 _lib.groot_last_error.restype = ctypes.c_char_p
@@ -845,3 +856,174 @@ def groot_adamw_step(tensors: AdamwTensors, step: int, lr: float, beta1: float =
         gs = _dev_ptr(grad_scale, "grad_scale")
     _check(_lib.groot_adamw_step(tensors.address, tensors.count, tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, step, lr,
                                  beta1, beta2, eps, weight_decay, gs, seed & 0xFFFFFFFF, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# routing rows to experts, the root-mean-square norm
+# ---------------------------------------------------------------------------------------------------------------
+GROOT_I8 = 3
+GROOT_SOFTMAX, GROOT_SIGMOID = range(2)
+_int32 = torch.int32
+
+
+def _launch_stream(stream, *tensors):
+    """The handle of a stream, by default of the current one.  The kernels run on the current device: a tensor or a stream of another
+    one is refused.  (None is no tensor.)"""
+    d = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != d:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {d}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(d)
+    if stream.device_index != d:
+        raise ValueError(f"the stream is of device {stream.device_index}, the current device is {d}")
+    return stream.cuda_stream
+
+
+def _rows_or_none(t, what, n, width, dtype):
+    return (None, width) if t is None else _rows(t, what, n, width, dtype)
+
+
+def _bytes_of(workspace):
+    """Pointer and size of a workspace; None has none."""
+    if workspace is None:
+        return None, 0
+    if not isinstance(workspace, _Tensor) or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def groot_route_workspace(n_rows: int, n_experts: int, top_k: int) -> int:
+    """Bytes of device workspace that groot_route needs (0: none)."""
+    b = ctypes.c_size_t(0)
+    _check(_lib.groot_route_workspace(n_rows, n_experts, top_k, ctypes.byref(b)))
+    return b.value
+
+
+def groot_route(scores, bias, experts, weights, places, offsets, workspace, gate: int = GROOT_SOFTMAX, sets: int = 1, open_sets: int = 1,
+                set_best: int = 1, renormalise: bool = True, factor: float = 1.0, stream=None) -> None:
+    """The top k experts of every row, their weights, and every choice's place in the order of the experts.  scores [n, experts],
+    bias float32 [experts] or None (counts for the choice only), experts and places int32 [n, k], weights float32 [n, k], offsets int64
+    [experts + 1]; workspace: a contiguous CUDA tensor of at least groot_route_workspace(n, experts, k) bytes, or None where that is 0.
+    gate: GROOT_SOFTMAX or GROOT_SIGMOID; sets, open_sets, set_best: the choice is among the open_sets of `sets` sets of neighbouring
+    experts whose set_best best experts come to most; renormalise: weights over their sum; factor: times this."""
+    d = _dtype(scores, "scores")
+    n, E = _matrix_rows(scores, "scores"), scores.shape[1]
+    _matrix_rows(experts, "experts")
+    k = experts.shape[1]
+    s, ss = _rows(scores, "scores", n, E, scores.dtype)
+    ws, size = _bytes_of(workspace)
+    _check(_lib.groot_route(d, s, ss, _array(bias, "bias", (E,), _float32), gate, sets, open_sets, set_best, 1 if renormalise else 0, factor,
+                            _array(experts, "experts", (n, k), _int32), _array(weights, "weights", (n, k), _float32),
+                            _array(places, "places", (n, k), _int32), _array(offsets, "offsets", (E + 1,), _int64), n, E, k, ws, size,
+                            _launch_stream(stream, scores, bias, experts, weights, places, offsets, workspace)))
+
+
+def groot_route_backward(scores, experts, dweights, dscores, gate: int = GROOT_SOFTMAX, renormalise: bool = True, factor: float = 1.0,
+                         stream=None) -> None:
+    """dscores [n, experts] from the gradient of the weights (dweights float32 [n, k]); the other arguments as in groot_route, experts as
+    it gave them."""
+    d, T = _dtype(scores, "scores"), scores.dtype
+    n, E = _matrix_rows(scores, "scores"), scores.shape[1]
+    _matrix_rows(experts, "experts")
+    k = experts.shape[1]
+    s, ss = _rows(scores, "scores", n, E, T)
+    g, gs = _rows(dscores, "dscores", n, E, T)
+    _check(_lib.groot_route_backward(d, s, ss, gate, 1 if renormalise else 0, factor, _array(experts, "experts", (n, k), _int32),
+                                     _array(dweights, "dweights", (n, k), _float32), g, gs, n, E, k,
+                                     _launch_stream(stream, scores, experts, dweights, dscores)))
+
+
+def groot_routed_rows(X, places, R, x_scale=None, r_scale=None, stream=None) -> None:
+    """R[places[i, s]] = X[i].  X [n, width] and R [places, width] of one type (int8 too), places int32 [n, k] as groot_route gave them;
+    x_scale float32 [n] and r_scale float32 [places] (both or none): a scale that goes with each row."""
+    T = X.dtype if isinstance(X, _Tensor) else None
+    d = GROOT_I8 if T is _int8 else _dtype(X, "X")
+    n, width = _matrix_rows(X, "X"), X.shape[1]
+    m = _matrix_rows(R, "R")
+    _matrix_rows(places, "places")
+    k = places.shape[1]
+    x, xs = _rows(X, "X", n, width, T)
+    r, rs = _rows(R, "R", m, width, T)
+    if (x_scale is None) != (r_scale is None):
+        raise ValueError("x_scale and r_scale go together")
+    _check(_lib.groot_routed_rows(d, x, xs, _array(x_scale, "x_scale", (n,), _float32), _array(places, "places", (n, k), _int32), k, r, rs,
+                                  _array(r_scale, "r_scale", (m,), _float32), n, m, width,
+                                  _launch_stream(stream, X, places, R, x_scale, r_scale)))
+
+
+def groot_routed_sum(R, places, weights, addend, out, stream=None) -> None:
+    """out[i] = addend[i] + sum over s of weights[i, s] R[places[i, s]].  R [places, width], out and addend (or None) [n, width] of one
+    type, places int32 [n, k], weights float32 [n, k] or None (ones)."""
+    d, T = _dtype(R, "R"), R.dtype
+    m, width = _matrix_rows(R, "R"), R.shape[1]
+    n = _matrix_rows(places, "places")
+    k = places.shape[1]
+    r, rs = _rows(R, "R", m, width, T)
+    a, as_ = _rows_or_none(addend, "addend", n, width, T)
+    o, os_ = _rows(out, "out", n, width, T)
+    _check(_lib.groot_routed_sum(d, r, rs, _array(places, "places", (n, k), _int32), _array(weights, "weights", (n, k), _float32), a, as_, k, o, os_,
+                                 n, m, width, _launch_stream(stream, R, places, weights, addend, out)))
+
+
+def groot_routed_sum_backward(dout, R, places, weights, dR, dweights, stream=None) -> None:
+    """dR[places[i, s]] = weights[i, s] dout[i], dweights[i, s] = dout[i] . R[places[i, s]].  dout [n, width], R and dR [places, width] of
+    one type, weights (or None for ones) and dweights float32 [n, k].  dR or dweights may be None, and R where dweights is."""
+    d, T = _dtype(dout, "dout"), dout.dtype
+    n, width = _matrix_rows(dout, "dout"), dout.shape[1]
+    _matrix_rows(places, "places")
+    k = places.shape[1]
+    if dR is None and dweights is None:
+        raise ValueError("dR or dweights must be given")
+    if R is None and dweights is not None:
+        raise ValueError("dweights needs R")
+    m = _matrix_rows(R if R is not None else dR, "R or dR")
+    g, gs = _rows(dout, "dout", n, width, T)
+    r, rs = _rows_or_none(R, "R", m, width, T)
+    o, os_ = _rows_or_none(dR, "dR", m, width, T)
+    _check(_lib.groot_routed_sum_backward(d, g, gs, r, rs, _array(places, "places", (n, k), _int32), _array(weights, "weights", (n, k), _float32), k,
+                                          o, os_, _array(dweights, "dweights", (n, k), _float32), n, m, width,
+                                          _launch_stream(stream, dout, R, places, weights, dR, dweights)))
+
+
+def groot_rms_norm(X, residual, gain, eps: float, Y, H=None, Q=None, q_scale=None, rstd=None, stream=None) -> None:
+    """h = X + residual, Y = h / sqrt(mean h^2 + eps) gain.  X, residual (or None), Y, H (the rows h) [n, width] of one type, gain [width] of
+    that type or None; Q int8 [n, width] and q_scale float32 [n]: the output cut to 8 bits, as groot_quantize_rows does; rstd float32 [n]
+    for the backward call.  Outputs that are None are not written; H and Y may be X or residual themselves."""
+    d, T = _dtype(X, "X"), X.dtype
+    n, width = _matrix_rows(X, "X"), X.shape[1]
+    x, xs = _rows(X, "X", n, width, T)
+    r, rs = _rows_or_none(residual, "residual", n, width, T)
+    h, hs = _rows_or_none(H, "H", n, width, T)
+    y, ys = _rows_or_none(Y, "Y", n, width, T)
+    q, qs = _rows_or_none(Q, "Q", n, width, _int8)
+    _check(_lib.groot_rms_norm(d, x, xs, r, rs, _array(gain, "gain", (width,), T), eps, h, hs, y, ys, q, qs,
+                               _array(q_scale, "q_scale", (n,), _float32), _array(rstd, "rstd", (n,), _float32), n, width,
+                               _launch_stream(stream, X, residual, gain, Y, H, Q, q_scale, rstd)))
+
+
+def groot_rms_norm_backward_workspace(n_rows: int, width: int, dtype) -> int:
+    """Bytes of device workspace that groot_rms_norm_backward needs for the gain's gradient."""
+    b = ctypes.c_size_t(0)
+    if dtype not in _DTYPES:
+        raise TypeError("dtype must be float32, bfloat16 or float16")
+    _check(_lib.groot_rms_norm_backward_workspace(_DTYPES[dtype], n_rows, width, ctypes.byref(b)))
+    return b.value
+
+
+def groot_rms_norm_backward(H, rstd, gain, dY, dX, dgain, workspace, dH=None, stream=None) -> None:
+    """dX = the gradient of X and of the residual alike, dgain [width] (of H's type or float32, or None) that of the gain.  H [n, width]: the
+    rows h that groot_rms_norm gave (X where there was no residual), rstd float32 [n] from the same call, dY [n, width], dH [n, width] or
+    None: the gradient that comes to h by another way.  workspace: a contiguous CUDA tensor of at least
+    groot_rms_norm_backward_workspace(n, width, H.dtype) bytes, or None where dgain is."""
+    d, T = _dtype(H, "H"), H.dtype
+    gd = d if dgain is None else _dtype(dgain, "dgain")
+    n, width = _matrix_rows(H, "H"), H.shape[1]
+    h, hs = _rows(H, "H", n, width, T)
+    y, ys = _rows(dY, "dY", n, width, T)
+    e, es = _rows_or_none(dH, "dH", n, width, T)
+    x, xs = _rows(dX, "dX", n, width, T)
+    ws, size = _bytes_of(workspace)
+    _check(_lib.groot_rms_norm_backward(d, h, hs, _array(rstd, "rstd", (n,), _float32), _array(gain, "gain", (width,), T), y, ys, e, es, x, xs, gd,
+                                        None if dgain is None else _array(dgain, "dgain", (width,), dgain.dtype), n, width, ws, size,
+                                        _launch_stream(stream, H, rstd, gain, dY, dH, dX, dgain, workspace)))

@@ -57,4 +57,83 @@ constexpr int kAdamwBlock = 256;         // values that share a scale
 int launch_adamw(const groot_adamw_tensor *tensors, int64_t n_tensors, int32_t param_dtype, int32_t grad_dtype, int32_t state_bits,
                  const AdamwFactors &f, const float *grad_scale, uint32_t step, uint32_t seed, void *stream);
 
+struct RouteArgs {
+    const void *scores;
+    int64_t score_bytes;         // from row to row
+    const float *bias;           // [E] or NULL
+    int32_t *experts;            // [n, k]
+    float *weights;              // [n, k]
+    int32_t *places;             // [n, k]
+    int64_t *offsets;            // [E + 1]
+    int64_t n;
+    int32_t dtype, E, k, gate, sets, open_sets, set_best;
+    bool renormalise;
+    bool by_value;               // the choice goes by probability + bias, not by the score
+    float factor;
+    int32_t values_at;           // byte of the workgroup's LDS (the launcher's)
+};
+size_t route_workspace(int64_t n, int32_t E);
+int launch_route(const RouteArgs &a, void *workspace, void *stream);
+
+struct RouteBackwardArgs {
+    const void *scores;
+    int64_t score_bytes;
+    const int32_t *experts;
+    const float *dweights;
+    void *dscores;
+    int64_t ds_bytes;
+    int64_t n;
+    int32_t dtype, E, k, gate;
+    bool renormalise;
+    float factor;
+};
+int launch_route_backward(const RouteBackwardArgs &a, void *stream);
+
+// rows at places[i, s] of R, which has `n_places` rows; a place outside is none
+struct RoutedArgs {
+    const void *X;               // [n, K]: rows to copy, or the gradient of the sum
+    int64_t x_stride;            // elements
+    const void *R;               // [n_places, K]
+    int64_t r_stride;
+    const int32_t *places;       // [n, k]
+    const float *weights;        // [n, k] or NULL for ones
+    const void *addend;          // [n, K] or NULL
+    int64_t addend_stride;
+    void *out;                   // [n, K], or [n_places, K]
+    int64_t out_stride;
+    const float *scale_in;       // [n] or NULL
+    float *scale_out;            // [n_places]
+    float *dweights;             // [n, k] or NULL
+    int64_t n, n_places;
+    int32_t k, K;
+};
+int launch_routed_rows(int32_t bytes, const RoutedArgs &a, void *stream);
+int launch_routed_sum(int32_t dtype, const RoutedArgs &a, void *stream);
+int launch_routed_sum_backward(int32_t dtype, const RoutedArgs &a, void *stream);
+
+struct NormArgs {
+    const void *X, *residual, *gain;         // residual, gain: or NULL
+    void *H, *Y;                             // or NULL
+    int8_t *Q;                               // or NULL
+    float *q_scale, *rstd;                   // rstd: or NULL
+    int64_t x_stride, residual_stride, h_stride, y_stride, q_stride;
+    int64_t n;
+    int32_t K;
+    double eps;
+};
+int launch_norm(int32_t dtype, const NormArgs &a, void *stream);
+
+struct NormBackwardArgs {
+    const void *H, *gain, *dY, *dH;          // gain, dH: or NULL
+    const float *rstd;
+    void *dX, *dgain;                        // dgain: or NULL
+    bool grad_f32;
+    int64_t h_stride, dy_stride, dh_stride, dx_stride;
+    int64_t n;
+    int32_t K;
+    float *partial;                          // [groups of rows, K]
+};
+size_t norm_backward_workspace(int32_t dtype, int64_t n, int32_t K);
+int launch_norm_backward(int32_t dtype, const NormBackwardArgs &a, void *stream);
+
 }  // namespace groot
