@@ -70,9 +70,10 @@ struct RouteArgs {
     bool renormalise;
     bool by_value;               // the choice goes by probability + bias, not by the score
     float factor;
-    int32_t values_at;           // byte of the workgroup's LDS (the launcher's)
+    int32_t set_lanes;           // lanes that hold a set, 0: it begins anywhere (the launcher's)
+    int32_t value_bytes;         // of LDS for the sets
 };
-size_t route_workspace(int64_t n, int32_t E);
+size_t route_workspace(int64_t n, int32_t E, int32_t k);
 int launch_route(const RouteArgs &a, void *workspace, void *stream);
 
 struct RouteBackwardArgs {

@@ -1,22 +1,30 @@
 // The choice of experts for every row, their weights, and every choice's place in the order of the experts.
 //   value c of an expert: its score where that orders as the probability does, otherwise softmax or sigmoid of the score, plus a bias
 //   top k of c (ties to the lowest expert) among the sets whose best members' sum is largest; weights factor x p, renormalised or not
-// A call cannot do without n E scores and 12 n k bytes of results.  Values that decide are compared in 64 bits, as an expert's number is
-// a whole one whatever lies next to it.
+// A call cannot do without n E scores and 12 n k bytes of results.  The scores are read once; what bounds the kernel is the search, in
+// instructions.
 //
-// Places: workgroups take kRouteRows rows each.  A row chooses an expert once, so the rows of a workgroup that chose an expert are the bits
-// of one 64-bit word, and a choice's rank is the number of bits below its row's: nothing depends on the order of atomics.  The ranks
+// The search: a key is a number of 64 bits, the value with the expert's number in its last ten bits, so that one comparison decides and
+// breaks ties (a score of fp32 leaves 29 bits free; a probability computed in 64 bits keeps 42, and what agrees in these counts as tied).
+// A lane has kEach = 16 neighbouring experts and sorts them by a network of minima and maxima; lists of the kList best then meet between
+// lanes: the larger of a list and the other one's reverse are the best of both, and a merging network sorts them.  Every lane of a row ends
+// with the row's list.
+//
+// Places: a workgroup takes 64 `words` rows.  A row chooses an expert once, so the rows of a workgroup that chose an expert are bits of
+// a few 64-bit words, and a choice's rank is the number of bits below its row's: nothing depends on the order of atomics.  The ranks
 // wait in `places` until the counts of all workgroups are known.
-#include <cfloat>
-
-#include "groot_dense_device.h"
+#include "groot_tile.h"
 
 namespace groot {
 
 namespace {
 
-constexpr int kRouteRows = 64;               // rows of a workgroup: bits of a word
+constexpr int kWordRows = 64;                // rows of a workgroup that a word holds
+constexpr int kNumberBits = 10;              // of an expert in a key
+constexpr uint32_t kNumbers = (1u << kNumberBits) - 1;
+constexpr int kSumGroups = 256;              // workgroups whose counts every workgroup of the second launch adds up by itself
 constexpr float kInf = __builtin_inff();
+constexpr double kClosed = -0x1p1023, kLeastOpen = -0x1p1022, kMostOpen = 0x1p1022;
 
 __device__ __forceinline__ float score_at(const void *row, int32_t dtype, int32_t e)
 {
@@ -25,45 +33,143 @@ __device__ __forceinline__ float score_at(const void *row, int32_t dtype, int32_
     return (float)((const f16_t *)row)[e];
 }
 
-template <int kLanes>
-__device__ __forceinline__ double top_of(double x)
+// the value of lane ^ (kAway, or the other lanes of twice as many that hold the same), for rows of lanes whose lower halves agree
+template <int kAway>
+__device__ __forceinline__ uint32_t other_lane(uint32_t x)
 {
-#pragma unroll
-    for (int d = 1; d < kLanes; d *= 2) x = fmax(x, __shfl_xor(x, d));
-    return x;
+    if constexpr (kAway == 1) return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false);        // quad_perm 1 0 3 2
+    else if constexpr (kAway == 2) return __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, false);   // quad_perm 2 3 0 1
+    else if constexpr (kAway == 4) return __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, false);  // row_half_mirror
+    else if constexpr (kAway == 8) return __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, false);  // row_mirror
+    else return __shfl_xor(x, kAway);
 }
-template <int kLanes>
-__device__ __forceinline__ double sum_of(double x)
+template <int kAway>
+__device__ __forceinline__ float other_lane(float x)
 {
-#pragma unroll
-    for (int d = 1; d < kLanes; d *= 2) x += __shfl_xor(x, d);
-    return x;
+    return __uint_as_float(other_lane<kAway>(__float_as_uint(x)));
 }
-template <int kLanes>
-__device__ __forceinline__ int32_t least_of(int32_t x)
+template <int kAway>
+__device__ __forceinline__ double other_lane(double x)
 {
-#pragma unroll
-    for (int d = 1; d < kLanes; d *= 2) {
-        const int32_t o = __shfl_xor(x, d);
-        x = o < x ? o : x;
-    }
-    return x;
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)other_lane<kAway>((uint32_t)(b >> 32)) << 32 | other_lane<kAway>((uint32_t)b));
 }
-// whether any of the row's lanes says so
+// over kLanes lanes, every one of which takes part
+template <int kLanes, int kAway = 1, typename T, typename F>
+__device__ __forceinline__ T over_lanes(T x, F both)
+{
+    if constexpr (kAway < kLanes) return over_lanes<kLanes, kAway * 2>(both(x, other_lane<kAway>(x)), both);
+    else return x;
+}
+template <int kLanes, typename T>
+__device__ __forceinline__ T top_of(T x)
+{
+    return over_lanes<kLanes>(x, [](T a, T b) { return a > b ? a : b; });
+}
+template <int kLanes, typename T>
+__device__ __forceinline__ T sum_of(T x)
+{
+    return over_lanes<kLanes>(x, [](T a, T b) { return a + b; });
+}
 template <int kLanes>
 __device__ __forceinline__ bool any_of(bool x)
 {
-    const uint64_t all = __ballot(x);
-    const int first = threadIdx.x % kWave / kLanes * kLanes;
-    return (all >> first & (kLanes == kWave ? ~0ull : (1ull << (kLanes % kWave)) - 1)) != 0;
+    return over_lanes<kLanes>((uint32_t)x, [](uint32_t a, uint32_t b) { return a | b; }) != 0;
 }
 
-__device__ __forceinline__ double log_sigmoid(double x) { return fmin(x, 0.0) - log1p(exp(-fabs(x))); }
+// e^x for x <= 0 to 2^-50 of itself: x = i log 2 + r, |r| <= log 2 / 2, and r's series up to r^12 / 12! (the next term is 2^-52)
+__device__ __forceinline__ double exp64(double x)
+{
+    x = fmax(x, -760.0);                                     // e^x is 0 there
+    const double i = __builtin_rint(x * 0x1.71547652b82fep+0);
+    double r = __builtin_fma(-i, 0x1.62e42fefa2000p-1, x);     // log 2 in two parts, i times the first is exact
+    r = __builtin_fma(-i, 0x1.9ef35793c7673p-41, r);
+    double p = 1.0 / 479001600;
+    p = __builtin_fma(p, r, 1.0 / 39916800);
+    p = __builtin_fma(p, r, 1.0 / 3628800);
+    p = __builtin_fma(p, r, 1.0 / 362880);
+    p = __builtin_fma(p, r, 1.0 / 40320);
+    p = __builtin_fma(p, r, 1.0 / 5040);
+    p = __builtin_fma(p, r, 1.0 / 720);
+    p = __builtin_fma(p, r, 1.0 / 120);
+    p = __builtin_fma(p, r, 1.0 / 24);
+    p = __builtin_fma(p, r, 1.0 / 6);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    return ldexp(p, (int)i);
+}
 
-// Exclusive sums of the workgroup's first E words of LDS, in place; the sum of all goes to word E.
+// The weight of a score up to a factor that the row shares.  softmax: e^(s - m), m the largest score.  sigmoid: e^min(s, 0) / (1 + e^-|s|),
+// with e^(min(s, 0) - m) in its place where weights are renormalised, so that low scores keep their ratios.
+__device__ __forceinline__ float weight_of(float s, float m, bool sigmoid)
+{
+    const float e = __expf((sigmoid ? fminf(s, 0.f) : s) - m);
+    return sigmoid ? e / (1.f + __expf(-__builtin_fabsf(s))) : e;
+}
+
+// the value with the number in its last bits, so that of equal values the lower number is the larger key
+__device__ __forceinline__ double key_of(double c, uint32_t number, uint32_t numbers)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, c);
+    const uint32_t low = (b >> 63) ? number : numbers - number;
+    return __builtin_bit_cast(double, (b & ~(uint64_t)numbers) | low);
+}
+__device__ __forceinline__ uint32_t number_of(double key, uint32_t numbers)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, key);
+    const uint32_t low = (uint32_t)b & numbers;
+    return (b >> 63) ? low : numbers - low;
+}
+
+__device__ __forceinline__ void order(double &a, double &b)  // descending
+{
+    const double most = fmax(a, b), least = fmin(a, b);
+    a = most;
+    b = least;
+}
+// Batcher's odd-even merge sort of kCount neighbouring keys, descending
+template <int kCount>
+__device__ __forceinline__ void sort_keys(double *x)
+{
+#pragma unroll
+    for (int p = 1; p < kCount; p *= 2)
+#pragma unroll
+        for (int d = p; d >= 1; d /= 2)
+#pragma unroll
+            for (int j = d % p; j + d < kCount; j += 2 * d)
+#pragma unroll
+                for (int i = 0; i < d; ++i)
+                    if (i + j + d < kCount && (i + j) / (2 * p) == (i + j + d) / (2 * p)) order(x[i + j], x[i + j + d]);
+}
+// x: the kCount largest of two descending lists, descending
+template <int kCount>
+__device__ __forceinline__ void merge_keys(double *x, const double *y)
+{
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) x[i] = fmax(x[i], y[kCount - 1 - i]);
+#pragma unroll
+    for (int d = kCount / 2; d >= 1; d /= 2)
+#pragma unroll
+        for (int i = 0; i < kCount; ++i)
+            if (!(i & d)) order(x[i], x[i + d]);
+}
+template <int kLanes, int kCount, int kAway = 1>
+__device__ __forceinline__ void merge_lanes(double *x)
+{
+    if constexpr (kAway < kLanes) {
+        double y[kCount];
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) y[i] = other_lane<kAway>(x[i]);
+        merge_keys<kCount>(x, y);
+        merge_lanes<kLanes, kCount, kAway * 2>(x);
+    }
+}
+
+// Exclusive sums of E words of LDS, in place; the sum of all goes to word E.  `waves`: a word for every wavefront.
 __device__ __forceinline__ void exclusive_sums(int32_t *x, int32_t E, int32_t *waves)
 {
-    const int tid = threadIdx.x, lane = tid % kWave, per = (E + kBlock - 1) / kBlock;
+    const int tid = threadIdx.x, lane = tid % kWave, threads = blockDim.x, per = (E + threads - 1) / threads;
     int32_t mine = 0;
     for (int i = 0; i < per; ++i)
         if (tid * per + i < E) mine += x[tid * per + i];
@@ -83,163 +189,274 @@ __device__ __forceinline__ void exclusive_sums(int32_t *x, int32_t E, int32_t *w
             x[tid * per + i] = before;
             before += here;
         }
-    if (tid == kBlock - 1) x[E] = before;
+    if (tid == threads - 1) x[E] = before;
     __syncthreads();
 }
 
-// kLanes lanes to a row, kEach experts a lane (expert v kLanes + lane)
-template <int kLanes, int kEach>
-__global__ __launch_bounds__(kBlock) void route_kernel(RouteArgs a, int32_t *__restrict__ counts)
+constexpr int kMaxWaves = 16;
+
+// the workgroup's LDS, in bytes
+struct RouteLds {
+    int32_t mask, prefix, waves, weights, chosen, values, total;
+    __host__ __device__ RouteLds(int32_t E, int32_t words, int32_t k, int32_t value_bytes)
+    {
+        const int32_t slots = kWordRows * words * k;
+        mask = 0;                                            // uint64 [E, words]: the rows that chose an expert
+        values = mask + E * words * 8;                       // double: values of sets, or of experts
+        prefix = values + value_bytes;                       // int32 [E + 1]
+        waves = prefix + (E + 1) * 4;                        // int32 [kMaxWaves]
+        weights = waves + kMaxWaves * 4;                     // float [slots]
+        chosen = weights + slots * 4;                        // int16 [slots]
+        total = chosen + slots * 2;
+    }
+};
+
+// i / k for i below 2^13 and k up to 32: the quotient's error of i / 2^18 stays below 1 / k
+__device__ __forceinline__ int32_t over(int32_t i, uint32_t inverse) { return (int32_t)((uint32_t)i * inverse >> 18); }
+constexpr uint32_t inverse_of(int32_t k) { return ((1u << 18) + k - 1) / k; }
+
+// kLanes lanes to a row, kEach neighbouring experts a lane, lists of kList keys (top_k of up to that many; beyond 16 they are taken one by one)
+template <int kLanes, int kEach, int kList>
+__global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__restrict__ counts, int32_t words)
 {
-    constexpr int kAtOnce = kBlock / kLanes;
     extern __shared__ char lds[];
-    uint64_t *const mask = (uint64_t *)lds;                               // [E] the rows that chose an expert
-    int32_t *const prefix = (int32_t *)(mask + a.E);                      // [E + 1]
-    int32_t *const waves = prefix + a.E + 1;                              // [kWavesPerBlock]
-    int16_t *const chosen = (int16_t *)(waves + kWavesPerBlock);          // [kRouteRows, k]
-    double *const values = (double *)(lds + a.values_at) + threadIdx.x / kLanes * a.E;    // [E] of the row, where sets are ranked
-    const int lane = threadIdx.x % kLanes;
-    for (int e = threadIdx.x; e < a.E; e += kBlock) mask[e] = 0;
+    const RouteLds at(a.E, words, a.k, a.value_bytes);
+    unsigned long long *const mask = (unsigned long long *)(lds + at.mask);
+    int32_t *const prefix = (int32_t *)(lds + at.prefix), *const waves = (int32_t *)(lds + at.waves);
+    float *const weights = (float *)(lds + at.weights);
+    int16_t *const chosen = (int16_t *)(lds + at.chosen);
+    const int threads = blockDim.x, lane = threadIdx.x % kLanes, at_once = threads / kLanes, rows = kWordRows * words;
+    const bool sigmoid = a.gate == GROOT_SIGMOID;
+    for (int e = threadIdx.x; e < a.E * words; e += threads) mask[e] = 0;
     __syncthreads();
-    for (int local = threadIdx.x / kLanes; local < kRouteRows; local += kAtOnce) {
-        const int64_t row = (int64_t)blockIdx.x * kRouteRows + local;
-        const bool real = row < a.n;                                      // the lanes of a row go together, rows beyond the last idle
-        const char *const scores = (const char *)a.scores + (real ? row : 0) * a.score_bytes;
-        double x[kEach];
+    const int64_t first = (int64_t)blockIdx.x * rows;
+    const int here = (int)(a.n - first < rows ? a.n - first : rows);      // rows of this workgroup
+    const int32_t begin = lane * kEach;
+    for (int pass = 0; pass < here; pass += at_once) {
+        const int local = pass + threadIdx.x / kLanes;
+        const bool real = local < here;                                   // rows beyond the last go along
+        const char *const scores = (const char *)a.scores + (first + (real ? local : here - 1)) * a.score_bytes;
+        float s[kEach];
+        auto load = [&](auto type) {
+            typedef decltype(type) T;
+            constexpr int kPer = 16 / sizeof(T);
+            const bool short_row = a.E < kPer;
+#pragma unroll
+            for (int i = 0; i < kEach / kPer; ++i) {
+                const int32_t e = begin + i * kPer;
+                const RowValues<T> v = row_values<T>(load16<T>(scores + e * (int)sizeof(T), (int64_t)(a.E - e) * (int)sizeof(T), short_row));
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) s[i * kPer + j] = e + j < a.E ? v.x[j] : -kInf;
+            }
+        };
+        if (a.dtype == GROOT_F32) load(float{});
+        else if (a.dtype == GROOT_BF16) load(bf16_t{});
+        else load(f16_t{});
+        float top = -kInf;
         bool broken = false;
-        double top = -kInf;
 #pragma unroll
         for (int v = 0; v < kEach; ++v) {
-            const int32_t e = v * kLanes + lane;
-            const float s = real && e < a.E ? score_at(scores, a.dtype, e) : -kInf;
-            broken |= s != s || (a.gate == GROOT_SOFTMAX && s == kInf);
-            x[v] = s;
-            top = fmax(top, x[v]);                                        // a NaN is passed over: the row is broken
+            broken |= s[v] != s[v];
+            top = fmaxf(top, s[v]);                                       // a NaN is passed over: the row is broken
         }
-        broken = any_of<kLanes>(broken);
         top = top_of<kLanes>(top);
-        const double base = top == -kInf ? 0.0 : top;
-        double sum = 0;
-        if (a.gate == GROOT_SOFTMAX && (a.by_value || !a.renormalise)) {
+        broken = any_of<kLanes>(broken) || (!sigmoid && top == kInf);
+        const float base = sigmoid || top == -kInf ? 0.f : top;
+        float sum = 1.f;                                                  // of e^(s - base), where weights go by it
+        double x[kEach];
+        if (!a.by_value) {
+            if (!sigmoid && !a.renormalise) {
+                sum = 0.f;
 #pragma unroll
-            for (int v = 0; v < kEach; ++v) sum += exp(x[v] - base);
-            sum = sum_of<kLanes>(sum);
-        }
-        auto probability = [&](double s) { return a.gate == GROOT_SOFTMAX ? exp(s - base) / sum : 1.0 / (1.0 + exp(-s)); };
-        if (a.by_value) {
+                for (int v = 0; v < kEach; ++v) sum += __expf(s[v] - base);
+                sum = sum_of<kLanes>(sum);
+            }
 #pragma unroll
             for (int v = 0; v < kEach; ++v) {
-                const int32_t e = v * kLanes + lane;
-                double c = probability(x[v]);
-                if (a.bias && e < a.E) c += (double)a.bias[e];
-                x[v] = x[v] == -kInf || !(c > -kInf) ? -(double)kInf : c;  // closed
+                const double c = fmin((double)(s[v] + 0.f), kMostOpen);   // -0 is 0
+                x[v] = s[v] == -kInf || broken ? kClosed : c;
             }
-        }
-        if (broken) {
+        } else {
+            double all = 0;
 #pragma unroll
-            for (int v = 0; v < kEach; ++v) x[v] = -kInf;
+            for (int v = 0; v < kEach; ++v) {
+                x[v] = exp64(sigmoid ? -__builtin_fabs((double)s[v]) : (double)s[v] - (double)base);
+                all += x[v];
+            }
+            if (!sigmoid) {
+                all = sum_of<kLanes>(all);
+                sum = (float)all;
+                all = 1.0 / all;
+            }
+#pragma unroll
+            for (int v = 0; v < kEach; ++v) {
+                double c = sigmoid ? (s[v] < 0.f ? x[v] : 1.0) / (1.0 + x[v]) : x[v] * all;
+                if (a.bias) c += begin + v < a.E ? (double)a.bias[begin + v] : 0.0;
+                const bool open = s[v] > -kInf && c > -__builtin_inf() && !broken;
+                x[v] = open ? fmin(c, kMostOpen) : kClosed;
+            }
         }
         if (a.open_sets < a.sets) {                                       // the same for all rows
             const int32_t size = a.E / a.sets;
+            // the values that a row's sets come to, the set's number in each; a set counts as many others as are above it
+            if (a.set_lanes) {                                            // a set is all of a few lanes' experts
+                double *const values = (double *)(lds + at.values) + threadIdx.x / kLanes * a.sets;
+                double most = kClosed, second = kClosed;
 #pragma unroll
-            for (int v = 0; v < kEach; ++v)
-                if (v * kLanes + lane < a.E) values[v * kLanes + lane] = x[v];
-            wave_sync();
-            uint64_t open = 0;
-            double value = -kInf;                                         // of set `lane` (rows of 16 lanes: up to four sets a lane)
-            double held[kWave / kLanes];
+                for (int v = 0; v < kEach; ++v) {
+                    second = fmax(second, fmin(most, x[v]));
+                    most = fmax(most, x[v]);
+                }
+                auto meet = [&](double o1, double o2) {
+                    second = fmax(fmax(second, o2), fmin(most, o1));
+                    most = fmax(most, o1);
+                };
+                if (a.set_lanes > 1) meet(other_lane<1>(most), other_lane<1>(second));
+                if (a.set_lanes > 2) meet(other_lane<2>(most), other_lane<2>(second));
+                if (a.set_lanes > 4) meet(other_lane<4>(most), other_lane<4>(second));
+                if (a.set_lanes > 8) meet(other_lane<8>(most), other_lane<8>(second));
+                if (a.set_lanes > 16) meet(other_lane<16>(most), other_lane<16>(second));
+                const int32_t set = lane / a.set_lanes;
+                const double mine = key_of(a.set_best == 2 && second > kLeastOpen ? fmin(most + second, kMostOpen) : most, (uint32_t)set, 63);
+                if (set < a.sets && lane % a.set_lanes == 0) values[set] = mine;
+                wave_sync();
+                int32_t above = 0;
+                for (int32_t i = 0; i < a.sets; ++i) above += values[i] > mine;
+                wave_sync();                                              // before the next rows' values
+                if (above >= a.open_sets) {
 #pragma unroll
-            for (int h = 0; h < kWave / kLanes; ++h) {
-                const int32_t set = h * kLanes + lane;
-                double first = -kInf, second = -kInf;
-                if (set < a.sets)
+                    for (int v = 0; v < kEach; ++v) x[v] = kClosed;
+                }
+            } else {
+                double *const values = (double *)(lds + at.values) + (int64_t)(threadIdx.x / kLanes) * (kLanes * kEach + a.sets), *const row = values + a.sets;
+#pragma unroll
+                for (int v = 0; v < kEach; ++v) row[begin + v] = x[v];
+                wave_sync();
+                for (int32_t set = lane; set < a.sets; set += kLanes) {
+                    double most = kClosed, second = kClosed;
                     for (int32_t i = 0; i < size; ++i) {
-                        const double c = values[set * size + i];
-                        if (c > first) {
-                            second = first;
-                            first = c;
-                        } else if (c > second) {
-                            second = c;
-                        }
+                        const double c = row[set * size + i];
+                        second = fmax(second, fmin(most, c));
+                        most = fmax(most, c);
                     }
-                held[h] = a.set_best == 2 && second > -kInf ? first + second : first;
-            }
-            for (int32_t r = 0; r < a.open_sets; ++r) {
-                value = -kInf;
-                int32_t at = a.sets;
+                    values[set] = key_of(a.set_best == 2 && second > kLeastOpen ? fmin(most + second, kMostOpen) : most, (uint32_t)set, 63);
+                }
+                wave_sync();
+                for (int32_t set = lane; set < a.sets; set += kLanes) {
+                    const double mine = values[set];
+                    int32_t above = 0;
+                    for (int32_t i = 0; i < a.sets; ++i) above += values[i] > mine;
+                    if (above >= a.open_sets)
+                        for (int32_t i = 0; i < size; ++i) row[set * size + i] = kClosed;
+                }
+                wave_sync();
 #pragma unroll
-                for (int h = 0; h < kWave / kLanes; ++h) {
-                    const int32_t set = h * kLanes + lane;
-                    if (set < a.sets && !(open >> set & 1) && (at == a.sets || held[h] > value)) {
-                        value = held[h];
-                        at = set;
+                for (int v = 0; v < kEach; ++v) x[v] = begin + v < a.E ? row[begin + v] : kClosed;
+                wave_sync();
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < kEach; ++v) x[v] = key_of(x[v], (uint32_t)(begin + v), kNumbers);
+        // the lane's lists, the lane's list, the row's
+#pragma unroll
+        for (int v = 0; v < kEach; v += kList) sort_keys<kList>(x + v);
+#pragma unroll
+        for (int half = kEach / 2; half >= kList; half /= 2)
+#pragma unroll
+            for (int v = 0; v < half; v += kList) merge_keys<kList>(x + v, x + v + half);
+        const float nan = __builtin_nanf("");
+        if (kList < 16 || a.k <= 16) {
+            merge_lanes<kLanes, kList>(x);
+            float m = -kInf;
+            float w[kList];
+#pragma unroll
+            for (int i = 0; i < kList; ++i) {
+                const bool taken = i < a.k && x[i] > kLeastOpen;
+                float at_slot;
+                if (a.by_value) at_slot = taken ? score_at(scores, a.dtype, (int32_t)number_of(x[i], kNumbers)) : -kInf;
+                else at_slot = taken ? (float)__builtin_bit_cast(double, __builtin_bit_cast(uint64_t, x[i]) & ~(uint64_t)kNumbers) : -kInf;
+                w[i] = at_slot;
+                m = fmaxf(m, sigmoid ? fminf(at_slot, 0.f) : at_slot);
+            }
+            m = a.renormalise ? (m == -kInf ? 0.f : m) : base;
+            float all = 0.f;
+#pragma unroll
+            for (int i = 0; i < kList; ++i) {
+                w[i] = w[i] == -kInf ? 0.f : weight_of(w[i], m, sigmoid);
+                all += w[i];
+            }
+            const float scale = a.factor / (a.renormalise ? all : sum);
+#pragma unroll
+            for (int i = 0; i < kList; ++i)
+                if (real && i < a.k && i % kLanes == lane) {
+                    const bool taken = x[i] > kLeastOpen;
+                    const int32_t e = taken ? (int32_t)number_of(x[i], kNumbers) : -1;
+                    weights[local * a.k + i] = broken ? nan : taken ? w[i] * scale : 0.f;
+                    chosen[local * a.k + i] = (int16_t)e;
+                    if (taken) atomicOr(&mask[e * words + local / kWordRows], 1ull << local % kWordRows);
+                }
+        } else if constexpr (kList == 16 && kEach == 16) {                // the lists hold all of a lane's experts
+            float m = -kInf, all = 0.f;
+            for (int32_t slot = 0; slot < a.k; ++slot) {
+                const double best = top_of<kLanes>(x[0]);
+                const bool mine = x[0] == best;
+#pragma unroll
+                for (int v = 0; v + 1 < kEach; ++v) x[v] = mine ? x[v + 1] : x[v];
+                if (mine) x[kEach - 1] = kClosed;
+                const bool taken = best > kLeastOpen;
+                const float at_slot = taken ? score_at(scores, a.dtype, (int32_t)number_of(best, kNumbers)) : -kInf;
+                const float low = sigmoid ? fminf(at_slot, 0.f) : at_slot;
+                // the sum at the largest score so far
+                const float higher = a.renormalise ? fmaxf(m, low) : base;
+                if (taken && a.renormalise) {
+                    all = all * __expf(m - higher) + weight_of(at_slot, higher, sigmoid);
+                    m = higher;
+                }
+                if (real && lane == 0) {
+                    weights[local * a.k + slot] = at_slot;
+                    chosen[local * a.k + slot] = (int16_t)(taken ? (int32_t)number_of(best, kNumbers) : -1);
+                    if (taken) {
+                        const int32_t e = (int32_t)number_of(best, kNumbers);
+                        atomicOr(&mask[e * words + local / kWordRows], 1ull << local % kWordRows);
                     }
                 }
-                const double best = top_of<kLanes>(value);
-                open |= 1ull << least_of<kLanes>(value == best ? at : a.sets);   // open_sets < sets: there is one left
             }
+            m = a.renormalise ? m : base;
+            const float scale = a.factor / (a.renormalise ? all : sum);
             wave_sync();
-#pragma unroll
-            for (int v = 0; v < kEach; ++v) {
-                const int32_t e = v * kLanes + lane;
-                if (e < a.E && !(open >> (e / size) & 1)) x[v] = -kInf;
-            }
-        }
-        int32_t mine = -1;                                                // expert of slot `lane`
-        for (int32_t slot = 0; slot < a.k; ++slot) {
-            double value = x[0];
-            int32_t at = 0;
-#pragma unroll
-            for (int v = 1; v < kEach; ++v)
-                if (x[v] > value) {
-                    value = x[v];
-                    at = v;
+            if (real)
+                for (int32_t slot = lane; slot < a.k; slot += kLanes) {
+                    const float at_slot = weights[local * a.k + slot];
+                    weights[local * a.k + slot] = broken ? nan : at_slot == -kInf ? 0.f : weight_of(at_slot, m, sigmoid) * scale;
                 }
-            const double best = top_of<kLanes>(value);
-            const int32_t e = least_of<kLanes>(value == best ? at * kLanes + lane : a.E);
-            const bool taken = best > -kInf;                              // none is left otherwise
-#pragma unroll
-            for (int v = 0; v < kEach; ++v)
-                if (taken && v * kLanes + lane == e) x[v] = -kInf;
-            if (lane == slot) mine = taken ? e : -1;
+            wave_sync();
         }
-        // weights: lane = slot
-        const double s = mine >= 0 ? (double)score_at(scores, a.dtype, mine) : 0.0;
-        double w;
-        if (a.renormalise) {
-            const double u = mine < 0 ? -kInf : a.gate == GROOT_SOFTMAX ? s : log_sigmoid(s);
-            const double most = top_of<kLanes>(u);
-            const double q = mine < 0 ? 0.0 : exp(u - most);
-            w = q / sum_of<kLanes>(q);
-        } else {
-            w = probability(s);
-        }
-        w = broken ? (double)__builtin_nanf("") : mine < 0 ? 0.0 : (double)a.factor * w;
-        if (real && lane < a.k) {
-            a.experts[row * a.k + lane] = mine;
-            a.weights[row * a.k + lane] = (float)w;
-        }
-        if (lane < a.k) chosen[local * a.k + lane] = real ? mine : -1;
-        if (real && mine >= 0) atomicOr((unsigned long long *)&mask[mine], 1ull << local);
     }
     __syncthreads();
     const bool alone = gridDim.x == 1;
-    for (int e = threadIdx.x; e < a.E; e += kBlock) {
-        const int32_t count = __popcll(mask[e]);
+    for (int e = threadIdx.x; e < a.E; e += threads) {
+        int32_t count = 0;
+        for (int w = 0; w < words; ++w) count += __popcll(mask[e * words + w]);
         if (alone) prefix[e] = count;
         else counts[(int64_t)blockIdx.x * a.E + e] = count;
     }
-    __syncthreads();
     if (alone) {
+        __syncthreads();
         exclusive_sums(prefix, a.E, waves);
-        for (int e = threadIdx.x; e <= a.E; e += kBlock) a.offsets[e] = prefix[e];
+        for (int e = threadIdx.x; e <= a.E; e += threads) a.offsets[e] = prefix[e];
     }
-    const int64_t first = (int64_t)blockIdx.x * kRouteRows;
-    const int32_t entries = (int32_t)(a.n - first < kRouteRows ? a.n - first : kRouteRows) * a.k;
-    for (int32_t i = threadIdx.x; i < entries; i += kBlock) {
-        const int32_t e = chosen[i];
-        const int32_t rank = e < 0 ? -1 : __popcll(mask[e] & ((1ull << (i / a.k)) - 1));
-        a.places[first * a.k + i] = alone && e >= 0 ? prefix[e] + rank : rank;
+    const uint32_t inverse = inverse_of(a.k);
+    for (int32_t i = threadIdx.x; i < here * a.k; i += threads) {
+        const int32_t e = chosen[i], local = over(i, inverse);
+        int32_t place = -1;
+        if (e >= 0) {
+            place = alone ? prefix[e] : 0;
+            for (int w = 0; w < local / kWordRows; ++w) place += __popcll(mask[e * words + w]);
+            place += __popcll(mask[e * words + local / kWordRows] & ((1ull << local % kWordRows) - 1));
+        }
+        a.experts[first * a.k + i] = e;
+        a.weights[first * a.k + i] = weights[i];
+        a.places[first * a.k + i] = place;
     }
 }
 
@@ -269,22 +486,45 @@ __global__ __launch_bounds__(1024) void route_scan_kernel(int32_t *__restrict__ 
     if (wave == 0) counts[(int64_t)groups * E + e] = all;
 }
 
-// ranks -> places
-__global__ __launch_bounds__(kBlock) void route_place_kernel(RouteArgs a, const int32_t *__restrict__ counts, int32_t groups)
+// ranks -> places.  kScanned: the counts are those of the workgroups before, and the sums stand behind them; otherwise this
+// workgroup adds them up, its threads in as many parts as there are for each expert.
+template <bool kScanned>
+__global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a, const int32_t *__restrict__ counts, int32_t groups, int32_t rows)
 {
     extern __shared__ char lds[];
-    int32_t *const prefix = (int32_t *)lds, *const waves = prefix + a.E + 1;
-    const int32_t *const mine = counts + (int64_t)blockIdx.x * a.E, *const all = counts + (int64_t)groups * a.E;
-    for (int e = threadIdx.x; e < a.E; e += kBlock) prefix[e] = all[e];
+    int32_t *const prefix = (int32_t *)lds, *const before = prefix + a.E + 1, *const waves = before + a.E;
+    const int threads = blockDim.x;
+    if constexpr (kScanned) {
+        for (int e = threadIdx.x; e < a.E; e += threads) {
+            prefix[e] = counts[(int64_t)groups * a.E + e];
+            before[e] = counts[(int64_t)blockIdx.x * a.E + e];
+        }
+    } else {
+        for (int e = threadIdx.x; e < a.E; e += threads) prefix[e] = before[e] = 0;
+        __syncthreads();
+        const int parts = threads / a.E > 1 ? threads / a.E : 1;
+        for (int i = threadIdx.x; i < a.E * parts; i += threads) {
+            const int part = i / a.E, e = i - part * a.E;
+            int32_t all = 0, mine = 0;
+#pragma unroll 8
+            for (int32_t g = part; g < groups; g += parts) {
+                const int32_t c = counts[(int64_t)g * a.E + e];
+                all += c;
+                mine += g < (int32_t)blockIdx.x ? c : 0;
+            }
+            atomicAdd(&prefix[e], all);
+            atomicAdd(&before[e], mine);
+        }
+    }
     __syncthreads();
     exclusive_sums(prefix, a.E, waves);
     if (blockIdx.x == 0)
-        for (int e = threadIdx.x; e <= a.E; e += kBlock) a.offsets[e] = prefix[e];
-    const int64_t first = (int64_t)blockIdx.x * kRouteRows;
-    const int32_t entries = (int32_t)(a.n - first < kRouteRows ? a.n - first : kRouteRows) * a.k;
-    for (int32_t i = threadIdx.x; i < entries; i += kBlock) {
+        for (int e = threadIdx.x; e <= a.E; e += threads) a.offsets[e] = prefix[e];
+    const int64_t first = (int64_t)blockIdx.x * rows;
+    const int32_t entries = (int32_t)(a.n - first < rows ? a.n - first : rows) * a.k;
+    for (int32_t i = threadIdx.x; i < entries; i += threads) {
         const int32_t e = a.experts[first * a.k + i];
-        if (e >= 0) a.places[first * a.k + i] += prefix[e] + mine[e];
+        if (e >= 0) a.places[first * a.k + i] += prefix[e] + before[e];
     }
 }
 
@@ -365,20 +605,43 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
     }
 }
 
-int64_t route_groups(int64_t n) { return n <= kRouteRows ? 1 : (n + kRouteRows - 1) / kRouteRows; }
+// Rows of a workgroup, in words of 64: one, and more where the workgroups would be more than one launch adds up by itself.
+int32_t route_words(int64_t n, int32_t E, int32_t k)
+{
+    int32_t words = 1;
+    while (words < 4 && (n + kWordRows * words - 1) / (kWordRows * words) > kSumGroups && RouteLds(E, words * 2, k, 0).total <= 32 * 1024) words *= 2;
+    return words;
+}
+int64_t route_groups(int64_t n, int32_t words) { return n <= 0 ? 1 : (n + kWordRows * words - 1) / (kWordRows * words); }
 
-template <int kLanes, int kEach>
+template <int kLanes, int kEach, int kList>
 int route_launch(RouteArgs a, int32_t *counts, hipStream_t stream)
 {
-    const int64_t groups = route_groups(a.n);
-    size_t lds = a.E * sizeof(uint64_t) + (a.E + 1 + kWavesPerBlock) * sizeof(int32_t) + kRouteRows * a.k * sizeof(int16_t);
-    lds = (lds + 7) / 8 * 8;
-    a.values_at = (int32_t)lds;
-    if (a.open_sets < a.sets) lds += (size_t)(kBlock / kLanes) * a.E * sizeof(double);
-    route_kernel<kLanes, kEach><<<(uint32_t)groups, kBlock, lds, stream>>>(a, counts);
+    const int32_t words = route_words(a.n, a.E, a.k), rows = kWordRows * words;
+    const int64_t groups = route_groups(a.n, words);
+    int threads = rows * kLanes < 1024 ? rows * kLanes : 1024;
+    a.set_lanes = 0;
+    a.value_bytes = 0;
+    if (a.open_sets < a.sets) {
+        const int32_t size = a.E / a.sets, lanes = size / kEach;
+        if (size % kEach == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 32) {
+            a.set_lanes = lanes;
+            a.value_bytes = threads / kLanes * a.sets * 8;
+        } else {
+            auto bytes = [&] { return threads / kLanes * (kLanes * kEach + a.sets) * 8; };
+            while (threads > kWave && bytes() > 32 * 1024) threads /= 2;
+            a.value_bytes = bytes();
+        }
+    }
+    route_kernel<kLanes, kEach, kList><<<(uint32_t)groups, threads, RouteLds(a.E, words, a.k, a.value_bytes).total, stream>>>(a, counts, words);
     if (groups > 1) {
-        route_scan_kernel<<<(a.E + kWave - 1) / kWave, 1024, 0, stream>>>(counts, (int32_t)groups, a.E);
-        route_place_kernel<<<(uint32_t)groups, kBlock, (a.E + 1 + kWavesPerBlock) * sizeof(int32_t), stream>>>(a, counts, (int32_t)groups);
+        const size_t lds = (2 * a.E + 1 + kMaxWaves) * sizeof(int32_t);
+        if (groups > kSumGroups) {
+            route_scan_kernel<<<(a.E + kWave - 1) / kWave, 1024, 0, stream>>>(counts, (int32_t)groups, a.E);
+            route_place_kernel<true><<<(uint32_t)groups, kBlock, lds, stream>>>(a, counts, (int32_t)groups, rows);
+        } else {
+            route_place_kernel<false><<<(uint32_t)groups, 1024, lds, stream>>>(a, counts, (int32_t)groups, rows);
+        }
     }
     return (int)hipGetLastError();
 }
@@ -393,28 +656,42 @@ int backward_launch(const RouteBackwardArgs &a, hipStream_t stream)
 
 }  // namespace
 
-size_t route_workspace(int64_t n, int32_t E)
+size_t route_workspace(int64_t n, int32_t E, int32_t k)
 {
-    const int64_t groups = route_groups(n);
+    const int64_t groups = route_groups(n, route_words(n, E, k));
     return groups == 1 ? 0 : (size_t)(groups + 1) * E * sizeof(int32_t);
 }
 
-// 16 lanes a row while they hold its experts and slots, a wavefront otherwise
-#define GROOT_BY_EXPERTS(call)                                                                                                           \
-    if (a.E > 256 || a.k > 16) {                                                                                                         \
-        if (a.E <= 512) return call<64, 8>;                                                                                              \
-        return call<64, 16>;                                                                                                             \
-    }                                                                                                                                    \
-    if (a.E <= 16) return call<16, 1>;                                                                                                   \
-    if (a.E <= 32) return call<16, 2>;                                                                                                   \
-    if (a.E <= 64) return call<16, 4>;                                                                                                   \
-    if (a.E <= 128) return call<16, 8>;                                                                                                  \
-    return call<16, 16>;
-
+// 16 experts a lane (8 where there are no more), lists as long as top_k needs
 typedef int (*RouteLaunch)(RouteArgs, int32_t *, hipStream_t);
+template <int kLanes>
+static RouteLaunch route_of_lanes(const RouteArgs &a)
+{
+    return a.k <= 4 ? route_launch<kLanes, 16, 4> : a.k <= 8 ? route_launch<kLanes, 16, 8> : route_launch<kLanes, 16, 16>;
+}
+static RouteLaunch route_for(const RouteArgs &a)
+{
+    if (a.E <= 8) return a.k <= 4 ? route_launch<1, 8, 4> : route_launch<1, 8, 8>;
+    if (a.E <= 16) return route_of_lanes<1>(a);
+    if (a.E <= 32) return route_of_lanes<2>(a);
+    if (a.E <= 64) return route_of_lanes<4>(a);
+    if (a.E <= 128) return route_of_lanes<8>(a);
+    if (a.E <= 256) return route_of_lanes<16>(a);
+    if (a.E <= 512) return route_of_lanes<32>(a);
+    return route_of_lanes<64>(a);
+}
+
+// 16 lanes a row while they hold its experts and slots, a wavefront otherwise
 typedef int (*BackwardLaunch)(const RouteBackwardArgs &, hipStream_t);
-static RouteLaunch route_for(const RouteArgs &a) { GROOT_BY_EXPERTS(route_launch) }
-static BackwardLaunch backward_for(const RouteBackwardArgs &a) { GROOT_BY_EXPERTS(backward_launch) }
+static BackwardLaunch backward_for(const RouteBackwardArgs &a)
+{
+    if (a.E > 256 || a.k > 16) return a.E <= 512 ? backward_launch<64, 8> : backward_launch<64, 16>;
+    if (a.E <= 16) return backward_launch<16, 1>;
+    if (a.E <= 32) return backward_launch<16, 2>;
+    if (a.E <= 64) return backward_launch<16, 4>;
+    if (a.E <= 128) return backward_launch<16, 8>;
+    return backward_launch<16, 16>;
+}
 
 int launch_route(const RouteArgs &a, void *workspace, void *stream) { return route_for(a)(a, (int32_t *)workspace, (hipStream_t)stream); }
 int launch_route_backward(const RouteBackwardArgs &a, void *stream) { return backward_for(a)(a, (hipStream_t)stream); }
