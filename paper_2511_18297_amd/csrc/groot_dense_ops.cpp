@@ -327,7 +327,7 @@ extern "C" groot_status groot_route_workspace(int64_t n_rows, int32_t n_experts,
     const char *who = "groot_route_workspace";
     if (!bytes) return bad(who, "bytes is NULL");
     GROOT_TRY(check_gate(who, n_rows, n_experts, top_k, GROOT_SOFTMAX, 0, 1.0));
-    *bytes = route_workspace(n_rows, n_experts, top_k);
+    *bytes = route_workspace(n_rows, n_experts);
     return GROOT_OK;
 }
 
@@ -350,7 +350,7 @@ extern "C" groot_status groot_route(int32_t dtype, const void *scores_dev, int64
     GROOT_TRY(check_matrix(who, "places", places_dev, n_rows, top_k, top_k, 4));
     if (!offsets_dev || !aligned(offsets_dev, 8)) return bad(who, "offsets must be given and 8-byte aligned");
     if (!aligned(bias_dev, 4)) return bad(who, "bias is not aligned to its type");
-    const size_t need = route_workspace(n_rows, n_experts, top_k);
+    const size_t need = route_workspace(n_rows, n_experts);
     if (need && (!workspace_dev || workspace_bytes < need)) return bad(who, "workspace too small (ask groot_route_workspace)");
     if (!aligned(workspace_dev, 16)) return bad(who, "the workspace must be 16-byte aligned");
     const Span in(scores_dev, n_rows, score_stride, n_experts, b), bs(bias_dev, bias_dev ? 1 : 0, n_experts, n_experts, 4),
@@ -362,7 +362,7 @@ extern "C" groot_status groot_route(int32_t dtype, const void *scores_dev, int64
             if (out[i].meets(out[j])) return bad(who, "two of the outputs and the workspace overlap");
     }
     RouteArgs a{scores_dev, score_stride * b, bias_dev, experts_dev, weights_dev, places_dev, offsets_dev, n_rows, dtype, n_experts, top_k, gate,
-                n_sets, open_sets, set_best, renormalise != 0, bias_dev != nullptr || set_best == 2, (float)factor, 0, 0};
+                n_sets, open_sets, set_best, renormalise != 0, bias_dev != nullptr || set_best == 2, (float)factor, 0, 0, 0, false, 0};
     return launched(who, launch_route(a, workspace_dev, hip_stream));
 }
 

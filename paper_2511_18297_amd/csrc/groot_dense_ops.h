@@ -70,10 +70,14 @@ struct RouteArgs {
     bool renormalise;
     bool by_value;               // the choice goes by probability + bias, not by the score
     float factor;
-    int32_t set_lanes;           // lanes that hold a set, 0: it begins anywhere (the launcher's)
+    // the launcher's
+    int32_t rows;                // of a workgroup
+    uint32_t inverse_k;
+    int32_t set_lanes;           // lanes that hold a set, 0: it begins anywhere
+    bool small_sets;             // a lane holds 2, 4, 8 or 16 whole sets
     int32_t value_bytes;         // of LDS for the sets
 };
-size_t route_workspace(int64_t n, int32_t E, int32_t k);
+size_t route_workspace(int64_t n, int32_t E);
 int launch_route(const RouteArgs &a, void *workspace, void *stream);
 
 struct RouteBackwardArgs {

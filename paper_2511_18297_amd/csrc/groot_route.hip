@@ -10,16 +10,16 @@
 // lanes: the larger of a list and the other one's reverse are the best of both, and a merging network sorts them.  Every lane of a row ends
 // with the row's list.
 //
-// Places: a workgroup takes 64 `words` rows.  A row chooses an expert once, so the rows of a workgroup that chose an expert are bits of
-// a few 64-bit words, and a choice's rank is the number of bits below its row's: nothing depends on the order of atomics.  The ranks
-// wait in `places` until the counts of all workgroups are known.
+// Places: a workgroup takes up to 64 rows.  A row chooses an expert once, so the rows of a workgroup that chose an expert are the bits of
+// one 64-bit word, and a choice's rank is the number of bits below its row's: nothing depends on the order of atomics.  The ranks wait
+// in `places` until the counts of all workgroups are known.
 #include "groot_tile.h"
 
 namespace groot {
 
 namespace {
 
-constexpr int kWordRows = 64;                // rows of a workgroup that a word holds
+constexpr int kRouteRows = 64;               // rows of a workgroup at most: bits of a word
 constexpr int kNumberBits = 10;              // of an expert in a key
 constexpr uint32_t kNumbers = (1u << kNumberBits) - 1;
 constexpr int kSumGroups = 256;              // workgroups whose counts every workgroup of the second launch adds up by itself
@@ -77,6 +77,43 @@ __device__ __forceinline__ bool any_of(bool x)
     return over_lanes<kLanes>((uint32_t)x, [](uint32_t a, uint32_t b) { return a | b; }) != 0;
 }
 
+// The scores of a lane's kEach experts from `begin` on; -inf beyond the last.  Where the experts are whole pieces of 16 bytes, these are
+// loaded, otherwise value by value.
+template <int kEach, typename T>
+__device__ __forceinline__ void load_scores_of(const char *row, int32_t E, int32_t begin, float (&s)[kEach])
+{
+    constexpr int kPer = 16 / sizeof(T);
+    if (E % kPer == 0) {
+        v4i v[kEach / kPer];
+#pragma unroll
+        for (int i = 0; i < kEach / kPer; ++i) {
+            const int32_t e = begin + i * kPer;
+            __builtin_memcpy(&v[i], row + (e < E ? e : 0) * (int)sizeof(T), 16);
+        }
+#pragma unroll
+        for (int i = 0; i < kEach / kPer; ++i) {
+            const RowValues<T> x = row_values<T>(v[i]);
+            const bool there = begin + i * kPer < E;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) s[i * kPer + j] = there ? x.x[j] : -kInf;
+        }
+    } else {
+        T x[kEach];
+        asm("" : "+v"(begin));                               // the addresses are computed here and not, for all calls, in front
+#pragma unroll
+        for (int v = 0; v < kEach; ++v) x[v] = ((const T *)row)[begin + v < E ? begin + v : E - 1];
+#pragma unroll
+        for (int v = 0; v < kEach; ++v) s[v] = begin + v < E ? (float)x[v] : -kInf;
+    }
+}
+template <int kEach>
+__device__ __forceinline__ void load_scores(const char *row, const RouteArgs &a, int32_t begin, float (&s)[kEach])
+{
+    if (a.dtype == GROOT_F32) load_scores_of<kEach, float>(row, a.E, begin, s);
+    else if (a.dtype == GROOT_BF16) load_scores_of<kEach, bf16_t>(row, a.E, begin, s);
+    else load_scores_of<kEach, f16_t>(row, a.E, begin, s);
+}
+
 // e^x for x <= 0 to 2^-50 of itself: x = i log 2 + r, |r| <= log 2 / 2, and r's series up to r^12 / 12! (the next term is 2^-52)
 __device__ __forceinline__ double exp64(double x)
 {
@@ -100,6 +137,14 @@ __device__ __forceinline__ double exp64(double x)
     return ldexp(p, (int)i);
 }
 
+// 1 / x for x in [1, 2] to 2^-51: the instruction's approximation and two of Newton's steps, which square its error of 2^-14 at most
+__device__ __forceinline__ double reciprocal64(double x)
+{
+    double y = __builtin_amdgcn_rcp(x);
+    y = __builtin_fma(__builtin_fma(-x, y, 1.0), y, y);
+    return __builtin_fma(__builtin_fma(-x, y, 1.0), y, y);
+}
+
 // The weight of a score up to a factor that the row shares.  softmax: e^(s - m), m the largest score.  sigmoid: e^min(s, 0) / (1 + e^-|s|),
 // with e^(min(s, 0) - m) in its place where weights are renormalised, so that low scores keep their ratios.
 __device__ __forceinline__ float weight_of(float s, float m, bool sigmoid)
@@ -108,26 +153,54 @@ __device__ __forceinline__ float weight_of(float s, float m, bool sigmoid)
     return sigmoid ? e / (1.f + __expf(-__builtin_fabsf(s))) : e;
 }
 
-// the value with the number in its last bits, so that of equal values the lower number is the larger key
+// The value with the number in its last bits, so that of equal values the lower number is the larger key: its complement where the value
+// is positive, the number where it is negative.
 __device__ __forceinline__ double key_of(double c, uint32_t number, uint32_t numbers)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, c);
-    const uint32_t low = (b >> 63) ? number : numbers - number;
-    return __builtin_bit_cast(double, (b & ~(uint64_t)numbers) | low);
+    const uint32_t high = (uint32_t)(b >> 32), low = ((uint32_t)b & ~numbers) | (number ^ numbers ^ (uint32_t)((int32_t)high >> 31 & (int32_t)numbers));
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
 }
 __device__ __forceinline__ uint32_t number_of(double key, uint32_t numbers)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, key);
-    const uint32_t low = (uint32_t)b & numbers;
-    return (b >> 63) ? low : numbers - low;
+    return ((uint32_t)b ^ ~(uint32_t)((int64_t)b >> 63)) & numbers;
+}
+__device__ __forceinline__ float score_of(double key)        // a key of a score
+{
+    return (float)__builtin_bit_cast(double, __builtin_bit_cast(uint64_t, key) & ~(uint64_t)kNumbers);
 }
 
+// The instructions themselves: keys are no NaN, and the language's maximum puts another one in front of it to be sure.
+__device__ __forceinline__ double larger(double a, double b)
+{
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ double smaller(double a, double b)
+{
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
 __device__ __forceinline__ void order(double &a, double &b)  // descending
 {
-    const double most = fmax(a, b), least = fmin(a, b);
+    const double most = larger(a, b), least = smaller(a, b);
     a = most;
     b = least;
 }
+// x[i] for an i that differs from lane to lane
+template <int kCount>
+__device__ __forceinline__ double picked(const double *x, int i)
+{
+    if constexpr (kCount == 1) return x[0];
+    else {
+        const double low = picked<kCount / 2>(x, i), high = picked<kCount / 2>(x + kCount / 2, i);
+        return i & (kCount / 2) ? high : low;
+    }
+}
+
 // Batcher's odd-even merge sort of kCount neighbouring keys, descending
 template <int kCount>
 __device__ __forceinline__ void sort_keys(double *x)
@@ -147,7 +220,7 @@ template <int kCount>
 __device__ __forceinline__ void merge_keys(double *x, const double *y)
 {
 #pragma unroll
-    for (int i = 0; i < kCount; ++i) x[i] = fmax(x[i], y[kCount - 1 - i]);
+    for (int i = 0; i < kCount; ++i) x[i] = larger(x[i], y[kCount - 1 - i]);
 #pragma unroll
     for (int d = kCount / 2; d >= 1; d /= 2)
 #pragma unroll
@@ -193,78 +266,90 @@ __device__ __forceinline__ void exclusive_sums(int32_t *x, int32_t E, int32_t *w
     __syncthreads();
 }
 
+// Sets of kSize neighbouring experts, several in a lane: `values` of the row's sets, and those that are not among the open ones closed.
+template <int kSize, int kEach>
+__device__ __forceinline__ void close_small_sets(double (&x)[kEach], double *values, const RouteArgs &a, int lane)
+{
+    constexpr int kOwn = kEach / kSize;
+    double mine[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+        double most = x[j * kSize], second = kClosed;
+#pragma unroll
+        for (int v = 1; v < kSize; ++v) {
+            second = larger(second, smaller(most, x[j * kSize + v]));
+            most = larger(most, x[j * kSize + v]);
+        }
+        const int32_t set = lane * kOwn + j;
+        mine[j] = key_of(a.set_best == 2 && second > kLeastOpen ? smaller(most + second, kMostOpen) : most, (uint32_t)set, 63);
+        if (set < a.sets) values[set] = mine[j];
+    }
+    wave_sync();
+    int32_t above[kOwn] = {};
+    for (int32_t i = 0; i < a.sets; ++i) {
+        const double v = values[i];
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) above[j] += v > mine[j];
+    }
+    wave_sync();                                             // before the next rows' values
+#pragma unroll
+    for (int v = 0; v < kEach; ++v) x[v] = above[v / kSize] >= a.open_sets ? kClosed : x[v];
+}
+
+constexpr int kRouteThreads = 512;           // of a workgroup at most
 constexpr int kMaxWaves = 16;
 
 // the workgroup's LDS, in bytes
 struct RouteLds {
     int32_t mask, prefix, waves, weights, chosen, values, total;
-    __host__ __device__ RouteLds(int32_t E, int32_t words, int32_t k, int32_t value_bytes)
+    __host__ __device__ RouteLds(int32_t E, int32_t rows, int32_t k, int32_t value_bytes)
     {
-        const int32_t slots = kWordRows * words * k;
-        mask = 0;                                            // uint64 [E, words]: the rows that chose an expert
-        values = mask + E * words * 8;                       // double: values of sets, or of experts
+        mask = 0;                                            // uint64 [E]: the rows that chose an expert
+        values = mask + E * 8;                               // double: values of sets, or of experts
         prefix = values + value_bytes;                       // int32 [E + 1]
         waves = prefix + (E + 1) * 4;                        // int32 [kMaxWaves]
-        weights = waves + kMaxWaves * 4;                     // float [slots]
-        chosen = weights + slots * 4;                        // int16 [slots]
-        total = chosen + slots * 2;
+        weights = waves + kMaxWaves * 4;                     // float [rows, k]
+        chosen = weights + rows * k * 4;                     // int16 [rows, k]
+        total = chosen + rows * k * 2;
     }
 };
 
-// i / k for i below 2^13 and k up to 32: the quotient's error of i / 2^18 stays below 1 / k
-__device__ __forceinline__ int32_t over(int32_t i, uint32_t inverse) { return (int32_t)((uint32_t)i * inverse >> 18); }
-constexpr uint32_t inverse_of(int32_t k) { return ((1u << 18) + k - 1) / k; }
+// i / k for i below 2^11 and k up to 32, from 2^16 / k rounded up: the error of i / 2^16 stays below 1 / k
+__device__ __forceinline__ int32_t over(int32_t i, uint32_t inverse) { return (int32_t)((uint32_t)i * inverse >> 16); }
+uint32_t inverse_of(int32_t k) { return ((1u << 16) + k - 1) / k; }
 
 // kLanes lanes to a row, kEach neighbouring experts a lane, lists of kList keys (top_k of up to that many; beyond 16 they are taken one by one)
-template <int kLanes, int kEach, int kList>
-__global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__restrict__ counts, int32_t words)
+template <int kLanes, int kEach, int kList, bool kByValue, bool kSets>
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int32_t *__restrict__ counts)
 {
     extern __shared__ char lds[];
-    const RouteLds at(a.E, words, a.k, a.value_bytes);
+    const RouteLds at(a.E, a.rows, a.k, a.value_bytes);
     unsigned long long *const mask = (unsigned long long *)(lds + at.mask);
     int32_t *const prefix = (int32_t *)(lds + at.prefix), *const waves = (int32_t *)(lds + at.waves);
     float *const weights = (float *)(lds + at.weights);
     int16_t *const chosen = (int16_t *)(lds + at.chosen);
-    const int threads = blockDim.x, lane = threadIdx.x % kLanes, at_once = threads / kLanes, rows = kWordRows * words;
+    const int threads = blockDim.x, lane = threadIdx.x % kLanes, at_once = threads / kLanes;
     const bool sigmoid = a.gate == GROOT_SIGMOID;
-    for (int e = threadIdx.x; e < a.E * words; e += threads) mask[e] = 0;
+    for (int e = threadIdx.x; e < a.E; e += threads) mask[e] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * rows;
-    const int here = (int)(a.n - first < rows ? a.n - first : rows);      // rows of this workgroup
+    const int64_t first = (int64_t)blockIdx.x * a.rows;
+    const int here = (int)(a.n - first < a.rows ? a.n - first : a.rows);  // rows of this workgroup
     const int32_t begin = lane * kEach;
     for (int pass = 0; pass < here; pass += at_once) {
         const int local = pass + threadIdx.x / kLanes;
         const bool real = local < here;                                   // rows beyond the last go along
         const char *const scores = (const char *)a.scores + (first + (real ? local : here - 1)) * a.score_bytes;
         float s[kEach];
-        auto load = [&](auto type) {
-            typedef decltype(type) T;
-            constexpr int kPer = 16 / sizeof(T);
-            const bool short_row = a.E < kPer;
+        load_scores<kEach>(scores, a, begin, s);
+        float top = s[0];                                                 // NaN if one of them is
 #pragma unroll
-            for (int i = 0; i < kEach / kPer; ++i) {
-                const int32_t e = begin + i * kPer;
-                const RowValues<T> v = row_values<T>(load16<T>(scores + e * (int)sizeof(T), (int64_t)(a.E - e) * (int)sizeof(T), short_row));
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) s[i * kPer + j] = e + j < a.E ? v.x[j] : -kInf;
-            }
-        };
-        if (a.dtype == GROOT_F32) load(float{});
-        else if (a.dtype == GROOT_BF16) load(bf16_t{});
-        else load(f16_t{});
-        float top = -kInf;
-        bool broken = false;
-#pragma unroll
-        for (int v = 0; v < kEach; ++v) {
-            broken |= s[v] != s[v];
-            top = fmaxf(top, s[v]);                                       // a NaN is passed over: the row is broken
-        }
-        top = top_of<kLanes>(top);
-        broken = any_of<kLanes>(broken) || (!sigmoid && top == kInf);
+        for (int v = 1; v < kEach; ++v) top = __builtin_elementwise_maximum(top, s[v]);
+        top = over_lanes<kLanes>(top, [](float x, float y) { return __builtin_elementwise_maximum(x, y); });
+        const bool broken = top != top || (!sigmoid && top == kInf);
         const float base = sigmoid || top == -kInf ? 0.f : top;
         float sum = 1.f;                                                  // of e^(s - base), where weights go by it
         double x[kEach];
-        if (!a.by_value) {
+        if constexpr (!kByValue) {
             if (!sigmoid && !a.renormalise) {
                 sum = 0.f;
 #pragma unroll
@@ -273,8 +358,11 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
             }
 #pragma unroll
             for (int v = 0; v < kEach; ++v) {
-                const double c = fmin((double)(s[v] + 0.f), kMostOpen);   // -0 is 0
-                x[v] = s[v] == -kInf || broken ? kClosed : c;
+                x[v] = fmax((double)(s[v] + 0.f), kClosed);               // -0 is 0, -inf is closed
+            }
+            if (sigmoid) {
+#pragma unroll
+                for (int v = 0; v < kEach; ++v) x[v] = fmin(x[v], kMostOpen);   // +inf
             }
         } else {
             double all = 0;
@@ -288,15 +376,16 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
                 sum = (float)all;
                 all = 1.0 / all;
             }
+            float bias[kEach] = {};
+            if (a.bias) load_scores_of<kEach, float>((const char *)a.bias, a.E, begin, bias);
 #pragma unroll
             for (int v = 0; v < kEach; ++v) {
-                double c = sigmoid ? (s[v] < 0.f ? x[v] : 1.0) / (1.0 + x[v]) : x[v] * all;
-                if (a.bias) c += begin + v < a.E ? (double)a.bias[begin + v] : 0.0;
-                const bool open = s[v] > -kInf && c > -__builtin_inf() && !broken;
-                x[v] = open ? fmin(c, kMostOpen) : kClosed;
+                const double p = sigmoid ? (s[v] < 0.f ? x[v] : 1.0) * reciprocal64(1.0 + x[v]) : x[v] * all;
+                const double c = p + (double)bias[v];
+                x[v] = s[v] > -kInf && c > -__builtin_inf() ? fmin(c, kMostOpen) : kClosed;
             }
         }
-        if (a.open_sets < a.sets) {                                       // the same for all rows
+        if constexpr (kSets) {
             const int32_t size = a.E / a.sets;
             // the values that a row's sets come to, the set's number in each; a set counts as many others as are above it
             if (a.set_lanes) {                                            // a set is all of a few lanes' experts
@@ -304,12 +393,12 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
                 double most = kClosed, second = kClosed;
 #pragma unroll
                 for (int v = 0; v < kEach; ++v) {
-                    second = fmax(second, fmin(most, x[v]));
-                    most = fmax(most, x[v]);
+                    second = larger(second, smaller(most, x[v]));
+                    most = larger(most, x[v]);
                 }
                 auto meet = [&](double o1, double o2) {
-                    second = fmax(fmax(second, o2), fmin(most, o1));
-                    most = fmax(most, o1);
+                    second = larger(larger(second, o2), smaller(most, o1));
+                    most = larger(most, o1);
                 };
                 if (a.set_lanes > 1) meet(other_lane<1>(most), other_lane<1>(second));
                 if (a.set_lanes > 2) meet(other_lane<2>(most), other_lane<2>(second));
@@ -327,6 +416,12 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
 #pragma unroll
                     for (int v = 0; v < kEach; ++v) x[v] = kClosed;
                 }
+            } else if (a.small_sets) {
+                double *const values = (double *)(lds + at.values) + threadIdx.x / kLanes * a.sets;
+                if (size == 1) close_small_sets<1>(x, values, a, lane);
+                else if (size == 2) close_small_sets<2>(x, values, a, lane);
+                else if (size == 4) close_small_sets<4>(x, values, a, lane);
+                else close_small_sets<8>(x, values, a, lane);
             } else {
                 double *const values = (double *)(lds + at.values) + (int64_t)(threadIdx.x / kLanes) * (kLanes * kEach + a.sets), *const row = values + a.sets;
 #pragma unroll
@@ -336,8 +431,8 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
                     double most = kClosed, second = kClosed;
                     for (int32_t i = 0; i < size; ++i) {
                         const double c = row[set * size + i];
-                        second = fmax(second, fmin(most, c));
-                        most = fmax(most, c);
+                        second = larger(second, smaller(most, c));
+                        most = larger(most, c);
                     }
                     values[set] = key_of(a.set_best == 2 && second > kLeastOpen ? fmin(most + second, kMostOpen) : most, (uint32_t)set, 63);
                 }
@@ -367,34 +462,44 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
         const float nan = __builtin_nanf("");
         if (kList < 16 || a.k <= 16) {
             merge_lanes<kLanes, kList>(x);
+            // every lane takes its share of the slots: slot j kWide + lane
+            constexpr int kWide = kLanes < kList ? kLanes : kList, kSlots = kList / kWide;
+            const int here_lane = lane % kWide;
+            float at_slot[kSlots];
+            int32_t expert[kSlots];
             float m = -kInf;
-            float w[kList];
 #pragma unroll
-            for (int i = 0; i < kList; ++i) {
-                const bool taken = i < a.k && x[i] > kLeastOpen;
-                float at_slot;
-                if (a.by_value) at_slot = taken ? score_at(scores, a.dtype, (int32_t)number_of(x[i], kNumbers)) : -kInf;
-                else at_slot = taken ? (float)__builtin_bit_cast(double, __builtin_bit_cast(uint64_t, x[i]) & ~(uint64_t)kNumbers) : -kInf;
-                w[i] = at_slot;
-                m = fmaxf(m, sigmoid ? fminf(at_slot, 0.f) : at_slot);
+            for (int j = 0; j < kSlots; ++j) {
+                const double key = picked<kWide>(x + j * kWide, here_lane);
+                const bool taken = key > kLeastOpen && !broken && j * kWide + lane < a.k && (kWide == kLanes || lane < kWide);
+                expert[j] = taken ? (int32_t)number_of(key, kNumbers) : -1;
+                at_slot[j] = !taken ? -kInf : kByValue ? score_at(scores, a.dtype, expert[j]) : score_of(key);
+                m = fmaxf(m, sigmoid ? fminf(at_slot[j], 0.f) : at_slot[j]);
             }
-            m = a.renormalise ? (m == -kInf ? 0.f : m) : base;
-            float all = 0.f;
-#pragma unroll
-            for (int i = 0; i < kList; ++i) {
-                w[i] = w[i] == -kInf ? 0.f : weight_of(w[i], m, sigmoid);
-                all += w[i];
+            float scale = a.factor;
+            if (a.renormalise) {
+                m = top_of<kLanes>(m);
+                m = m == -kInf ? 0.f : m;
+            } else {
+                m = base;
+                scale /= sum;
             }
-            const float scale = a.factor / (a.renormalise ? all : sum);
+            float w[kSlots], all = 0.f;
 #pragma unroll
-            for (int i = 0; i < kList; ++i)
-                if (real && i < a.k && i % kLanes == lane) {
-                    const bool taken = x[i] > kLeastOpen;
-                    const int32_t e = taken ? (int32_t)number_of(x[i], kNumbers) : -1;
-                    weights[local * a.k + i] = broken ? nan : taken ? w[i] * scale : 0.f;
-                    chosen[local * a.k + i] = (int16_t)e;
-                    if (taken) atomicOr(&mask[e * words + local / kWordRows], 1ull << local % kWordRows);
+            for (int j = 0; j < kSlots; ++j) {
+                w[j] = expert[j] < 0 ? 0.f : weight_of(at_slot[j], m, sigmoid);
+                all += w[j];
+            }
+            if (a.renormalise) scale /= sum_of<kLanes>(all);
+#pragma unroll
+            for (int j = 0; j < kSlots; ++j) {
+                const int slot = j * kWide + lane;
+                if (real && slot < a.k && (kWide == kLanes || lane < kWide)) {
+                    weights[local * a.k + slot] = broken ? nan : expert[j] < 0 ? 0.f : w[j] * scale;
+                    chosen[local * a.k + slot] = (int16_t)expert[j];
+                    if (expert[j] >= 0) atomicOr(&mask[expert[j]], 1ull << local);
                 }
+            }
         } else if constexpr (kList == 16 && kEach == 16) {                // the lists hold all of a lane's experts
             float m = -kInf, all = 0.f;
             for (int32_t slot = 0; slot < a.k; ++slot) {
@@ -403,7 +508,7 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
 #pragma unroll
                 for (int v = 0; v + 1 < kEach; ++v) x[v] = mine ? x[v + 1] : x[v];
                 if (mine) x[kEach - 1] = kClosed;
-                const bool taken = best > kLeastOpen;
+                const bool taken = best > kLeastOpen && !broken;
                 const float at_slot = taken ? score_at(scores, a.dtype, (int32_t)number_of(best, kNumbers)) : -kInf;
                 const float low = sigmoid ? fminf(at_slot, 0.f) : at_slot;
                 // the sum at the largest score so far
@@ -416,8 +521,7 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
                     weights[local * a.k + slot] = at_slot;
                     chosen[local * a.k + slot] = (int16_t)(taken ? (int32_t)number_of(best, kNumbers) : -1);
                     if (taken) {
-                        const int32_t e = (int32_t)number_of(best, kNumbers);
-                        atomicOr(&mask[e * words + local / kWordRows], 1ull << local % kWordRows);
+                        atomicOr(&mask[number_of(best, kNumbers)], 1ull << local);
                     }
                 }
             }
@@ -435,8 +539,7 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
     __syncthreads();
     const bool alone = gridDim.x == 1;
     for (int e = threadIdx.x; e < a.E; e += threads) {
-        int32_t count = 0;
-        for (int w = 0; w < words; ++w) count += __popcll(mask[e * words + w]);
+        const int32_t count = __popcll(mask[e]);
         if (alone) prefix[e] = count;
         else counts[(int64_t)blockIdx.x * a.E + e] = count;
     }
@@ -445,15 +548,10 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
         exclusive_sums(prefix, a.E, waves);
         for (int e = threadIdx.x; e <= a.E; e += threads) a.offsets[e] = prefix[e];
     }
-    const uint32_t inverse = inverse_of(a.k);
     for (int32_t i = threadIdx.x; i < here * a.k; i += threads) {
-        const int32_t e = chosen[i], local = over(i, inverse);
+        const int32_t e = chosen[i];
         int32_t place = -1;
-        if (e >= 0) {
-            place = alone ? prefix[e] : 0;
-            for (int w = 0; w < local / kWordRows; ++w) place += __popcll(mask[e * words + w]);
-            place += __popcll(mask[e * words + local / kWordRows] & ((1ull << local % kWordRows) - 1));
-        }
+        if (e >= 0) place = __popcll(mask[e] & ((1ull << over(i, a.inverse_k)) - 1)) + (alone ? prefix[e] : 0);
         a.experts[first * a.k + i] = e;
         a.weights[first * a.k + i] = weights[i];
         a.places[first * a.k + i] = place;
@@ -461,35 +559,49 @@ __global__ __launch_bounds__(1024) void route_kernel(RouteArgs a, int32_t *__res
 }
 
 // counts of the workgroups before each, expert by expert, in place, and every expert's sum in the row behind the last
-__global__ __launch_bounds__(1024) void route_scan_kernel(int32_t *__restrict__ counts, int32_t groups, int32_t E)
+constexpr int kScanExperts = 16, kScanParts = 64;
+__global__ __launch_bounds__(kScanExperts * kScanParts) void route_scan_kernel(int32_t *__restrict__ counts, int32_t groups, int32_t E)
 {
-    __shared__ int32_t sums[16][kWave];
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int32_t e = blockIdx.x * kWave + lane, each = (groups + 15) / 16;
-    const int32_t begin = wave * each, end = begin + each < groups ? begin + each : groups;
-    int32_t sum = 0;
+    __shared__ int32_t sums[kScanParts][kScanExperts];
+    const int part = threadIdx.x / kScanExperts, at = threadIdx.x % kScanExperts;
+    const int32_t e = blockIdx.x * kScanExperts + at, each = (groups + kScanParts - 1) / kScanParts;
+    const int32_t begin = part * each, end = begin + each < groups ? begin + each : groups;
+    constexpr int kHeld = 16;                                // of a part in registers: 1024 workgroups' counts are read once
+    int32_t held[kHeld], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        held[i] = e < E && begin + i < end ? counts[(int64_t)(begin + i) * E + e] : 0;
+        sum += held[i];
+    }
     if (e < E)
-        for (int32_t g = begin; g < end; ++g) sum += counts[(int64_t)g * E + e];
-    sums[wave][lane] = sum;
+        for (int32_t g = begin + kHeld; g < end; ++g) sum += counts[(int64_t)g * E + e];
+    sums[part][at] = sum;
     __syncthreads();
     int32_t before = 0, all = 0;
-    for (int w = 0; w < 16; ++w) {
-        before += w < wave ? sums[w][lane] : 0;
-        all += sums[w][lane];
+#pragma unroll 16
+    for (int p = 0; p < kScanParts; ++p) {
+        const int32_t s = sums[p][at];
+        before += p < part ? s : 0;
+        all += s;
     }
     if (e >= E) return;
-    for (int32_t g = begin; g < end; ++g) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        if (begin + i < end) counts[(int64_t)(begin + i) * E + e] = before;
+        before += held[i];
+    }
+    for (int32_t g = begin + kHeld; g < end; ++g) {
         const int32_t here = counts[(int64_t)g * E + e];
         counts[(int64_t)g * E + e] = before;
         before += here;
     }
-    if (wave == 0) counts[(int64_t)groups * E + e] = all;
+    if (part == 0) counts[(int64_t)groups * E + e] = all;
 }
 
 // ranks -> places.  kScanned: the counts are those of the workgroups before, and the sums stand behind them; otherwise this
 // workgroup adds them up, its threads in as many parts as there are for each expert.
 template <bool kScanned>
-__global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a, const int32_t *__restrict__ counts, int32_t groups, int32_t rows)
+__global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a, const int32_t *__restrict__ counts, int32_t groups)
 {
     extern __shared__ char lds[];
     int32_t *const prefix = (int32_t *)lds, *const before = prefix + a.E + 1, *const waves = before + a.E;
@@ -520,8 +632,8 @@ __global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a, const in
     exclusive_sums(prefix, a.E, waves);
     if (blockIdx.x == 0)
         for (int e = threadIdx.x; e <= a.E; e += threads) a.offsets[e] = prefix[e];
-    const int64_t first = (int64_t)blockIdx.x * rows;
-    const int32_t entries = (int32_t)(a.n - first < rows ? a.n - first : rows) * a.k;
+    const int64_t first = (int64_t)blockIdx.x * a.rows;
+    const int32_t entries = (int32_t)(a.n - first < a.rows ? a.n - first : a.rows) * a.k;
     for (int32_t i = threadIdx.x; i < entries; i += threads) {
         const int32_t e = a.experts[first * a.k + i];
         if (e >= 0) a.places[first * a.k + i] += prefix[e] + before[e];
@@ -605,42 +717,58 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
     }
 }
 
-// Rows of a workgroup, in words of 64: one, and more where the workgroups would be more than one launch adds up by itself.
-int32_t route_words(int64_t n, int32_t E, int32_t k)
+// lanes of a row
+int32_t route_lanes(int32_t E)
 {
-    int32_t words = 1;
-    while (words < 4 && (n + kWordRows * words - 1) / (kWordRows * words) > kSumGroups && RouteLds(E, words * 2, k, 0).total <= 32 * 1024) words *= 2;
-    return words;
+    int32_t lanes = 1;
+    while (lanes * 16 < E) lanes *= 2;
+    return lanes;
 }
-int64_t route_groups(int64_t n, int32_t words) { return n <= 0 ? 1 : (n + kWordRows * words - 1) / (kWordRows * words); }
+// Rows of a workgroup.  All of them where its threads hold them at once: one launch.  Otherwise few, down to a wavefront's, while the
+// workgroups are no more than the second launch adds up by itself.
+int32_t route_rows(int64_t n, int32_t E)
+{
+    const int32_t lanes = route_lanes(E);
+    if (n <= kRouteRows && n * lanes <= kRouteThreads) return kRouteRows;
+    int32_t rows = kWave / lanes;
+    while (rows < kRouteRows && (n + rows - 1) / rows > kSumGroups) rows *= 2;
+    return rows;
+}
+int64_t route_groups(int64_t n, int32_t rows) { return n <= 0 ? 1 : (n + rows - 1) / rows; }
 
-template <int kLanes, int kEach, int kList>
+template <int kLanes, int kEach, int kList, bool kByValue, bool kSets>
 int route_launch(RouteArgs a, int32_t *counts, hipStream_t stream)
 {
-    const int32_t words = route_words(a.n, a.E, a.k), rows = kWordRows * words;
-    const int64_t groups = route_groups(a.n, words);
-    int threads = rows * kLanes < 1024 ? rows * kLanes : 1024;
+    a.rows = route_rows(a.n, a.E);
+    a.inverse_k = inverse_of(a.k);
+    const int64_t groups = route_groups(a.n, a.rows);
+    int threads = (int)(a.n < a.rows ? (a.n < 1 ? 1 : a.n) : a.rows) * kLanes;
+    threads = threads >= kRouteThreads ? kRouteThreads : (threads + kWave - 1) / kWave * kWave;
     a.set_lanes = 0;
+    a.small_sets = false;
     a.value_bytes = 0;
-    if (a.open_sets < a.sets) {
+    if (kSets) {
         const int32_t size = a.E / a.sets, lanes = size / kEach;
         if (size % kEach == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 32) {
             a.set_lanes = lanes;
             a.value_bytes = threads / kLanes * a.sets * 8;
+        } else if (size == 1 || size == 2 || size == 4 || size == 8) {
+            a.small_sets = true;
+            a.value_bytes = threads / kLanes * a.sets * 8;
         } else {
             auto bytes = [&] { return threads / kLanes * (kLanes * kEach + a.sets) * 8; };
-            while (threads > kWave && bytes() > 32 * 1024) threads /= 2;
+            while (threads > kWave && bytes() > 32 * 1024) threads = (threads / 2 + kWave - 1) / kWave * kWave;
             a.value_bytes = bytes();
         }
     }
-    route_kernel<kLanes, kEach, kList><<<(uint32_t)groups, threads, RouteLds(a.E, words, a.k, a.value_bytes).total, stream>>>(a, counts, words);
+    route_kernel<kLanes, kEach, kList, kByValue, kSets><<<(uint32_t)groups, threads, RouteLds(a.E, a.rows, a.k, a.value_bytes).total, stream>>>(a, counts);
     if (groups > 1) {
         const size_t lds = (2 * a.E + 1 + kMaxWaves) * sizeof(int32_t);
         if (groups > kSumGroups) {
-            route_scan_kernel<<<(a.E + kWave - 1) / kWave, 1024, 0, stream>>>(counts, (int32_t)groups, a.E);
-            route_place_kernel<true><<<(uint32_t)groups, kBlock, lds, stream>>>(a, counts, (int32_t)groups, rows);
+            route_scan_kernel<<<(a.E + kScanExperts - 1) / kScanExperts, kScanExperts * kScanParts, 0, stream>>>(counts, (int32_t)groups, a.E);
+            route_place_kernel<true><<<(uint32_t)groups, kBlock, lds, stream>>>(a, counts, (int32_t)groups);
         } else {
-            route_place_kernel<false><<<(uint32_t)groups, 1024, lds, stream>>>(a, counts, (int32_t)groups, rows);
+            route_place_kernel<false><<<(uint32_t)groups, 1024, lds, stream>>>(a, counts, (int32_t)groups);
         }
     }
     return (int)hipGetLastError();
@@ -656,29 +784,32 @@ int backward_launch(const RouteBackwardArgs &a, hipStream_t stream)
 
 }  // namespace
 
-size_t route_workspace(int64_t n, int32_t E, int32_t k)
+size_t route_workspace(int64_t n, int32_t E)
 {
-    const int64_t groups = route_groups(n, route_words(n, E, k));
+    const int64_t groups = route_groups(n, route_rows(n, E));
     return groups == 1 ? 0 : (size_t)(groups + 1) * E * sizeof(int32_t);
 }
 
 // 16 experts a lane (8 where there are no more), lists as long as top_k needs
 typedef int (*RouteLaunch)(RouteArgs, int32_t *, hipStream_t);
-template <int kLanes>
+template <int kLanes, bool kByValue, bool kSets>
 static RouteLaunch route_of_lanes(const RouteArgs &a)
 {
-    return a.k <= 4 ? route_launch<kLanes, 16, 4> : a.k <= 8 ? route_launch<kLanes, 16, 8> : route_launch<kLanes, 16, 16>;
+    return a.k <= 4   ? route_launch<kLanes, 16, 4, kByValue, kSets>
+           : a.k <= 8 ? route_launch<kLanes, 16, 8, kByValue, kSets>
+                      : route_launch<kLanes, 16, 16, kByValue, kSets>;
 }
+template <bool kByValue, bool kSets>
 static RouteLaunch route_for(const RouteArgs &a)
 {
-    if (a.E <= 8) return a.k <= 4 ? route_launch<1, 8, 4> : route_launch<1, 8, 8>;
-    if (a.E <= 16) return route_of_lanes<1>(a);
-    if (a.E <= 32) return route_of_lanes<2>(a);
-    if (a.E <= 64) return route_of_lanes<4>(a);
-    if (a.E <= 128) return route_of_lanes<8>(a);
-    if (a.E <= 256) return route_of_lanes<16>(a);
-    if (a.E <= 512) return route_of_lanes<32>(a);
-    return route_of_lanes<64>(a);
+    if (a.E <= 8) return a.k <= 4 ? route_launch<1, 8, 4, kByValue, kSets> : route_launch<1, 8, 8, kByValue, kSets>;
+    if (a.E <= 16) return route_of_lanes<1, kByValue, kSets>(a);
+    if (a.E <= 32) return route_of_lanes<2, kByValue, kSets>(a);
+    if (a.E <= 64) return route_of_lanes<4, kByValue, kSets>(a);
+    if (a.E <= 128) return route_of_lanes<8, kByValue, kSets>(a);
+    if (a.E <= 256) return route_of_lanes<16, kByValue, kSets>(a);
+    if (a.E <= 512) return route_of_lanes<32, kByValue, kSets>(a);
+    return route_of_lanes<64, kByValue, kSets>(a);
 }
 
 // 16 lanes a row while they hold its experts and slots, a wavefront otherwise
@@ -693,7 +824,12 @@ static BackwardLaunch backward_for(const RouteBackwardArgs &a)
     return backward_launch<16, 16>;
 }
 
-int launch_route(const RouteArgs &a, void *workspace, void *stream) { return route_for(a)(a, (int32_t *)workspace, (hipStream_t)stream); }
+int launch_route(const RouteArgs &a, void *workspace, void *stream)
+{
+    const bool sets = a.open_sets < a.sets;
+    const RouteLaunch launch = a.by_value ? (sets ? route_for<true, true>(a) : route_for<true, false>(a)) : (sets ? route_for<false, true>(a) : route_for<false, false>(a));
+    return launch(a, (int32_t *)workspace, (hipStream_t)stream);
+}
 int launch_route_backward(const RouteBackwardArgs &a, void *stream) { return backward_for(a)(a, (hipStream_t)stream); }
 
 }  // namespace groot
