@@ -19,6 +19,53 @@ __device__ __forceinline__ float quotient(float x, float s, float r)
     return __builtin_fmaf(__builtin_fmaf(-q, s, x), r, q);
 }
 
+// What another lane holds, for sums and the like over kLanes neighbouring lanes: lanes 1, 2, 4 and 8 away by a move inside of 16 lanes (the
+// last two reversed: lanes that are less far apart hold the same by then), 16 and 32 away by an exchange that gives every lane both values.
+template <int kAway>
+__device__ __forceinline__ void pair_lanes(uint32_t x, uint32_t *a, uint32_t *b)
+{
+    *a = x;
+    if constexpr (kAway == 1) *b = __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false);        // quad_perm 1 0 3 2
+    else if constexpr (kAway == 2) *b = __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, false);   // quad_perm 2 3 0 1
+    else if constexpr (kAway == 4) *b = __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, false);  // row_half_mirror
+    else if constexpr (kAway == 8) *b = __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, false);  // row_mirror
+    else {
+        const auto r = kAway == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        *a = r[0];
+        *b = r[1];
+    }
+}
+template <int kAway>
+__device__ __forceinline__ void pair_lanes(float x, float *a, float *b)
+{
+    uint32_t u, v;
+    pair_lanes<kAway>(__float_as_uint(x), &u, &v);
+    *a = __uint_as_float(u);
+    *b = __uint_as_float(v);
+}
+template <int kAway>
+__device__ __forceinline__ void pair_lanes(double x, double *a, double *b)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    uint32_t ul, vl, uh, vh;
+    pair_lanes<kAway>((uint32_t)bits, &ul, &vl);
+    pair_lanes<kAway>((uint32_t)(bits >> 32), &uh, &vh);
+    *a = __builtin_bit_cast(double, (uint64_t)uh << 32 | ul);
+    *b = __builtin_bit_cast(double, (uint64_t)vh << 32 | vl);
+}
+// `both` of the values of kLanes neighbouring lanes, in every one of them; all of them take part, and `both` does not mind the order
+template <int kLanes, int kAway = 1, typename T, typename F>
+__device__ __forceinline__ T over_lanes(T x, F both)
+{
+    if constexpr (kAway < kLanes) {
+        T a, b;
+        pair_lanes<kAway>(x, &a, &b);
+        return over_lanes<kLanes, kAway * 2>(both(a, b), both);
+    } else {
+        return x;
+    }
+}
+
 // a value that is the same in every lane, as a scalar
 __device__ __forceinline__ int64_t uniform(int64_t x)
 {

@@ -1,7 +1,7 @@
 // Root-mean-square norm of rows, with the residual's addition in front, an output in 8 bits behind, and its gradients.
 //   h = x + residual, rounded to the type;  rstd = 1 / sqrt(mean h^2 + eps), in 64 bits and rounded once;  y = (h rstd) gain in fp32
 //   scale = max |y| fl(1 / 127), codes = y / scale to the nearest
-//   dx = rstd (a - h rstd^2 mean(a h)) + dh with a = dy gain;  dgain = sum over the rows of dy (h rstd)
+//   dx = rstd (a - u mean(a u)) + dh with u = h rstd, a = dy gain;  dgain = sum over the rows of dy u
 // The sum of the squares is in 64 bits so that rstd, and with it every code, is the same whatever order the lanes add in.
 // Bound by HBM: a row is read once and stays in registers as it is held.
 //
@@ -13,34 +13,35 @@ namespace groot {
 
 namespace {
 
-template <typename T>
+// Where a lane's piece lies in every row.
 struct Piece {
-    int64_t at;                              // byte of the row
-    int first;                               // values that the piece before has counted; all of them where there is no such piece
-    bool real;
+    int32_t at;                              // its first value
+    int32_t first;                           // values that the piece before has counted
+    bool real;                               // there is such a piece
 };
 
 template <typename T>
-__device__ __forceinline__ Piece<T> piece(int32_t i, int32_t K)
+__device__ __forceinline__ Piece piece(int32_t i, int32_t K)
 {
     constexpr int kPer = 16 / sizeof(T);
     const int32_t begin = i * kPer;
-    if (K < kPer) return Piece<T>{0, i == 0 ? 0 : kPer, i == 0};
-    if (begin >= K) return Piece<T>{(int64_t)(K - kPer) * (int64_t)sizeof(T), kPer, false};
+    if (K < kPer) return Piece{0, 0, i == 0};
+    if (begin >= K) return Piece{K - kPer, 0, false};        // the row's last one is loaded, and nothing stays of it
     const int32_t at = begin + kPer <= K ? begin : K - kPer;
-    return Piece<T>{(int64_t)at * (int64_t)sizeof(T), begin - at, true};
+    return Piece{at, begin - at, true};
 }
 
+// kShort: a row of less than 16 bytes
 template <typename T, bool kShort>
-__device__ __forceinline__ v4i load_piece(const T *row, int64_t at, int32_t K)
+__device__ __forceinline__ v4i load_piece(const T *row, const Piece &p, int32_t K)
 {
     if constexpr (kShort) return short16<T>((const char *)row, (int64_t)K * (int64_t)sizeof(T));
     v4i v;
-    __builtin_memcpy(&v, (const char *)row + at, 16);
+    __builtin_memcpy(&v, row + p.at, 16);
     return v;
 }
 template <typename T, bool kShort>
-__device__ __forceinline__ void store_held(T *row, int64_t at, int32_t K, v4i v)
+__device__ __forceinline__ void store_piece(T *row, const Piece &p, int32_t K, v4i v)
 {
     if constexpr (kShort) {
         T e[16 / sizeof(T)];
@@ -49,27 +50,34 @@ __device__ __forceinline__ void store_held(T *row, int64_t at, int32_t K, v4i v)
         for (int k = 0; k < (int)(16 / sizeof(T)); ++k)
             if (k < K) row[k] = e[k];
     } else {
-        __builtin_memcpy((char *)row + at, &v, 16);
+        __builtin_memcpy(row + p.at, &v, 16);
     }
 }
 template <typename T>
 __device__ __forceinline__ v4i rounded(const RowValues<T> &x)
 {
     constexpr int kPer = 16 / sizeof(T);
-    T e[kPer];
+    typedef T vt __attribute__((ext_vector_type(kPer)));
+    vt e;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) e[k] = (T)x.x[k];         // the one rounding
-    v4i v;
-    __builtin_memcpy(&v, e, 16);
-    return v;
+    return __builtin_bit_cast(v4i, e);
+}
+// ones for where there is no gain
+template <typename T>
+__device__ __forceinline__ v4i ones()
+{
+    RowValues<T> x;
+#pragma unroll
+    for (float &v : x.x) v = 1.f;
+    return rounded<T>(x);
 }
 
-// Sums and maxima over the kLanes lanes of a row; every lane has them.  `lds`: a word for each wavefront of the row, twice.
+// Sums and maxima over the kLanes lanes of a row; every lane has them.  `lds`: a word for each wavefront of the workgroup.
 template <int kLanes>
 __device__ __forceinline__ double row_sum(double x, double *lds)
 {
-#pragma unroll
-    for (int d = 1; d < (kLanes < kWave ? kLanes : kWave); d *= 2) x += __shfl_xor(x, d);
+    x = over_lanes<(kLanes < kWave ? kLanes : kWave)>(x, [](double a, double b) { return a + b; });
     if constexpr (kLanes > kWave) {
         __syncthreads();                                     // the row before has read its words
         if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = x;
@@ -81,20 +89,31 @@ __device__ __forceinline__ double row_sum(double x, double *lds)
     return x;
 }
 template <int kLanes>
-__device__ __forceinline__ float row_most(float x, double *lds)
+__device__ __forceinline__ uint32_t row_most(uint32_t x, double *lds)
 {
-    x = row_top_of<(kLanes < kWave ? kLanes : kWave)>(x);
+    x = over_lanes<(kLanes < kWave ? kLanes : kWave)>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
     if constexpr (kLanes > kWave) {
-        float *const tops = (float *)lds;
+        uint32_t *const tops = (uint32_t *)lds;
         __syncthreads();
         if (threadIdx.x % kWave == 0) tops[threadIdx.x / kWave] = x;
         __syncthreads();
-        x = row_top_of<kLanes / kWave>(tops[threadIdx.x % (kLanes / kWave)]);
+#pragma unroll
+        for (int w = 0; w < kLanes / kWave; ++w) x = tops[w] > x ? tops[w] : x;
     }
     return x;
 }
 
 constexpr int block_of(int lanes) { return lanes > kBlock ? lanes : kBlock; }
+
+// four values cut to 8 bits; r: the scale's reciprocal, where the scale is of an ordinary size
+__device__ __forceinline__ uint32_t four_codes(const float *y, float scale, float r)
+{
+    constexpr float kRound = 12582912.f;                     // 1.5 * 2^23: what is added to it is rounded to an integer
+    uint32_t q[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = __float_as_uint(quotient(y[e], scale, r) + kRound);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u), __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), 0x05040100u);
+}
 
 template <typename T, int kLanes, int kKeep, bool kShort>
 __global__ __launch_bounds__(block_of(kLanes)) void norm_kernel(NormArgs a)
@@ -102,82 +121,93 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_kernel(NormArgs a)
     constexpr int kPer = 16 / sizeof(T), kThreads = block_of(kLanes), kRows = kThreads / kLanes;
     __shared__ double words[kThreads / kWave];
     const int lane = threadIdx.x % kLanes;
-    const T *const gain = (const T *)a.gain;
+    Piece p[kKeep];
+    v4i gain[kKeep];
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+        p[i] = piece<T>(i * kLanes + lane, a.K);
+        gain[i] = a.gain ? load_piece<T, kShort>((const T *)a.gain, p[i], a.K) : ones<T>();
+    }
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += (int64_t)gridDim.x * kRows) {
         const int64_t mine = first + threadIdx.x / kLanes, row = mine < a.n ? mine : a.n - 1;   // rows beyond the last go along and store nothing
+        const bool real = mine < a.n;
         const T *const x = (const T *)a.X + row * a.x_stride;
         v4i h[kKeep];
-        double sum = 0;
 #pragma unroll
-        for (int i = 0; i < kKeep; ++i) h[i] = load_piece<T, kShort>(x, piece<T>(i * kLanes + lane, a.K).at, a.K);
+        for (int i = 0; i < kKeep; ++i) h[i] = load_piece<T, kShort>(x, p[i], a.K);
         if (a.residual) {
             const T *const r = (const T *)a.residual + row * a.residual_stride;
+            v4i other[kKeep];
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i) other[i] = load_piece<T, kShort>(r, p[i], a.K);
 #pragma unroll
             for (int i = 0; i < kKeep; ++i) {
                 RowValues<T> u = row_values<T>(h[i]);
-                const RowValues<T> v = row_values<T>(load_piece<T, kShort>(r, piece<T>(i * kLanes + lane, a.K).at, a.K));
+                const RowValues<T> v = row_values<T>(other[i]);
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) u.x[e] += v.x[e];
                 h[i] = rounded<T>(u);
             }
         }
+        double sum = 0;
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-            const int counted = piece<T>(i * kLanes + lane, a.K).first;
+            if (!p[i].real) continue;
             const RowValues<T> u = row_values<T>(h[i]);
+            if (p[i].first == 0) {
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                const double v = e >= counted ? (double)u.x[e] : 0.0;
-                sum = __builtin_fma(v, v, sum);
+                for (int e = 0; e < kPer; ++e) sum = __builtin_fma((double)u.x[e], (double)u.x[e], sum);
+            } else {                                         // the last piece of a row that is no whole number of them
+                for (int e = kPer - 1; e >= 0; --e)
+                    if (e >= p[i].first) sum = __builtin_fma((double)u.x[e], (double)u.x[e], sum);
             }
         }
         sum = row_sum<kLanes>(sum, words);
         const float rstd = (float)(1.0 / sqrt(sum / a.K + a.eps));
-        const bool real = mine < a.n;
-        auto values = [&](int i, int64_t at) {
-            RowValues<T> u = row_values<T>(h[i]);
-            const RowValues<T> g = gain ? row_values<T>(load_piece<T, kShort>(gain, at, a.K)) : RowValues<T>{};
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) u.x[e] = gain ? (u.x[e] * rstd) * g.x[e] : u.x[e] * rstd;
-            return u;
-        };
+        RowValues<T> y[kKeep];
         uint32_t seen = 0;
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-            const Piece<T> p = piece<T>(i * kLanes + lane, a.K);
-            if (!p.real) continue;
-            if (real && a.H) store_held<T, kShort>((T *)a.H + row * a.h_stride, p.at, a.K, h[i]);
-            const RowValues<T> y = values(i, p.at);
-            if (real && a.Y) store_held<T, kShort>((T *)a.Y + row * a.y_stride, p.at, a.K, rounded<T>(y));
+            y[i] = row_values<T>(h[i]);
+            const RowValues<T> g = row_values<T>(gain[i]);
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
-                const uint32_t m = __float_as_uint(y.x[e]) & 0x7FFFFFFFu;
+                y[i].x[e] = (y[i].x[e] * rstd) * g.x[e];
+                const uint32_t m = __float_as_uint(y[i].x[e]) & 0x7FFFFFFFu;
                 if (!kShort || e < a.K) seen = m > seen ? m : seen;
             }
+            if (!real || !p[i].real) continue;
+            if (a.H) store_piece<T, kShort>((T *)a.H + row * a.h_stride, p[i], a.K, h[i]);
+            if (a.Y) store_piece<T, kShort>((T *)a.Y + row * a.y_stride, p[i], a.K, rounded<T>(y[i]));
         }
         if (real && a.rstd && lane == 0) a.rstd[row] = rstd;
-        if (a.Q) {
-            const float scale = row_scale(row_most<kLanes>(__uint_as_float(seen), words));
-            if (real && lane == 0) a.q_scale[row] = scale;
+        if (!a.Q) continue;
+        const float scale = row_scale(__uint_as_float(row_most<kLanes>(seen, words)));
+        if (!real) continue;
+        if (lane == 0) a.q_scale[row] = scale;
+        const bool usual = scale > 0x1p-96f;                 // the same for a row
+        const float r = usual ? 1.f / scale : 0.f;
 #pragma unroll
-            for (int i = 0; i < kKeep; ++i) {
-                const Piece<T> p = piece<T>(i * kLanes + lane, a.K);
-                if (!p.real || !real) continue;
-                const RowValues<T> y = values(i, p.at);
-                alignas(8) int8_t codes[kPer];
+        for (int i = 0; i < kKeep; ++i) {
+            if (!p[i].real) continue;
+            uint32_t codes[kPer / 4];
+            if (usual) {
+#pragma unroll
+                for (int e = 0; e < kPer; e += 4) codes[e / 4] = four_codes(y[i].x + e, scale, r);
+            } else {
 #pragma unroll
                 for (int e = 0; e < kPer; e += 4) {
-                    const v4f four = {y.x[e], y.x[e + 1], y.x[e + 2], y.x[e + 3]};
-                    row_codes<float>(__builtin_bit_cast(v4i, four), scale, codes + e);
+                    const v4f four = {y[i].x[e], y[i].x[e + 1], y[i].x[e + 2], y[i].x[e + 3]};
+                    row_codes<float>(__builtin_bit_cast(v4i, four), scale, (int8_t *)&codes[e / 4]);
                 }
-                int8_t *const to = a.Q + row * a.q_stride + p.at / (int64_t)sizeof(T);
-                if constexpr (kShort) {
+            }
+            int8_t *const to = a.Q + row * a.q_stride + p[i].at;
+            if constexpr (kShort) {
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e)
-                        if (e < a.K) to[e] = codes[e];
-                } else {
-                    __builtin_memcpy(to, codes, kPer);
-                }
+                for (int e = 0; e < kPer; ++e)
+                    if (e < a.K) to[e] = (int8_t)(codes[e / 4] >> (8 * (e % 4)));
+            } else {
+                __builtin_memcpy(to, codes, kPer);
             }
         }
     }
@@ -190,75 +220,99 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBac
     constexpr int kPer = 16 / sizeof(T), kThreads = block_of(kLanes), kRows = kThreads / kLanes;
     __shared__ double words[kThreads / kWave];
     const int lane = threadIdx.x % kLanes;
-    const T *const gain = (const T *)a.gain;
+    Piece p[kKeep];
+    v4i gain[kKeep];
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+        p[i] = piece<T>(i * kLanes + lane, a.K);
+        gain[i] = a.gain ? load_piece<T, kShort>((const T *)a.gain, p[i], a.K) : ones<T>();
+    }
     float parts[kKeep][kPer] = {};
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += (int64_t)gridDim.x * kRows) {
         const int64_t mine = first + threadIdx.x / kLanes, row = mine < a.n ? mine : a.n - 1;
         const bool real = mine < a.n;
         const float rstd = a.rstd[row];
-        v4i h[kKeep], dy[kKeep];
+        v4i h[kKeep], dy[kKeep], dh[kKeep];
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-            const int64_t at = piece<T>(i * kLanes + lane, a.K).at;
-            h[i] = load_piece<T, kShort>((const T *)a.H + row * a.h_stride, at, a.K);
-            dy[i] = load_piece<T, kShort>((const T *)a.dY + row * a.dy_stride, at, a.K);
+            h[i] = load_piece<T, kShort>((const T *)a.H + row * a.h_stride, p[i], a.K);
+            dy[i] = load_piece<T, kShort>((const T *)a.dY + row * a.dy_stride, p[i], a.K);
         }
-        auto scaled = [&](int i, int64_t at) {
-            RowValues<T> u = row_values<T>(dy[i]);
-            if (gain) {
-                const RowValues<T> g = row_values<T>(load_piece<T, kShort>(gain, at, a.K));
+        if (a.dH) {
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) u.x[e] *= g.x[e];
-            }
-            return u;
-        };
+            for (int i = 0; i < kKeep; ++i) dh[i] = load_piece<T, kShort>((const T *)a.dH + row * a.dh_stride, p[i], a.K);
+        }
         double sum = 0;
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-            const Piece<T> p = piece<T>(i * kLanes + lane, a.K);
-            const RowValues<T> u = scaled(i, p.at), x = row_values<T>(h[i]), d = row_values<T>(dy[i]);
+            if (!real || !p[i].real) continue;
+            const RowValues<T> x = row_values<T>(h[i]), d = row_values<T>(dy[i]), g = row_values<T>(gain[i]);
             float here = 0.f;
+            if (p[i].first == 0) {
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                const bool counts = e >= p.first && (!kShort || e < a.K);
-                here += counts ? u.x[e] * x.x[e] : 0.f;
-                parts[i][e] += counts && real ? d.x[e] * (x.x[e] * rstd) : 0.f;
+                for (int e = 0; e < kPer; ++e) {
+                    const float t = d.x[e] * (x.x[e] * rstd);
+                    here += t * g.x[e];
+                    parts[i][e] += t;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const float t = d.x[e] * (x.x[e] * rstd);
+                    here += e >= p[i].first ? t * g.x[e] : 0.f;
+                    parts[i][e] += t;                        // of the values that come twice, one is written
+                }
             }
             sum += here;
         }
         sum = row_sum<kLanes>(sum, words);
-        const float c = rstd * rstd * (float)(sum / a.K);
+        const float c = (float)(sum / a.K);
         if (!real) continue;
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-            const Piece<T> p = piece<T>(i * kLanes + lane, a.K);
-            if (!p.real) continue;
-            RowValues<T> u = scaled(i, p.at);
-            const RowValues<T> x = row_values<T>(h[i]);
+            if (!p[i].real) continue;
+            RowValues<T> u = row_values<T>(dy[i]);
+            const RowValues<T> x = row_values<T>(h[i]), g = row_values<T>(gain[i]);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) u.x[e] = rstd * (u.x[e] - x.x[e] * c);
+            for (int e = 0; e < kPer; ++e) u.x[e] = rstd * (u.x[e] * g.x[e] - (x.x[e] * rstd) * c);
             if (a.dH) {
-                const RowValues<T> v = row_values<T>(load_piece<T, kShort>((const T *)a.dH + row * a.dh_stride, p.at, a.K));
+                const RowValues<T> v = row_values<T>(dh[i]);
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) u.x[e] += v.x[e];
             }
-            store_held<T, kShort>((T *)a.dX + row * a.dx_stride, p.at, a.K, rounded<T>(u));
+            store_piece<T, kShort>((T *)a.dX + row * a.dx_stride, p[i], a.K, rounded<T>(u));
         }
     }
     if (!a.dgain) return;
-    // each group of lanes writes its own sums: [workgroups * kRows, K]
-    float *const to = a.partial + ((int64_t)blockIdx.x * kRows + threadIdx.x / kLanes) * a.K;
+    // the workgroup's rows meet in LDS, in their order; lane by lane, so that a value is counted where its piece is
+    float *const to = a.partial + (int64_t)blockIdx.x * a.K;
+    if constexpr (kRows > 1) {
+        extern __shared__ float sums[];                      // [kRows, kLanes kKeep kPer]
+        constexpr int kRow = kLanes * kKeep * kPer;
 #pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-        const Piece<T> p = piece<T>(i * kLanes + lane, a.K);
-        const int32_t begin = (int32_t)(p.at / (int64_t)sizeof(T));
+        for (int i = 0; i < kKeep; ++i)
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (p.real && e >= p.first && begin + e < a.K) to[begin + e] = parts[i][e];
+            for (int e = 0; e < kPer; ++e) sums[threadIdx.x / kLanes * kRow + (i * kPer + e) * kLanes + lane] = parts[i][e];
+        __syncthreads();
+        for (int at = threadIdx.x; at < kRow; at += kThreads) {
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) sum += sums[r * kRow + at];
+            const int from = at % kLanes, e = at / kLanes % kPer;
+            const Piece place = piece<T>(at / kLanes / kPer * kLanes + from, a.K);
+            if (place.real && e >= place.first && place.at + e < a.K) to[place.at + e] = sum;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (p[i].real && e >= p[i].first && p[i].at + e < a.K) to[p[i].at + e] = parts[i][e];
+        }
     }
 }
 
-constexpr int kGainCols = 32, kGainRows = 32;
+constexpr int kGainCols = 16, kGainRows = 64;
 
 template <typename O>
 __global__ __launch_bounds__(1024) void norm_gain_kernel(const float *__restrict__ partial, int64_t groups, int32_t K, O *__restrict__ dgain)
@@ -268,7 +322,10 @@ __global__ __launch_bounds__(1024) void norm_gain_kernel(const float *__restrict
     const int32_t k = blockIdx.x * kGainCols + col;
     double sum = 0;
     if (k < K)
+    {
+#pragma unroll 8
         for (int64_t g = part; g < groups; g += kGainRows) sum += (double)partial[g * K + k];
+    }
     sums[part][col] = sum;
     __syncthreads();
     if (part || k >= K) return;
@@ -286,31 +343,40 @@ NormShape norm_shape(int32_t K, int bytes)
     const int64_t pieces = ((int64_t)K * bytes + 15) / 16;
     if (K * (int64_t)bytes < 16) return {16, 1, true};
     if (pieces <= 16) return {16, 1, false};
+    if (pieces <= 32) return {16, 2, false};
     if (pieces <= 64) return {64, 1, false};
+    if (pieces <= 128) return {64, 2, false};
     if (pieces <= 256) return {64, 4, false};
+    if (pieces <= 512) return {256, 2, false};
     if (pieces <= 1024) return {256, 4, false};
-    if (pieces <= 2048) return {256, 8, false};
+    if (pieces <= 2048) return {512, 4, false};
+    if (pieces <= 4096) return {1024, 4, false};
     if (pieces <= 8192) return {1024, 8, false};
     return {1024, 16, false};
 }
 
+constexpr int rows_of(int lanes) { return block_of(lanes) / lanes; }
 int64_t norm_blocks(int64_t n, const NormShape &s, int64_t most)
 {
-    const int rows = block_of(s.lanes) / s.lanes;
-    const int64_t b = (n + rows - 1) / rows;
+    const int64_t b = (n + rows_of(s.lanes) - 1) / rows_of(s.lanes);
     return b < most ? b : most;
 }
-constexpr int64_t kBackwardBlocks = 512;
+// Workgroups of the backward call: as many as run at a time, and no more, as each writes a row of partial sums.
+int64_t backward_blocks(int64_t n, const NormShape &s) { return norm_blocks(n, s, s.lanes <= kWave ? 2048 : s.lanes <= kBlock ? 1024 : 256); }
 
 #define GROOT_NORM_SHAPES(use)                                                                                                           \
     if (s.is_short) use(16, 1, true)                                                                                                     \
-    else if (s.lanes == 16) use(16, 1, false)                                                                                            \
+    else if (s.lanes == 16 && s.keep == 1) use(16, 1, false)                                                                             \
+    else if (s.lanes == 16) use(16, 2, false)                                                                                            \
     else if (s.lanes == 64 && s.keep == 1) use(64, 1, false)                                                                             \
+    else if (s.lanes == 64 && s.keep == 2) use(64, 2, false)                                                                             \
     else if (s.lanes == 64) use(64, 4, false)                                                                                            \
-    else if (s.lanes == 256 && s.keep == 4) use(256, 4, false)                                                                           \
-    else if (s.lanes == 256) use(256, 8, false)                                                                                          \
+    else if (s.lanes == 256 && s.keep == 2) use(256, 2, false)                                                                           \
+    else if (s.lanes == 256) use(256, 4, false)                                                                                          \
+    else if (s.lanes == 512) use(512, 4, false)                                                                                          \
+    else if (s.keep == 4) use(1024, 4, false)                                                                                            \
     else if (s.keep == 8) use(1024, 8, false)                                                                                            \
-    else use(1024, 16, false)
+    else if constexpr (sizeof(T) == 4) use(1024, 16, false)
 
 template <typename T>
 int norm_launch(const NormArgs &a, hipStream_t stream)
@@ -327,13 +393,17 @@ template <typename T>
 int norm_backward_launch(const NormBackwardArgs &a, hipStream_t stream)
 {
     const NormShape s = norm_shape(a.K, sizeof(T));
-    const uint32_t blocks = (uint32_t)norm_blocks(a.n, s, kBackwardBlocks);
-#define GROOT_NORM(lanes, keep, is_short) { norm_backward_kernel<T, lanes, keep, is_short><<<blocks, block_of(lanes), 0, stream>>>(a); }
+    const uint32_t blocks = (uint32_t)backward_blocks(a.n, s);
+#define GROOT_NORM(lanes, keep, is_short)                                                                                                \
+    {                                                                                                                                    \
+        norm_backward_kernel<T, lanes, keep, is_short>                                                                                   \
+            <<<blocks, block_of(lanes), rows_of(lanes) > 1 ? block_of(lanes) * keep * 16 / sizeof(T) * sizeof(float) : 0, stream>>>(a);  \
+    }
     if (blocks) { GROOT_NORM_SHAPES(GROOT_NORM) }
 #undef GROOT_NORM
     if (a.dgain) {
         const uint32_t cols = (a.K + kGainCols - 1) / kGainCols;
-        const int64_t groups = (int64_t)blocks * (block_of(s.lanes) / s.lanes);
+        const int64_t groups = blocks;
         if (a.grad_f32) norm_gain_kernel<<<cols, 1024, 0, stream>>>(a.partial, groups, a.K, (float *)a.dgain);
         else norm_gain_kernel<<<cols, 1024, 0, stream>>>(a.partial, groups, a.K, (T *)a.dgain);
     }
@@ -345,7 +415,7 @@ int norm_backward_launch(const NormBackwardArgs &a, hipStream_t stream)
 size_t norm_backward_workspace(int32_t dtype, int64_t n, int32_t K)
 {
     const NormShape s = norm_shape(K, dtype == GROOT_F32 ? 4 : 2);
-    return (size_t)norm_blocks(n, s, kBackwardBlocks) * (block_of(s.lanes) / s.lanes) * K * sizeof(float);
+    return (size_t)backward_blocks(n, s) * K * sizeof(float);
 }
 
 int launch_norm(int32_t dtype, const NormArgs &a, void *stream)

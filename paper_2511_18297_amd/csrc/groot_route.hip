@@ -33,34 +33,6 @@ __device__ __forceinline__ float score_at(const void *row, int32_t dtype, int32_
     return (float)((const f16_t *)row)[e];
 }
 
-// the value of lane ^ (kAway, or the other lanes of twice as many that hold the same), for rows of lanes whose lower halves agree
-template <int kAway>
-__device__ __forceinline__ uint32_t other_lane(uint32_t x)
-{
-    if constexpr (kAway == 1) return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false);        // quad_perm 1 0 3 2
-    else if constexpr (kAway == 2) return __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, false);   // quad_perm 2 3 0 1
-    else if constexpr (kAway == 4) return __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, false);  // row_half_mirror
-    else if constexpr (kAway == 8) return __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, false);  // row_mirror
-    else return __shfl_xor(x, kAway);
-}
-template <int kAway>
-__device__ __forceinline__ float other_lane(float x)
-{
-    return __uint_as_float(other_lane<kAway>(__float_as_uint(x)));
-}
-template <int kAway>
-__device__ __forceinline__ double other_lane(double x)
-{
-    const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    return __builtin_bit_cast(double, (uint64_t)other_lane<kAway>((uint32_t)(b >> 32)) << 32 | other_lane<kAway>((uint32_t)b));
-}
-// over kLanes lanes, every one of which takes part
-template <int kLanes, int kAway = 1, typename T, typename F>
-__device__ __forceinline__ T over_lanes(T x, F both)
-{
-    if constexpr (kAway < kLanes) return over_lanes<kLanes, kAway * 2>(both(x, other_lane<kAway>(x)), both);
-    else return x;
-}
 template <int kLanes, typename T>
 __device__ __forceinline__ T top_of(T x)
 {
@@ -233,7 +205,7 @@ __device__ __forceinline__ void merge_lanes(double *x)
     if constexpr (kAway < kLanes) {
         double y[kCount];
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) y[i] = other_lane<kAway>(x[i]);
+        for (int i = 0; i < kCount; ++i) pair_lanes<kAway>(x[i], &x[i], &y[i]);
         merge_keys<kCount>(x, y);
         merge_lanes<kLanes, kCount, kAway * 2>(x);
     }
@@ -264,6 +236,17 @@ __device__ __forceinline__ void exclusive_sums(int32_t *x, int32_t E, int32_t *w
         }
     if (tid == threads - 1) x[E] = before;
     __syncthreads();
+}
+
+// the two largest of a set, of what lanes kAway apart hold of it
+template <int kAway>
+__device__ __forceinline__ void meet_sets(double &most, double &second)
+{
+    double m1, m2, s1, s2;
+    pair_lanes<kAway>(most, &m1, &m2);
+    pair_lanes<kAway>(second, &s1, &s2);
+    most = larger(m1, m2);
+    second = larger(larger(s1, s2), smaller(m1, m2));
 }
 
 // Sets of kSize neighbouring experts, several in a lane: `values` of the row's sets, and those that are not among the open ones closed.
@@ -396,15 +379,11 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int32
                     second = larger(second, smaller(most, x[v]));
                     most = larger(most, x[v]);
                 }
-                auto meet = [&](double o1, double o2) {
-                    second = larger(larger(second, o2), smaller(most, o1));
-                    most = larger(most, o1);
-                };
-                if (a.set_lanes > 1) meet(other_lane<1>(most), other_lane<1>(second));
-                if (a.set_lanes > 2) meet(other_lane<2>(most), other_lane<2>(second));
-                if (a.set_lanes > 4) meet(other_lane<4>(most), other_lane<4>(second));
-                if (a.set_lanes > 8) meet(other_lane<8>(most), other_lane<8>(second));
-                if (a.set_lanes > 16) meet(other_lane<16>(most), other_lane<16>(second));
+                if (a.set_lanes > 1) meet_sets<1>(most, second);
+                if (a.set_lanes > 2) meet_sets<2>(most, second);
+                if (a.set_lanes > 4) meet_sets<4>(most, second);
+                if (a.set_lanes > 8) meet_sets<8>(most, second);
+                if (a.set_lanes > 16) meet_sets<16>(most, second);
                 const int32_t set = lane / a.set_lanes;
                 const double mine = key_of(a.set_best == 2 && second > kLeastOpen ? fmin(most + second, kMostOpen) : most, (uint32_t)set, 63);
                 if (set < a.sets && lane % a.set_lanes == 0) values[set] = mine;
