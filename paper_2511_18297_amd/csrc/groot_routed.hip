@@ -11,151 +11,308 @@ namespace groot {
 
 namespace {
 
+// where piece `i` of a row of `bytes` begins
+__device__ __forceinline__ int64_t piece_at(int64_t i, int64_t bytes) { return i * 16 + 16 <= bytes || bytes < 16 ? i * 16 : bytes - 16; }
+
+typedef v4i piece_t __attribute__((aligned(1)));
+// kOnce: past the caches
+template <bool kOnce>
+__device__ __forceinline__ v4i get(const char *p)
+{
+    if constexpr (kOnce) return __builtin_nontemporal_load((const piece_t *)p);
+    else return *(const piece_t *)p;
+}
+template <bool kOnce>
+__device__ __forceinline__ void put(char *p, v4i v)
+{
+    if constexpr (kOnce) __builtin_nontemporal_store(v, (piece_t *)p);
+    else *(piece_t *)p = v;
+}
+
+// A place of the row, the same in all of its lanes: -1 for none.  Rows of a whole wavefront read it as a scalar.
+template <int kLanes>
+__device__ __forceinline__ int64_t row_of(int64_t row)
+{
+    return kLanes >= kWave ? uniform(row) : row;
+}
 __device__ __forceinline__ int64_t place_at(const RoutedArgs &a, int64_t row, int32_t slot)
 {
     const int32_t p = a.places[row * a.k + slot];
     return p >= 0 && p < a.n_places ? p : -1;
 }
 
-// where piece `i` of a row of `bytes` begins
-__device__ __forceinline__ int64_t piece_at(int64_t i, int64_t bytes) { return i * 16 + 16 <= bytes || bytes < 16 ? i * 16 : bytes - 16; }
-
-// kLanes lanes to a row's kLanes pieces; the numbers of rows and of groups of pieces are the grid's
-template <int kLanes>
+// A workgroup's rows: kLanes lanes each, blockDim.x / kLanes of them at a time; blockIdx.y is the row's part of a.part pieces.
+// kPieces of them in a lane at a time; a lane's beyond the last go along with another one, which is stored more than once, alike.
+template <int kLanes, int kPieces, bool kOnce>
 __global__ __launch_bounds__(kBlock) void routed_rows_kernel(RoutedArgs a, int64_t bytes, int64_t x_bytes, int64_t r_bytes)
 {
-    const int lane = threadIdx.x % kLanes;
-    const int64_t pieces = (bytes + 15) / 16, parts = (pieces + kLanes - 1) / kLanes;
-    for (int64_t u = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kLanes; u < a.n * parts; u += (int64_t)gridDim.x * (kBlock / kLanes)) {
-        const int64_t row = u / parts, i = u % parts * kLanes + lane;
-        if (i >= pieces) continue;
+    const int lane = threadIdx.x % kLanes, rows = blockDim.x / kLanes;
+    const int64_t pieces = (bytes + 15) / 16, begin = (int64_t)blockIdx.y * a.part, end = begin + a.part < pieces ? begin + a.part : pieces;
+    for (int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / kLanes; r < a.n; r += (int64_t)gridDim.x * rows) {
+        const int64_t row = row_of<kLanes>(r);
         const char *const x = (const char *)a.X + row * x_bytes;
-        const int64_t at = piece_at(i, bytes);
-        v4i v;
-        if (bytes >= 16) __builtin_memcpy(&v, x + at, 16);
-        const float scale = a.scale_in && i == 0 ? a.scale_in[row] : 0.f;
-        for (int32_t s = 0; s < a.k; ++s) {
-            const int64_t p = place_at(a, row, s);
-            if (p < 0) continue;
-            char *const to = (char *)a.out + p * r_bytes;
-            if (bytes >= 16) __builtin_memcpy(to + at, &v, 16);
-            else
-                for (int b = 0; b < (int)bytes; ++b) to[b] = x[b];
-            if (a.scale_in && i == 0) a.scale_out[p] = scale;
+        if (bytes < 16) {
+            if (lane == 0)
+                for (int32_t s = 0; s < a.k; ++s) {
+                    const int64_t p = place_at(a, row, s);
+                    for (int b = 0; b < (int)bytes && p >= 0; ++b) ((char *)a.out + p * r_bytes)[b] = x[b];
+                }
+        } else {
+            for (int64_t i = begin + lane; i < end; i += kLanes * kPieces) {
+                int64_t at[kPieces];
+                v4i v[kPieces];
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) {
+                    at[j] = piece_at(i + j * kLanes < end ? i + j * kLanes : i, bytes);
+                    v[j] = get<true>(x + at[j]);
+                }
+                for (int32_t s = 0; s < a.k; ++s) {
+                    const int64_t p = place_at(a, row, s);
+                    if (p < 0) continue;
+                    char *const to = (char *)a.out + p * r_bytes;
+#pragma unroll
+                    for (int j = 0; j < kPieces; ++j) put<kOnce>(to + at[j], v[j]);
+                }
+            }
         }
+        if (a.scale_in && blockIdx.y == 0)
+            for (int32_t s = lane; s < a.k; s += kLanes) {
+                const int64_t p = place_at(a, row, s);
+                if (p >= 0) a.scale_out[p] = a.scale_in[row];
+            }
     }
 }
 
-template <typename T>
-__device__ __forceinline__ v4i piece_of(const char *row, int64_t at, int32_t K, bool is_short)
+template <typename T, bool kShort, bool kOnce>
+__device__ __forceinline__ v4i piece_of(const char *row, int64_t at, int32_t K)
 {
-    if (is_short) return short16<T>(row, K * (int64_t)sizeof(T));
-    v4i v;
-    __builtin_memcpy(&v, row + at, 16);
-    return v;
+    if constexpr (kShort) return short16<T>(row, K * (int64_t)sizeof(T));
+    else return get<kOnce>(row + at);
 }
-template <typename T>
-__device__ __forceinline__ void store_piece(char *row, int64_t at, int32_t K, bool is_short, const float (&x)[16 / sizeof(T)])
+template <typename T, bool kShort, bool kOnce>
+__device__ __forceinline__ void store_piece(char *row, int64_t at, int32_t K, const float (&x)[16 / sizeof(T)])
 {
     constexpr int kPer = 16 / sizeof(T);
-    T e[kPer];
+    typedef T vt __attribute__((ext_vector_type(kPer)));
+    vt e;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) e[k] = (T)x[k];           // the one rounding
-    if (is_short) {
+    if constexpr (kShort) {
+#pragma unroll
         for (int k = 0; k < kPer; ++k)
             if (k < K) ((T *)row)[k] = e[k];
     } else {
-        __builtin_memcpy(row + at, e, 16);
+        put<kOnce>(row + at, __builtin_bit_cast(v4i, e));
     }
 }
+// the pieces of the rows at kBatch places from `slot` on; a slot without a place has a row of zeros, so that no load waits for a branch
+template <typename T, int kBatch, int kPieces, bool kShort>
+__device__ __forceinline__ void slot_pieces(const RoutedArgs &a, int64_t row, int32_t slot, const int64_t (&at)[kPieces], int64_t (&p)[kBatch],
+                                            v4i (&v)[kBatch][kPieces])
+{
+#pragma unroll
+    for (int s = 0; s < kBatch; ++s) p[s] = slot + s < a.k ? place_at(a, row, slot + s) : -1;
+#pragma unroll
+    for (int s = 0; s < kBatch; ++s)
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const char *const from = (const char *)((const T *)a.R + (p[s] < 0 ? 0 : p[s]) * a.r_stride);
+            if constexpr (kShort) v[s][j] = p[s] < 0 ? v4i{0, 0, 0, 0} : piece_of<T, true, false>(from, at[j], a.K);
+            else v[s][j] = piece_of<T, false, false>(p[s] < 0 ? (const char *)&g_zeros : from, p[s] < 0 ? 0 : at[j], a.K);
+        }
+}
 
-template <typename T, int kLanes>
+template <typename T, int kLanes, int kPieces, bool kShort, bool kOnce>
 __global__ __launch_bounds__(kBlock) void routed_sum_kernel(RoutedArgs a)
 {
-    constexpr int kPer = 16 / sizeof(T);
-    const int lane = threadIdx.x % kLanes;
-    const int64_t bytes = (int64_t)a.K * sizeof(T), pieces = (bytes + 15) / 16, parts = (pieces + kLanes - 1) / kLanes;
-    const bool is_short = bytes < 16;
-    for (int64_t u = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kLanes; u < a.n * parts; u += (int64_t)gridDim.x * (kBlock / kLanes)) {
-        const int64_t row = u / parts, i = u % parts * kLanes + lane;
-        if (i >= pieces) continue;
-        const int64_t at = piece_at(i, bytes);
-        float sum[kPer];
-        RowValues<T> v{};
-        if (a.addend) v = row_values<T>(piece_of<T>((const char *)((const T *)a.addend + row * a.addend_stride), at, a.K, is_short));
+    constexpr int kPer = 16 / sizeof(T), kBatch = 4;
+    const int lane = threadIdx.x % kLanes, rows = blockDim.x / kLanes;
+    const int64_t bytes = (int64_t)a.K * sizeof(T), pieces = (bytes + 15) / 16;
+    const int64_t begin = (int64_t)blockIdx.y * a.part, end = begin + a.part < pieces ? begin + a.part : pieces;
+    for (int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / kLanes; r < a.n; r += (int64_t)gridDim.x * rows) {
+        const int64_t row = row_of<kLanes>(r);
+        const char *const addend = a.addend ? (const char *)((const T *)a.addend + row * a.addend_stride) : nullptr;
+        for (int64_t i = begin + lane; i < end; i += kLanes * kPieces) {
+            int64_t at[kPieces];
+            float sum[kPieces][kPer];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) sum[e] = v.x[e];
-        for (int32_t s = 0; s < a.k; ++s) {
-            const int64_t p = place_at(a, row, s);
-            const float w = a.weights ? a.weights[row * a.k + s] : 1.f;
-            if (p >= 0) v = row_values<T>(piece_of<T>((const char *)((const T *)a.R + p * a.r_stride), at, a.K, is_short));
-            else v = RowValues<T>{};                         // no place: a row of zeros, which a weight of NaN still shows in
+            for (int j = 0; j < kPieces; ++j) {
+                at[j] = piece_at(i + j * kLanes < end ? i + j * kLanes : i, bytes);
+                const RowValues<T> v = a.addend ? row_values<T>(piece_of<T, kShort, true>(addend, at[j], a.K)) : RowValues<T>{};
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) sum[e] += w * v.x[e];
+                for (int e = 0; e < kPer; ++e) sum[j][e] = v.x[e];
+            }
+            for (int32_t slot = 0; slot < a.k; slot += kBatch) {
+                int64_t p[kBatch];
+                v4i v[kBatch][kPieces];
+                slot_pieces<T, kBatch, kPieces, kShort>(a, row, slot, at, p, v);
+#pragma unroll
+                for (int s = 0; s < kBatch; ++s) {
+                    if (slot + s >= a.k) break;
+                    const float w = a.weights ? a.weights[row * a.k + slot + s] : 1.f;    // a NaN shows without a place too
+#pragma unroll
+                    for (int j = 0; j < kPieces; ++j) {
+                        const RowValues<T> x = row_values<T>(v[s][j]);
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e) sum[j][e] += w * x.x[e];
+                    }
+                }
+            }
+            char *const to = (char *)((T *)a.out + row * a.out_stride);
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) store_piece<T, kShort, kOnce>(to, at[j], a.K, sum[j]);
         }
-        store_piece<T>((char *)((T *)a.out + row * a.out_stride), at, a.K, is_short, sum);
     }
 }
 
-template <typename T, int kLanes>
+// kPieces > 0: a row's gradient stays in registers over its slots, kPieces pieces in each of kLanes lanes; 0: rows of any width, whose
+// gradient is read again for every slot
+template <typename T, int kLanes, int kPieces, bool kShort, bool kOnce>
 __global__ __launch_bounds__(kBlock) void routed_sum_backward_kernel(RoutedArgs a)
 {
-    constexpr int kPer = 16 / sizeof(T);
-    const int lane = threadIdx.x % kLanes;
-    const int64_t bytes = (int64_t)a.K * sizeof(T), pieces = (bytes + 15) / 16;
-    const bool is_short = bytes < 16;
-    for (int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kLanes; row < a.n; row += (int64_t)gridDim.x * (kBlock / kLanes)) {
+    constexpr int kPer = 16 / sizeof(T), kBatch = 2, kHeld = kPieces ? kPieces : 1;
+    const int lane = threadIdx.x % kLanes, rows = blockDim.x / kLanes;
+    const int64_t bytes = (int64_t)a.K * sizeof(T);
+    const int32_t pieces = (int32_t)((bytes + 15) / 16);
+    for (int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / kLanes; r < a.n; r += (int64_t)gridDim.x * rows) {
+        const int64_t row = row_of<kLanes>(r);
         const char *const d_row = (const char *)((const T *)a.X + row * a.x_stride);
-        for (int32_t s = 0; s < a.k; ++s) {
-            const int64_t p = place_at(a, row, s);
-            const float w = a.weights ? a.weights[row * a.k + s] : 1.f;
-            const char *const r_row = (const char *)((const T *)a.R + (p < 0 ? 0 : p) * a.r_stride);
-            float dot = 0.f;
-            for (int64_t i = lane; i < pieces && p >= 0; i += kLanes) {
-                const int64_t at = piece_at(i, bytes);
-                const RowValues<T> d = row_values<T>(piece_of<T>(d_row, at, a.K, is_short));
-                if (a.dweights) {
-                    const RowValues<T> r = row_values<T>(piece_of<T>(r_row, at, a.K, is_short));
-                    const int64_t before = (i * 16 - at) / (int64_t)sizeof(T);    // values that the piece before has counted
+        v4i d[kHeld];
+        int64_t at[kHeld];
+        int counted[kHeld];                                  // values that the piece before has counted
+        auto locate = [&](int32_t i, int j) {
+            at[j] = piece_at(i < pieces ? i : pieces - 1, bytes);
+            counted[j] = i >= pieces ? kPer : bytes < 16 ? 0 : (int)((i * (int64_t)16 - at[j]) / (int64_t)sizeof(T));
+            d[j] = piece_of<T, kShort, true>(d_row, at[j], a.K);
+        };
+        if (kPieces) {
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e) dot += e >= before ? d.x[e] * r.x[e] : 0.f;
-                }
-                if (a.out) {
-                    float x[kPer];
+            for (int j = 0; j < kHeld; ++j) locate(lane + j * kLanes, j);
+        }
+        for (int32_t slot = 0; slot < a.k; slot += kBatch) {
+            float dot[kBatch] = {}, w[kBatch];
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e) x[e] = w * d.x[e];
-                    store_piece<T>((char *)((T *)a.out + p * a.out_stride), at, a.K, is_short, x);
+            for (int s = 0; s < kBatch; ++s) w[s] = a.weights && slot + s < a.k ? a.weights[row * a.k + slot + s] : 1.f;
+            for (int32_t i = 0; i < (kPieces ? 1 : pieces); i += kLanes) {
+                if (!kPieces) locate(i + lane, 0);
+                int64_t p[kBatch];
+                v4i v[kBatch][kHeld];
+                if (a.dweights) slot_pieces<T, kBatch, kHeld, kShort>(a, row, slot, at, p, v);
+#pragma unroll
+                for (int s = 0; s < kBatch; ++s) {
+                    if (!a.dweights) p[s] = slot + s < a.k ? place_at(a, row, slot + s) : -1;
+                    if (p[s] < 0) continue;
+#pragma unroll
+                    for (int j = 0; j < kHeld; ++j) {
+                        const RowValues<T> g = row_values<T>(d[j]);
+                        if (a.dweights) {
+                            const RowValues<T> x = row_values<T>(v[s][j]);
+                            float sum = 0.f;
+                            if (counted[j] == 0) {
+#pragma unroll
+                                for (int e = 0; e < kPer; ++e) sum += g.x[e] * x.x[e];
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < kPer; ++e) sum += e >= counted[j] ? g.x[e] * x.x[e] : 0.f;
+                            }
+                            dot[s] += sum;
+                        }
+                        if (a.out) {
+                            float x[kPer];
+#pragma unroll
+                            for (int e = 0; e < kPer; ++e) x[e] = w[s] * g.x[e];
+                            store_piece<T, kShort, kOnce>((char *)((T *)a.out + p[s] * a.out_stride), at[j], a.K, x);
+                        }
+                    }
                 }
             }
             if (a.dweights) {
 #pragma unroll
-                for (int m = 1; m < kLanes; m *= 2) dot += __shfl_xor(dot, m);
-                if (lane == 0) a.dweights[row * a.k + s] = dot;
+                for (int s = 0; s < kBatch; ++s) {
+                    dot[s] = over_lanes<kLanes>(dot[s], [](float x, float y) { return x + y; });
+                    if (lane == 0 && slot + s < a.k) a.dweights[row * a.k + slot + s] = dot[s];
+                }
             }
         }
     }
 }
 
-uint32_t blocks_for(int64_t units, int lanes)
+// Threads of a workgroup and the grid: where rows alone are too few wavefronts for the GPU, each is cut into parts.
+struct RoutedShape {
+    int threads;
+    dim3 grid;
+};
+constexpr int64_t kEnoughWaves = 4096;       // four to a SIMD
+RoutedShape routed_shape(RoutedArgs *a, int64_t pieces, int lanes)
 {
-    const int64_t b = (units * lanes + kBlock - 1) / kBlock;
-    return (uint32_t)(b < (1 << 20) ? b : 1 << 20);
+    const int64_t waves = lanes >= kWave ? a->n * (lanes / kWave) : (a->n + kWave / lanes - 1) / (kWave / lanes);
+    const int64_t most = (pieces + lanes - 1) / lanes;       // parts of one piece a lane
+    int64_t parts = 1;
+    while (parts * 2 <= most && waves * parts * 2 <= kEnoughWaves) parts *= 2;
+    int64_t part = (pieces + parts - 1) / parts;
+    part = (part + lanes - 1) / lanes * lanes;
+    a->part = (int32_t)part;
+    const int threads = lanes > kWave || waves * parts >= 4 * 256 ? kBlock : kWave;
+    const int64_t blocks = (a->n + threads / lanes - 1) / (threads / lanes);
+    return {threads, dim3((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), (uint32_t)((pieces + part - 1) / part))};
 }
+// outputs that the L2 of the eight XCDs would not hold for the next call anyway go past it
+bool beyond_caches(int64_t rows, int64_t bytes) { return rows * bytes > (32 << 20); }
 
-template <typename T>
-int sum_launch(const RoutedArgs &a, hipStream_t stream)
+template <typename T, bool kOnce>
+int sum_launch(RoutedArgs a, hipStream_t stream)
 {
     const int64_t pieces = ((int64_t)a.K * sizeof(T) + 15) / 16;
-    if (pieces <= 16) routed_sum_kernel<T, 16><<<blocks_for(a.n, 16), kBlock, 0, stream>>>(a);
-    else routed_sum_kernel<T, 64><<<blocks_for(a.n * ((pieces + 63) / 64), 64), kBlock, 0, stream>>>(a);
+#define GROOT_SUM(lanes, per_lane, is_short)                                                                                             \
+    {                                                                                                                                    \
+        const RoutedShape s = routed_shape(&a, pieces, lanes);                                                                           \
+        routed_sum_kernel<T, lanes, per_lane, is_short, kOnce><<<s.grid, s.threads, 0, stream>>>(a);                                     \
+    }
+    // a workgroup takes a whole row at once where it can
+    if (a.K * sizeof(T) < 16) GROOT_SUM(16, 1, true)
+    else if (pieces <= 16) GROOT_SUM(16, 1, false)
+    else if (pieces <= 64) GROOT_SUM(64, 1, false)
+    else if (pieces <= 128) GROOT_SUM(64, 2, false)
+    else if (pieces <= 256) GROOT_SUM(256, 1, false)
+    else GROOT_SUM(256, 2, false)
+#undef GROOT_SUM
     return (int)hipGetLastError();
 }
-template <typename T>
-int sum_backward_launch(const RoutedArgs &a, hipStream_t stream)
+template <typename T, bool kOnce>
+int sum_backward_launch(RoutedArgs a, hipStream_t stream)
 {
     const int64_t pieces = ((int64_t)a.K * sizeof(T) + 15) / 16;
-    if (pieces <= 16) routed_sum_backward_kernel<T, 16><<<blocks_for(a.n, 16), kBlock, 0, stream>>>(a);
-    else routed_sum_backward_kernel<T, 64><<<blocks_for(a.n, 64), kBlock, 0, stream>>>(a);
+#define GROOT_SUM(lanes, held, is_short)                                                                                                 \
+    {                                                                                                                                    \
+        const RoutedShape s = routed_shape(&a, 1, lanes);                                                                                \
+        routed_sum_backward_kernel<T, lanes, held, is_short, kOnce><<<s.grid, s.threads, 0, stream>>>(a);                                \
+    }
+    if (a.K * sizeof(T) < 16) GROOT_SUM(16, 1, true)
+    else if (pieces <= 16) GROOT_SUM(16, 1, false)
+    else if (pieces <= 64) GROOT_SUM(64, 1, false)
+    else if (pieces <= 128) GROOT_SUM(64, 2, false)
+    else if (pieces <= 256) GROOT_SUM(64, 4, false)
+    else if (pieces <= 512) GROOT_SUM(64, 8, false)
+    else GROOT_SUM(64, 0, false)
+#undef GROOT_SUM
+    return (int)hipGetLastError();
+}
+template <bool kOnce>
+int rows_launch(RoutedArgs a, int32_t value_bytes, hipStream_t stream)
+{
+    const int64_t bytes = (int64_t)a.K * value_bytes, pieces = (bytes + 15) / 16;
+#define GROOT_ROWS(lanes, per_lane)                                                                                                      \
+    {                                                                                                                                    \
+        const RoutedShape s = routed_shape(&a, pieces, lanes);                                                                           \
+        routed_rows_kernel<lanes, per_lane, kOnce>                                                                                       \
+            <<<s.grid, s.threads, 0, stream>>>(a, bytes, a.x_stride * value_bytes, a.out_stride * value_bytes);                          \
+    }
+    if (pieces <= 16) GROOT_ROWS(16, 1)
+    else if (pieces <= 64) GROOT_ROWS(64, 1)
+    else if (pieces <= 128) GROOT_ROWS(64, 2)
+    else if (pieces <= 256) GROOT_ROWS(256, 1)
+    else GROOT_ROWS(256, 2)
+#undef GROOT_ROWS
     return (int)hipGetLastError();
 }
 
@@ -163,27 +320,26 @@ int sum_backward_launch(const RoutedArgs &a, hipStream_t stream)
 
 int launch_routed_rows(int32_t value_bytes, const RoutedArgs &a, void *stream)
 {
-    const int64_t bytes = (int64_t)a.K * value_bytes, pieces = (bytes + 15) / 16;
     hipStream_t s = (hipStream_t)stream;
-    if (pieces <= 16) routed_rows_kernel<16><<<blocks_for(a.n, 16), kBlock, 0, s>>>(a, bytes, a.x_stride * value_bytes, a.out_stride * value_bytes);
-    else routed_rows_kernel<64><<<blocks_for(a.n * ((pieces + 63) / 64), 64), kBlock, 0, s>>>(a, bytes, a.x_stride * value_bytes, a.out_stride * value_bytes);
-    return (int)hipGetLastError();
+    return beyond_caches(a.n * a.k, (int64_t)a.K * value_bytes) ? rows_launch<true>(a, value_bytes, s) : rows_launch<false>(a, value_bytes, s);
 }
 
 int launch_routed_sum(int32_t dtype, const RoutedArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == GROOT_F32) return sum_launch<float>(a, s);
-    if (dtype == GROOT_BF16) return sum_launch<bf16_t>(a, s);
-    return sum_launch<f16_t>(a, s);
+    const bool once = beyond_caches(a.n, (int64_t)a.K * (dtype == GROOT_F32 ? 4 : 2));
+    if (dtype == GROOT_F32) return once ? sum_launch<float, true>(a, s) : sum_launch<float, false>(a, s);
+    if (dtype == GROOT_BF16) return once ? sum_launch<bf16_t, true>(a, s) : sum_launch<bf16_t, false>(a, s);
+    return once ? sum_launch<f16_t, true>(a, s) : sum_launch<f16_t, false>(a, s);
 }
 
 int launch_routed_sum_backward(int32_t dtype, const RoutedArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == GROOT_F32) return sum_backward_launch<float>(a, s);
-    if (dtype == GROOT_BF16) return sum_backward_launch<bf16_t>(a, s);
-    return sum_backward_launch<f16_t>(a, s);
+    const bool once = beyond_caches(a.n * a.k, (int64_t)a.K * (dtype == GROOT_F32 ? 4 : 2));
+    if (dtype == GROOT_F32) return once ? sum_backward_launch<float, true>(a, s) : sum_backward_launch<float, false>(a, s);
+    if (dtype == GROOT_BF16) return once ? sum_backward_launch<bf16_t, true>(a, s) : sum_backward_launch<bf16_t, false>(a, s);
+    return once ? sum_backward_launch<f16_t, true>(a, s) : sum_backward_launch<f16_t, false>(a, s);
 }
 
 }  // namespace groot
