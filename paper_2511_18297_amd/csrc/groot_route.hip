@@ -322,6 +322,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int32
         const int local = pass + threadIdx.x / kLanes;
         const bool real = local < here;                                   // rows beyond the last go along
         const char *const scores = (const char *)a.scores + (first + (real ? local : here - 1)) * a.score_bytes;
+        float bias[kByValue ? kEach : 1] = {};
+        if constexpr (kByValue) {
+            if (a.bias) load_scores_of<kEach, float>((const char *)a.bias, a.E, begin, bias);
+        }
         float s[kEach];
         load_scores<kEach>(scores, a, begin, s);
         float top = s[0];                                                 // NaN if one of them is
@@ -359,8 +363,6 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int32
                 sum = (float)all;
                 all = 1.0 / all;
             }
-            float bias[kEach] = {};
-            if (a.bias) load_scores_of<kEach, float>((const char *)a.bias, a.E, begin, bias);
 #pragma unroll
             for (int v = 0; v < kEach; ++v) {
                 const double p = sigmoid ? (s[v] < 0.f ? x[v] : 1.0) * reciprocal64(1.0 + x[v]) : x[v] * all;
@@ -639,7 +641,7 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
             d[v] = 0.f;
         }
         broken = any_of<kLanes>(broken);
-        top = (float)top_of<kLanes>(top);
+        top = top_of<kLanes>(top);
         const float base = top == -kInf ? 0.f : top;
         // slots: lane = slot
         int32_t mine = -1;
@@ -652,9 +654,9 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
         const float s = mine >= 0 ? score_at(scores, a.dtype, mine) : -kInf;
         float at_log = 0.f;                                   // the gradient at the slot's log p, or at its score
         if (a.renormalise) {
-            const float u = mine < 0 ? -kInf : a.gate == GROOT_SOFTMAX ? s : fminf(s, 0.f) - log1pf(expf(-fabsf(s)));
-            const float most = (float)top_of<kLanes>(u);
-            const float q = mine < 0 ? 0.f : expf(u - most);
+            const bool sigmoid = a.gate == GROOT_SIGMOID;
+            const float most = top_of<kLanes>(sigmoid ? fminf(s, 0.f) : s);
+            const float q = mine < 0 || s == -kInf ? 0.f : weight_of(s, most, sigmoid);
             const float all = (float)sum_of<kLanes>(q);       // every lane takes part
             const float w = mine < 0 ? 0.f : q / all;
             const float mean = (float)sum_of<kLanes>((double)w * dw);
@@ -663,12 +665,12 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
         double sum = 0;
         if (a.gate == GROOT_SOFTMAX && !a.renormalise) {
 #pragma unroll
-            for (int v = 0; v < kEach; ++v) sum += (double)expf(x[v] - base);
+            for (int v = 0; v < kEach; ++v) sum += (double)__expf(x[v] - base);
             sum = sum_of<kLanes>(sum);
-            const float p = mine < 0 ? 0.f : expf(s - base) / (float)sum;
+            const float p = mine < 0 ? 0.f : __expf(s - base) / (float)sum;
             at_log = a.factor * p * dw;
         } else if (!a.renormalise && mine >= 0) {
-            at_log = a.factor * dw / (1.f + expf(-s));
+            at_log = a.factor * dw / (1.f + __expf(-s));
         }
         const float total = a.gate == GROOT_SOFTMAX && !a.renormalise ? (float)sum_of<kLanes>(at_log) : 0.f;
         for (int32_t slot = 0; slot < a.k; ++slot) {
@@ -682,8 +684,8 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
         for (int v = 0; v < kEach; ++v) {
             const int32_t e = v * kLanes + lane;
             float r = d[v];
-            if (a.gate == GROOT_SIGMOID) r *= 1.f / (1.f + expf(x[v]));
-            else if (!a.renormalise && top > -kInf) r -= expf(x[v] - base) / (float)sum * total;
+            if (a.gate == GROOT_SIGMOID) r *= 1.f / (1.f + __expf(x[v]));
+            else if (!a.renormalise && top > -kInf) r -= __expf(x[v] - base) / (float)sum * total;
             if (x[v] == -kInf) r = 0.f;
             if (broken) r = __builtin_nanf("");
             if (e < a.E) {
