@@ -670,7 +670,8 @@ groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int64_t n_tenso
  *   their number.  Rows of R behind it are not written.
  * groot_route_backward: dscores (of dtype, fully overwritten) from the gradient
  *   of the weights; the choice has none.  NaN in rows whose weights are NaN, 0 at -inf.
- * workspace of groot_route: device, 16-byte aligned, groot_route_workspace bytes (may be 0).
+ * workspace of groot_route: device, 16-byte aligned, groot_route_workspace bytes (may be 0),
+ *   contents overwritten, owned by the caller and for one call at a time.
  * 1 <= n_experts <= 1024, 1 <= top_k <= 32, n_sets <= 64, top_k at most what
  * the open sets hold, n_rows * top_k < 2^31.
  *
@@ -688,7 +689,7 @@ groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int64_t n_tenso
  * Results are the same from run to run.  The calls only enqueue on hip_stream and
  * allocate nothing.  Outputs must not overlap each other or inputs.  Errors: EINVAL
  * (NULL, unknown dtype or gate, alignment, sizes, strides, overlap, workspace too small),
- * ERANGE (2^31 slots or places), EHIP.
+ * ERANGE (2^31 slots or places, more rows than a launch holds), EHIP.
  * ------------------------------------------------------------------------- */
 #define GROOT_I8 3                           /* groot_routed_rows only */
 typedef enum { GROOT_SOFTMAX = 0, GROOT_SIGMOID = 1 } groot_gate;
@@ -737,8 +738,9 @@ groot_status groot_routed_sum_backward(int32_t dtype, const void *dout_dev, int6
  *   dY (h rstd).  H: the rows h as groot_rms_norm gave them (X without a
  *   residual), rstd from the same call.  The rows' parts of dgain meet in a fixed
  *   order.  Outputs overlap nothing.
- * workspace (device, 16-byte aligned, contents overwritten): at least
- *   groot_rms_norm_backward_workspace bytes; not needed where dgain is NULL.
+ * workspace (device, 16-byte aligned, contents overwritten, owned by the caller and for
+ *   one call at a time): at least groot_rms_norm_backward_workspace bytes; not needed
+ *   where dgain is NULL.
  * 1 <= width <= 65536, eps > 0.  The calls only enqueue on hip_stream and
  * allocate nothing.  Errors: EINVAL, EHIP.
  * ------------------------------------------------------------------------- */

@@ -742,6 +742,7 @@ int route_launch(RouteArgs a, int32_t *counts, hipStream_t stream)
             a.value_bytes = bytes();
         }
     }
+    if (!fits_launch(groups, threads)) return kErrTooManyTiles;
     route_kernel<kLanes, kEach, kList, kByValue, kSets><<<(uint32_t)groups, threads, RouteLds(a.E, a.rows, a.k, a.value_bytes).total, stream>>>(a, counts);
     if (groups > 1) {
         const size_t lds = (2 * a.E + 1 + kMaxWaves) * sizeof(int32_t);
