@@ -651,8 +651,8 @@ groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int64_t n_tenso
  * scores [n_rows, n_experts] of dtype, `score_stride` elements from row to row.
  * gate: p = GROOT_SOFTMAX or GROOT_SIGMOID of a row's scores.
  * The choice goes by c = p + bias[e] (bias: float [n_experts], counts for the
- *   choice only), computed in 64 bits and compared by its 42 leading ones; without a bias, and with
- *   set_best = 1, by the scores themselves.  An expert is closed to a row where its score is
+ *   choice only), computed in 64 bits and compared by its 42 leading ones; without a bias, where
+ *   no sets are closed or set_best = 1, by the scores themselves.  An expert is closed to a row where its score is
  *   -inf or its bias -inf or NaN.
  * Sets: the experts make n_sets sets of neighbours (n_sets divides n_experts);
  *   a set counts what its set_best (1 or 2) best open experts' c come to, and the

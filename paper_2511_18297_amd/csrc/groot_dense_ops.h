@@ -111,7 +111,7 @@ struct RoutedArgs {
     float *dweights;             // [n, k] or NULL
     int64_t n, n_places;
     int32_t k, K;
-    int32_t part;                // pieces of a row that a workgroup takes (the launcher's)
+    int32_t part;                // pieces, or slots, of a row that a workgroup takes (the launcher's)
 };
 int launch_routed_rows(int32_t bytes, const RoutedArgs &a, void *stream);
 int launch_routed_sum(int32_t dtype, const RoutedArgs &a, void *stream);

@@ -86,7 +86,7 @@ __device__ __forceinline__ double row_sum(double x, double *lds)
         __syncthreads();
         x = 0;
 #pragma unroll
-        for (int w = 0; w < kLanes / kWave; ++w) x += lds[w];
+        for (int w = 0; w < kLanes / kWave; ++w) x += lds[threadIdx.x / kLanes * (kLanes / kWave) + w];
     }
     return x;
 }
@@ -100,7 +100,10 @@ __device__ __forceinline__ uint32_t row_most(uint32_t x, double *lds)
         if (threadIdx.x % kWave == 0) tops[threadIdx.x / kWave] = x;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kLanes / kWave; ++w) x = tops[w] > x ? tops[w] : x;
+        for (int w = 0; w < kLanes / kWave; ++w) {
+            const uint32_t top = tops[threadIdx.x / kLanes * (kLanes / kWave) + w];
+            x = top > x ? top : x;
+        }
     }
     return x;
 }
@@ -348,8 +351,11 @@ NormShape norm_shape(int32_t K, int bytes)
     if (pieces <= 32) return {16, 2, false};
     if (pieces <= 64) return {64, 1, false};
     if (pieces <= 128) return {64, 2, false};
+    if (pieces <= 192) return {64, 3, false};
     if (pieces <= 256) return {64, 4, false};
+    if (pieces <= 384) return {128, 3, false};
     if (pieces <= 512) return {256, 2, false};
+    if (pieces <= 768) return {256, 3, false};
     if (pieces <= 1024) return {256, 4, false};
     if (pieces <= 2048) return {512, 4, false};
     if (pieces <= 4096) return {1024, 4, false};
@@ -365,7 +371,7 @@ int64_t norm_blocks(int64_t n, const NormShape &s, int64_t most)
 }
 // Workgroups of the backward call: whole multiples of the 256 CUs, as each writes a row of partial sums.  16384 rows of 4096 in bfloat16, 512,
 // 768, 1024, 2048 of them: 108, 104, 107, 119 us with the sums; 8.4 M rows of 64 in fp32, 512, 1024, 2048, 8192: 1555, 1218, 1226, 1405.
-int64_t backward_blocks(int64_t n, const NormShape &s) { return norm_blocks(n, s, s.lanes <= kWave ? 1024 : s.lanes == 256 ? 768 : s.lanes == 512 ? 512 : 256); }
+int64_t backward_blocks(int64_t n, const NormShape &s) { return norm_blocks(n, s, s.lanes <= kWave ? 1024 : s.lanes <= 256 ? 768 : s.lanes == 512 ? 512 : 256); }
 
 #define GROOT_NORM_SHAPES(use)                                                                                                           \
     if (s.is_short) use(16, 1, true)                                                                                                     \
@@ -373,8 +379,11 @@ int64_t backward_blocks(int64_t n, const NormShape &s) { return norm_blocks(n, s
     else if (s.lanes == 16) use(16, 2, false)                                                                                            \
     else if (s.lanes == 64 && s.keep == 1) use(64, 1, false)                                                                             \
     else if (s.lanes == 64 && s.keep == 2) use(64, 2, false)                                                                             \
+    else if (s.lanes == 64 && s.keep == 3) use(64, 3, false)                                                                             \
     else if (s.lanes == 64) use(64, 4, false)                                                                                            \
+    else if (s.lanes == 128) use(128, 3, false)                                                                                          \
     else if (s.lanes == 256 && s.keep == 2) use(256, 2, false)                                                                           \
+    else if (s.lanes == 256 && s.keep == 3) use(256, 3, false)                                                                           \
     else if (s.lanes == 256) use(256, 4, false)                                                                                          \
     else if (s.lanes == 512) use(512, 4, false)                                                                                          \
     else if (s.keep == 4) use(1024, 4, false)                                                                                            \

@@ -23,6 +23,7 @@ constexpr int kRouteRows = 64;               // rows of a workgroup at most: bit
 constexpr int kNumberBits = 10;              // of an expert in a key
 constexpr uint32_t kNumbers = (1u << kNumberBits) - 1;
 constexpr int kSumGroups = 256;              // workgroups whose counts every workgroup of the second launch adds up by itself
+typedef v4i piece_t __attribute__((aligned(1)));
 constexpr float kInf = __builtin_inff();
 constexpr double kClosed = -0x1p1023, kLeastOpen = -0x1p1022, kMostOpen = 0x1p1022;
 
@@ -49,19 +50,15 @@ __device__ __forceinline__ bool any_of(bool x)
     return over_lanes<kLanes>((uint32_t)x, [](uint32_t a, uint32_t b) { return a | b; }) != 0;
 }
 
-// The scores of a lane's kEach experts from `begin` on; -inf beyond the last.  Where the experts are whole pieces of 16 bytes, these are
-// loaded, otherwise value by value.
+// The scores of a lane's kEach experts from `begin` on; -inf beyond the last.
 template <int kEach, typename T>
 __device__ __forceinline__ void load_scores_of(const char *row, int32_t E, int32_t begin, float (&s)[kEach])
 {
     constexpr int kPer = 16 / sizeof(T);
-    if (E % kPer == 0) {
-        v4i v[kEach / kPer];
+    v4i v[kEach / kPer];
+    if (E % kPer == 0) {                                     // whole pieces of 16 bytes
 #pragma unroll
-        for (int i = 0; i < kEach / kPer; ++i) {
-            const int32_t e = begin + i * kPer;
-            __builtin_memcpy(&v[i], row + (e < E ? e : 0) * (int)sizeof(T), 16);
-        }
+        for (int i = 0; i < kEach / kPer; ++i) v[i] = *(const piece_t *)(row + (begin + i * kPer < E ? begin + i * kPer : 0) * (int)sizeof(T));
 #pragma unroll
         for (int i = 0; i < kEach / kPer; ++i) {
             const RowValues<T> x = row_values<T>(v[i]);
@@ -70,12 +67,21 @@ __device__ __forceinline__ void load_scores_of(const char *row, int32_t E, int32
             for (int j = 0; j < kPer; ++j) s[i * kPer + j] = there ? x.x[j] : -kInf;
         }
     } else {
-        T x[kEach];
-        asm("" : "+v"(begin));                               // the addresses are computed here and not, for all calls, in front
+        const bool short_row = E < kPer;
+        asm("" : "+v"(begin));                               // what follows is computed here and not, for all calls, in front
 #pragma unroll
-        for (int v = 0; v < kEach; ++v) x[v] = ((const T *)row)[begin + v < E ? begin + v : E - 1];
+        for (int i = 0; i < kEach / kPer; ++i) {
+            const int32_t e = begin + i * kPer, at = e + kPer <= E ? e : E - kPer;   // the row's last piece in place of what there is not
+            v[i] = short_row ? short16<T>(row + e * (int)sizeof(T), (E - e) * (int)sizeof(T)) : *(const piece_t *)(row + at * (int)sizeof(T));
+        }
 #pragma unroll
-        for (int v = 0; v < kEach; ++v) s[v] = begin + v < E ? (float)x[v] : -kInf;
+        for (int i = 0; i < kEach / kPer; ++i) {
+            const int32_t left = E - (begin + i * kPer);
+            if (!short_row && left < kPer) v[i] = cut16(v[i], left * (int)sizeof(T));
+            const RowValues<T> x = row_values<T>(v[i]);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) s[i * kPer + j] = j < left ? x.x[j] : -kInf;
+        }
     }
 }
 template <int kEach>
@@ -279,6 +285,9 @@ __device__ __forceinline__ void close_small_sets(double (&x)[kEach], double *val
     for (int v = 0; v < kEach; ++v) x[v] = above[v / kSize] >= a.open_sets ? kClosed : x[v];
 }
 
+// words of a workgroup's counts: a byte for each expert
+__host__ __device__ constexpr int32_t count_words(int32_t E) { return (E + 3) / 4; }
+
 constexpr int kRouteThreads = 512;           // of a workgroup at most
 constexpr int kMaxWaves = 16;
 
@@ -303,7 +312,7 @@ uint32_t inverse_of(int32_t k) { return ((1u << 16) + k - 1) / k; }
 
 // kLanes lanes to a row, kEach neighbouring experts a lane, lists of kList keys (top_k of up to that many; beyond 16 they are taken one by one)
 template <int kLanes, int kEach, int kList, bool kByValue, bool kSets>
-__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int32_t *__restrict__ counts)
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, uint32_t *__restrict__ counts)
 {
     extern __shared__ char lds[];
     const RouteLds at(a.E, a.rows, a.k, a.value_bytes);
@@ -519,12 +528,16 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int32
     }
     __syncthreads();
     const bool alone = gridDim.x == 1;
-    for (int e = threadIdx.x; e < a.E; e += threads) {
-        const int32_t count = __popcll(mask[e]);
-        if (alone) prefix[e] = count;
-        else counts[(int64_t)blockIdx.x * a.E + e] = count;
-    }
-    if (alone) {
+    if (!alone) {
+        const int32_t words = count_words(a.E);
+        for (int w = threadIdx.x; w < words; w += threads) {
+            uint32_t four = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) four |= (uint32_t)__popcll(mask[4 * w + i < a.E ? 4 * w + i : a.E - 1]) << (8 * i);   // beyond the last: nobody's
+            counts[(int64_t)blockIdx.x * words + w] = four;
+        }
+    } else {
+        for (int e = threadIdx.x; e < a.E; e += threads) prefix[e] = __popcll(mask[e]);
         __syncthreads();
         exclusive_sums(prefix, a.E, waves);
         for (int e = threadIdx.x; e <= a.E; e += threads) a.offsets[e] = prefix[e];
@@ -539,23 +552,25 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int32
     }
 }
 
-// counts of the workgroups before each, expert by expert, in place, and every expert's sum in the row behind the last
+// before[g, e]: the counts of the workgroups before g; the row behind the last: every expert's sum
 constexpr int kScanExperts = 16, kScanParts = 64;
-__global__ __launch_bounds__(kScanExperts * kScanParts) void route_scan_kernel(int32_t *__restrict__ counts, int32_t groups, int32_t E)
+__global__ __launch_bounds__(kScanExperts * kScanParts) void route_scan_kernel(const uint32_t *__restrict__ counts, int32_t *__restrict__ before_at, int32_t groups,
+                                                                               int32_t E)
 {
     __shared__ int32_t sums[kScanParts][kScanExperts];
     const int part = threadIdx.x / kScanExperts, at = threadIdx.x % kScanExperts;
-    const int32_t e = blockIdx.x * kScanExperts + at, each = (groups + kScanParts - 1) / kScanParts;
+    const int32_t e = blockIdx.x * kScanExperts + at, each = (groups + kScanParts - 1) / kScanParts, pitch = count_words(E) * 4;
     const int32_t begin = part * each, end = begin + each < groups ? begin + each : groups;
+    auto count = [&](int32_t g) { return (int32_t)((const uint8_t *)counts)[(int64_t)g * pitch + e]; };
     constexpr int kHeld = 16;                                // of a part in registers: 1024 workgroups' counts are read once
     int32_t held[kHeld], sum = 0;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-        held[i] = e < E && begin + i < end ? counts[(int64_t)(begin + i) * E + e] : 0;
+        held[i] = e < E && begin + i < end ? count(begin + i) : 0;
         sum += held[i];
     }
     if (e < E)
-        for (int32_t g = begin + kHeld; g < end; ++g) sum += counts[(int64_t)g * E + e];
+        for (int32_t g = begin + kHeld; g < end; ++g) sum += count(g);
     sums[part][at] = sum;
     __syncthreads();
     int32_t before = 0, all = 0;
@@ -568,45 +583,53 @@ __global__ __launch_bounds__(kScanExperts * kScanParts) void route_scan_kernel(i
     if (e >= E) return;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-        if (begin + i < end) counts[(int64_t)(begin + i) * E + e] = before;
+        if (begin + i < end) before_at[(int64_t)(begin + i) * E + e] = before;
         before += held[i];
     }
     for (int32_t g = begin + kHeld; g < end; ++g) {
-        const int32_t here = counts[(int64_t)g * E + e];
-        counts[(int64_t)g * E + e] = before;
-        before += here;
+        before_at[(int64_t)g * E + e] = before;
+        before += count(g);
     }
-    if (part == 0) counts[(int64_t)groups * E + e] = all;
+    if (part == 0) before_at[(int64_t)groups * E + e] = all;
 }
 
-// ranks -> places.  kScanned: the counts are those of the workgroups before, and the sums stand behind them; otherwise this
-// workgroup adds them up, its threads in as many parts as there are for each expert.
+// ranks -> places.  kScanned: with the sums of route_scan_kernel; otherwise this workgroup adds the counts up, four experts a thread
+// and its threads in as many parts as there are for these (the sums of 256 counts of up to 64 stay below 2^16: two to a word).
 template <bool kScanned>
-__global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a, const int32_t *__restrict__ counts, int32_t groups)
+__global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a, const uint32_t *__restrict__ counts, const int32_t *__restrict__ before_at, int32_t groups)
 {
     extern __shared__ char lds[];
     int32_t *const prefix = (int32_t *)lds, *const before = prefix + a.E + 1, *const waves = before + a.E;
     const int threads = blockDim.x;
     if constexpr (kScanned) {
         for (int e = threadIdx.x; e < a.E; e += threads) {
-            prefix[e] = counts[(int64_t)groups * a.E + e];
-            before[e] = counts[(int64_t)blockIdx.x * a.E + e];
+            prefix[e] = before_at[(int64_t)groups * a.E + e];
+            before[e] = before_at[(int64_t)blockIdx.x * a.E + e];
         }
     } else {
+        static_assert(kSumGroups * kRouteRows < 65536, "sums of 16 bits");
         for (int e = threadIdx.x; e < a.E; e += threads) prefix[e] = before[e] = 0;
         __syncthreads();
-        const int parts = threads / a.E > 1 ? threads / a.E : 1;
-        for (int i = threadIdx.x; i < a.E * parts; i += threads) {
-            const int part = i / a.E, e = i - part * a.E;
-            int32_t all = 0, mine = 0;
+        const int words = count_words(a.E), parts = threads / words;        // 1024 threads, 256 words at the most
+        const int part = threadIdx.x / words, w = threadIdx.x - part * words;
+        if (part < parts) {
+            uint32_t all_even = 0, all_odd = 0, mine_even = 0, mine_odd = 0;
 #pragma unroll 8
             for (int32_t g = part; g < groups; g += parts) {
-                const int32_t c = counts[(int64_t)g * a.E + e];
-                all += c;
-                mine += g < (int32_t)blockIdx.x ? c : 0;
+                const uint32_t c = counts[(int64_t)g * words + w], even = c & 0x00FF00FFu, odd = c >> 8 & 0x00FF00FFu;
+                const bool earlier = g < (int32_t)blockIdx.x;
+                all_even += even;
+                all_odd += odd;
+                mine_even += earlier ? even : 0;
+                mine_odd += earlier ? odd : 0;
             }
-            atomicAdd(&prefix[e], all);
-            atomicAdd(&before[e], mine);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = 4 * w + i;
+                if (e >= a.E) break;
+                atomicAdd(&prefix[e], (int32_t)((i % 2 ? all_odd : all_even) >> (i / 2 * 16) & 0xFFFF));
+                atomicAdd(&before[e], (int32_t)((i % 2 ? mine_odd : mine_even) >> (i / 2 * 16) & 0xFFFF));
+            }
         }
     }
     __syncthreads();
@@ -621,80 +644,121 @@ __global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a, const in
     }
 }
 
+// kEach neighbouring scores of a row; where they begin beyond E none of them exist
+template <int kEach, typename T>
+__device__ __forceinline__ void row_scores(const char *row, int32_t E, int32_t begin, bool whole, float (&x)[kEach])
+{
+    typedef T vt __attribute__((ext_vector_type(kEach)));
+    typedef vt at_any __attribute__((aligned(sizeof(T) == 4 ? 4 : 2)));
+    if (whole) {
+        const vt v = *(const at_any *)(row + (begin < E ? begin : 0) * (int)sizeof(T));
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) x[k] = begin < E ? (float)v[k] : -kInf;
+    } else {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) x[k] = begin + k < E ? (float)((const T *)row)[begin + k] : -kInf;
+    }
+}
+template <int kEach, typename T>
+__device__ __forceinline__ void put_scores(char *row, int32_t E, int32_t begin, bool whole, const float (&x)[kEach])
+{
+    typedef T vt __attribute__((ext_vector_type(kEach)));
+    typedef vt at_any __attribute__((aligned(sizeof(T) == 4 ? 4 : 2)));
+    if (whole) {
+        vt v;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) v[k] = (T)x[k];      // the one rounding
+        if (begin < E) *(at_any *)(row + begin * (int)sizeof(T)) = v;
+    } else {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            if (begin + k < E) ((T *)row)[begin + k] = (T)x[k];
+    }
+}
+
 // ds of a row.  softmax: l = log p, p_j (g_j - sum g p) with g the gradients at the chosen weights; renormalised over the chosen ones.
-// sigmoid: the gradient at log p times 1 - p.
+// sigmoid: the gradient at log p times 1 - p.  kLanes lanes to a row with kEach neighbouring experts each, and a slot.
 template <int kLanes, int kEach>
 __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArgs a)
 {
+    __shared__ float chosen_at[kBlock * kEach];              // the gradients at the chosen experts of the workgroup's rows
     const int lane = threadIdx.x % kLanes;
+    const int32_t begin = lane * kEach;
+    float *const at = chosen_at + threadIdx.x / kLanes * (kLanes * kEach);
+    const bool whole = a.E % kEach == 0, sigmoid = a.gate == GROOT_SIGMOID;
     for (int64_t row = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kLanes; row < a.n; row += (int64_t)gridDim.x * (kBlock / kLanes)) {
         const char *const scores = (const char *)a.scores + row * a.score_bytes;
-        float x[kEach], d[kEach];
-        bool broken = false;
-        float top = -kInf;
-#pragma unroll
-        for (int v = 0; v < kEach; ++v) {
-            const int32_t e = v * kLanes + lane;
-            x[v] = e < a.E ? score_at(scores, a.dtype, e) : -kInf;
-            broken |= x[v] != x[v] || (a.gate == GROOT_SOFTMAX && x[v] == kInf);
-            top = fmaxf(top, x[v]);
-            d[v] = 0.f;
-        }
-        broken = any_of<kLanes>(broken);
-        top = top_of<kLanes>(top);
-        const float base = top == -kInf ? 0.f : top;
         // slots: lane = slot
         int32_t mine = -1;
-        float dw = 0.f;
+        float dw = 0.f, s = -kInf;
         if (lane < a.k) {
             mine = a.experts[row * a.k + lane];
             mine = mine >= 0 && mine < a.E ? mine : -1;
-            if (mine >= 0) dw = a.dweights[row * a.k + lane];
-        }
-        const float s = mine >= 0 ? score_at(scores, a.dtype, mine) : -kInf;
-        float at_log = 0.f;                                   // the gradient at the slot's log p, or at its score
-        if (a.renormalise) {
-            const bool sigmoid = a.gate == GROOT_SIGMOID;
-            const float most = top_of<kLanes>(sigmoid ? fminf(s, 0.f) : s);
-            const float q = mine < 0 || s == -kInf ? 0.f : weight_of(s, most, sigmoid);
-            const float all = (float)sum_of<kLanes>(q);       // every lane takes part
-            const float w = mine < 0 ? 0.f : q / all;
-            const float mean = (float)sum_of<kLanes>((double)w * dw);
-            at_log = mine < 0 ? 0.f : a.factor * w * (dw - mean);
-        }
-        double sum = 0;
-        if (a.gate == GROOT_SOFTMAX && !a.renormalise) {
-#pragma unroll
-            for (int v = 0; v < kEach; ++v) sum += (double)__expf(x[v] - base);
-            sum = sum_of<kLanes>(sum);
-            const float p = mine < 0 ? 0.f : __expf(s - base) / (float)sum;
-            at_log = a.factor * p * dw;
-        } else if (!a.renormalise && mine >= 0) {
-            at_log = a.factor * dw / (1.f + __expf(-s));
-        }
-        const float total = a.gate == GROOT_SOFTMAX && !a.renormalise ? (float)sum_of<kLanes>(at_log) : 0.f;
-        for (int32_t slot = 0; slot < a.k; ++slot) {
-            const int32_t e = __shfl(mine, slot, kLanes);
-            const float g = __shfl(at_log, slot, kLanes);
-#pragma unroll
-            for (int v = 0; v < kEach; ++v)
-                if (e == v * kLanes + lane) d[v] += g;
-        }
-#pragma unroll
-        for (int v = 0; v < kEach; ++v) {
-            const int32_t e = v * kLanes + lane;
-            float r = d[v];
-            if (a.gate == GROOT_SIGMOID) r *= 1.f / (1.f + __expf(x[v]));
-            else if (!a.renormalise && top > -kInf) r -= __expf(x[v] - base) / (float)sum * total;
-            if (x[v] == -kInf) r = 0.f;
-            if (broken) r = __builtin_nanf("");
-            if (e < a.E) {
-                char *const to = (char *)a.dscores + row * a.ds_bytes;
-                if (a.dtype == GROOT_F32) ((float *)to)[e] = r;
-                else if (a.dtype == GROOT_BF16) ((bf16_t *)to)[e] = (bf16_t)r;
-                else ((f16_t *)to)[e] = (f16_t)r;
+            if (mine >= 0) {
+                dw = a.dweights[row * a.k + lane];
+                s = score_at(scores, a.dtype, mine);
             }
         }
+        float x[kEach];
+        if (a.dtype == GROOT_F32) row_scores<kEach, float>(scores, a.E, begin, whole, x);
+        else if (a.dtype == GROOT_BF16) row_scores<kEach, bf16_t>(scores, a.E, begin, whole, x);
+        else row_scores<kEach, f16_t>(scores, a.E, begin, whole, x);
+        float top = x[0];                                    // NaN if one of them is
+#pragma unroll
+        for (int v = 1; v < kEach; ++v) top = __builtin_elementwise_maximum(top, x[v]);
+        top = over_lanes<kLanes>(top, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
+        const bool broken = top != top || (!sigmoid && top == kInf);
+        const float base = top == -kInf ? 0.f : top;
+        float at_log = 0.f;                                  // the gradient at the slot's log p
+        float sum = 1.f, total = 0.f;
+        if (a.renormalise) {
+            const float most = top_of<kLanes>(sigmoid ? fminf(s, 0.f) : s);
+            const float q = mine < 0 || s == -kInf ? 0.f : weight_of(s, most, sigmoid);
+            const float all = sum_of<kLanes>(q);             // every lane takes part
+            const float w = mine < 0 ? 0.f : q / all;
+            const float mean = sum_of<kLanes>(w * dw);
+            at_log = mine < 0 ? 0.f : a.factor * w * (dw - mean);
+        } else if (!sigmoid) {
+            sum = 0.f;
+#pragma unroll
+            for (int v = 0; v < kEach; ++v) sum += __expf(x[v] - base);
+            sum = sum_of<kLanes>(sum);
+            at_log = mine < 0 ? 0.f : a.factor * dw * (__expf(s - base) / sum);
+            total = sum_of<kLanes>(at_log);
+        } else if (mine >= 0) {
+            at_log = a.factor * dw * weight_of(s, 0.f, true);
+        }
+        // an expert that is named twice (not by groot_route) gets both, in the order of the slots
+        if (mine >= 0) at[mine] = __int_as_float(lane);
+        wave_sync();
+        const bool twice = any_of<kLanes>(mine >= 0 && __float_as_int(at[mine]) != lane);
+        wave_sync();
+#pragma unroll
+        for (int v = 0; v < kEach; ++v) at[begin + v] = 0.f;
+        wave_sync();
+        if (!twice) {
+            if (mine >= 0) at[mine] = at_log;
+        } else {
+            for (int32_t slot = 0; slot < a.k; ++slot) {
+                if (lane == slot && mine >= 0) at[mine] += at_log;
+                wave_sync();
+            }
+        }
+        wave_sync();
+        float r[kEach];
+#pragma unroll
+        for (int v = 0; v < kEach; ++v) {
+            r[v] = at[begin + v];
+            if (sigmoid) r[v] *= 1.f / (1.f + __expf(x[v]));
+            else if (!a.renormalise) r[v] -= __expf(x[v] - base) / sum * total;
+            if (x[v] == -kInf) r[v] = 0.f;
+            if (broken) r[v] = __builtin_nanf("");
+        }
+        wave_sync();                                         // before the next row's
+        char *const to = (char *)a.dscores + row * a.ds_bytes;
+        if (a.dtype == GROOT_F32) put_scores<kEach, float>(to, a.E, begin, whole, r);
+        else if (a.dtype == GROOT_BF16) put_scores<kEach, bf16_t>(to, a.E, begin, whole, r);
+        else put_scores<kEach, f16_t>(to, a.E, begin, whole, r);
     }
 }
 
@@ -715,10 +779,11 @@ int32_t route_rows(int64_t n, int32_t E)
     while (rows < kRouteRows && (n + rows - 1) / rows > kSumGroups) rows *= 2;
     return rows;
 }
+size_t count_bytes(int64_t groups, int32_t E) { return ((size_t)groups * count_words(E) * 4 + 15) / 16 * 16; }
 int64_t route_groups(int64_t n, int32_t rows) { return n <= 0 ? 1 : (n + rows - 1) / rows; }
 
 template <int kLanes, int kEach, int kList, bool kByValue, bool kSets>
-int route_launch(RouteArgs a, int32_t *counts, hipStream_t stream)
+int route_launch(RouteArgs a, uint32_t *counts, hipStream_t stream)
 {
     a.rows = route_rows(a.n, a.E);
     a.inverse_k = inverse_of(a.k);
@@ -746,11 +811,12 @@ int route_launch(RouteArgs a, int32_t *counts, hipStream_t stream)
     route_kernel<kLanes, kEach, kList, kByValue, kSets><<<(uint32_t)groups, threads, RouteLds(a.E, a.rows, a.k, a.value_bytes).total, stream>>>(a, counts);
     if (groups > 1) {
         const size_t lds = (2 * a.E + 1 + kMaxWaves) * sizeof(int32_t);
+        int32_t *const before = (int32_t *)((char *)counts + count_bytes(groups, a.E));
         if (groups > kSumGroups) {
-            route_scan_kernel<<<(a.E + kScanExperts - 1) / kScanExperts, kScanExperts * kScanParts, 0, stream>>>(counts, (int32_t)groups, a.E);
-            route_place_kernel<true><<<(uint32_t)groups, kBlock, lds, stream>>>(a, counts, (int32_t)groups);
+            route_scan_kernel<<<(a.E + kScanExperts - 1) / kScanExperts, kScanExperts * kScanParts, 0, stream>>>(counts, before, (int32_t)groups, a.E);
+            route_place_kernel<true><<<(uint32_t)groups, kBlock, lds, stream>>>(a, counts, before, (int32_t)groups);
         } else {
-            route_place_kernel<false><<<(uint32_t)groups, 1024, lds, stream>>>(a, counts, (int32_t)groups);
+            route_place_kernel<false><<<(uint32_t)groups, 1024, lds, stream>>>(a, counts, before, (int32_t)groups);
         }
     }
     return (int)hipGetLastError();
@@ -769,11 +835,11 @@ int backward_launch(const RouteBackwardArgs &a, hipStream_t stream)
 size_t route_workspace(int64_t n, int32_t E)
 {
     const int64_t groups = route_groups(n, route_rows(n, E));
-    return groups == 1 ? 0 : (size_t)(groups + 1) * E * sizeof(int32_t);
+    return groups == 1 ? 0 : count_bytes(groups, E) + (groups > kSumGroups ? (size_t)(groups + 1) * E * sizeof(int32_t) : 0);
 }
 
 // 16 experts a lane (8 where there are no more), lists as long as top_k needs
-typedef int (*RouteLaunch)(RouteArgs, int32_t *, hipStream_t);
+typedef int (*RouteLaunch)(RouteArgs, uint32_t *, hipStream_t);
 template <int kLanes, bool kByValue, bool kSets>
 static RouteLaunch route_of_lanes(const RouteArgs &a)
 {
@@ -810,7 +876,7 @@ int launch_route(const RouteArgs &a, void *workspace, void *stream)
 {
     const bool sets = a.open_sets < a.sets;
     const RouteLaunch launch = a.by_value ? (sets ? route_for<true, true>(a) : route_for<true, false>(a)) : (sets ? route_for<false, true>(a) : route_for<false, false>(a));
-    return launch(a, (int32_t *)workspace, (hipStream_t)stream);
+    return launch(a, (uint32_t *)workspace, (hipStream_t)stream);
 }
 int launch_route_backward(const RouteBackwardArgs &a, void *stream) { return backward_for(a)(a, (hipStream_t)stream); }
 

@@ -107,11 +107,11 @@ __device__ __forceinline__ void store_piece(char *row, int64_t at, int32_t K, co
 }
 // the pieces of the rows at kBatch places from `slot` on; a slot without a place has a row of zeros, so that no load waits for a branch
 template <typename T, int kBatch, int kPieces, bool kShort>
-__device__ __forceinline__ void slot_pieces(const RoutedArgs &a, int64_t row, int32_t slot, const int64_t (&at)[kPieces], int64_t (&p)[kBatch],
+__device__ __forceinline__ void slot_pieces(const RoutedArgs &a, int64_t row, int32_t slot, int32_t slots, const int64_t (&at)[kPieces], int64_t (&p)[kBatch],
                                             v4i (&v)[kBatch][kPieces])
 {
 #pragma unroll
-    for (int s = 0; s < kBatch; ++s) p[s] = slot + s < a.k ? place_at(a, row, slot + s) : -1;
+    for (int s = 0; s < kBatch; ++s) p[s] = slot + s < slots ? place_at(a, row, slot + s) : -1;
 #pragma unroll
     for (int s = 0; s < kBatch; ++s)
 #pragma unroll
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kBlock) void routed_sum_kernel(RoutedArgs a)
             for (int32_t slot = 0; slot < a.k; slot += kBatch) {
                 int64_t p[kBatch];
                 v4i v[kBatch][kPieces];
-                slot_pieces<T, kBatch, kPieces, kShort>(a, row, slot, at, p, v);
+                slot_pieces<T, kBatch, kPieces, kShort>(a, row, slot, a.k, at, p, v);
 #pragma unroll
                 for (int s = 0; s < kBatch; ++s) {
                     if (slot + s >= a.k) break;
@@ -170,10 +170,12 @@ __global__ __launch_bounds__(kBlock) void routed_sum_kernel(RoutedArgs a)
 template <typename T, int kLanes, int kPieces, bool kShort, bool kOnce>
 __global__ __launch_bounds__(kBlock) void routed_sum_backward_kernel(RoutedArgs a)
 {
-    constexpr int kPer = 16 / sizeof(T), kBatch = 2, kHeld = kPieces ? kPieces : 1;
+    constexpr int kPer = 16 / sizeof(T), kBatch = 2, kHeld = kPieces ? kPieces : 1, kParts = kLanes > kWave ? kLanes / kWave : 1;
+    __shared__ float dots[kLanes > kWave ? 32 * kParts : 1];     // top_k is 32 at the most
     const int lane = threadIdx.x % kLanes, rows = blockDim.x / kLanes;
     const int64_t bytes = (int64_t)a.K * sizeof(T);
     const int32_t pieces = (int32_t)((bytes + 15) / 16);
+    const int32_t first_slot = blockIdx.y * a.part, slots = first_slot + a.part < a.k ? first_slot + a.part : a.k;   // of this workgroup
     for (int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / kLanes; r < a.n; r += (int64_t)gridDim.x * rows) {
         const int64_t row = row_of<kLanes>(r);
         const char *const d_row = (const char *)((const T *)a.X + row * a.x_stride);
@@ -189,18 +191,18 @@ __global__ __launch_bounds__(kBlock) void routed_sum_backward_kernel(RoutedArgs 
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) locate(lane + j * kLanes, j);
         }
-        for (int32_t slot = 0; slot < a.k; slot += kBatch) {
+        for (int32_t slot = first_slot; slot < slots; slot += kBatch) {
             float dot[kBatch] = {}, w[kBatch];
 #pragma unroll
-            for (int s = 0; s < kBatch; ++s) w[s] = a.weights && slot + s < a.k ? a.weights[row * a.k + slot + s] : 1.f;
+            for (int s = 0; s < kBatch; ++s) w[s] = a.weights && slot + s < slots ? a.weights[row * a.k + slot + s] : 1.f;
             for (int32_t i = 0; i < (kPieces ? 1 : pieces); i += kLanes) {
                 if (!kPieces) locate(i + lane, 0);
                 int64_t p[kBatch];
                 v4i v[kBatch][kHeld];
-                if (a.dweights) slot_pieces<T, kBatch, kHeld, kShort>(a, row, slot, at, p, v);
+                if (a.dweights) slot_pieces<T, kBatch, kHeld, kShort>(a, row, slot, slots, at, p, v);
 #pragma unroll
                 for (int s = 0; s < kBatch; ++s) {
-                    if (!a.dweights) p[s] = slot + s < a.k ? place_at(a, row, slot + s) : -1;
+                    if (!a.dweights) p[s] = slot + s < slots ? place_at(a, row, slot + s) : -1;
                     if (p[s] < 0) continue;
 #pragma unroll
                     for (int j = 0; j < kHeld; ++j) {
@@ -229,9 +231,26 @@ __global__ __launch_bounds__(kBlock) void routed_sum_backward_kernel(RoutedArgs 
             if (a.dweights) {
 #pragma unroll
                 for (int s = 0; s < kBatch; ++s) {
-                    dot[s] = over_lanes<kLanes>(dot[s], [](float x, float y) { return x + y; });
-                    if (lane == 0 && slot + s < a.k) a.dweights[row * a.k + slot + s] = dot[s];
+                    dot[s] = over_lanes<(kLanes < kWave ? kLanes : kWave)>(dot[s], [](float x, float y) { return x + y; });
+                    if constexpr (kLanes > kWave) {
+                        if (threadIdx.x % kWave == 0 && slot + s < slots) dots[(slot + s) * kParts + threadIdx.x / kWave] = dot[s];
+                    } else {
+                        if (lane == 0 && slot + s < slots) a.dweights[row * a.k + slot + s] = dot[s];
+                    }
                 }
+            }
+        }
+        if constexpr (kLanes > kWave) {
+            if (a.dweights) {                                // the wavefronts' parts of every slot
+                __syncthreads();
+                const int32_t slot = first_slot + threadIdx.x;
+                if (slot < slots) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kParts; ++w) sum += dots[slot * kParts + w];
+                    a.dweights[row * a.k + slot] = sum;
+                }
+                __syncthreads();                             // before the next row's
             }
         }
     }
@@ -284,16 +303,22 @@ int sum_backward_launch(RoutedArgs a, hipStream_t stream)
     const int64_t pieces = ((int64_t)a.K * sizeof(T) + 15) / 16;
 #define GROOT_SUM(lanes, held, is_short)                                                                                                 \
     {                                                                                                                                    \
-        const RoutedShape s = routed_shape(&a, 1, lanes);                                                                                \
+        RoutedShape s = routed_shape(&a, 1, lanes);                                                                                      \
+        a.part = few_rows ? 2 : a.k;                                                                                                     \
+        s.grid.y = (a.k + a.part - 1) / a.part;                                                                                          \
         routed_sum_backward_kernel<T, lanes, held, is_short, kOnce><<<s.grid, s.threads, 0, stream>>>(a);                                \
     }
+    // a wavefront to a row, and a workgroup where rows are wide or few; very few rows: one for every two slots
+    const bool few = a.n < 2048, few_rows = a.n < 1024;
     if (a.K * sizeof(T) < 16) GROOT_SUM(16, 1, true)
     else if (pieces <= 16) GROOT_SUM(16, 1, false)
     else if (pieces <= 64) GROOT_SUM(64, 1, false)
     else if (pieces <= 128) GROOT_SUM(64, 2, false)
-    else if (pieces <= 256) GROOT_SUM(64, 4, false)
-    else if (pieces <= 512) GROOT_SUM(64, 8, false)
-    else GROOT_SUM(64, 0, false)
+    else if (pieces <= 256 && !few) GROOT_SUM(64, 4, false)
+    else if (pieces <= 256) GROOT_SUM(256, 1, false)
+    else if (pieces <= 512) GROOT_SUM(256, 2, false)
+    else if (pieces <= 1024) GROOT_SUM(256, 4, false)
+    else GROOT_SUM(256, 0, false)
 #undef GROOT_SUM
     return (int)hipGetLastError();
 }
