@@ -74,7 +74,8 @@ struct RouteArgs {
     int32_t rows;                // of a workgroup
     uint32_t inverse_k;
     int32_t set_lanes;           // lanes that hold a set, 0: it begins anywhere
-    bool small_sets;             // a lane holds 2, 4, 8 or 16 whole sets
+    bool small_sets;             // a lane holds whole sets
+    bool wide_sets;              // a lane's experts belong to two sets at the most
     int32_t value_bytes;         // of LDS for the sets
 };
 size_t route_workspace(int64_t n, int32_t E);

@@ -285,6 +285,51 @@ __device__ __forceinline__ void close_small_sets(double (&x)[kEach], double *val
     for (int v = 0; v < kEach; ++v) x[v] = above[v / kSize] >= a.open_sets ? kClosed : x[v];
 }
 
+// Sets of 16 experts or more that begin anywhere: a lane's experts belong to two at the most, those up to `border` to its first one.
+// `values`: what the row's sets come to, behind them the two largest that each lane holds of each of its two sets.
+template <int kLanes, int kEach>
+__device__ __forceinline__ void close_wide_sets(double (&x)[kEach], double *values, const RouteArgs &a, int lane, int32_t size)
+{
+    double *const held = values + a.sets;                    // [kLanes, 2 sets, 2 values]
+    const int32_t begin = lane * kEach, set = begin / size, border = (set + 1) * size - begin;
+    double most[2] = {kClosed, kClosed}, second[2] = {kClosed, kClosed};
+#pragma unroll
+    for (int v = 0; v < kEach; ++v) {
+        const double c[2] = {v < border ? x[v] : kClosed, v < border ? kClosed : x[v]};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            second[j] = larger(second[j], smaller(most[j], c[j]));
+            most[j] = larger(most[j], c[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        held[lane * 4 + j * 2] = most[j];
+        held[lane * 4 + j * 2 + 1] = second[j];
+    }
+    wave_sync();
+    for (int32_t s = lane; s < a.sets; s += kLanes) {
+        double m = kClosed, n = kClosed;
+        for (int32_t l = s * size / kEach; l <= ((s + 1) * size - 1) / kEach; ++l) {
+            const double *const h = held + l * 4 + (s - l * kEach / size) * 2;
+            n = larger(larger(n, h[1]), smaller(m, h[0]));
+            m = larger(m, h[0]);
+        }
+        values[s] = key_of(a.set_best == 2 && n > kLeastOpen ? smaller(m + n, kMostOpen) : m, (uint32_t)s, 63);
+    }
+    wave_sync();
+    const double own[2] = {values[set < a.sets ? set : 0], values[set + 1 < a.sets ? set + 1 : 0]};
+    int32_t above[2] = {};
+    for (int32_t i = 0; i < a.sets; ++i) {
+        const double v = values[i];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) above[j] += v > own[j];
+    }
+    wave_sync();                                             // before the next rows'
+#pragma unroll
+    for (int v = 0; v < kEach; ++v) x[v] = above[v < border ? 0 : 1] >= a.open_sets ? kClosed : x[v];
+}
+
 // words of a workgroup's counts: a byte for each expert
 __host__ __device__ constexpr int32_t count_words(int32_t E) { return (E + 3) / 4; }
 
@@ -406,6 +451,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, uint3
 #pragma unroll
                     for (int v = 0; v < kEach; ++v) x[v] = kClosed;
                 }
+            } else if (a.wide_sets) {
+                close_wide_sets<kLanes, kEach>(x, (double *)(lds + at.values) + threadIdx.x / kLanes * (a.sets + 4 * kLanes), a, lane, size);
             } else if (a.small_sets) {
                 double *const values = (double *)(lds + at.values) + threadIdx.x / kLanes * a.sets;
                 if (size == 1) close_small_sets<1>(x, values, a, lane);
@@ -791,13 +838,16 @@ int route_launch(RouteArgs a, uint32_t *counts, hipStream_t stream)
     int threads = (int)(a.n < a.rows ? (a.n < 1 ? 1 : a.n) : a.rows) * kLanes;
     threads = threads >= kRouteThreads ? kRouteThreads : (threads + kWave - 1) / kWave * kWave;
     a.set_lanes = 0;
-    a.small_sets = false;
+    a.small_sets = a.wide_sets = false;
     a.value_bytes = 0;
     if (kSets) {
         const int32_t size = a.E / a.sets, lanes = size / kEach;
         if (size % kEach == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 32) {
             a.set_lanes = lanes;
             a.value_bytes = threads / kLanes * a.sets * 8;
+        } else if (size >= kEach) {
+            a.wide_sets = true;
+            a.value_bytes = threads / kLanes * (a.sets + 4 * kLanes) * 8;
         } else if (size == 1 || size == 2 || size == 4 || size == 8) {
             a.small_sets = true;
             a.value_bytes = threads / kLanes * a.sets * 8;
