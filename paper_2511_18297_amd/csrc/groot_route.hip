@@ -357,7 +357,7 @@ uint32_t inverse_of(int32_t k) { return ((1u << 16) + k - 1) / k; }
 
 // kLanes lanes to a row, kEach neighbouring experts a lane, lists of kList keys (top_k of up to that many; beyond 16 they are taken one by one)
 template <int kLanes, int kEach, int kList, bool kByValue, bool kSets>
-__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, uint32_t *__restrict__ counts)
+__global__ __launch_bounds__(kRouteThreads, 4) void route_kernel(RouteArgs a, uint32_t *__restrict__ counts)
 {
     extern __shared__ char lds[];
     const RouteLds at(a.E, a.rows, a.k, a.value_bytes);
@@ -365,14 +365,16 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, uint3
     int32_t *const prefix = (int32_t *)(lds + at.prefix), *const waves = (int32_t *)(lds + at.waves);
     float *const weights = (float *)(lds + at.weights);
     int16_t *const chosen = (int16_t *)(lds + at.chosen);
-    const int threads = blockDim.x, lane = threadIdx.x % kLanes, at_once = threads / kLanes;
+    const int threads = blockDim.x, at_once = threads / kLanes;
     const bool sigmoid = a.gate == GROOT_SIGMOID;
     for (int e = threadIdx.x; e < a.E; e += threads) mask[e] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * a.rows;
     const int here = (int)(a.n - first < a.rows ? a.n - first : a.rows);  // rows of this workgroup
-    const int32_t begin = lane * kEach;
     for (int pass = 0; pass < here; pass += at_once) {
+        int lane = threadIdx.x % kLanes;
+        asm("" : "+v"(lane));                                             // nothing that goes by it is computed in front of the loop and held
+        const int32_t begin = lane * kEach;
         const int local = pass + threadIdx.x / kLanes;
         const bool real = local < here;                                   // rows beyond the last go along
         const char *const scores = (const char *)a.scores + (first + (real ? local : here - 1)) * a.score_bytes;
