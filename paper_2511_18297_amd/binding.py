@@ -866,31 +866,70 @@ GROOT_SOFTMAX, GROOT_SIGMOID = range(2)
 _int32 = torch.int32
 
 
-def _launch_stream(stream, *tensors):
-    """The handle of a stream, by default of the current one.  The kernels run on the current device: a tensor or a stream of another
-    one is refused.  (None is no tensor.)"""
-    d = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != d:
-            raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {d}")
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(d)
-    if stream.device_index != d:
-        raise ValueError(f"the stream is of device {stream.device_index}, the current device is {d}")
-    return stream.cuda_stream
+# A small call is 3 us on the GPU and 4 in the launch: a tensor is looked at once for everything, and what is wrong with it is found
+# out only where something is.
+def _matrix(t, what):
+    """Rows, width and the current device; the kernels run there, and every tensor has to be there too."""
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a CUDA tensor")
+    try:
+        n, width = t.shape
+    except ValueError:
+        raise TypeError(f"{what} must be a matrix") from None
+    return n, width, torch._C._cuda_getDevice()
 
 
-def _rows_or_none(t, what, n, width, dtype):
-    return (None, width) if t is None else _rows(t, what, n, width, dtype)
+def _refuse(t, what, shape, dtype, device):
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what} must be {tuple(shape)}, is {tuple(t.shape)}")
+    raise ValueError(f"{what} is on device {t.get_device()}, the current device is {device}")
 
 
-def _bytes_of(workspace):
-    """Pointer and size of a workspace; None has none."""
-    if workspace is None:
+def _rows_at(t, what, shape, dtype, device):
+    """Pointer and row stride of a matrix whose rows are contiguous, any distance apart."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _refuse(t, what, shape, dtype, device)
+    stride, inner = t.stride()
+    n, width = shape
+    if stride < width:
+        if n > 1:
+            raise ValueError(f"{what} must have rows that do not overlap")
+        stride = width
+    if inner != 1 and width > 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    return t.data_ptr(), stride
+
+
+def _flat_at(t, what, shape, dtype, device):
+    """Pointer of a contiguous tensor."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _refuse(t, what, shape, dtype, device)
+    if not t.is_contiguous():
+        raise TypeError(f"{what} must be a contiguous CUDA tensor")
+    return t.data_ptr()
+
+
+def _workspace_at(t, device):
+    """Pointer and size; None has none."""
+    if t is None:
         return None, 0
-    if not isinstance(workspace, _Tensor) or not workspace.is_cuda or not workspace.is_contiguous():
+    if not isinstance(t, _Tensor) or not t.is_cuda or not t.is_contiguous():
         raise TypeError("workspace must be a contiguous CUDA tensor")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if t.get_device() != device:
+        _refuse(t, "workspace", t.shape, t.dtype, device)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _stream_on(stream, device):
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError(f"the stream is of device {stream.device_index}, the current device is {device}")
+    return stream.cuda_stream
 
 
 def groot_route_workspace(n_rows: int, n_experts: int, top_k: int) -> int:
@@ -907,99 +946,92 @@ def groot_route(scores, bias, experts, weights, places, offsets, workspace, gate
     [experts + 1]; workspace: a contiguous CUDA tensor of at least groot_route_workspace(n, experts, k) bytes, or None where that is 0.
     gate: GROOT_SOFTMAX or GROOT_SIGMOID; sets, open_sets, set_best: the choice is among the open_sets of `sets` sets of neighbouring
     experts whose set_best best experts come to most; renormalise: weights over their sum; factor: times this."""
-    d = _dtype(scores, "scores")
-    n, E = _matrix_rows(scores, "scores"), scores.shape[1]
-    _matrix_rows(experts, "experts")
-    k = experts.shape[1]
-    s, ss = _rows(scores, "scores", n, E, scores.dtype)
-    ws, size = _bytes_of(workspace)
-    _check(_lib.groot_route(d, s, ss, _array(bias, "bias", (E,), _float32), gate, sets, open_sets, set_best, 1 if renormalise else 0, factor,
-                            _array(experts, "experts", (n, k), _int32), _array(weights, "weights", (n, k), _float32),
-                            _array(places, "places", (n, k), _int32), _array(offsets, "offsets", (E + 1,), _int64), n, E, k, ws, size,
-                            _launch_stream(stream, scores, bias, experts, weights, places, offsets, workspace)))
+    n, E, at = _matrix(scores, "scores")
+    k = _matrix(experts, "experts")[1]
+    s, ss = _rows_at(scores, "scores", (n, E), scores.dtype, at)
+    slots = (n, k)
+    ws, size = _workspace_at(workspace, at)
+    _check(_lib.groot_route(_dtype(scores, "scores"), s, ss, None if bias is None else _flat_at(bias, "bias", (E,), _float32, at), gate, sets, open_sets, set_best,
+                            1 if renormalise else 0, factor, _flat_at(experts, "experts", slots, _int32, at),
+                            _flat_at(weights, "weights", slots, _float32, at), _flat_at(places, "places", slots, _int32, at),
+                            _flat_at(offsets, "offsets", (E + 1,), _int64, at), n, E, k, ws, size, _stream_on(stream, at)))
 
 
 def groot_route_backward(scores, experts, dweights, dscores, gate: int = GROOT_SOFTMAX, renormalise: bool = True, factor: float = 1.0,
                          stream=None) -> None:
     """dscores [n, experts] from the gradient of the weights (dweights float32 [n, k]); the other arguments as in groot_route, experts as
     it gave them."""
-    d, T = _dtype(scores, "scores"), scores.dtype
-    n, E = _matrix_rows(scores, "scores"), scores.shape[1]
-    _matrix_rows(experts, "experts")
-    k = experts.shape[1]
-    s, ss = _rows(scores, "scores", n, E, T)
-    g, gs = _rows(dscores, "dscores", n, E, T)
-    _check(_lib.groot_route_backward(d, s, ss, gate, 1 if renormalise else 0, factor, _array(experts, "experts", (n, k), _int32),
-                                     _array(dweights, "dweights", (n, k), _float32), g, gs, n, E, k,
-                                     _launch_stream(stream, scores, experts, dweights, dscores)))
+    n, E, at = _matrix(scores, "scores")
+    k = _matrix(experts, "experts")[1]
+    T = scores.dtype
+    s, ss = _rows_at(scores, "scores", (n, E), T, at)
+    g, gs = _rows_at(dscores, "dscores", (n, E), T, at)
+    _check(_lib.groot_route_backward(_dtype(scores, "scores"), s, ss, gate, 1 if renormalise else 0, factor, _flat_at(experts, "experts", (n, k), _int32, at),
+                                     _flat_at(dweights, "dweights", (n, k), _float32, at), g, gs, n, E, k, _stream_on(stream, at)))
 
 
 def groot_routed_rows(X, places, R, x_scale=None, r_scale=None, stream=None) -> None:
     """R[places[i, s]] = X[i].  X [n, width] and R [places, width] of one type (int8 too), places int32 [n, k] as groot_route gave them;
     x_scale float32 [n] and r_scale float32 [places] (both or none): a scale that goes with each row."""
-    T = X.dtype if isinstance(X, _Tensor) else None
-    d = GROOT_I8 if T is _int8 else _dtype(X, "X")
-    n, width = _matrix_rows(X, "X"), X.shape[1]
-    m = _matrix_rows(R, "R")
-    _matrix_rows(places, "places")
-    k = places.shape[1]
-    x, xs = _rows(X, "X", n, width, T)
-    r, rs = _rows(R, "R", m, width, T)
+    n, width, at = _matrix(X, "X")
+    T = X.dtype
+    m, k = _matrix(R, "R")[0], _matrix(places, "places")[1]
+    x, xs = _rows_at(X, "X", (n, width), T, at)
+    r, rs = _rows_at(R, "R", (m, width), T, at)
     if (x_scale is None) != (r_scale is None):
         raise ValueError("x_scale and r_scale go together")
-    _check(_lib.groot_routed_rows(d, x, xs, _array(x_scale, "x_scale", (n,), _float32), _array(places, "places", (n, k), _int32), k, r, rs,
-                                  _array(r_scale, "r_scale", (m,), _float32), n, m, width,
-                                  _launch_stream(stream, X, places, R, x_scale, r_scale)))
+    _check(_lib.groot_routed_rows(GROOT_I8 if T is _int8 else _dtype(X, "X"), x, xs, None if x_scale is None else _flat_at(x_scale, "x_scale", (n,), _float32, at),
+                                  _flat_at(places, "places", (n, k), _int32, at), k, r, rs,
+                                  None if r_scale is None else _flat_at(r_scale, "r_scale", (m,), _float32, at), n, m, width, _stream_on(stream, at)))
 
 
 def groot_routed_sum(R, places, weights, addend, out, stream=None) -> None:
     """out[i] = addend[i] + sum over s of weights[i, s] R[places[i, s]].  R [places, width], out and addend (or None) [n, width] of one
     type, places int32 [n, k], weights float32 [n, k] or None (ones)."""
-    d, T = _dtype(R, "R"), R.dtype
-    m, width = _matrix_rows(R, "R"), R.shape[1]
-    n = _matrix_rows(places, "places")
-    k = places.shape[1]
-    r, rs = _rows(R, "R", m, width, T)
-    a, as_ = _rows_or_none(addend, "addend", n, width, T)
-    o, os_ = _rows(out, "out", n, width, T)
-    _check(_lib.groot_routed_sum(d, r, rs, _array(places, "places", (n, k), _int32), _array(weights, "weights", (n, k), _float32), a, as_, k, o, os_,
-                                 n, m, width, _launch_stream(stream, R, places, weights, addend, out)))
+    m, width, at = _matrix(R, "R")
+    n, k, _ = _matrix(places, "places")
+    T = R.dtype
+    r, rs = _rows_at(R, "R", (m, width), T, at)
+    a, as_ = (None, width) if addend is None else _rows_at(addend, "addend", (n, width), T, at)
+    o, os_ = _rows_at(out, "out", (n, width), T, at)
+    _check(_lib.groot_routed_sum(_dtype(R, "R"), r, rs, _flat_at(places, "places", (n, k), _int32, at),
+                                 None if weights is None else _flat_at(weights, "weights", (n, k), _float32, at), a, as_, k, o, os_, n, m, width,
+                                 _stream_on(stream, at)))
 
 
 def groot_routed_sum_backward(dout, R, places, weights, dR, dweights, stream=None) -> None:
     """dR[places[i, s]] = weights[i, s] dout[i], dweights[i, s] = dout[i] . R[places[i, s]].  dout [n, width], R and dR [places, width] of
     one type, weights (or None for ones) and dweights float32 [n, k].  dR or dweights may be None, and R where dweights is."""
-    d, T = _dtype(dout, "dout"), dout.dtype
-    n, width = _matrix_rows(dout, "dout"), dout.shape[1]
-    _matrix_rows(places, "places")
-    k = places.shape[1]
+    n, width, at = _matrix(dout, "dout")
+    T, k = dout.dtype, _matrix(places, "places")[1]
     if dR is None and dweights is None:
         raise ValueError("dR or dweights must be given")
     if R is None and dweights is not None:
         raise ValueError("dweights needs R")
-    m = _matrix_rows(R if R is not None else dR, "R or dR")
-    g, gs = _rows(dout, "dout", n, width, T)
-    r, rs = _rows_or_none(R, "R", m, width, T)
-    o, os_ = _rows_or_none(dR, "dR", m, width, T)
-    _check(_lib.groot_routed_sum_backward(d, g, gs, r, rs, _array(places, "places", (n, k), _int32), _array(weights, "weights", (n, k), _float32), k,
-                                          o, os_, _array(dweights, "dweights", (n, k), _float32), n, m, width,
-                                          _launch_stream(stream, dout, R, places, weights, dR, dweights)))
+    m = _matrix(R if R is not None else dR, "R or dR")[0]
+    g, gs = _rows_at(dout, "dout", (n, width), T, at)
+    r, rs = (None, width) if R is None else _rows_at(R, "R", (m, width), T, at)
+    o, os_ = (None, width) if dR is None else _rows_at(dR, "dR", (m, width), T, at)
+    _check(_lib.groot_routed_sum_backward(_dtype(dout, "dout"), g, gs, r, rs, _flat_at(places, "places", (n, k), _int32, at),
+                                          None if weights is None else _flat_at(weights, "weights", (n, k), _float32, at), k, o, os_,
+                                          None if dweights is None else _flat_at(dweights, "dweights", (n, k), _float32, at), n, m, width,
+                                          _stream_on(stream, at)))
 
 
 def groot_rms_norm(X, residual, gain, eps: float, Y, H=None, Q=None, q_scale=None, rstd=None, stream=None) -> None:
     """h = X + residual, Y = h / sqrt(mean h^2 + eps) gain.  X, residual (or None), Y, H (the rows h) [n, width] of one type, gain [width] of
     that type or None; Q int8 [n, width] and q_scale float32 [n]: the output cut to 8 bits, as groot_quantize_rows does; rstd float32 [n]
     for the backward call.  Outputs that are None are not written; H and Y may be X or residual themselves."""
-    d, T = _dtype(X, "X"), X.dtype
-    n, width = _matrix_rows(X, "X"), X.shape[1]
-    x, xs = _rows(X, "X", n, width, T)
-    r, rs = _rows_or_none(residual, "residual", n, width, T)
-    h, hs = _rows_or_none(H, "H", n, width, T)
-    y, ys = _rows_or_none(Y, "Y", n, width, T)
-    q, qs = _rows_or_none(Q, "Q", n, width, _int8)
-    _check(_lib.groot_rms_norm(d, x, xs, r, rs, _array(gain, "gain", (width,), T), eps, h, hs, y, ys, q, qs,
-                               _array(q_scale, "q_scale", (n,), _float32), _array(rstd, "rstd", (n,), _float32), n, width,
-                               _launch_stream(stream, X, residual, gain, Y, H, Q, q_scale, rstd)))
+    n, width, at = _matrix(X, "X")
+    T, shape = X.dtype, (n, width)
+    x, xs = _rows_at(X, "X", shape, T, at)
+    r, rs = (None, width) if residual is None else _rows_at(residual, "residual", shape, T, at)
+    h, hs = (None, width) if H is None else _rows_at(H, "H", shape, T, at)
+    y, ys = (None, width) if Y is None else _rows_at(Y, "Y", shape, T, at)
+    q, qs = (None, width) if Q is None else _rows_at(Q, "Q", shape, _int8, at)
+    _check(_lib.groot_rms_norm(_dtype(X, "X"), x, xs, r, rs, None if gain is None else _flat_at(gain, "gain", (width,), T, at), eps, h, hs, y, ys, q, qs,
+                               None if q_scale is None else _flat_at(q_scale, "q_scale", (n,), _float32, at),
+                               None if rstd is None else _flat_at(rstd, "rstd", (n,), _float32, at), n, width, _stream_on(stream, at)))
 
 
 def groot_rms_norm_backward_workspace(n_rows: int, width: int, dtype) -> int:
@@ -1016,14 +1048,15 @@ def groot_rms_norm_backward(H, rstd, gain, dY, dX, dgain, workspace, dH=None, st
     rows h that groot_rms_norm gave (X where there was no residual), rstd float32 [n] from the same call, dY [n, width], dH [n, width] or
     None: the gradient that comes to h by another way.  workspace: a contiguous CUDA tensor of at least
     groot_rms_norm_backward_workspace(n, width, H.dtype) bytes, or None where dgain is."""
-    d, T = _dtype(H, "H"), H.dtype
+    n, width, at = _matrix(H, "H")
+    T, shape = H.dtype, (n, width)
+    d = _dtype(H, "H")
     gd = d if dgain is None else _dtype(dgain, "dgain")
-    n, width = _matrix_rows(H, "H"), H.shape[1]
-    h, hs = _rows(H, "H", n, width, T)
-    y, ys = _rows(dY, "dY", n, width, T)
-    e, es = _rows_or_none(dH, "dH", n, width, T)
-    x, xs = _rows(dX, "dX", n, width, T)
-    ws, size = _bytes_of(workspace)
-    _check(_lib.groot_rms_norm_backward(d, h, hs, _array(rstd, "rstd", (n,), _float32), _array(gain, "gain", (width,), T), y, ys, e, es, x, xs, gd,
-                                        None if dgain is None else _array(dgain, "dgain", (width,), dgain.dtype), n, width, ws, size,
-                                        _launch_stream(stream, H, rstd, gain, dY, dH, dX, dgain, workspace)))
+    h, hs = _rows_at(H, "H", shape, T, at)
+    y, ys = _rows_at(dY, "dY", shape, T, at)
+    e, es = (None, width) if dH is None else _rows_at(dH, "dH", shape, T, at)
+    x, xs = _rows_at(dX, "dX", shape, T, at)
+    ws, size = _workspace_at(workspace, at)
+    _check(_lib.groot_rms_norm_backward(d, h, hs, _flat_at(rstd, "rstd", (n,), _float32, at), None if gain is None else _flat_at(gain, "gain", (width,), T, at), y, ys, e,
+                                        es, x, xs, gd, None if dgain is None else _flat_at(dgain, "dgain", (width,), dgain.dtype, at), n, width, ws, size,
+                                        _stream_on(stream, at)))
