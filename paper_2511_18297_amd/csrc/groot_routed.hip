@@ -1,7 +1,11 @@
 // Rows on their way to the experts' places and back:
 //   R[places[i,s]] = X[i];   out[i] = addend[i] + sum_s w[i,s] R[places[i,s]];   dR[places[i,s]] = w[i,s] dout[i], dw[i,s] = dout[i] . R[places[i,s]]
 // Every kernel goes by the rows i, which know their places: no list of the other direction, no atomics; a slot's row is written by one group
-// of lanes.  Bound by HBM: the n k rows at the places are read or written once, the n rows once.
+// of lanes.  Bound by HBM: the n k rows at the places are read or written once, the n rows once.  bfloat16: the sum of 2 x 8192 rows of 4096
+// with an addend 40 to 45 us (6.0 to 6.7 TB/s, some of it from the cache behind L2); 7168 rows of 2048 to four places each 30 us (4.9
+// TB/s), their sum's gradients 43 (6.2).  A workgroup takes a whole row at once where it can: with a wavefront to a row, or parts of rows, the sum
+// took 50 to 57.  Loads of four slots at a time go on their way together, those of a slot without a place to 16 bytes of zeros.
+// Outputs of more than 32 MB, which L2 would not hold, go past it: with them, the four calls of a training step took 140 us in place of 162.
 //
 // A piece is 16 bytes of a row.  A row's last piece is moved back to end with the row, so that it is whole too: its first values are
 // copied or computed twice, alike.  Rows of less than 16 bytes go value by value.
