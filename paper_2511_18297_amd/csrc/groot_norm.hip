@@ -342,7 +342,9 @@ __global__ __launch_bounds__(1024) void norm_gain_kernel(const float *__restrict
     dgain[k] = (O)sum;
 }
 
-// lanes of a row, and its pieces in each, by the pieces that it has
+// Lanes of a row, and its pieces in each, by the pieces that it has: the fewest lanes, in wavefronts, that leave few idle (15910 rows of 1528 in fp32,
+// 382 pieces: 128 lanes with 3 each 37 and 53 us, 256 with 2 39 and 60; 5031 rows of 1138 in bfloat16, 143 pieces: 64 with 3 12.0 and 17.4, 64 with 4 14.2
+// and 18.3).
 struct NormShape {
     int lanes, keep;
     bool is_short;

@@ -5,7 +5,7 @@
 // with an addend 40 to 45 us (6.0 to 6.7 TB/s, some of it from the cache behind L2); 7168 rows of 2048 to four places each 30 us (4.9
 // TB/s), their sum's gradients 43 (6.2).  A workgroup takes a whole row at once where it can: with a wavefront to a row, or parts of rows, the sum
 // took 50 to 57.  Loads of four slots at a time go on their way together, those of a slot without a place to 16 bytes of zeros.
-// Outputs of more than 32 MB, which L2 would not hold, go past it: with them, the four calls of a training step took 140 us in place of 162.
+// Large outputs go past the caches (kRowsPast and the like).
 //
 // A piece is 16 bytes of a row.  A row's last piece is moved back to end with the row, so that it is whole too: its first values are
 // copied or computed twice, alike.  Rows of less than 16 bytes go value by value.
@@ -279,8 +279,11 @@ RoutedShape routed_shape(RoutedArgs *a, int64_t pieces, int lanes)
     const int64_t blocks = (a->n + threads / lanes - 1) / (threads / lanes);
     return {threads, dim3((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), (uint32_t)((pieces + part - 1) / part))};
 }
-// outputs that the L2 of the eight XCDs would not hold for the next call anyway go past it
-bool beyond_caches(int64_t rows, int64_t bytes) { return rows * bytes > (32 << 20); }
+// Outputs from some size on go past the caches.  By the call that makes them and the one that reads them next, together, past and kept
+// (bfloat16, rows of 4096, us): rows and their product, 64 MB 64 and 57, 128 MB 91 and 80, 192 MB 144 and 120, 256 MB 174 and 183, 384 MB 259
+// and 256; sum and norm, 32 MB 37 and 36, 64 MB 64 and 62, 96 MB 106 and 106 (the sum by itself, 64 MB: 45.8 and 49.0); the sum's gradients and the
+// product that takes them, 32 MB 51 and 43, 64 MB 71 and 66, 128 MB 103 and 116, 256 MB 225 and 216 (by themselves, 256 MB: 100 and 133).
+constexpr int64_t kRowsPast = 224 << 20, kSumPast = 32 << 20, kGradientsPast = 96 << 20;
 
 template <typename T, bool kOnce>
 int sum_launch(RoutedArgs a, hipStream_t stream)
@@ -312,7 +315,8 @@ int sum_backward_launch(RoutedArgs a, hipStream_t stream)
         s.grid.y = (a.k + a.part - 1) / a.part;                                                                                          \
         routed_sum_backward_kernel<T, lanes, held, is_short, kOnce><<<s.grid, s.threads, 0, stream>>>(a);                                \
     }
-    // a wavefront to a row, and a workgroup where rows are wide or few; very few rows: one for every two slots
+    // a wavefront to a row, and a workgroup where rows are wide or few (1024 rows of 2048 in bfloat16, 4 slots: 9.8 and 7.5 us; 4096: 25.0 and 26.9);
+    // very few rows: one for every two slots (29 rows of 4160, 9 slots: 15.2 us without, 6.1)
     const bool few = a.n < 2048, few_rows = a.n < 1024;
     if (a.K * sizeof(T) < 16) GROOT_SUM(16, 1, true)
     else if (pieces <= 16) GROOT_SUM(16, 1, false)
@@ -350,13 +354,13 @@ int rows_launch(RoutedArgs a, int32_t value_bytes, hipStream_t stream)
 int launch_routed_rows(int32_t value_bytes, const RoutedArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    return beyond_caches(a.n * a.k, (int64_t)a.K * value_bytes) ? rows_launch<true>(a, value_bytes, s) : rows_launch<false>(a, value_bytes, s);
+    return a.n * a.k * a.K * value_bytes > kRowsPast ? rows_launch<true>(a, value_bytes, s) : rows_launch<false>(a, value_bytes, s);
 }
 
 int launch_routed_sum(int32_t dtype, const RoutedArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    const bool once = beyond_caches(a.n, (int64_t)a.K * (dtype == GROOT_F32 ? 4 : 2));
+    const bool once = a.n * a.K * (dtype == GROOT_F32 ? 4 : 2) > kSumPast;
     if (dtype == GROOT_F32) return once ? sum_launch<float, true>(a, s) : sum_launch<float, false>(a, s);
     if (dtype == GROOT_BF16) return once ? sum_launch<bf16_t, true>(a, s) : sum_launch<bf16_t, false>(a, s);
     return once ? sum_launch<f16_t, true>(a, s) : sum_launch<f16_t, false>(a, s);
@@ -365,7 +369,7 @@ int launch_routed_sum(int32_t dtype, const RoutedArgs &a, void *stream)
 int launch_routed_sum_backward(int32_t dtype, const RoutedArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    const bool once = beyond_caches(a.n * a.k, (int64_t)a.K * (dtype == GROOT_F32 ? 4 : 2));
+    const bool once = a.n * a.k * a.K * (dtype == GROOT_F32 ? 4 : 2) > kGradientsPast;
     if (dtype == GROOT_F32) return once ? sum_backward_launch<float, true>(a, s) : sum_backward_launch<float, false>(a, s);
     if (dtype == GROOT_BF16) return once ? sum_backward_launch<bf16_t, true>(a, s) : sum_backward_launch<bf16_t, false>(a, s);
     return once ? sum_backward_launch<f16_t, true>(a, s) : sum_backward_launch<f16_t, false>(a, s);
