@@ -138,7 +138,7 @@ struct NormBackwardArgs {
     int64_t h_stride, dy_stride, dh_stride, dx_stride;
     int64_t n;
     int32_t K;
-    float *partial;                          // [groups of rows, K]
+    float *partial;                          // [workgroups, K]
 };
 size_t norm_backward_workspace(int32_t dtype, int64_t n, int32_t K);
 int launch_norm_backward(int32_t dtype, const NormBackwardArgs &a, void *stream);

@@ -4,7 +4,7 @@
 //   dx = rstd (a - u mean(a u)) + dh with u = h rstd, a = dy gain;  dgain = sum over the rows of dy u
 // The sum of the squares is in 64 bits so that rstd, and with it every code, is the same whatever order the lanes add in.
 // Bound by HBM: a row is read once and stays in registers as it is held.  8192 rows of 4096 in float16 with a residual, H and 8 bits out: 41 us
-// (5.7 TB/s); 16384 rows in bfloat16, forward 88 us (6.1 TB/s), backward 98 (5.5: three rows in, one out) and 6 for the gain's gradient; 8.4 M
+// (5.7 TB/s); 16384 rows in bfloat16, forward 90 us (6.0 TB/s), backward 89 (6.0: three rows in, one out) and 6 for the gain's gradient; 8.4 M
 // rows of 64 in fp32 0.73 ms (5.9) and 1.21 (5.3).  Of the backward call's time its instructions take a quarter: more rows on their way at a
 // time (1.29 ms) and the next row's loads in front (1.45) made it slower, as did loads that keep their lines (1.28).
 // The lanes of a row, and the pieces in each, are the fewest that hold it: with twice the lanes that rows of 4096 need, forward took 112 us.
@@ -35,16 +35,16 @@ __device__ __forceinline__ Piece piece(int32_t i, int32_t K)
     return Piece{at, begin - at, true};
 }
 
-// kShort: a row of less than 16 bytes
-template <typename T, bool kShort>
+typedef v4i piece_t __attribute__((aligned(2)));
+// kShort: a row of less than 16 bytes; kOnce: rows that no cache is to keep
+template <typename T, bool kShort, bool kOnce>
 __device__ __forceinline__ v4i load_piece(const T *row, const Piece &p, int32_t K)
 {
     if constexpr (kShort) return short16<T>((const char *)row, (int64_t)K * (int64_t)sizeof(T));
-    typedef v4i piece_t __attribute__((aligned(2)));
-    return __builtin_nontemporal_load((const piece_t *)(row + p.at));
+    else if constexpr (kOnce) return __builtin_nontemporal_load((const piece_t *)(row + p.at));
+    else return *(const piece_t *)(row + p.at);
 }
-// kStream: past the caches, where nobody reads it soon
-template <typename T, bool kShort, bool kStream = false>
+template <typename T, bool kShort>
 __device__ __forceinline__ void store_piece(T *row, const Piece &p, int32_t K, v4i v)
 {
     if constexpr (kShort) {
@@ -54,9 +54,7 @@ __device__ __forceinline__ void store_piece(T *row, const Piece &p, int32_t K, v
         for (int k = 0; k < (int)(16 / sizeof(T)); ++k)
             if (k < K) row[k] = e[k];
     } else {
-        typedef v4i piece_t __attribute__((aligned(2)));
-        if (kStream) __builtin_nontemporal_store(v, (piece_t *)(row + p.at));
-        else *(piece_t *)(row + p.at) = v;
+        *(piece_t *)(row + p.at) = v;
     }
 }
 template <typename T>
@@ -124,7 +122,7 @@ __device__ __forceinline__ uint32_t four_codes(const float *y, float scale, floa
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u), __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), 0x05040100u);
 }
 
-template <typename T, int kLanes, int kKeep, bool kShort>
+template <typename T, int kLanes, int kKeep, bool kShort, bool kOnce>
 __global__ __launch_bounds__(block_of(kLanes)) void norm_kernel(NormArgs a)
 {
     constexpr int kPer = 16 / sizeof(T), kThreads = block_of(kLanes), kRows = kThreads / kLanes;
@@ -135,7 +133,7 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_kernel(NormArgs a)
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
         p[i] = piece<T>(i * kLanes + lane, a.K);
-        gain[i] = a.gain ? load_piece<T, kShort>((const T *)a.gain, p[i], a.K) : ones<T>();
+        gain[i] = a.gain ? load_piece<T, kShort, false>((const T *)a.gain, p[i], a.K) : ones<T>();
     }
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += (int64_t)gridDim.x * kRows) {
         const int64_t mine = first + threadIdx.x / kLanes, row = mine < a.n ? mine : a.n - 1;   // rows beyond the last go along and store nothing
@@ -143,12 +141,12 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_kernel(NormArgs a)
         const T *const x = (const T *)a.X + row * a.x_stride;
         v4i h[kKeep];
 #pragma unroll
-        for (int i = 0; i < kKeep; ++i) h[i] = load_piece<T, kShort>(x, p[i], a.K);
+        for (int i = 0; i < kKeep; ++i) h[i] = load_piece<T, kShort, kOnce>(x, p[i], a.K);
         if (a.residual) {
             const T *const r = (const T *)a.residual + row * a.residual_stride;
             v4i other[kKeep];
 #pragma unroll
-            for (int i = 0; i < kKeep; ++i) other[i] = load_piece<T, kShort>(r, p[i], a.K);
+            for (int i = 0; i < kKeep; ++i) other[i] = load_piece<T, kShort, kOnce>(r, p[i], a.K);
 #pragma unroll
             for (int i = 0; i < kKeep; ++i) {
                 RowValues<T> u = row_values<T>(h[i]);
@@ -223,7 +221,7 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_kernel(NormArgs a)
 }
 
 // The rows of a workgroup add up their part of the gain's gradient, each lane its own columns; the parts meet in norm_gain_kernel.
-template <typename T, int kLanes, int kKeep, bool kShort>
+template <typename T, int kLanes, int kKeep, bool kShort, bool kOnce, bool kPast>
 __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBackwardArgs a)
 {
     constexpr int kPer = 16 / sizeof(T), kThreads = block_of(kLanes), kRows = kThreads / kLanes;
@@ -234,7 +232,7 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBac
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
         p[i] = piece<T>(i * kLanes + lane, a.K);
-        gain[i] = a.gain ? load_piece<T, kShort>((const T *)a.gain, p[i], a.K) : ones<T>();
+        gain[i] = a.gain ? load_piece<T, kShort, false>((const T *)a.gain, p[i], a.K) : ones<T>();
     }
     float parts[kKeep][kPer] = {};
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += (int64_t)gridDim.x * kRows) {
@@ -244,12 +242,12 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBac
         v4i h[kKeep], dy[kKeep], dh[kKeep];
 #pragma unroll
         for (int i = 0; i < kKeep; ++i) {
-            h[i] = load_piece<T, kShort>((const T *)a.H + row * a.h_stride, p[i], a.K);
-            dy[i] = load_piece<T, kShort>((const T *)a.dY + row * a.dy_stride, p[i], a.K);
+            h[i] = load_piece<T, kShort, kOnce>((const T *)a.H + row * a.h_stride, p[i], a.K);
+            dy[i] = load_piece<T, kShort, kOnce>((const T *)a.dY + row * a.dy_stride, p[i], a.K);
         }
         if (a.dH) {
 #pragma unroll
-            for (int i = 0; i < kKeep; ++i) dh[i] = load_piece<T, kShort>((const T *)a.dH + row * a.dh_stride, p[i], a.K);
+            for (int i = 0; i < kKeep; ++i) dh[i] = load_piece<T, kShort, kOnce>((const T *)a.dH + row * a.dh_stride, p[i], a.K);
         }
         double sum = 0;
 #pragma unroll
@@ -289,7 +287,8 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBac
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) u.x[e] += v.x[e];
             }
-            store_piece<T, kShort, true>((T *)a.dX + row * a.dx_stride, p[i], a.K, rounded<T>(u));
+            if constexpr (!kShort && kPast) __builtin_nontemporal_store(rounded<T>(u), (piece_t *)((T *)a.dX + row * a.dx_stride + p[i].at));
+            else store_piece<T, kShort>((T *)a.dX + row * a.dx_stride, p[i], a.K, rounded<T>(u));
         }
     }
     if (!a.dgain) return;
@@ -320,6 +319,11 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBac
         }
     }
 }
+
+// Rows of more bytes are read past the caches, and a gradient of more is written past them.  Rows of 4096 in bfloat16, loads past and kept, us: 32 MB,
+// the inputs in the caches already, forward 27 and 22, backward 37 and 34; 128 MB 82 and 93, 99 and 104.  The gradient past and kept, by itself and
+// with the product that takes it: 64 MB 61 and 57, 93 and 84; 128 MB 102 and 99, 150 and 139; 256 MB 184 and 181, 275 and 285.
+constexpr int64_t kLoadsPast = 32 << 20, kGradientsPast = 192 << 20;
 
 constexpr int kGainCols = 16, kGainRows = 64;
 
@@ -375,9 +379,15 @@ int64_t norm_blocks(int64_t n, const NormShape &s, int64_t most)
     const int64_t b = (n + rows_of(s.lanes) - 1) / rows_of(s.lanes);
     return b < most ? b : most;
 }
-// Workgroups of the backward call: whole multiples of the 256 CUs, as each writes a row of partial sums.  16384 rows of 4096 in bfloat16, 512,
-// 768, 1024, 2048 of them: 108, 104, 107, 119 us with the sums; 8.4 M rows of 64 in fp32, 512, 1024, 2048, 8192: 1555, 1218, 1226, 1405.
-int64_t backward_blocks(int64_t n, const NormShape &s) { return norm_blocks(n, s, s.lanes <= kWave ? 1024 : s.lanes <= 256 ? 768 : s.lanes == 512 ? 512 : 256); }
+// Workgroups of the backward call: whole multiples of the 256 CUs with four turns of rows each at least, as each writes a row of partial sums. 512, 1024
+// and 2048 rows of 4096 in bfloat16, 256 of them: 14.1, 17.2 and 23.5 us with the sums, 512: 16.2, 17.9 and 22.0, 1024: 16.1, 25.4 and 28.5; 16384 rows,
+// 512, 768, 1024, 2048: 108, 104, 107, 119 us; 8.4 M rows of 64 in fp32, 512, 1024, 2048, 8192: 1555, 1218, 1226, 1405.
+int64_t backward_blocks(int64_t n, const NormShape &s)
+{
+    const int64_t turns = norm_blocks(n, s, INT64_MAX), most = s.lanes <= kWave ? 1024 : s.lanes <= 256 ? 768 : s.lanes == 512 ? 512 : 256;
+    const int64_t blocks = (turns / 4 + 255) / 256 * 256;
+    return turns < 256 ? turns : blocks < 256 ? 256 : blocks < most ? blocks : most;
+}
 
 #define GROOT_NORM_SHAPES(use)                                                                                                           \
     if (s.is_short) use(16, 1, true)                                                                                                     \
@@ -396,25 +406,25 @@ int64_t backward_blocks(int64_t n, const NormShape &s) { return norm_blocks(n, s
     else if (s.keep == 8) use(1024, 8, false)                                                                                            \
     else if constexpr (sizeof(T) == 4) use(1024, 16, false)
 
-template <typename T>
+template <typename T, bool kOnce>
 int norm_launch(const NormArgs &a, hipStream_t stream)
 {
     const NormShape s = norm_shape(a.K, sizeof(T));
     const uint32_t blocks = (uint32_t)norm_blocks(a.n, s, 1 << 20);
-#define GROOT_NORM(lanes, keep, is_short) { norm_kernel<T, lanes, keep, is_short><<<blocks, block_of(lanes), 0, stream>>>(a); }
+#define GROOT_NORM(lanes, keep, is_short) { norm_kernel<T, lanes, keep, is_short, kOnce><<<blocks, block_of(lanes), 0, stream>>>(a); }
     GROOT_NORM_SHAPES(GROOT_NORM)
 #undef GROOT_NORM
     return (int)hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool kOnce, bool kPast>
 int norm_backward_launch(const NormBackwardArgs &a, hipStream_t stream)
 {
     const NormShape s = norm_shape(a.K, sizeof(T));
     const uint32_t blocks = (uint32_t)backward_blocks(a.n, s);
 #define GROOT_NORM(lanes, keep, is_short)                                                                                                \
     {                                                                                                                                    \
-        norm_backward_kernel<T, lanes, keep, is_short>                                                                                   \
+        norm_backward_kernel<T, lanes, keep, is_short, kOnce, kPast>                                                                                   \
             <<<blocks, block_of(lanes), rows_of(lanes) > 1 ? block_of(lanes) * keep * 16 / sizeof(T) * sizeof(float) : 0, stream>>>(a);  \
     }
     if (blocks) { GROOT_NORM_SHAPES(GROOT_NORM) }
@@ -439,17 +449,26 @@ size_t norm_backward_workspace(int32_t dtype, int64_t n, int32_t K)
 int launch_norm(int32_t dtype, const NormArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == GROOT_F32) return norm_launch<float>(a, s);
-    if (dtype == GROOT_BF16) return norm_launch<bf16_t>(a, s);
-    return norm_launch<f16_t>(a, s);
+    const bool once = a.n * a.K * (dtype == GROOT_F32 ? 4 : 2) > kLoadsPast;
+    if (dtype == GROOT_F32) return once ? norm_launch<float, true>(a, s) : norm_launch<float, false>(a, s);
+    if (dtype == GROOT_BF16) return once ? norm_launch<bf16_t, true>(a, s) : norm_launch<bf16_t, false>(a, s);
+    return once ? norm_launch<f16_t, true>(a, s) : norm_launch<f16_t, false>(a, s);
 }
 
+template <typename T>
+static int norm_backward_for(const NormBackwardArgs &a, hipStream_t stream)
+{
+    const int64_t bytes = a.n * a.K * (int64_t)sizeof(T);
+    return bytes > kGradientsPast ? norm_backward_launch<T, true, true>(a, stream)
+           : bytes > kLoadsPast   ? norm_backward_launch<T, true, false>(a, stream)
+                                  : norm_backward_launch<T, false, false>(a, stream);
+}
 int launch_norm_backward(int32_t dtype, const NormBackwardArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == GROOT_F32) return norm_backward_launch<float>(a, s);
-    if (dtype == GROOT_BF16) return norm_backward_launch<bf16_t>(a, s);
-    return norm_backward_launch<f16_t>(a, s);
+    if (dtype == GROOT_F32) return norm_backward_for<float>(a, s);
+    if (dtype == GROOT_BF16) return norm_backward_for<bf16_t>(a, s);
+    return norm_backward_for<f16_t>(a, s);
 }
 
 }  // namespace groot
