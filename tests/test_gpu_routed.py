@@ -240,6 +240,19 @@ def test_masks_infinities_and_nan(gate, renormalise, sets, E):
     assert int(got[3][-1]) == 0
 
 
+@pytest.mark.parametrize("gate", GATES)
+@pytest.mark.parametrize("sets", ((1, 1, 1), (6, 2, 1), (6, 2, 2), (24, 4, 2), (3, 1, 2), (8, 3, 2), (2, 1, 2)))
+def test_a_bias_of_plus_infinity_comes_first(gate, sets):
+    """experts with it tie with one another, as their sets do, and are closed where their score is -inf"""
+    scores, bias = made(140, 48, torch.float32, 22)
+    bias[7], bias[30], bias[31] = INF, INF, INF
+    scores[::3, 30] = -INF
+    check_route(scores, bias, 2, **how(gate, *sets, True))
+    bias[:] = INF
+    bias[40] = torch.finfo(torch.float32).min
+    check_route(scores, bias, 2, **how(gate, *sets, False))
+
+
 def test_no_rows():
     for E in (8, 600):
         got = own_route(torch.empty((0, E), device="cuda"), None, 2, **how())
@@ -338,6 +351,23 @@ def test_route_backward_of_broken_rows_and_foreign_experts():
             g[e] += 2
         want = p[row] * (g - (g * p[row]).sum())
         assert torch.allclose(ds[3 + row].double(), want, rtol=1e-5, atol=1e-6)
+
+
+@pytest.mark.parametrize("gate", GATES)
+@pytest.mark.parametrize("renormalise", (False, True))
+def test_route_backward_of_slots_without_an_expert(gate, renormalise):
+    """what stands in their gradient counts for nothing, NaN neither"""
+    scores, _ = made(70, 24, torch.bfloat16, 62)
+    experts = own_route(scores, None, 5, **how(gate, renormalise=renormalise))[0]
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    experts = torch.where(torch.rand((70, 5), generator=gen, device="cuda") < 0.4, torch.full_like(experts, -1), experts)
+    dw = torch.randn((70, 5), generator=gen, device="cuda")
+    results = []
+    for there in (0.0, NAN, INF):
+        ds = torch.full_like(scores, NAN)
+        G.groot_route_backward(scores, experts, torch.where(experts < 0, torch.full_like(dw, there), dw), ds, gate=GATES[gate], renormalise=renormalise)
+        results.append(ds)
+    assert not torch.isnan(results[0]).any() and all(torch.equal(results[0], r) for r in results[1:])
 
 
 # ---------------------------------------------------------------------------------------------------------------
