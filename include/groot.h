@@ -661,7 +661,10 @@ groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int64_t n_tenso
  * experts int32 [n_rows, top_k]: the top_k experts of largest c, descending;
  *   ties, here and between sets, go to the lowest number.  -1 where none is left.
  * weights float [n_rows, top_k]: factor p, or with `renormalise` factor p
- *   over the sum of p of the row's chosen experts; 0 where there is none.  A row
+ *   over the sum of p of the row's chosen experts; 0 where there is none.  Computed in
+ *   64 bits and rounded once, but for the sum over all experts of a softmax that is not
+ *   renormalised, where the choice goes by the scores: its terms are in fp32, and it is
+ *   within 2^-19 of itself at the most (2^-23 as a rule).  A row
  *   with a NaN among its scores, or with +inf under softmax, has no
  *   experts and weights of NaN, which show in groot_routed_sum.
  * places int32 [n_rows, top_k]: where (row, slot) comes when all are put in the
@@ -669,7 +672,8 @@ groot_status groot_adamw_step(const groot_adamw_tensor *tensors, int64_t n_tenso
  * offsets int64 [n_experts + 1]: where each expert's places begin; the last is
  *   their number.  Rows of R behind it are not written.
  * groot_route_backward: dscores (of dtype, fully overwritten) from the gradient
- *   of the weights; the choice has none.  NaN in rows whose weights are NaN, 0 at -inf.
+ *   of the weights; the choice has none.  Terms in 64 bits (with that sum as above), put
+ *   together in fp32.  NaN in rows whose weights are NaN, 0 at -inf.
  * workspace of groot_route: device, 16-byte aligned, groot_route_workspace bytes (may be 0),
  *   contents overwritten, owned by the caller and for one call at a time.
  * 1 <= n_experts <= 1024, 1 <= top_k <= 32, n_sets <= 64, top_k at most what

@@ -362,7 +362,7 @@ extern "C" groot_status groot_route(int32_t dtype, const void *scores_dev, int64
             if (out[i].meets(out[j])) return bad(who, "two of the outputs and the workspace overlap");
     }
     RouteArgs a{scores_dev, score_stride * b, bias_dev, experts_dev, weights_dev, places_dev, offsets_dev, n_rows, dtype, n_experts, top_k, gate,
-                n_sets, open_sets, set_best, renormalise != 0, bias_dev != nullptr || (set_best == 2 && open_sets < n_sets), (float)factor, 0, 0, 0, false, false, 0};
+                n_sets, open_sets, set_best, renormalise != 0, bias_dev != nullptr || (set_best == 2 && open_sets < n_sets), factor, 0, 0, 0, false, false, 0};
     return launched(who, launch_route(a, workspace_dev, hip_stream));
 }
 
@@ -383,7 +383,7 @@ extern "C" groot_status groot_route_backward(int32_t dtype, const void *scores_d
     if (to.meets(in) || to.meets(e) || to.meets(d)) return bad(who, "dscores overlaps an input");
     if (n_rows == 0) return GROOT_OK;
     RouteBackwardArgs a{scores_dev, score_stride * b, experts_dev, dweights_dev, dscores_dev, ds_stride * b, n_rows, dtype, n_experts, top_k, gate,
-                        renormalise != 0, (float)factor};
+                        renormalise != 0, factor};
     return launched(who, launch_route_backward(a, hip_stream));
 }
 

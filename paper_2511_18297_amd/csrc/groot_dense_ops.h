@@ -69,7 +69,7 @@ struct RouteArgs {
     int32_t dtype, E, k, gate, sets, open_sets, set_best;
     bool renormalise;
     bool by_value;               // the choice goes by probability + bias, not by the score
-    float factor;
+    double factor;
     // the launcher's
     int32_t rows;                // of a workgroup
     uint32_t inverse_k;
@@ -91,7 +91,7 @@ struct RouteBackwardArgs {
     int64_t n;
     int32_t dtype, E, k, gate;
     bool renormalise;
-    float factor;
+    double factor;
 };
 int launch_route_backward(const RouteBackwardArgs &a, void *stream);
 

@@ -121,7 +121,26 @@ __device__ __forceinline__ double exp64(double x)
     return ldexp(p, (int)i);
 }
 
-// 1 / x for x in [1, 2] to 2^-51: the instruction's approximation and two of Newton's steps, which square its error of 2^-14 at most
+// e^x for x <= 0 to 2^-31 of itself, for what fp32 holds in the end (e^-700 below -700): the same with r's series up to r^8 / 8!.  i comes out of an addition
+// that leaves it in the last bits, and is added to the exponent's: conversions and ldexp take four times an addition's cycles.
+__device__ __forceinline__ double exp31(double x)
+{
+    constexpr double kRound = 0x1.8p52;
+    x = fmax(x, -700.0);
+    const double shifted = __builtin_fma(x, 0x1.71547652b82fep+0, kRound), r = __builtin_fma(kRound - shifted, 0x1.62e42fefa39efp-1, x);
+    double p = 1.0 / 40320;
+    p = __builtin_fma(p, r, 1.0 / 5040);
+    p = __builtin_fma(p, r, 1.0 / 720);
+    p = __builtin_fma(p, r, 1.0 / 120);
+    p = __builtin_fma(p, r, 1.0 / 24);
+    p = __builtin_fma(p, r, 1.0 / 6);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + (__builtin_bit_cast(uint64_t, shifted) << 52));
+}
+
+// 1 / x to 2^-51: the instruction's approximation and two of Newton's steps, which square its error of 2^-14 at most
 __device__ __forceinline__ double reciprocal64(double x)
 {
     double y = __builtin_amdgcn_rcp(x);
@@ -130,11 +149,29 @@ __device__ __forceinline__ double reciprocal64(double x)
 }
 
 // The weight of a score up to a factor that the row shares.  softmax: e^(s - m), m the largest score.  sigmoid: e^min(s, 0) / (1 + e^-|s|),
-// with e^(min(s, 0) - m) in its place where weights are renormalised, so that low scores keep their ratios.
-__device__ __forceinline__ float weight_of(float s, float m, bool sigmoid)
+// with e^(min(s, 0) - m) in its place where weights are renormalised, so that low scores keep their ratios.  In 64 bits, as the sums of them
+// are, and a weight is rounded once: in fp32 the difference and its product with log2(e) alone cost |s - m| half steps (55 were seen).
+__device__ __forceinline__ double weight_of(float s, float m, bool sigmoid)
 {
-    const float e = __expf((sigmoid ? fminf(s, 0.f) : s) - m);
-    return sigmoid ? e / (1.f + __expf(-__builtin_fabsf(s))) : e;
+    const double e = exp31((double)(sigmoid ? fminf(s, 0.f) : s) - (double)m);
+    return sigmoid ? e * reciprocal64(1.0 + exp31(-__builtin_fabs((double)s))) : e;
+}
+// The softmax's sum over all experts is of terms in fp32, in pairs: a term p that is |x| below the largest is off by 2.5 |x| + 2 half steps, and p |x| adds
+// up to 4.4 of the sum at the most (1024 experts).  In 64 bits: 65536 rows of 128, top 8: 23.9 us in place of 20.4.
+template <int kCount>
+__device__ __forceinline__ float tree_sum(float (&x)[kCount])
+{
+#pragma unroll
+    for (int d = 1; d < kCount; d *= 2)
+#pragma unroll
+        for (int i = 0; i + d < kCount; i += 2 * d) x[i] += x[i + d];
+    return x[0];
+}
+// 1 - sigmoid(s)
+__device__ __forceinline__ double rest_of(float s)
+{
+    const double e = exp31(-__builtin_fabs((double)s));
+    return (s > 0.f ? e : 1.0) * reciprocal64(1.0 + e);
 }
 
 // The value with the number in its last bits, so that of equal values the lower number is the larger key: its complement where the value
@@ -396,14 +433,14 @@ __global__ __launch_bounds__(kRouteThreads, 4) void route_kernel(RouteArgs a, ui
         top = over_lanes<kLanes>(top, [](float x, float y) { return __builtin_elementwise_maximum(x, y); });
         const bool broken = top != top || (!sigmoid && top == kInf);
         const float base = sigmoid || top == -kInf ? 0.f : top;
-        float sum = 1.f;                                                  // of e^(s - base), where weights go by it
+        double sum = 1.0;                                                 // of e^(s - base), where weights go by it
         double x[kEach];
         if constexpr (!kByValue) {
             if (!sigmoid && !a.renormalise) {
-                sum = 0.f;
+                float term[kEach];
 #pragma unroll
-                for (int v = 0; v < kEach; ++v) sum += __expf(s[v] - base);
-                sum = sum_of<kLanes>(sum);
+                for (int v = 0; v < kEach; ++v) term[v] = __expf(s[v] - base);
+                sum = (double)sum_of<kLanes>(tree_sum(term));
             }
 #pragma unroll
             for (int v = 0; v < kEach; ++v) {
@@ -422,7 +459,7 @@ __global__ __launch_bounds__(kRouteThreads, 4) void route_kernel(RouteArgs a, ui
             }
             if (!sigmoid) {
                 all = sum_of<kLanes>(all);
-                sum = (float)all;
+                sum = all;
                 all = 1.0 / all;
             }
 #pragma unroll
@@ -521,32 +558,29 @@ __global__ __launch_bounds__(kRouteThreads, 4) void route_kernel(RouteArgs a, ui
                 at_slot[j] = !taken ? -kInf : kByValue ? score_at(scores, a.dtype, expert[j]) : score_of(key);
                 m = fmaxf(m, sigmoid ? fminf(at_slot[j], 0.f) : at_slot[j]);
             }
-            float scale = a.factor;
             if (a.renormalise) {
                 m = top_of<kLanes>(m);
                 m = m == -kInf ? 0.f : m;
             } else {
                 m = base;
-                scale /= sum;
             }
-            float w[kSlots], all = 0.f;
+            double w[kSlots], all = 0.0;
 #pragma unroll
             for (int j = 0; j < kSlots; ++j) {
-                w[j] = expert[j] < 0 ? 0.f : weight_of(at_slot[j], m, sigmoid);
+                w[j] = expert[j] < 0 ? 0.0 : weight_of(at_slot[j], m, sigmoid);
                 all += w[j];
             }
-            if (a.renormalise) scale /= sum_of<kLanes>(all);
+            const double scale = a.factor * reciprocal64(a.renormalise ? sum_of<kLanes>(all) : sum);
 #pragma unroll
             for (int j = 0; j < kSlots; ++j) {
                 const int slot = j * kWide + lane;
                 if (real && slot < a.k && (kWide == kLanes || lane < kWide)) {
-                    weights[local * a.k + slot] = broken ? nan : expert[j] < 0 ? 0.f : w[j] * scale;
+                    weights[local * a.k + slot] = broken ? nan : expert[j] < 0 ? 0.f : (float)(w[j] * scale);
                     chosen[local * a.k + slot] = (int16_t)expert[j];
                     if (expert[j] >= 0) atomicOr(&mask[expert[j]], 1ull << local);
                 }
             }
         } else if constexpr (kList == 16 && kEach == 16) {                // the lists hold all of a lane's experts
-            float m = -kInf, all = 0.f;
             for (int32_t slot = 0; slot < a.k; ++slot) {
                 const double best = top_of<kLanes>(x[0]);
                 const bool mine = x[0] == best;
@@ -554,30 +588,32 @@ __global__ __launch_bounds__(kRouteThreads, 4) void route_kernel(RouteArgs a, ui
                 for (int v = 0; v + 1 < kEach; ++v) x[v] = mine ? x[v + 1] : x[v];
                 if (mine) x[kEach - 1] = kClosed;
                 const bool taken = best > kLeastOpen && !broken;
-                const float at_slot = taken ? score_at(scores, a.dtype, (int32_t)number_of(best, kNumbers)) : -kInf;
-                const float low = sigmoid ? fminf(at_slot, 0.f) : at_slot;
-                // the sum at the largest score so far
-                const float higher = a.renormalise ? fmaxf(m, low) : base;
-                if (taken && a.renormalise) {
-                    all = all * __expf(m - higher) + weight_of(at_slot, higher, sigmoid);
-                    m = higher;
-                }
+                const int32_t expert = taken ? (int32_t)number_of(best, kNumbers) : -1;
                 if (real && lane == 0) {
-                    weights[local * a.k + slot] = at_slot;
-                    chosen[local * a.k + slot] = (int16_t)(taken ? (int32_t)number_of(best, kNumbers) : -1);
-                    if (taken) {
-                        atomicOr(&mask[number_of(best, kNumbers)], 1ull << local);
-                    }
+                    weights[local * a.k + slot] = taken ? score_at(scores, a.dtype, expert) : -kInf;
+                    chosen[local * a.k + slot] = (int16_t)expert;
+                    if (taken) atomicOr(&mask[expert], 1ull << local);
                 }
             }
-            m = a.renormalise ? m : base;
-            const float scale = a.factor / (a.renormalise ? all : sum);
             wave_sync();
-            if (real)
-                for (int32_t slot = lane; slot < a.k; slot += kLanes) {
-                    const float at_slot = weights[local * a.k + slot];
-                    weights[local * a.k + slot] = broken ? nan : at_slot == -kInf ? 0.f : weight_of(at_slot, m, sigmoid) * scale;
-                }
+            // every lane takes its share of the slots: slot j kLanes + lane
+            const int32_t slots = real ? a.k : 0;
+            float m = -kInf;
+            for (int32_t slot = lane; slot < slots; slot += kLanes) m = fmaxf(m, sigmoid ? fminf(weights[local * a.k + slot], 0.f) : weights[local * a.k + slot]);
+            if (a.renormalise) {
+                m = top_of<kLanes>(m);
+                m = m == -kInf ? 0.f : m;
+            } else {
+                m = base;
+            }
+            double all = 0.0;
+            if (a.renormalise)
+                for (int32_t slot = lane; slot < slots; slot += kLanes) all += weight_of(weights[local * a.k + slot], m, sigmoid);
+            const double scale = a.factor * reciprocal64(a.renormalise ? sum_of<kLanes>(all) : sum);
+            for (int32_t slot = lane; slot < slots; slot += kLanes) {
+                const float at_slot = weights[local * a.k + slot];
+                weights[local * a.k + slot] = broken ? nan : at_slot == -kInf ? 0.f : (float)(weight_of(at_slot, m, sigmoid) * scale);
+            }
             wave_sync();
         }
     }
@@ -732,7 +768,7 @@ __device__ __forceinline__ void put_scores(char *row, int32_t E, int32_t begin, 
 }
 
 // ds of a row.  softmax: l = log p, p_j (g_j - sum g p) with g the gradients at the chosen weights; renormalised over the chosen ones.
-// sigmoid: the gradient at log p times 1 - p.  kLanes lanes to a row with kEach neighbouring experts each, and a slot.
+// sigmoid: the gradient at log p times 1 - p.  In 64 bits up to the products that are rounded to wait in LDS and registers.  kLanes lanes to a row with kEach neighbouring experts each, and a slot.
 template <int kLanes, int kEach>
 __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArgs a)
 {
@@ -764,25 +800,29 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
         top = over_lanes<kLanes>(top, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
         const bool broken = top != top || (!sigmoid && top == kInf);
         const float base = top == -kInf ? 0.f : top;
-        float at_log = 0.f;                                  // the gradient at the slot's log p
-        float sum = 1.f, total = 0.f;
+        double at_log = 0.0;                                 // the gradient at the slot's log p, under a sigmoid times 1 - p
+        float e[kEach], shared = 0.f;                        // without renormalisation under a softmax: an expert's e^(x - base), and what all have for each
+        constexpr int kSlots = kLanes < 32 ? kLanes : 32;    // lanes that can have one
         if (a.renormalise) {
-            const float most = top_of<kLanes>(sigmoid ? fminf(s, 0.f) : s);
-            const float q = mine < 0 || s == -kInf ? 0.f : weight_of(s, most, sigmoid);
-            const float all = sum_of<kLanes>(q);             // every lane takes part
-            const float w = mine < 0 ? 0.f : q / all;
-            const float mean = sum_of<kLanes>(w * dw);
-            at_log = mine < 0 ? 0.f : a.factor * w * (dw - mean);
+            const float most = top_of<kSlots>(sigmoid ? fminf(s, 0.f) : s);
+            const double q = mine < 0 || s == -kInf ? 0.0 : weight_of(s, most, sigmoid);
+            const double all = sum_of<kSlots>(q), with_dw = sum_of<kSlots>(q * (double)dw);   // every lane takes part
+            const double over_all = reciprocal64(all);
+            at_log = mine < 0 ? 0.0 : a.factor * (q * over_all) * ((double)dw - with_dw * over_all);
         } else if (!sigmoid) {
-            sum = 0.f;
+            float term[kEach];
 #pragma unroll
-            for (int v = 0; v < kEach; ++v) sum += __expf(x[v] - base);
-            sum = sum_of<kLanes>(sum);
-            at_log = mine < 0 ? 0.f : a.factor * dw * (__expf(s - base) / sum);
-            total = sum_of<kLanes>(at_log);
+            for (int v = 0; v < kEach; ++v) {
+                term[v] = e[v] = __expf(x[v] - base);
+            }
+            const double over_sum = reciprocal64((double)sum_of<kLanes>(tree_sum(term)));
+            at_log = mine < 0 ? 0.0 : a.factor * (double)dw * (exp31((double)s - (double)base) * over_sum);
+            shared = (float)(sum_of<kLanes>(at_log) * over_sum);
         } else if (mine >= 0) {
-            at_log = a.factor * dw * weight_of(s, 0.f, true);
+            at_log = a.factor * (double)dw * weight_of(s, 0.f, true);
         }
+        if (sigmoid && mine >= 0) at_log *= rest_of(s);
+        const float at_slot = (float)at_log;
         // an expert that is named twice (not by groot_route) gets both, in the order of the slots
         if (mine >= 0) at[mine] = __int_as_float(lane);
         wave_sync();
@@ -792,10 +832,10 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
         for (int v = 0; v < kEach; ++v) at[begin + v] = 0.f;
         wave_sync();
         if (!twice) {
-            if (mine >= 0) at[mine] = at_log;
+            if (mine >= 0) at[mine] = at_slot;
         } else {
             for (int32_t slot = 0; slot < a.k; ++slot) {
-                if (lane == slot && mine >= 0) at[mine] += at_log;
+                if (lane == slot && mine >= 0) at[mine] += at_slot;
                 wave_sync();
             }
         }
@@ -804,8 +844,7 @@ __global__ __launch_bounds__(kBlock) void route_backward_kernel(RouteBackwardArg
 #pragma unroll
         for (int v = 0; v < kEach; ++v) {
             r[v] = at[begin + v];
-            if (sigmoid) r[v] *= 1.f / (1.f + __expf(x[v]));
-            else if (!a.renormalise) r[v] -= __expf(x[v] - base) / sum * total;
+            if (!sigmoid && !a.renormalise) r[v] -= e[v] * shared;
             if (x[v] == -kInf) r[v] = 0.f;
             if (broken) r[v] = __builtin_nanf("");
         }
