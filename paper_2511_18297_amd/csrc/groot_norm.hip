@@ -320,10 +320,14 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBac
     }
 }
 
-// Rows of more bytes are read past the caches, and a gradient of more is written past them.  Rows of 4096 in bfloat16, loads past and kept, us: 32 MB,
-// the inputs in the caches already, forward 27 and 22, backward 37 and 34; 128 MB 82 and 93, 99 and 104.  The gradient past and kept, by itself and
-// with the product that takes it: 64 MB 61 and 57, 93 and 84; 128 MB 102 and 99, 150 and 139; 256 MB 184 and 181, 275 and 285.
-constexpr int64_t kLoadsPast = 32 << 20, kGradientsPast = 192 << 20;
+// Rows of more bytes are read past the caches, and a gradient of more is written past them.  Rows of 4096 in bfloat16, past and kept, us, with the product
+// in front that makes the rows (or their gradient) and, the second pair, the one behind that takes the norm's:
+//   forward loads    32 MB 46 and 44, 65 and 63; 48 MB 67 and 63, 95 and 91; 64 MB 80 and 79, 106 and 115; 96 MB 116 and 121, 160 and 173; 128 MB 151 and 167, 211
+//                    and 222; 192 MB 240 and 255, 323 and 328; 256 MB 316 and 335, 421 and 418
+//   backward loads   32 MB 56 and 53; 48 MB 78 and 75; 64 MB 91 and 92; 96 MB 128 and 130; 128 MB 165 and 182; 192 MB 233 and 268; 256 MB 305 and 305
+//   gradient         by itself and with the product that takes it: 64 MB 61 and 57, 93 and 84; 128 MB 102 and 99, 150 and 139; 256 MB 184 and 181, 275 and 285
+// (by itself, all in the caches: forward 64 MB 44 and 41, 128 MB 81 and 94; backward 58 and 55, 97 and 108).
+constexpr int64_t kLoadsPast = 56 << 20, kGradientsPast = 192 << 20;
 
 constexpr int kGainCols = 16, kGainRows = 64;
 

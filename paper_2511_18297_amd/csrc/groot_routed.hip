@@ -279,11 +279,16 @@ RoutedShape routed_shape(RoutedArgs *a, int64_t pieces, int lanes)
     const int64_t blocks = (a->n + threads / lanes - 1) / (threads / lanes);
     return {threads, dim3((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), (uint32_t)((pieces + part - 1) / part))};
 }
-// Outputs from some size on go past the caches.  By the call that makes them and the one that reads them next, together, past and kept
-// (bfloat16, rows of 4096, us): rows and their product, 64 MB 64 and 57, 128 MB 91 and 80, 192 MB 144 and 120, 256 MB 174 and 183, 384 MB 259
-// and 256; sum and norm, 32 MB 37 and 36, 64 MB 64 and 62, 96 MB 106 and 106 (the sum by itself, 64 MB: 45.8 and 49.0); the sum's gradients and the
-// product that takes them, 32 MB 51 and 43, 64 MB 71 and 66, 128 MB 103 and 116, 256 MB 225 and 216 (by themselves, 256 MB: 100 and 133).
-constexpr int64_t kRowsPast = 224 << 20, kSumPast = 32 << 20, kGradientsPast = 96 << 20;
+// Outputs from some size on go past the caches.  By the call that makes them and those that read them next, together, past and kept
+// (bfloat16, rows of 4096, us):
+//   rows and their product      64 MB 64 and 57, 128 MB 91 and 80, 192 MB 144 and 120, 256 MB 174 and 183, 384 MB 259 and 256
+//   sum and norm                32 MB 37.1 and 36.2, 64 MB 64.2 and 62.9, 96 MB 104 and 106, 128 MB 147 and 142, 192 MB 218 and 224, 256 MB 288 and 300
+//   sum and product             32 MB 45.2 and 45.1, 64 MB 74 and 68, 96 MB 102 and 105, 128 MB 136 and 147, 256 MB 265 and 283, 384 MB 394 and 418
+//   product, sum and norm       64 MB 138 and 138, 96 MB 207 and 213, 128 MB 286 and 301, 256 MB 593 and 600
+//   sum's gradients, product    32 MB 51 and 43, 64 MB 72 and 66, 96 MB 85 and 82, 128 MB 103 and 112, 192 MB 178 and 184, 256 MB 226 and 230
+//   the same, weights' gradient 64 MB 103 and 97, 96 MB 125 and 123, 128 MB 161 and 166, 192 MB 255 and 249, 256 MB 319 and 317, 384 MB 464 and 463
+// (by themselves: the sum 64 MB 39.9 and 40.5, 128 MB 76 and 98; its gradients 96 MB 40 and 41, 192 MB 75 and 101).
+constexpr int64_t kRowsPast = 224 << 20, kSumPast = 80 << 20, kGradientsPast = 112 << 20;
 
 template <typename T, bool kOnce>
 int sum_launch(RoutedArgs a, hipStream_t stream)
