@@ -383,9 +383,12 @@ int64_t norm_blocks(int64_t n, const NormShape &s, int64_t most)
     const int64_t b = (n + rows_of(s.lanes) - 1) / rows_of(s.lanes);
     return b < most ? b : most;
 }
-// Workgroups of the backward call: whole multiples of the 256 CUs with four turns of rows each at least, as each writes a row of partial sums. 512, 1024
-// and 2048 rows of 4096 in bfloat16, 256 of them: 14.1, 17.2 and 23.5 us with the sums, 512: 16.2, 17.9 and 22.0, 1024: 16.1, 25.4 and 28.5; 16384 rows,
-// 512, 768, 1024, 2048: 108, 104, 107, 119 us; 8.4 M rows of 64 in fp32, 512, 1024, 2048, 8192: 1555, 1218, 1226, 1405.
+// Workgroups of the backward call: whole multiples of the 256 CUs, the least that leave no more than four turns of rows to each while there are fewer than
+// `most` (so 256 of them up to 1024 turns, and just above a multiple each has little more than two), as each writes a row of partial sums.  With the sums, us:
+// 512, 1024, 1100, 2048 and 3000 rows of 4096 in bfloat16, 256 of them: 13.7, 16.4, 17.8, 22.7 and 28.9, 512: 18.4, 18.5, 18.7, 22.3 and 26.6, 768: 18.4, 22.3,
+// 22.3, 25.8 and 30.0; 5031 rows of 1138, 1258 turns, 256 and 512: 18.7 and 16.1; 17600 rows of 64 in fp32, 1100 turns: 8.0 and 6.7; 16384 rows of 4096, 256, 512,
+// 768, 1024, 2048: 129, 99, 100, 100, 110; 8.4 M rows of 64, 512, 1024, 2048, 8192: 1541, 1202, 1214, 1388.  Rounded down in place of up: 1100 rows of 4096 18.5 and
+// 17.6, 3000 rows 29.7 and 26.4, but 5031 rows of 1138 15.7 and 18.1, 17600 rows of 64 6.8 and 8.1.
 int64_t backward_blocks(int64_t n, const NormShape &s)
 {
     const int64_t turns = norm_blocks(n, s, INT64_MAX), most = s.lanes <= kWave ? 1024 : s.lanes <= 256 ? 768 : s.lanes == 512 ? 512 : 256;
