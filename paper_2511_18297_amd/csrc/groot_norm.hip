@@ -326,7 +326,9 @@ __global__ __launch_bounds__(block_of(kLanes)) void norm_backward_kernel(NormBac
 //                    and 222; 192 MB 240 and 255, 323 and 328; 256 MB 316 and 335, 421 and 418
 //   backward loads   32 MB 56 and 53; 48 MB 78 and 75; 64 MB 91 and 92; 96 MB 128 and 130; 128 MB 165 and 182; 192 MB 233 and 268; 256 MB 305 and 305
 //   gradient         by itself and with the product that takes it: 64 MB 61 and 57, 93 and 84; 128 MB 102 and 99, 150 and 139; 256 MB 184 and 181, 275 and 285
-// (by itself, all in the caches: forward 64 MB 44 and 41, 128 MB 81 and 94; backward 58 and 55, 97 and 108).
+// (by itself, all in the caches: forward 64 MB 44 and 41, 128 MB 81 and 94; backward 58 and 55, 97 and 108; with four sets of buffers in turn past is never the
+// slower: 32 MB 70 and 76, 48 MB 112 and 115, 64 MB 132 and 133, backward 57 and 60, 82 and 83, 97 and 99, the gradient with two products 128 MB 224 and 227, 192 MB
+// 368 and 358, 256 MB 413 and 422).
 constexpr int64_t kLoadsPast = 56 << 20, kGradientsPast = 192 << 20;
 
 constexpr int kGainCols = 16, kGainRows = 64;

@@ -5,7 +5,7 @@
 // with an addend 40 to 45 us (6.0 to 6.7 TB/s, some of it from the cache behind L2); 7168 rows of 2048 to four places each 28 us (5.3
 // TB/s), their sum's gradients 43 (6.2).  A workgroup takes a whole row at once where it can: with a wavefront to a row, or parts of rows, the sum
 // took 50 to 57.  Loads of four slots at a time go on their way together, those of a slot without a place to 16 bytes of zeros.
-// Large outputs go past the caches (kRowsPast and the like).
+// Large outputs go past the caches (kRowsPast, kSumPast).
 //
 // A piece is 16 bytes of a row.  A row's last piece is moved back to end with the row, so that it is whole too: its first values are
 // copied or computed twice, alike.  Rows of less than 16 bytes go value by value.
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kBlock) void routed_sum_kernel(RoutedArgs a)
 
 // kPieces > 0: a row's gradient stays in registers over its slots, kPieces pieces in each of kLanes lanes; 0: rows of any width, whose
 // gradient is read again for every slot
-template <typename T, int kLanes, int kPieces, bool kShort, bool kOnce>
+template <typename T, int kLanes, int kPieces, bool kShort>
 __global__ __launch_bounds__(kBlock) void routed_sum_backward_kernel(RoutedArgs a)
 {
     constexpr int kPer = 16 / sizeof(T), kBatch = 2, kHeld = kPieces ? kPieces : 1, kParts = kLanes > kWave ? kLanes / kWave : 1;
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kBlock) void routed_sum_backward_kernel(RoutedArgs 
                             float x[kPer];
 #pragma unroll
                             for (int e = 0; e < kPer; ++e) x[e] = w[s] * g.x[e];
-                            store_piece<T, kShort, kOnce>((char *)((T *)a.out + p[s] * a.out_stride), at[j], a.K, x);
+                            store_piece<T, kShort, false>((char *)((T *)a.out + p[s] * a.out_stride), at[j], a.K, x);
                         }
                     }
                 }
@@ -279,16 +279,17 @@ RoutedShape routed_shape(RoutedArgs *a, int64_t pieces, int lanes)
     const int64_t blocks = (a->n + threads / lanes - 1) / (threads / lanes);
     return {threads, dim3((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), (uint32_t)((pieces + part - 1) / part))};
 }
-// Outputs from some size on go past the caches.  By the call that makes them and those that read them next, together, past and kept
-// (bfloat16, rows of 4096, us):
-//   rows and their product      64 MB 64 and 57, 128 MB 91 and 80, 192 MB 144 and 120, 256 MB 174 and 183, 384 MB 259 and 256
-//   sum and norm                32 MB 37.1 and 36.2, 64 MB 64.2 and 62.9, 96 MB 104 and 106, 128 MB 147 and 142, 192 MB 218 and 224, 256 MB 288 and 300
-//   sum and product             32 MB 45.2 and 45.1, 64 MB 74 and 68, 96 MB 102 and 105, 128 MB 136 and 147, 256 MB 265 and 283, 384 MB 394 and 418
-//   product, sum and norm       64 MB 138 and 138, 96 MB 207 and 213, 128 MB 286 and 301, 256 MB 593 and 600
-//   sum's gradients, product    32 MB 51 and 43, 64 MB 72 and 66, 96 MB 85 and 82, 128 MB 103 and 112, 192 MB 178 and 184, 256 MB 226 and 230
-//   the same, weights' gradient 64 MB 103 and 97, 96 MB 125 and 123, 128 MB 161 and 166, 192 MB 255 and 249, 256 MB 319 and 317, 384 MB 464 and 463
-// (by themselves: the sum 64 MB 39.9 and 40.5, 128 MB 76 and 98; its gradients 96 MB 40 and 41, 192 MB 75 and 101).
-constexpr int64_t kRowsPast = 224 << 20, kSumPast = 80 << 20, kGradientsPast = 112 << 20;
+// Copied rows and sums from some size on go past the caches.  By the call that makes them and those around it, past and kept (bfloat16, rows of 4096,
+// us a set of buffers; first one set over and over, then four in turn):
+//   rows, their product           64 MB 64 and 57, 128 MB 91 and 80, 192 MB 144 and 120, 256 MB 174 and 183, 384 MB 259 and 256
+//   norm, rows, their product     four sets: 64 MB 77 and 85, 128 MB 111 and 123, 192 MB 168 and 181, 256 MB 203 and 231, 384 MB 305 and 333
+//   sum, norm                     32 MB 37 and 36, 64 MB 64 and 63, 96 MB 104 and 106, 192 MB 218 and 224; four: 64 MB 79 and 73, 96 MB 110 and 111
+//   sum, product                  32 MB 45 and 45, 64 MB 74 and 68, 96 MB 102 and 105, 128 MB 136 and 147, 256 MB 265 and 283
+//   product, sum, norm, product   four sets: 48 MB 157 and 159, 64 MB 198 and 194, 96 MB 270 and 275, 128 MB 351 and 366, 192 MB 539 and 554
+// (the sum by itself, four sets: 64 MB 48 and 52, 96 MB 69 and 76).  The sum's gradients are kept at every size: with the two products that read them,
+// four sets, 64 MB 116 and 113, 128 MB 173 and 167, 256 MB 319 and 309, 512 MB 595 and 586; one set, 128 MB 161 and 166, 256 MB 319 and 317 (by
+// themselves 128 MB 67 and 69).
+constexpr int64_t kRowsPast = 224 << 20, kSumPast = 80 << 20;
 
 template <typename T, bool kOnce>
 int sum_launch(RoutedArgs a, hipStream_t stream)
@@ -309,7 +310,7 @@ int sum_launch(RoutedArgs a, hipStream_t stream)
 #undef GROOT_SUM
     return (int)hipGetLastError();
 }
-template <typename T, bool kOnce>
+template <typename T>
 int sum_backward_launch(RoutedArgs a, hipStream_t stream)
 {
     const int64_t pieces = ((int64_t)a.K * sizeof(T) + 15) / 16;
@@ -318,7 +319,7 @@ int sum_backward_launch(RoutedArgs a, hipStream_t stream)
         RoutedShape s = routed_shape(&a, 1, lanes);                                                                                      \
         a.part = few_rows ? 2 : a.k;                                                                                                     \
         s.grid.y = (a.k + a.part - 1) / a.part;                                                                                          \
-        routed_sum_backward_kernel<T, lanes, held, is_short, kOnce><<<s.grid, s.threads, 0, stream>>>(a);                                \
+        routed_sum_backward_kernel<T, lanes, held, is_short><<<s.grid, s.threads, 0, stream>>>(a);                                       \
     }
     // a wavefront to a row, and a workgroup where rows are wide or few (1024 rows of 2048 in bfloat16, 4 slots: 9.8 and 7.5 us; 4096: 25.0 and 26.9);
     // very few rows: one for every two slots (29 rows of 4160, 9 slots: 15.2 us without, 6.1)
@@ -374,10 +375,9 @@ int launch_routed_sum(int32_t dtype, const RoutedArgs &a, void *stream)
 int launch_routed_sum_backward(int32_t dtype, const RoutedArgs &a, void *stream)
 {
     hipStream_t s = (hipStream_t)stream;
-    const bool once = a.n * a.k * a.K * (dtype == GROOT_F32 ? 4 : 2) > kGradientsPast;
-    if (dtype == GROOT_F32) return once ? sum_backward_launch<float, true>(a, s) : sum_backward_launch<float, false>(a, s);
-    if (dtype == GROOT_BF16) return once ? sum_backward_launch<bf16_t, true>(a, s) : sum_backward_launch<bf16_t, false>(a, s);
-    return once ? sum_backward_launch<f16_t, true>(a, s) : sum_backward_launch<f16_t, false>(a, s);
+    if (dtype == GROOT_F32) return sum_backward_launch<float>(a, s);
+    if (dtype == GROOT_BF16) return sum_backward_launch<bf16_t>(a, s);
+    return sum_backward_launch<f16_t>(a, s);
 }
 
 }  // namespace groot
