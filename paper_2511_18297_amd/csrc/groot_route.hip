@@ -912,7 +912,8 @@ int route_launch(RouteArgs a, uint32_t *counts, hipStream_t stream)
         int32_t *const before = (int32_t *)((char *)counts + count_bytes(groups, a.E));
         if (groups > kSumGroups) {
             route_scan_kernel<<<(a.E + kScanExperts - 1) / kScanExperts, kScanExperts * kScanParts, 0, stream>>>(counts, before, (int32_t)groups, a.E);
-            route_place_kernel<true><<<(uint32_t)groups, kBlock, lds, stream>>>(a, counts, before, (int32_t)groups);
+            const int fit = fits_launch(groups, kBlock) ? kBlock : threads;   // from 2^30 rows on a launch holds no more lanes than the search's
+            route_place_kernel<true><<<(uint32_t)groups, fit, lds, stream>>>(a, counts, before, (int32_t)groups);
         } else {
             route_place_kernel<false><<<(uint32_t)groups, 1024, lds, stream>>>(a, counts, before, (int32_t)groups);
         }

@@ -163,3 +163,23 @@ def test_norm_and_its_gradients(kind, pieces, odd):
     dY.copy_(torch.randint(-1, 2, (n, K), generator=gen, device="cuda", dtype=torch.int8))
     G.groot_rms_norm_backward(H, torch.ones_like(rstd), None, dY, dX, dgain, work)
     assert torch.equal(dgain.double(), (H * dY).sum(0, dtype=torch.float64))
+
+
+def test_routing_more_rows_than_a_launch_of_256_lanes_a_workgroup_holds():
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("not enough memory")
+    n = (1 << 30) + 70
+    scores = torch.randint(0, 3, (n, 2), device="cuda", dtype=torch.int8, generator=torch.Generator(device="cuda").manual_seed(260)).half()
+    experts, places = (torch.full((n, 1), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    weights, offsets = torch.full((n, 1), NAN, device="cuda"), torch.full((3,), -7, dtype=torch.int64, device="cuda")
+    work = torch.empty(G.groot_route_workspace(n, 2, 1), dtype=torch.uint8, device="cuda")
+    G.groot_route(scores, None, experts, weights, places, offsets, work)
+    second = scores[:, 1] > scores[:, 0]                     # ties go to the first
+    assert torch.equal(experts[:, 0], second.int()) and bool((weights == 1).all())
+    upto = torch.cumsum(second, 0, dtype=torch.int32)
+    firsts = n - int(upto[-1])
+    assert offsets.tolist() == [0, firsts, n]
+    for i in range(0, n, 1 << 26):
+        u, s = upto[i:i + (1 << 26)], second[i:i + (1 << 26)]
+        row = torch.arange(i, i + len(u), dtype=torch.int32, device="cuda")
+        assert torch.equal(places[i:i + (1 << 26), 0], torch.where(s, firsts + u - 1, row - u)), i
