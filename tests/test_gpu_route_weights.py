@@ -17,7 +17,7 @@ from util import ensure_built
 
 ensure_built()
 import paper_2511_18297_amd as G  # noqa: E402
-from test_gpu_routed import GATES, LEAST, TYPES, UNIT, how, own_route  # noqa: E402
+from test_gpu_routed import GATES, LEAST, TYPES, UNIT, check_route, how, own_route  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,26 @@ def test_gradients_of_scores_far_apart(kind, gate, renormalise, spread):
         want, terms = torch.from_numpy(part).cuda(), torch.from_numpy(whole).cuda()
         err, bound = (ds.double() - want).abs(), 4 * U * terms + 1.01 * UNIT[T] * want.abs() + 2 * LEAST[T]
         assert bool((err <= bound).all()), f"{E} experts, top {k}: {float((err / bound).max())} of the tolerance"
+
+
+@pytest.mark.parametrize("gate", GATES)
+@pytest.mark.parametrize("renormalise", (False, True))
+@pytest.mark.parametrize("sets", ((1, 1, 1), (4, 3, 2)))
+@pytest.mark.parametrize("E, k", [(24, 18), (48, 24), (400, 17), (1024, 32)])
+def test_many_slots_of_masked_rows(gate, renormalise, sets, E, k):
+    """more slots than a row has experts left, rows without one, infinities and NaN"""
+    scores, bias = scores_of(E, torch.float32, 2.0, 700 + E)
+    scores[3] = -math.inf
+    scores[4, 1:] = -math.inf
+    scores[5, k - 2:] = -math.inf
+    scores[6, : E - 3] = -math.inf
+    scores[7, 3], scores[8, 5], scores[9] = math.nan, math.inf, math.nan
+    scores[10] = torch.finfo(torch.float32).min
+    scores[11, 1:] = torch.finfo(torch.float32).min
+    scores[150:] = -math.inf
+    check_route(scores, None, k, **how(gate, *sets, renormalise))
+    bias[0], bias[1], bias[2] = -math.inf, math.nan, 3.0
+    if gate == "sigmoid":
+        scores[10] = 2.0                                     # values of 0 and of numbers next to it are no values of their own with a bias
+        scores[11, 1:] = 1.0
+    check_route(scores, bias, k, **how(gate, *sets, renormalise))
