@@ -2,10 +2,10 @@
 //   value c of an expert: its score where that orders as the probability does, otherwise softmax or sigmoid of the score, plus a bias
 //   top k of c (ties to the lowest expert) among the sets whose best members' sum is largest; weights factor x p, renormalised or not
 // A call cannot do without n E scores and 12 n k bytes of results.  The scores are read once; what bounds the kernel is the search, in
-// instructions where there are many rows (65536 rows of 128 scores in fp32, top 8: 13.5 us, 2.9 TB/s; 635 vector instructions a wavefront
+// instructions where there are many rows (65536 rows of 128 scores in fp32, top 8: 14.4 us, 2.8 TB/s; 666 vector instructions a wavefront
 // of 8 rows, the vector units busy in 60 % of the time) and in latency where there are few (one row of 64: 3.4 us; 16384 rows of 64, one
-// wavefront to a SIMD: 6.3).  Probabilities in 64 bits are a third of the instructions where they decide (16384 rows of 256 in
-// bfloat16, sigmoid with a bias, 4 of 8 sets: 20 us).  Taken one by one, k maxima over a row's lanes took 31 us in place of 13.5.
+// wavefront to a SIMD: 7).  Probabilities in 64 bits are a third of the instructions where they decide (16384 rows of 256 in
+// bfloat16, sigmoid with a bias, 4 of 8 sets: 20 us).  Taken one by one, k maxima over a row's lanes took 31 us where the lists took 13.5.
 //
 // The search: a key is a number of 64 bits, the value with the expert's number in its last ten bits, so that one comparison decides and
 // breaks ties (a score of fp32 leaves 29 bits free; a probability computed in 64 bits keeps 42, and what agrees in these counts as tied).
@@ -15,8 +15,9 @@
 //
 // Places: a workgroup takes up to 64 rows.  A row chooses an expert once, so the rows of a workgroup that chose an expert are the bits of
 // one 64-bit word, and a choice's rank is the number of bits below its row's: nothing depends on the order of atomics.  The ranks wait
-// in `places` until the counts of all workgroups are known: every workgroup of a second launch adds them up (4 to 5.5 us), beyond 256
-// workgroups a launch between the two does (5 us; 256 counts of 256 experts in bytes are 64 KB to read for each workgroup).
+// in `places` until the counts of all workgroups are known: every workgroup of a second launch adds them up (4 to 6 us), beyond 256
+// workgroups a launch between the two does (256 counts of 256 experts in bytes are 64 KB to read for each workgroup).  That one takes 5 us for the 1024
+// counts of 65536 rows and grows with them, 16 experts to a workgroup: 60 us for 1 M rows, 0.8 and 1.4 ms of 1.05 and 2.05 for 8.4 M of 8 and 64.
 #include "groot_tile.h"
 
 namespace groot {
@@ -157,7 +158,7 @@ __device__ __forceinline__ double weight_of(float s, float m, bool sigmoid)
     return sigmoid ? e * reciprocal64(1.0 + exp31(-__builtin_fabs((double)s))) : e;
 }
 // The softmax's sum over all experts is of terms in fp32, in pairs: a term p that is |x| below the largest is off by 2.5 |x| + 2 half steps, and p |x| adds
-// up to 4.4 of the sum at the most (1024 experts).  In 64 bits: 65536 rows of 128, top 8: 23.9 us in place of 20.4.
+// up to 4.4 of the sum at the most (1024 experts).  In 64 bits: 65536 rows of 128, top 8: 23.9 us in place of 20.6.
 template <int kCount>
 __device__ __forceinline__ float tree_sum(float (&x)[kCount])
 {

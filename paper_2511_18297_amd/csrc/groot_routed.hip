@@ -2,9 +2,10 @@
 //   R[places[i,s]] = X[i];   out[i] = addend[i] + sum_s w[i,s] R[places[i,s]];   dR[places[i,s]] = w[i,s] dout[i], dw[i,s] = dout[i] . R[places[i,s]]
 // Every kernel goes by the rows i, which know their places: no list of the other direction, no atomics; a slot's row is written by one group
 // of lanes.  Bound by HBM: the n k rows at the places are read or written once, the n rows once.  bfloat16: the sum of 2 x 8192 rows of 4096
-// with an addend 40 to 45 us (6.0 to 6.7 TB/s, some of it from the cache behind L2); 7168 rows of 2048 to four places each 28 us (5.3
-// TB/s), their sum's gradients 43 (6.2).  A workgroup takes a whole row at once where it can: with a wavefront to a row, or parts of rows, the sum
-// took 50 to 57.  Loads of four slots at a time go on their way together, those of a slot without a place to 16 bytes of zeros.
+// with an addend 50 us (5.4 TB/s, the sums stay in the caches), of 2 x 12288 66 (6.1, past them); 7168 rows of 2048 to four places each 28 us (5.3
+// TB/s), their sum's gradients 43 (6.2), their sum 41 (4.5) and the gradient of the rows 44 to 48 (3.4: one load of four answers on its way in a lane,
+// and the places' before it).  A workgroup takes a whole row at once where it can: with a wavefront to a row, or parts of rows, a sum took 50 to 57
+// us that takes 45 so.  Loads of four slots at a time go on their way together, those of a slot without a place to 16 bytes of zeros.
 // Large outputs go past the caches (kRowsPast, kSumPast).
 //
 // A piece is 16 bytes of a row.  A row's last piece is moved back to end with the row, so that it is whole too: its first values are
